@@ -205,6 +205,76 @@ void pconv_free(pconv_handle *h);
 int pconv_maxpool2x2(const void *x_dev, void *y_dev, int n, int c, int h, int w,
                      pconv_layout layout, pconv_dtype dtype, void *hip_stream);
 
+/* ---- layers in 8-bit integers: what of a pruned network is no 3x3 layer ------------------------
+ *
+ * The 1x1 layers (channels last: a row of the product for each pixel) and the fully connected ones
+ * (a row for each image) are products of matrices, here of 8-bit integers with one scale for each row
+ * of the activations and one for each output channel:
+ *
+ *   scale[r]  = max_k |x[r][k]| / 127          (the nearest fp32 number)
+ *   q[r][k]   = x[r][k] / scale[r]             (the nearest fp32 number, then the nearest whole one, ties to even)
+ *   y[r][o]   = act( (sum_k q[r][k] * w[o][k]) * (scale[r] * w_scale[o]) + bias[o] )
+ *
+ * Sums are whole numbers of 32 bits and exact.  A row of zeros (also one whose scale is below the smallest fp32 number) has
+ * scale 0 and zeros; a row that holds an infinity or a NaN has scale NaN and zeros, so that all its outputs are NaN.
+ * act is ReLU (which keeps NaN) or the identity.  Matrices are stored row by row, `stride` elements from one row's
+ * first element to the next's, at least the row's length; rows may begin anywhere their type may (those at multiples of
+ * 16 bytes are read fastest).  A size of 0 is legal: with k = 0 the sums are 0.  All calls are asynchronous on hip_stream,
+ * allocate nothing, keep nothing from one call to the next and give the same bits from run to run.
+ * Outputs must not overlap inputs.  A call whose size needs more than 2^32 threads gives PCONV_UNSUPPORTED.
+ *
+ * pconv_quantize_rows - q and scale of x [rows][cols], fp32 or bf16.  Weights are quantised by the same call, one row for
+ * each output channel.
+ */
+int pconv_quantize_rows(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, int64_t rows, int64_t cols,
+                        int8_t *q_dev, int64_t q_stride, float *scale_dev, void *hip_stream);
+
+/* pconv_matmul_i8 - y [m][n] of a [m][k] and b [n][k], both 8-bit, with a_scale [m], b_scale [n] and bias [n] (or NULL).
+ * y is fp32, or bf16 rounded to nearest even.  `work`: device memory of at least pconv_matmul_i8_workspace bytes (mostly 0),
+ * aligned to 16 bytes, used in stream order until the call's work is done, its contents are lost.
+ * m and n up to 2^31 - 1, k up to 131071 (where 32 bits hold any sum).
+ * Errors: PCONV_INVALID_ARG (null pointers, sizes or strides out of range, too little work space), PCONV_UNSUPPORTED,
+ * PCONV_HIP_ERROR (launch failed). */
+int64_t pconv_matmul_i8_workspace(int64_t m, int64_t n, int64_t k);
+int pconv_matmul_i8(const int8_t *a_dev, int64_t a_stride, const float *a_scale, const int8_t *b_dev, int64_t b_stride,
+                    const float *b_scale, const float *bias_dev, void *y_dev, int64_t y_stride, pconv_dtype y_dtype,
+                    int64_t m, int64_t n, int64_t k, int fuse_relu, void *work, int64_t work_bytes, void *hip_stream);
+
+/* pconv_linear_i8 - pconv_quantize_rows of x [m][k] and pconv_matmul_i8 with the weights w [n][k], in one call and with
+ * the same results.  The quantised activations stay in the work space, or on the chip where the call is small. */
+int64_t pconv_linear_i8_workspace(int64_t m, int64_t n, int64_t k, pconv_dtype x_dtype);
+int pconv_linear_i8(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, const int8_t *w_dev, int64_t w_stride,
+                    const float *w_scale, const float *bias_dev, void *y_dev, int64_t y_stride, pconv_dtype y_dtype,
+                    int64_t m, int64_t n, int64_t k, int fuse_relu, void *work, int64_t work_bytes, void *hip_stream);
+
+/* ---- gradients of a training step ---------------------------------------------------------------
+ *
+ * Pruning (pconv_project between the steps of a training loop) moves weights at once; the gradients of the next step are
+ * limited so that it does not follow:
+ *
+ *   norm = sqrt( sum over all tensors and elements of g^2 )        out = g * min(1, max_norm / (norm + eps))
+ *
+ * Squares are summed in fp64 in a fixed order.  A norm that is NaN makes all outputs NaN, an infinite one makes them 0, and
+ * NaN where g is infinite.  A tensor is a plain run of counts[i] >= 0 elements, fp32 or bf16, that begins
+ * anywhere its type may.
+ *
+ *   grads      host, [num] device pointers (not read where counts[i] == 0)
+ *   counts     host, [num], together up to 2^45;  num up to 2^24;  dtypes, out_dtypes  host, [num] of pconv_dtype
+ *   outs       host, [num] device pointers; outs[i] may be grads[i] with the same type (nothing is written then where the
+ *              factor is 1) and must overlap no other tensor
+ *   norm_dev   device, receives the norm (fp32; infinite if it is no fp32 number, the factor is right all the same)
+ *   max_norm >= 0 (may be infinite), eps >= 0
+ *   work       device memory, pconv_grad_workspace(num) bytes, aligned to 16 bytes, used in stream order
+ *
+ * The arrays on the host are read during the call.  Asynchronous on hip_stream, allocate nothing.
+ * Errors: PCONV_INVALID_ARG, PCONV_HIP_ERROR. */
+int64_t pconv_grad_workspace(int64_t num);
+int pconv_grad_norm(const void *const *grads, const int64_t *counts, const int32_t *dtypes, int64_t num,
+                    float *norm_dev, void *work, int64_t work_bytes, void *hip_stream);
+int pconv_clip_grads(const void *const *grads, void *const *outs, const int64_t *counts, const int32_t *dtypes,
+                     const int32_t *out_dtypes, int64_t num, float max_norm, float eps, float *norm_dev,
+                     void *work, int64_t work_bytes, void *hip_stream);
+
 /* ---- inspection of a handle (tests, benchmarks) --------------------------------------- */
 
 typedef struct {

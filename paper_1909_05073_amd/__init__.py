@@ -105,6 +105,23 @@ def lib():
     L.pconv_pool2x2_fusion.argtypes = [vp, ip, ip, ip, ip, ip]
     L.pconv_debug_measure_fma_peak.restype = ip
     L.pconv_debug_measure_fma_peak.argtypes = [C.POINTER(C.c_double)]
+    i64 = C.c_int64
+    L.pconv_quantize_rows.restype = ip
+    L.pconv_quantize_rows.argtypes = [vp, i64, ip, i64, i64, vp, i64, vp, vp]
+    L.pconv_matmul_i8_workspace.restype = i64
+    L.pconv_matmul_i8_workspace.argtypes = [i64, i64, i64]
+    L.pconv_matmul_i8.restype = ip
+    L.pconv_matmul_i8.argtypes = [vp, i64, vp, vp, i64, vp, vp, vp, i64, ip, i64, i64, i64, ip, vp, i64, vp]
+    L.pconv_linear_i8_workspace.restype = i64
+    L.pconv_linear_i8_workspace.argtypes = [i64, i64, i64, ip]
+    L.pconv_linear_i8.restype = ip
+    L.pconv_linear_i8.argtypes = [vp, i64, ip, vp, i64, vp, vp, vp, i64, ip, i64, i64, i64, ip, vp, i64, vp]
+    L.pconv_grad_workspace.restype = i64
+    L.pconv_grad_workspace.argtypes = [i64]
+    L.pconv_grad_norm.restype = ip
+    L.pconv_grad_norm.argtypes = [vp, vp, vp, i64, vp, vp, i64, vp]
+    L.pconv_clip_grads.restype = ip
+    L.pconv_clip_grads.argtypes = [vp, vp, vp, vp, vp, i64, C.c_float, C.c_float, vp, vp, i64, vp]
     L.pconv_last_error.restype = C.c_char_p
     L.pconv_last_error.argtypes = []
     _lib = L
@@ -117,6 +134,8 @@ EXPORTED_SYMBOLS = ["pconv_project", "pconv_pack", "pconv_conv2d", "pconv_conv2d
                     "pconv_debug_unpack",
                     "pconv_set_kernel_policy", "pconv_debug_set_tiling", "pconv_debug_set_flat_shape", "pconv_debug_plan", "pconv_debug_set_spin_limit",
                     "pconv_get_async_error", "pconv_pool2x2_fusion", "pconv_debug_measure_fma_peak",
+                    "pconv_quantize_rows", "pconv_matmul_i8", "pconv_matmul_i8_workspace", "pconv_linear_i8",
+                    "pconv_linear_i8_workspace", "pconv_grad_workspace", "pconv_grad_norm", "pconv_clip_grads",
                     "pconv_last_error"]
 
 
@@ -425,3 +444,317 @@ def maxpool2x2(x, layout="nchw"):
     pconv_maxpool2x2(x.data_ptr(), y.data_ptr(), n, c, h, w, lay, dt,
                      _stream(x.get_device()))
     return y
+
+
+# ---- layers in 8-bit integers ------------------------------------------------------------
+
+def _type_of(t, what):
+    import torch
+    if t.dtype == torch.float32:
+        return F32
+    if t.dtype == torch.bfloat16:
+        return BF16
+    raise ValueError(f"{what} must be float32 or bfloat16")
+
+
+def _device_index(*tensors) -> int:
+    """The one device that the tensors (or None) are on, which has to be torch's current one."""
+    import torch
+    at = -1
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError("all tensors must be CUDA tensors")
+        i = t.get_device()
+        if at >= 0 and i != at:
+            raise ValueError("all tensors must be on one device")
+        at = i
+    if at >= 0 and at != torch.cuda.current_device():
+        raise ValueError("the tensors' device must be the current one")
+    return at
+
+
+def _rows(t, what):
+    """(rows, columns, elements from row to row) of a tensor [..., columns] whose rows can be walked with one stride."""
+    if t.dim() < 1:
+        raise ValueError(f"{what} must have at least one dimension")
+    if t.dim() != 2:
+        if t.dim() > 2 and not t.is_contiguous():
+            try:
+                t = t.view(-1, t.shape[-1])
+            except RuntimeError:
+                raise ValueError(f"the rows of {what} must lie one stride apart") from None
+        else:
+            k = t.shape[-1]
+            if t.dim() == 1 and k > 1 and t.stride(0) != 1:
+                raise ValueError(f"{what} must be contiguous along its last dimension")
+            return (t.numel() // k if k else _prod(t.shape[:-1])), k, k
+    m, k = t.shape
+    step, one = t.stride()
+    if k > 1 and one != 1:
+        raise ValueError(f"{what} must be contiguous along its last dimension")
+    if m > 1 and step < k:
+        raise ValueError(f"the rows of {what} must not overlap")
+    return m, k, max(step, k)
+
+
+def _prod(sizes) -> int:
+    n = 1
+    for s in sizes:
+        n *= s
+    return n
+
+
+def _scratch(size: int, like):
+    """Work space out of torch's pool for a call on the current stream."""
+    import torch
+    if torch.cuda.is_current_stream_capturing() and not _graph_pool_serves(like.device):
+        raise RuntimeError("the stream is being captured by others than torch: call the pconv_... function with work space of your own")
+    return torch.empty(size, dtype=torch.uint8, device=like.device)
+
+
+def _per_channel(t, n, what):
+    import torch
+    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{what} must be {n} contiguous float32 numbers")
+    return t.data_ptr()
+
+
+def _output(out, shape, dtype, like):
+    """(tensor, elements from row to row) for a result of that shape."""
+    import torch
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=like.device)
+    elif out.dtype != dtype or out.shape != torch.Size(shape):
+        raise ValueError(f"out must be {dtype} of shape {tuple(shape)}")
+    return out, _rows(out, "out")[2]
+
+
+def pconv_quantize_rows(x_ptr: int, x_stride: int, x_dtype, rows: int, cols: int, q_ptr: int, q_stride: int,
+                        scale_ptr: int, stream: int = 0):
+    """Raw-pointer call, one to one with the C entry point."""
+    _check(lib().pconv_quantize_rows(x_ptr or None, x_stride, _DTYPE[x_dtype], rows, cols, q_ptr or None, q_stride,
+                                     scale_ptr or None, stream or None))
+
+
+def pconv_matmul_i8_workspace(m: int, n: int, k: int) -> int:
+    return lib().pconv_matmul_i8_workspace(m, n, k)
+
+
+def pconv_matmul_i8(a_ptr: int, a_stride: int, a_scale: int, b_ptr: int, b_stride: int, b_scale: int, bias_ptr, y_ptr: int,
+                    y_stride: int, y_dtype, m: int, n: int, k: int, fuse_relu: bool = False, work: int = 0,
+                    work_bytes: int = 0, stream: int = 0):
+    """Raw-pointer call, one to one with the C entry point."""
+    _check(lib().pconv_matmul_i8(a_ptr or None, a_stride, a_scale or None, b_ptr or None, b_stride, b_scale or None,
+                                 bias_ptr or None, y_ptr or None, y_stride, _DTYPE[y_dtype], m, n, k, int(bool(fuse_relu)),
+                                 work or None, work_bytes, stream or None))
+
+
+def pconv_linear_i8_workspace(m: int, n: int, k: int, x_dtype=F32) -> int:
+    return lib().pconv_linear_i8_workspace(m, n, k, _DTYPE[x_dtype])
+
+
+def pconv_linear_i8(x_ptr: int, x_stride: int, x_dtype, w_ptr: int, w_stride: int, w_scale: int, bias_ptr, y_ptr: int,
+                    y_stride: int, y_dtype, m: int, n: int, k: int, fuse_relu: bool = False, work: int = 0,
+                    work_bytes: int = 0, stream: int = 0):
+    """Raw-pointer call, one to one with the C entry point."""
+    _check(lib().pconv_linear_i8(x_ptr or None, x_stride, _DTYPE[x_dtype], w_ptr or None, w_stride, w_scale or None,
+                                 bias_ptr or None, y_ptr or None, y_stride, _DTYPE[y_dtype], m, n, k, int(bool(fuse_relu)),
+                                 work or None, work_bytes, stream or None))
+
+
+def quantize_rows(x):
+    """x: CUDA tensor [..., k], fp32 or bf16.  Returns (q [..., k] int8, scale [...] fp32): x is about q * scale[..., None].
+
+    The rows of q lie a multiple of 16 bytes apart, as matmul_i8 and linear_i8 read them fastest."""
+    import torch
+    dtype = _type_of(x, "x")
+    index = _device_index(x)
+    m, k, step = _rows(x, "x")
+    lead = tuple(x.shape[:-1])
+    wide = (k + 15) // 16 * 16
+    q = torch.empty(lead + (wide,), dtype=torch.int8, device=x.device)
+    scale = torch.empty(lead, dtype=torch.float32, device=x.device)
+    rc = (_lib or lib()).pconv_quantize_rows(x.data_ptr() or None, step, dtype, m, k, q.data_ptr() or None, wide,
+                                             scale.data_ptr() or None, _stream(index))
+    if rc != OK:
+        _check(rc)
+    return (q if wide == k else q[..., :k]), scale
+
+
+def matmul_i8(a, a_scale, b, b_scale, bias=None, relu: bool = False, out_dtype=None, out=None):
+    """a [..., k], b [n, k]: int8 CUDA tensors.  Returns act((a @ b.T) * a_scale[..., None] * b_scale + bias) [..., n].
+
+    a_scale [...], b_scale [n], bias [n]: fp32.  out_dtype: torch.float32 (unless `out` says otherwise) or torch.bfloat16."""
+    import torch
+    if a.dtype != torch.int8 or b.dtype != torch.int8 or b.dim() != 2:
+        raise ValueError("a [..., k] and b [n, k] must be int8")
+    index = _device_index(a, a_scale, b, b_scale, bias, out)
+    m, k, a_step = _rows(a, "a")
+    n, kb, b_step = _rows(b, "b")
+    if k != kb:
+        raise ValueError("a and b must have rows of one length")
+    if out_dtype is None:
+        out_dtype = out.dtype if out is not None else torch.float32
+    y, y_step = _output(out, tuple(a.shape[:-1]) + (n,), out_dtype, a)
+    y_type = _type_of(y, "out")
+    sa, sb = _per_channel(a_scale, m, "a_scale"), _per_channel(b_scale, n, "b_scale")
+    bp = _per_channel(bias, n, "bias") if bias is not None else None
+    L = _lib or lib()
+    size = L.pconv_matmul_i8_workspace(m, n, k)
+    work = _scratch(size, a) if size > 0 else None
+    rc = L.pconv_matmul_i8(a.data_ptr() or None, a_step, sa or None, b.data_ptr() or None, b_step, sb or None, bp or None,
+                           y.data_ptr() or None, y_step, y_type, m, n, k, 1 if relu else 0,
+                           work.data_ptr() if work is not None else None, size, _stream(index))
+    if rc != OK:
+        _check(rc)
+    return y
+
+
+def linear_i8(x, w, w_scale, bias=None, relu: bool = False, out_dtype=None, out=None):
+    """x [..., k]: CUDA tensor, fp32 or bf16; w [n, k] int8 and w_scale [n] as quantize_rows gives them for the weights.
+
+    Returns matmul_i8(*quantize_rows(x), w, w_scale, bias, relu) [..., n], of x's type unless `out_dtype` or `out` says
+    otherwise."""
+    import torch
+    x_type = _type_of(x, "x")
+    if w.dtype != torch.int8 or w.dim() != 2:
+        raise ValueError("w [n, k] must be int8")
+    index = _device_index(x, w, w_scale, bias, out)
+    m, k, x_step = _rows(x, "x")
+    n, kw, w_step = _rows(w, "w")
+    if k != kw:
+        raise ValueError("x and w must have rows of one length")
+    if out_dtype is None:
+        out_dtype = out.dtype if out is not None else x.dtype
+    y, y_step = _output(out, tuple(x.shape[:-1]) + (n,), out_dtype, x)
+    y_type = _type_of(y, "out")
+    sw = _per_channel(w_scale, n, "w_scale")
+    bp = _per_channel(bias, n, "bias") if bias is not None else None
+    L = _lib or lib()
+    size = L.pconv_linear_i8_workspace(m, n, k, x_type)
+    work = _scratch(size, x) if size > 0 else None
+    rc = L.pconv_linear_i8(x.data_ptr() or None, x_step, x_type, w.data_ptr() or None, w_step, sw or None, bp or None,
+                           y.data_ptr() or None, y_step, y_type, m, n, k, 1 if relu else 0,
+                           work.data_ptr() if work is not None else None, size, _stream(index))
+    if rc != OK:
+        _check(rc)
+    return y
+
+
+# ---- gradients of a training step ----------------------------------------------------------
+
+def pconv_grad_workspace(num: int) -> int:
+    return lib().pconv_grad_workspace(num)
+
+
+def pconv_grad_norm(grads, counts, dtypes, num: int, norm_ptr: int, work: int, work_bytes: int, stream: int = 0):
+    """Raw call, one to one with the C entry point; the first three are ctypes arrays."""
+    _check(lib().pconv_grad_norm(grads, counts, dtypes, num, norm_ptr or None, work or None, work_bytes, stream or None))
+
+
+def pconv_clip_grads(grads, outs, counts, dtypes, out_dtypes, num: int, max_norm: float, eps: float, norm_ptr: int, work: int,
+                     work_bytes: int, stream: int = 0):
+    """Raw call, one to one with the C entry point; the first five are ctypes arrays."""
+    _check(lib().pconv_clip_grads(grads, outs, counts, dtypes, out_dtypes, num, max_norm, eps, norm_ptr or None, work or None,
+                                  work_bytes, stream or None))
+
+
+def _dense(t) -> bool:
+    """Whether the tensor's elements fill one run of memory, each place once, in whatever order of dimensions."""
+    if t.is_contiguous():
+        return True
+    want = 1
+    for step, size in sorted((st, sz) for st, sz in zip(t.stride(), t.shape) if sz != 1):
+        if step != want:
+            return False
+        want *= size
+    return True
+
+
+class GradList:
+    """The gradients of a network's tensors, to be measured and limited together.
+
+    grads: CUDA tensors on one device, fp32 or bf16, each dense (contiguous in some order of its dimensions).  out: where
+    the limited gradients go, a tensor of the same shape and strides, fp32 or bf16, for each; without it they are
+    changed in place.  The list keeps the tensors: it is made once for buffers that stay (zero_grad(set_to_none=False)) and
+    again when they are replaced."""
+
+    def __init__(self, grads, out=None):
+        grads = list(grads)
+        outs = grads if out is None else list(out)
+        if len(outs) != len(grads):
+            raise ValueError("out must hold a tensor for each gradient")
+        self.grads, self.out = grads, outs
+        self._index = _device_index(*grads, *(outs if out is not None else ()))
+        for g, o in zip(grads, outs):
+            if not _dense(g):
+                raise ValueError("a gradient must be dense")
+            if o is not g and (o.shape != g.shape or (o.stride() != g.stride() and o.numel() > 1 and
+                                                      not (o.is_contiguous() and g.is_contiguous()))):
+                raise ValueError("an output must have the shape and the strides of its gradient")
+        num = self._num = len(grads)
+        types = [_type_of(g, "gradients") for g in grads]
+        out_types = [_type_of(o, "outputs") for o in outs]
+        self._counts = (C.c_int64 * num)(*(g.numel() for g in grads))
+        self._in = (C.c_void_p * num)(*(g.data_ptr() for g in grads))
+        self._to = (C.c_void_p * num)(*(o.data_ptr() for o in outs))
+        self._types, self._out_types = (C.c_int32 * num)(*types), (C.c_int32 * num)(*out_types)
+        self._refuse_overlaps(types, out_types)
+        self._size = lib().pconv_grad_workspace(num)
+
+    def _refuse_overlaps(self, types, out_types):
+        """No output may lie over another one, or over a gradient that is not its own."""
+        runs = []
+        for g, o, n, tg, to in zip(self._in, self._to, self._counts, types, out_types):
+            if n:
+                runs.append((o, o + n * (2 if to == BF16 else 4), True))
+                if (g, tg) != (o, to):
+                    runs.append((g, g + n * (2 if tg == BF16 else 4), False))
+        any_end = out_end = 0
+        for start, end, written in sorted(runs):
+            if start < (any_end if written else out_end):
+                raise ValueError("outputs overlap each other or other gradients")
+            any_end = max(any_end, end)
+            if written:
+                out_end = max(out_end, end)
+
+    def _begin(self):
+        import torch
+        if self._num == 0:
+            raise ValueError("the list is empty")
+        like = self.grads[0]
+        if self._index != torch.cuda.current_device():
+            raise ValueError("the tensors' device must be the current one")
+        work = _scratch(self._size, like)
+        return torch.empty((), dtype=torch.float32, device=like.device), work
+
+    def norm(self):
+        """The 2-norm of all gradients together, a tensor of one fp32 number on their device."""
+        norm, work = self._begin()
+        rc = (_lib or lib()).pconv_grad_norm(self._in, self._counts, self._types, self._num, norm.data_ptr(), work.data_ptr(),
+                                             self._size, _stream(self._index))
+        if rc != OK:
+            _check(rc)
+        return norm
+
+    def clip(self, max_norm: float, eps: float = 1e-6):
+        """Multiplies all gradients by min(1, max_norm / (norm + eps)).  Returns the norm, as norm() does."""
+        norm, work = self._begin()
+        rc = (_lib or lib()).pconv_clip_grads(self._in, self._to, self._counts, self._types, self._out_types, self._num,
+                                              max_norm, eps, norm.data_ptr(), work.data_ptr(), self._size,
+                                              _stream(self._index))
+        if rc != OK:
+            _check(rc)
+        return norm
+
+
+def grad_norm(grads):
+    """The 2-norm of all gradients together; see GradList."""
+    return GradList(grads).norm()
+
+
+def clip_grad_norm(grads, max_norm: float, eps: float = 1e-6, out=None):
+    """Limits the norm of all gradients together, in place unless `out` says otherwise; see GradList.  Returns the norm."""
+    return GradList(grads, out).clip(max_norm, eps)

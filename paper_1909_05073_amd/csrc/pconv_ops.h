@@ -1,0 +1,44 @@
+// What pconv_ops_capi.cpp and the kernels of the 8-bit layers and the gradients share.
+#ifndef PCONV_OPS_H
+#define PCONV_OPS_H
+
+#include <cstdint>
+
+#include "pconv.h"
+
+namespace pconv {
+
+// y [m][n] = act((a [m][k] . b [n][k]) * (sa[m] * sb[n]) + bias[n]); strides in elements (those of a and b in bytes too).
+struct I8Product {
+    const int8_t *a, *b;
+    const float *sa, *sb, *bias;
+    void *y;
+    int64_t lda, ldb, ldy;
+    int m, n, k;
+    int relu, y_bf16;
+};
+
+// Launchers: arguments checked, sizes not 0.  They return a pconv_status.
+int launch_quantize_rows(const void *x, int64_t ldx, int bf16, int64_t rows, int64_t cols, int8_t *q, int64_t ldq,
+                         int64_t q_cols, float *scale, void *stream);
+int launch_matmul_i8(const I8Product &p, void *stream);
+
+// Up to kGradTensors tensors travel in the arguments of one launch (4 KiB).
+constexpr int kGradTensors = 160, kGradChunk = 16384, kGradBlocks = 2048;
+struct GradTable {
+    const void *in[kGradTensors];
+    void *out[kGradTensors];
+    uint32_t start[kGradTensors];      // first chunk of the tensor (ascending)
+    uint16_t last[kGradTensors];       // elements of its last chunk, less one
+    uint16_t types[kGradTensors];      // bit 0: input bf16, bit 1: output bf16
+    int32_t count;
+    uint32_t chunks;
+};
+int launch_grad_norm(const GradTable &t, unsigned blocks, double *partials, void *stream);
+int launch_grad_total(const double *partials, unsigned count, double *total, float *norm, void *stream);
+int launch_grad_scale(const GradTable &t, unsigned blocks, const double *partials, unsigned count, float max_norm, float eps,
+                      float *norm, void *stream);
+
+}  // namespace pconv
+
+#endif

@@ -1,0 +1,204 @@
+// extern "C" boundary of the 8-bit layers and the gradients (see include/pconv.h for the contract).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+
+#include "pconv_internal.h"
+#include "pconv_ops.h"
+
+using namespace pconv;
+
+namespace {
+
+constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1, kMaxK = 131071;
+constexpr int64_t kMaxTensors = 1 << 24, kMaxElements = int64_t(1) << 45;    // fewer than 2^32 chunks together
+
+int invalid(const char *who, const char *what)
+{
+    set_error(std::string(who) + ": " + what);
+    return PCONV_INVALID_ARG;
+}
+
+bool is_dtype(int t) { return t == PCONV_F32 || t == PCONV_BF16; }
+int64_t round16(int64_t v) { return (v + 15) / 16 * 16; }
+
+// rows of `len` elements that lie `stride` apart: within the range of a byte offset in 64 bits
+bool stride_fits(int64_t rows, int64_t len, int64_t stride) { return stride >= len && stride <= (int64_t(1) << 58) / (rows > 0 ? rows : 1); }
+
+// What both products check of their weights and outputs, and the product itself but for its activations.
+int check_product(const char *who, const int8_t *b, int64_t ldb, const float *sb, const float *bias, void *y, int64_t ldy, int y_dtype,
+                  int64_t m, int64_t n, int64_t k, int relu, I8Product &p)
+{
+    if (m < 0 || n < 0 || k < 0 || m > kMaxRows || n > kMaxRows) return invalid(who, "m and n must be 0 .. 2^31 - 1");
+    if (k > kMaxK) return invalid(who, "k must be 0 .. 131071");
+    if (!is_dtype(y_dtype)) return invalid(who, "unknown dtype of y");
+    if (m == 0 || n == 0) return PCONV_OK;
+    if (!sb || !y || (k && !b)) return invalid(who, "null pointer argument");
+    if (!stride_fits(n, k, ldb) || !stride_fits(m, n, ldy)) return invalid(who, "rows must lie at least their length apart");
+    p = I8Product{nullptr, b, nullptr, sb, bias, y, 0, ldb, ldy, int(m), int(n), int(k), relu ? 1 : 0, y_dtype == PCONV_BF16};
+    return PCONV_OK;
+}
+
+// A table of up to kGradTensors of the tensors from `at` on, which moves there; false where there are none left.
+bool next_table(const void *const *in, void *const *out, const int64_t *counts, const int32_t *types, const int32_t *out_types,
+                int64_t num, int64_t &at, GradTable &t)
+{
+    t.count = 0; t.chunks = 0;
+    for (; at < num && t.count < kGradTensors; ++at) {
+        const int64_t n = counts[at];
+        if (n == 0) continue;
+        const int64_t chunks = (n + kGradChunk - 1) / kGradChunk;
+        const int i = t.count++;
+        t.in[i] = in[at];
+        t.out[i] = out ? out[at] : nullptr;
+        t.start[i] = t.chunks;
+        t.last[i] = uint16_t((n - 1) % kGradChunk);
+        t.types[i] = uint16_t((types[at] == PCONV_BF16 ? 1 : 0) | (out && out_types[at] == PCONV_BF16 ? 2 : 0));
+        t.chunks += uint32_t(chunks);
+    }
+    return t.count > 0;
+}
+
+int check_grads(const char *who, const void *const *in, const int64_t *counts, const int32_t *types, int64_t num, float *norm,
+                void *work, int64_t work_bytes)
+{
+    if (num < 0 || num > kMaxTensors) return invalid(who, "num must be 0 .. 2^24");
+    if (!norm || !work || (num && (!in || !counts || !types))) return invalid(who, "null pointer argument");
+    if (reinterpret_cast<uintptr_t>(work) % 16 != 0) return invalid(who, "the work space must be aligned to 16 bytes");
+    if (work_bytes < pconv_grad_workspace(num)) return invalid(who, "the work space is too small");
+    int64_t total = 0;
+    for (int64_t i = 0; i < num; ++i) {
+        if (counts[i] < 0 || counts[i] > kMaxElements || (total += counts[i]) > kMaxElements) return invalid(who, "counts must be 0 .. 2^45, and so their sum");
+        if (counts[i] && !in[i]) return invalid(who, "null pointer of a tensor");
+        if (!is_dtype(types[i])) return invalid(who, "unknown dtype of a tensor");
+        if (reinterpret_cast<uintptr_t>(in[i]) % (types[i] == PCONV_BF16 ? 2 : 4) != 0) return invalid(who, "a tensor must be aligned to its type");
+    }
+    return PCONV_OK;
+}
+
+// The sums of squares of all tables, to work[1 ..]; how many there are.
+int sum_squares(const void *const *in, const int64_t *counts, const int32_t *types, int64_t num, double *work, void *stream,
+                unsigned &sums, int &tables)
+{
+    const int64_t most = (num + kGradTensors - 1) / kGradTensors;
+    const unsigned cap = most <= 1 ? unsigned(kGradBlocks) : unsigned(std::max<int64_t>(64, kGradBlocks / most));
+    sums = 0; tables = 0;
+    GradTable t;
+    for (int64_t at = 0; next_table(in, nullptr, counts, types, nullptr, num, at, t); ++tables) {
+        const unsigned blocks = std::min(t.chunks, cap);
+        if (const int rc = launch_grad_norm(t, blocks, work + 1 + sums, stream)) return rc;
+        sums += blocks;
+    }
+    return PCONV_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int pconv_quantize_rows(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, int64_t rows, int64_t cols,
+                        int8_t *q_dev, int64_t q_stride, float *scale_dev, void *hip_stream)
+{
+    const char *who = "pconv_quantize_rows";
+    if (rows < 0 || cols < 0 || rows > kMaxRows || cols > kMaxRows) return invalid(who, "rows and cols must be 0 .. 2^31 - 1");
+    if (!is_dtype(int(x_dtype))) return invalid(who, "unknown dtype");
+    if (rows == 0) return PCONV_OK;
+    if (!scale_dev || (cols && (!x_dev || !q_dev))) return invalid(who, "null pointer argument");
+    if (!stride_fits(rows, cols, x_stride) || !stride_fits(rows, cols, q_stride)) return invalid(who, "rows must lie at least their length apart");
+    return launch_quantize_rows(x_dev, x_stride, x_dtype == PCONV_BF16, rows, cols, q_dev, q_stride, cols, scale_dev, hip_stream);
+}
+
+int64_t pconv_matmul_i8_workspace(int64_t, int64_t, int64_t) { return 0; }
+
+int pconv_matmul_i8(const int8_t *a_dev, int64_t a_stride, const float *a_scale, const int8_t *b_dev, int64_t b_stride,
+                    const float *b_scale, const float *bias_dev, void *y_dev, int64_t y_stride, pconv_dtype y_dtype,
+                    int64_t m, int64_t n, int64_t k, int fuse_relu, void *, int64_t, void *hip_stream)
+{
+    const char *who = "pconv_matmul_i8";
+    I8Product p;
+    if (const int rc = check_product(who, b_dev, b_stride, b_scale, bias_dev, y_dev, y_stride, int(y_dtype), m, n, k, fuse_relu, p)) return rc;
+    if (m == 0 || n == 0) return PCONV_OK;
+    if (!a_scale || (k && !a_dev)) return invalid(who, "null pointer argument");
+    if (!stride_fits(m, k, a_stride)) return invalid(who, "rows must lie at least their length apart");
+    p.a = a_dev; p.lda = a_stride; p.sa = a_scale;
+    return launch_matmul_i8(p, hip_stream);
+}
+
+int64_t pconv_linear_i8_workspace(int64_t m, int64_t, int64_t k, pconv_dtype)
+{
+    return m > 0 && k >= 0 && m <= kMaxRows && k <= kMaxK ? round16(4 * m) + m * round16(k) : 0;
+}
+
+int pconv_linear_i8(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, const int8_t *w_dev, int64_t w_stride,
+                    const float *w_scale, const float *bias_dev, void *y_dev, int64_t y_stride, pconv_dtype y_dtype,
+                    int64_t m, int64_t n, int64_t k, int fuse_relu, void *work, int64_t work_bytes, void *hip_stream)
+{
+    const char *who = "pconv_linear_i8";
+    if (!is_dtype(int(x_dtype))) return invalid(who, "unknown dtype of x");
+    I8Product p;
+    if (const int rc = check_product(who, w_dev, w_stride, w_scale, bias_dev, y_dev, y_stride, int(y_dtype), m, n, k, fuse_relu, p)) return rc;
+    if (m == 0 || n == 0) return PCONV_OK;
+    if (k && !x_dev) return invalid(who, "null pointer argument");
+    if (!stride_fits(m, k, x_stride)) return invalid(who, "rows must lie at least their length apart");
+    const int64_t need = pconv_linear_i8_workspace(m, n, k, x_dtype);
+    if (need > 0 && (!work || work_bytes < need)) return invalid(who, "the work space is too small");
+    if (reinterpret_cast<uintptr_t>(work) % 16 != 0) return invalid(who, "the work space must be aligned to 16 bytes");
+    float *const scale = static_cast<float *>(work);
+    int8_t *const q = static_cast<int8_t *>(work) + round16(4 * m);
+    const int64_t ldq = round16(k);
+    if (const int rc = launch_quantize_rows(x_dev, x_stride, x_dtype == PCONV_BF16, m, k, q, ldq, ldq, scale, hip_stream)) return rc;
+    p.a = q; p.lda = ldq; p.sa = scale;
+    return launch_matmul_i8(p, hip_stream);
+}
+
+int64_t pconv_grad_workspace(int64_t num)
+{
+    // one sum for the total, and those of the launches: of kGradBlocks workgroups together, at least 64 each
+    const int64_t tables = (std::max<int64_t>(num, 0) + kGradTensors - 1) / kGradTensors;
+    return 16 + 8 * std::max<int64_t>(kGradBlocks, 64 * (2 * tables + 1));
+}
+
+int pconv_grad_norm(const void *const *grads, const int64_t *counts, const int32_t *dtypes, int64_t num,
+                    float *norm_dev, void *work, int64_t work_bytes, void *hip_stream)
+{
+    if (const int rc = check_grads("pconv_grad_norm", grads, counts, dtypes, num, norm_dev, work, work_bytes)) return rc;
+    double *const sums = static_cast<double *>(work);
+    unsigned count; int tables;
+    if (const int rc = sum_squares(grads, counts, dtypes, num, sums, hip_stream, count, tables)) return rc;
+    return launch_grad_total(sums + 1, count, sums, norm_dev, hip_stream);
+}
+
+int pconv_clip_grads(const void *const *grads, void *const *outs, const int64_t *counts, const int32_t *dtypes,
+                     const int32_t *out_dtypes, int64_t num, float max_norm, float eps, float *norm_dev,
+                     void *work, int64_t work_bytes, void *hip_stream)
+{
+    const char *who = "pconv_clip_grads";
+    if (const int rc = check_grads(who, grads, counts, dtypes, num, norm_dev, work, work_bytes)) return rc;
+    if (num && (!outs || !out_dtypes)) return invalid(who, "null pointer argument");
+    if (!(max_norm >= 0.0f)) return invalid(who, "max_norm must be at least 0");
+    if (!(eps >= 0.0f) || std::isinf(eps)) return invalid(who, "eps must be a number of at least 0");
+    for (int64_t i = 0; i < num; ++i) {
+        if (counts[i] && !outs[i]) return invalid(who, "null pointer of an output");
+        if (!is_dtype(out_dtypes[i])) return invalid(who, "unknown dtype of an output");
+        if (reinterpret_cast<uintptr_t>(outs[i]) % (out_dtypes[i] == PCONV_BF16 ? 2 : 4) != 0) return invalid(who, "an output must be aligned to its type");
+        if (counts[i] && outs[i] == grads[i] && out_dtypes[i] != dtypes[i]) return invalid(who, "an output in its gradient's place must have its type");
+    }
+    double *const sums = static_cast<double *>(work);
+    unsigned count; int tables;
+    if (const int rc = sum_squares(grads, counts, dtypes, num, sums, hip_stream, count, tables)) return rc;
+    const double *from = sums + 1;
+    if (tables != 1) {                                   // (none: the norm of nothing is 0)
+        if (const int rc = launch_grad_total(from, count, sums, norm_dev, hip_stream)) return rc;
+        from = sums; count = 1;
+    }
+    GradTable t;
+    for (int64_t at = 0; next_table(grads, outs, counts, dtypes, out_dtypes, num, at, t);) {
+        const unsigned blocks = std::min(t.chunks, unsigned(kGradBlocks));
+        if (const int rc = launch_grad_scale(t, blocks, from, count, max_norm, eps, tables == 1 ? norm_dev : nullptr, hip_stream)) return rc;
+    }
+    return PCONV_OK;
+}
+
+}  // extern "C"
