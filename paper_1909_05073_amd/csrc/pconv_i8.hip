@@ -18,6 +18,7 @@ namespace pconv {
 namespace {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef __bf16 b4 __attribute__((ext_vector_type(4)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
@@ -206,19 +207,37 @@ __device__ __forceinline__ v4i load16(const int8_t *row, int at, int len)
     return v;
 }
 
-// Four neighbouring channels of one row of y.  ReLU keeps NaN.
-__device__ __forceinline__ void finish(const I8Product &p, int m, int n, v4i acc, bool wide)
+// Four neighbouring channels of one row of y, from n on.  ReLU keeps NaN.
+struct Channels { f4 scale, bias; };
+
+__device__ __forceinline__ Channels channels_at(const I8Product &p, int n)
+{
+    Channels c;
+    if (n + 4 <= p.n) {
+        __builtin_memcpy(&c.scale, p.sb + n, 16);
+        if (p.bias) __builtin_memcpy(&c.bias, p.bias + n, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int at = min(n + i, p.n - 1);
+            c.scale[i] = p.sb[at];
+            if (p.bias) c.bias[i] = p.bias[at];
+        }
+    }
+    if (!p.bias) c.bias = f4{0, 0, 0, 0};
+    return c;
+}
+
+__device__ __forceinline__ void finish(const I8Product &p, int m, int n, v4i acc, float sa, const Channels &c)
 {
     if (m >= p.m || n >= p.n) return;
-    const float sa = p.sa[m];
     f4 v;
-    const int have = min(4, p.n - n);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int at = min(n + i, p.n - 1);
-        v[i] = float(acc[i]) * (sa * p.sb[at]) + (p.bias ? p.bias[at] : 0.0f);
+        v[i] = float(acc[i]) * (sa * c.scale[i]) + c.bias[i];
         if (p.relu) v[i] = v[i] < 0.0f ? 0.0f : v[i];
     }
+    const int have = min(4, p.n - n);
     const int64_t to = int64_t(m) * p.ldy + n;
     if (p.y_bf16) {
         __bf16 *y = static_cast<__bf16 *>(p.y) + to;
@@ -232,85 +251,225 @@ __device__ __forceinline__ void finish(const I8Product &p, int m, int n, v4i acc
     }
 }
 
-// Tiles of BM rows of y and BN channels, WM x WN waves; stages of BK bytes of k pass through LDS, two at a time.  A
-// row of a stage is eight pieces of 16 bytes, stored in an order that depends on the row so that the eight rows that
-// are read at once lie in different banks.
-template <int BM, int BN, int WM, int WN>
-__global__ void __launch_bounds__(WM * WN * 64)
-matmul_i8_kernel(const I8Product p)
+__device__ __forceinline__ v4u buffer_at(const int8_t *p)
 {
-    constexpr int BK = 128, THREADS = WM * WN * 64, TM = BM / WM, TN = BN / WN, MT = TM / 16, NT = TN / 16;
-    constexpr int PA = BM * 8 / THREADS, PB = BN * 8 / THREADS;
-    __shared__ v4i lds[2][(BM + BN) * 8];
-    const int tid = int(threadIdx.x), lane = tid & 63, wave = tid >> 6;
-    const int tiles_n = (p.n + BN - 1) / BN;
-    const int m0 = int(blockIdx.x / unsigned(tiles_n)) * BM, n0 = int(blockIdx.x % unsigned(tiles_n)) * BN;
-    const int wm = (wave / WN) * TM, wn = (wave % WN) * TN;
+    const uint64_t at = reinterpret_cast<uint64_t>(p);
+    v4u r;
+    r.x = __builtin_amdgcn_readfirstlane(uint32_t(at));
+    r.y = __builtin_amdgcn_readfirstlane(uint32_t(at >> 32) & 0xFFFFu);
+    r.z = 0xFFFFFFFFu;
+    r.w = 0x00020000u;
+    return r;
+}
 
-    v4i ra[PA], rb[PB];
-    auto fetch = [&](int k0) {
-#pragma unroll
-        for (int i = 0; i < PA; ++i) {
-            const int at = i * THREADS + tid, row = min(m0 + at / 8, p.m - 1);
-            ra[i] = load16(p.a + int64_t(row) * p.lda, k0 + (at & 7) * 16, p.k);
-        }
-#pragma unroll
-        for (int i = 0; i < PB; ++i) {
-            const int at = i * THREADS + tid, row = min(n0 + at / 8, p.n - 1);
-            rb[i] = load16(p.b + int64_t(row) * p.ldb, k0 + (at & 7) * 16, p.k);
-        }
-    };
-    auto store = [&](int buf) {
-#pragma unroll
-        for (int i = 0; i < PA; ++i) {
-            const int at = i * THREADS + tid, row = at / 8;
-            lds[buf][row * 8 + ((at & 7) ^ (row & 7))] = ra[i];
-        }
-#pragma unroll
-        for (int i = 0; i < PB; ++i) {
-            const int at = i * THREADS + tid, row = at / 8;
-            lds[buf][BM * 8 + row * 8 + ((at & 7) ^ (row & 7))] = rb[i];
-        }
-    };
+// Which tile a workgroup computes.  Workgroups go round the 8 XCDs, each of which has a level-2 cache of its own: an XCD gets
+// a run of tiles, and a run goes down GROUP tiles of rows before it goes on to the next tile of channels, so that the tiles that
+// run at one time on an XCD share rows of both operands.
+__device__ __forceinline__ void tile_at(unsigned id, unsigned tiles_m, unsigned tiles_n, unsigned &tm, unsigned &tn)
+{
+    constexpr unsigned XCDS = 8, GROUP = 8;
+    const unsigned all = tiles_m * tiles_n, x = id % XCDS, per = all / XCDS, more = all % XCDS;
+    const unsigned t = x * per + min(x, more) + id / XCDS;
+    const unsigned g = t / (GROUP * tiles_n), in = t % (GROUP * tiles_n), rows = min(GROUP, tiles_m - g * GROUP);
+    tm = g * GROUP + in % rows;
+    tn = in / rows;
+}
+
+// Tiles of BM rows of y and BN channels, WM x WN waves.  128 bytes of k of all the tile's rows are a stage; S stages lie in
+// LDS.  A row of a stage is eight pieces of 16 bytes, stored in an order that depends on the row so that the eight rows that are
+// read at once lie in different banks.
+//
+// DMA: stages go from memory to LDS past the registers, S - 1 of them ahead of the one that is multiplied; a wave waits for its own
+// loads of the next stage, and the barrier then tells it that everybody's are there and that the stage before is read.  What
+// is left of k behind the last whole stage goes through registers, and so does everything where rows do not begin at
+// multiples of 16 bytes (DMA = false; one stage ahead).
+//
+// A wave's channels are dealt to the matrix instructions so that a lane holds 4 * NG neighbouring ones.
+//
+// `splits` workgroups share a tile, each with its part of k; their sums go to `part` [splits][m][n4], n4 = n rounded up to four.
+template <int BM, int BN, int WM, int WN, int S, bool DMA>
+__global__ void __launch_bounds__(WM * WN * 64)
+matmul_i8_kernel(const I8Product p, int splits, int *part)
+{
+    constexpr int BK = 128, NW = WM * WN, TM = BM / WM, TN = BN / WN, MT = TM / 16, NT = TN / 16;
+    constexpr int NG = NT < 4 ? NT : 4, SH = NG == 4 ? 4 : NG == 2 ? 3 : 2;
+    constexpr int PA = BM / 8 / NW, PB = BN / 8 / NW;    // blocks of eight rows that a wave stages
+    static_assert(PA * NW * 8 == BM && PB * NW * 8 == BN && NT % NG == 0, "");
+    __shared__ v4i lds[S * (BM + BN) * 8];
+    constexpr int STAGE = (BM + BN) * 8;
+    const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const unsigned tiles_n = unsigned(p.n + BN - 1) / BN, tiles_m = unsigned(p.m + BM - 1) / BM;
+    unsigned tm, tn;
+    tile_at(blockIdx.x / unsigned(splits), tiles_m, tiles_n, tm, tn);
+    const int split = int(blockIdx.x % unsigned(splits));
+    const int m0 = int(tm) * BM, n0 = int(tn) * BN;
+    const int wm = (wave / WN) * TM, wn = (wave % WN) * TN;
+    // this workgroup's part of k: whole stages but for the last one's end
+    const int stages = (p.k + BK - 1) / BK;
+    const int s_begin = int(int64_t(stages) * split / splits), s_end = int(int64_t(stages) * (split + 1) / splits);
+    const int k_begin = s_begin * BK, k_end = min(s_end * BK, p.k);
+
+    // order of the pieces of a row of weights: bits 0, 1 and SH of the row tell the rows that are read at once apart
+    auto key_b = [](int row) { return (row & 3) | (((row >> SH) & 1) << 2); };
+
     v4i acc[MT][NT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = v4i{0, 0, 0, 0};
-    fetch(0);
-    store(0);
-    __syncthreads();
-    int buf = 0;
-    for (int k0 = 0; k0 < p.k; k0 += BK, buf ^= 1) {
-        const bool more = k0 + BK < p.k;
-        if (more) fetch(k0 + BK);
+
+    auto multiply = [&](const v4i *st) {
 #pragma unroll
         for (int kk = 0; kk < 2; ++kk) {
             v4i a[MT], b[NT];
-            const int piece = kk * 4 + (lane >> 4);
+            const int piece = kk * 4 + (lane >> 4), r = lane & 15;
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
-                const int row = wm + i * 16 + (lane & 15);
-                a[i] = lds[buf][row * 8 + (piece ^ (row & 7))];
+                const int row = wm + i * 16 + r;
+                a[i] = st[row * 8 + (piece ^ (row & 7))];
             }
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                const int row = wn + j * 16 + (lane & 15);
-                b[j] = lds[buf][BM * 8 + row * 8 + (piece ^ (row & 7))];
+                const int row = wn + (j / NG) * (16 * NG) + (r >> 2) * (4 * NG) + (j % NG) * 4 + (r & 3);
+                b[j] = st[BM * 8 + row * 8 + (piece ^ key_b(row))];
             }
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
                 for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b[j], a[i], acc[i][j], 0, 0, 0);
         }
-        if (more) store(buf ^ 1);
+    };
+
+    // through registers: a thread fetches the pieces at its place in every block of eight rows
+    v4i ra[PA], rb[PB];
+    auto fetch = [&](int k0) {
+        const int at = k0 + (lane & 7) * 16;
+#pragma unroll
+        for (int i = 0; i < PA; ++i) {
+            const int row = min(m0 + (i * NW + wave) * 8 + (lane >> 3), p.m - 1);
+            ra[i] = load16(p.a + int64_t(row) * p.lda, at, k_end);
+        }
+#pragma unroll
+        for (int i = 0; i < PB; ++i) {
+            const int row = min(n0 + (i * NW + wave) * 8 + (lane >> 3), p.n - 1);
+            rb[i] = load16(p.b + int64_t(row) * p.ldb, at, k_end);
+        }
+    };
+    auto store = [&](v4i *st) {
+#pragma unroll
+        for (int i = 0; i < PA; ++i) {
+            const int row = (i * NW + wave) * 8 + (lane >> 3);
+            st[row * 8 + ((lane & 7) ^ (row & 7))] = ra[i];
+        }
+#pragma unroll
+        for (int i = 0; i < PB; ++i) {
+            const int row = (i * NW + wave) * 8 + (lane >> 3);
+            st[BM * 8 + row * 8 + ((lane & 7) ^ key_b(row))] = rb[i];
+        }
+    };
+
+    if (DMA) {
+        const v4u at_a = buffer_at(p.a + int64_t(m0) * p.lda + k_begin), at_b = buffer_at(p.b + int64_t(n0) * p.ldb + k_begin);
+        uint32_t off_a[PA], off_b[PB];
+#pragma unroll
+        for (int i = 0; i < PA; ++i) {
+            const int row = (i * NW + wave) * 8 + (lane >> 3);
+            off_a[i] = uint32_t(min(row, p.m - 1 - m0)) * uint32_t(p.lda) + uint32_t(((lane & 7) ^ (row & 7)) * 16);
+        }
+#pragma unroll
+        for (int i = 0; i < PB; ++i) {
+            const int row = (i * NW + wave) * 8 + (lane >> 3);
+            off_b[i] = uint32_t(min(row, p.n - 1 - n0)) * uint32_t(p.ldb) + uint32_t(((lane & 7) ^ key_b(row)) * 16);
+        }
+        const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds)) + uint32_t(wave) * 1024u;
+        // (written as assembly so that the compiler does not wait for these loads before every read of LDS)
+        auto stage = [&](int s) {
+            const uint32_t to = base + uint32_t(s % S) * uint32_t(STAGE * 16), k0 = uint32_t(s) * BK;
+#pragma unroll
+            for (int i = 0; i < PA; ++i)
+                asm volatile("s_mov_b32 m0, %1\n s_nop 0\n buffer_load_dwordx4 %0, %2, %3 offen lds"
+                             ::"v"(off_a[i]), "s"(to + uint32_t(i * NW * 1024)), "s"(at_a), "s"(k0) : "memory");
+#pragma unroll
+            for (int i = 0; i < PB; ++i)
+                asm volatile("s_mov_b32 m0, %1\n s_nop 0\n buffer_load_dwordx4 %0, %2, %3 offen lds"
+                             ::"v"(off_b[i]), "s"(to + uint32_t(BM * 128 + i * NW * 1024)), "s"(at_b), "s"(k0) : "memory");
+        };
+        constexpr int L = PA + PB;
+        static_assert((S - 2) * L <= 63, "");
+        const int whole = (k_end - k_begin) / BK;
+#pragma unroll
+        for (int s = 0; s < S - 1; ++s)
+            if (s < whole) stage(s);
+        for (int s = 0; s < whole; ++s) {
+            // the loads of stage s are done when at most those of the stages behind it are under way
+            const int behind = min(S - 2, whole - 1 - s);
+            if (behind == S - 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n s_barrier" ::"n"((S - 2) * L) : "memory");
+            else if (S > 3 && behind == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n s_barrier" ::"n"(L) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n s_barrier" ::: "memory");
+            if (s + S - 1 < whole) stage(s + S - 1);
+            multiply(lds + (s % S) * STAGE);
+        }
+        if (k_begin + whole * BK < k_end) {
+            fetch(k_begin + whole * BK);
+            __syncthreads();
+            store(lds);
+            __syncthreads();
+            multiply(lds);
+        }
+    } else {
+        if (k_begin < k_end) {
+            fetch(k_begin);
+            store(lds);
+        }
         __syncthreads();
+        int buf = 0;
+        for (int k0 = k_begin; k0 < k_end; k0 += BK, buf ^= 1) {
+            const bool more = k0 + BK < k_end;
+            if (more) fetch(k0 + BK);
+            multiply(lds + buf * STAGE);
+            if (more) store(lds + (buf ^ 1) * STAGE);
+            __syncthreads();
+        }
     }
+
+    const int r = lane & 15;
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+    for (int j = 0; j < NT; ++j) {
+        const int n = n0 + wn + (j / NG) * (16 * NG) + (lane >> 4) * (4 * NG) + (j % NG) * 4;
+        if (splits > 1) {
+            const int64_t n4 = (int64_t(p.n) + 3) / 4 * 4;
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
-            finish(p, m0 + wm + i * 16 + (lane & 15), n0 + wn + j * 16 + (lane >> 4) * 4, acc[i][j], true);
+            for (int i = 0; i < MT; ++i) {
+                const int m = m0 + wm + i * 16 + r;
+                if (m < p.m && n < p.n) __builtin_memcpy(part + (int64_t(split) * p.m + m) * n4 + n, &acc[i][j], 16);
+            }
+            continue;
+        }
+        const Channels c = channels_at(p, n);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const int m = m0 + wm + i * 16 + r;
+            finish(p, m, n, acc[i][j], p.sa[min(m, p.m - 1)], c);
+        }
+    }
+}
+
+// y of the sums of `splits` parts of k; a thread has four channels.
+__global__ void __launch_bounds__(256)
+matmul_i8_join_kernel(const I8Product p, int splits, const int *__restrict__ part)
+{
+    const int64_t quads = (int64_t(p.n) + 3) / 4, all = quads * p.m;
+    for (int64_t t = int64_t(blockIdx.x) * 256 + threadIdx.x; t < all; t += int64_t(gridDim.x) * 256) {
+        const int m = int(t / quads), n = int(t % quads) * 4;
+        v4i s = {0, 0, 0, 0};
+#pragma unroll 4
+        for (int i = 0; i < splits; ++i) {
+            v4i v;
+            __builtin_memcpy(&v, part + (int64_t(i) * all + t) * 4, 16);
+            s += v;
+        }
+        finish(p, m, n, s, p.sa[m], channels_at(p, n));
+    }
 }
 
 // Few rows: 16 channels a workgroup, whose waves share the length of k in steps of 256 bytes and add their sums in LDS.
@@ -349,7 +508,8 @@ matmul_i8_rows_kernel(const I8Product p)
         v4i s = lds[0][i][lane];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) s += lds[w][i][lane];
-        finish(p, i * 16 + (lane & 15), n0 + (lane >> 4) * 4, s, true);
+        const int m = i * 16 + (lane & 15), n = n0 + (lane >> 4) * 4;
+        finish(p, m, n, s, p.sa[min(m, p.m - 1)], channels_at(p, n));
     }
 }
 
@@ -377,20 +537,68 @@ int launch_quantize_rows(const void *x, int64_t ldx, int bf16, int64_t rows, int
     return check_launch("pconv_quantize_rows");
 }
 
-int launch_matmul_i8(const I8Product &p, void *stream)
+namespace {
+
+// How a product of more rows than matmul_i8_rows_kernel serves is cut up: the tile (an index into launch_tiles) and over how
+// many workgroups the length of k is split.
+struct Cut { int tile, splits; };
+
+constexpr int kTileM[] = {32, 64, 128, 256}, kTileN[] = {128, 128, 128, 256};
+
+Cut cut_of(int64_t m, int64_t n, int64_t k)
+{
+    const auto tiles = [&](int t) { return ((m + kTileM[t] - 1) / kTileM[t]) * ((n + kTileN[t] - 1) / kTileN[t]); };
+    Cut c{m <= 32 ? 0 : m <= 64 ? 1 : 2, 1};
+    if (tiles(3) >= 256) c.tile = 3;
+    else if (c.tile == 2 && tiles(2) < 256 && tiles(1) >= 2 * tiles(2) && tiles(1) <= 512) c.tile = 1;
+    const int64_t stages = (k + 127) / 128;
+    if (tiles(c.tile) <= 128 && stages >= 8)
+        c.splits = int(std::min<int64_t>(std::min<int64_t>(256 / tiles(c.tile), stages / 4), 32));
+    return c;
+}
+
+template <int BM, int BN, int WM, int WN, int S>
+void launch_tiles(const I8Product &p, int splits, int *part, bool dma, hipStream_t st)
+{
+    const unsigned grid = unsigned(((int64_t(p.m) + BM - 1) / BM) * ((int64_t(p.n) + BN - 1) / BN) * splits);
+    if (dma) hipLaunchKernelGGL((matmul_i8_kernel<BM, BN, WM, WN, S, true>), dim3(grid), dim3(WM * WN * 64), 0, st, p, splits, part);
+    else hipLaunchKernelGGL((matmul_i8_kernel<BM, BN, WM, WN, 2, false>), dim3(grid), dim3(WM * WN * 64), 0, st, p, splits, part);
+}
+
+constexpr int64_t kRowsM = 16;                           // matmul_i8_rows_kernel serves up to so many rows
+
+}  // namespace
+
+int64_t matmul_i8_part_bytes(int64_t m, int64_t n, int64_t k)
+{
+    if (m <= kRowsM) return 0;
+    const Cut c = cut_of(m, n, k);
+    return c.splits > 1 ? c.splits * m * ((n + 3) / 4 * 4) * 4 : 0;
+}
+
+int launch_matmul_i8(const I8Product &p, void *part, void *stream)
 {
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (p.m <= 64) {
-        const unsigned grid = unsigned((p.n + 15) / 16);
-        if (p.m <= 16) hipLaunchKernelGGL((matmul_i8_rows_kernel<1, 8>), dim3(grid), dim3(512), 0, st, p);
-        else if (p.m <= 32) hipLaunchKernelGGL((matmul_i8_rows_kernel<2, 8>), dim3(grid), dim3(512), 0, st, p);
-        else hipLaunchKernelGGL((matmul_i8_rows_kernel<4, 8>), dim3(grid), dim3(512), 0, st, p);
+    if (p.m <= kRowsM) {
+        hipLaunchKernelGGL((matmul_i8_rows_kernel<1, 8>), dim3(unsigned((p.n + 15) / 16)), dim3(512), 0, st, p);
         return check_launch("pconv_matmul_i8 (few rows)");
     }
-    const int64_t tiles = ((int64_t(p.m) + 127) / 128) * ((int64_t(p.n) + 127) / 128);
-    if (tiles >= int64_t(1) << 24) { set_error("pconv_matmul_i8: too many workgroups"); return PCONV_UNSUPPORTED; }
-    hipLaunchKernelGGL((matmul_i8_kernel<128, 128, 2, 2>), dim3(unsigned(tiles)), dim3(256), 0, st, p);
-    return check_launch("pconv_matmul_i8");
+    const Cut c = cut_of(p.m, p.n, p.k);
+    const int64_t tiles = ((int64_t(p.m) + kTileM[c.tile] - 1) / kTileM[c.tile]) * ((int64_t(p.n) + kTileN[c.tile] - 1) / kTileN[c.tile]);
+    if (tiles * c.splits >= int64_t(1) << 23) { set_error("pconv_matmul_i8: too many workgroups"); return PCONV_UNSUPPORTED; }
+    // rows at multiples of 16 bytes, a tile's rows within 32 bits
+    const auto fits = [](const int8_t *at, int64_t ld) { return reinterpret_cast<uintptr_t>(at) % 16 == 0 && ld % 16 == 0 && ld <= 1 << 23; };
+    const bool dma = fits(p.a, p.lda) && fits(p.b, p.ldb);
+    int *const sums = static_cast<int *>(part);
+    if (c.tile == 0) launch_tiles<32, 128, 1, 4, 4>(p, c.splits, sums, dma, st);
+    else if (c.tile == 1) launch_tiles<64, 128, 2, 2, 3>(p, c.splits, sums, dma, st);
+    else if (c.tile == 2) launch_tiles<128, 128, 2, 2, 2>(p, c.splits, sums, dma, st);
+    else launch_tiles<256, 256, 2, 4, 2>(p, c.splits, sums, dma, st);
+    if (const int rc = check_launch("pconv_matmul_i8")) return rc;
+    if (c.splits == 1) return PCONV_OK;
+    const int64_t quads = (int64_t(p.n) + 3) / 4 * p.m;
+    hipLaunchKernelGGL(matmul_i8_join_kernel, dim3(unsigned(std::min<int64_t>((quads + 255) / 256, 1 << 16))), dim3(256), 0, st, p, c.splits, sums);
+    return check_launch("pconv_matmul_i8 (joining the parts of k)");
 }
 
 }  // namespace pconv

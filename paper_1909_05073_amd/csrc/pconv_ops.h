@@ -21,7 +21,9 @@ struct I8Product {
 // Launchers: arguments checked, sizes not 0.  They return a pconv_status.
 int launch_quantize_rows(const void *x, int64_t ldx, int bf16, int64_t rows, int64_t cols, int8_t *q, int64_t ldq,
                          int64_t q_cols, float *scale, void *stream);
-int launch_matmul_i8(const I8Product &p, void *stream);
+// bytes of work space (sums of parts of k) that the product takes, and the product
+int64_t matmul_i8_part_bytes(int64_t m, int64_t n, int64_t k);
+int launch_matmul_i8(const I8Product &p, void *part, void *stream);
 
 // Up to kGradTensors tensors travel in the arguments of one launch (4 KiB).
 constexpr int kGradTensors = 160, kGradChunk = 16384, kGradBlocks = 2048;

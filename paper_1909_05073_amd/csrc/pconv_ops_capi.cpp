@@ -27,6 +27,15 @@ int64_t round16(int64_t v) { return (v + 15) / 16 * 16; }
 // rows of `len` elements that lie `stride` apart: within the range of a byte offset in 64 bits
 bool stride_fits(int64_t rows, int64_t len, int64_t stride) { return stride >= len && stride <= (int64_t(1) << 58) / (rows > 0 ? rows : 1); }
 
+bool sizes_fit(int64_t m, int64_t n, int64_t k) { return m > 0 && n > 0 && k >= 0 && m <= kMaxRows && n <= kMaxRows && k <= kMaxK; }
+
+int check_work(const char *who, const void *work, int64_t have, int64_t need)
+{
+    if (need > 0 && (!work || have < need)) return invalid(who, "the work space is too small");
+    if (need > 0 && reinterpret_cast<uintptr_t>(work) % 16 != 0) return invalid(who, "the work space must be aligned to 16 bytes");
+    return PCONV_OK;
+}
+
 // What both products check of their weights and outputs, and the product itself but for its activations.
 int check_product(const char *who, const int8_t *b, int64_t ldb, const float *sb, const float *bias, void *y, int64_t ldy, int y_dtype,
                   int64_t m, int64_t n, int64_t k, int relu, I8Product &p)
@@ -110,11 +119,14 @@ int pconv_quantize_rows(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype
     return launch_quantize_rows(x_dev, x_stride, x_dtype == PCONV_BF16, rows, cols, q_dev, q_stride, cols, scale_dev, hip_stream);
 }
 
-int64_t pconv_matmul_i8_workspace(int64_t, int64_t, int64_t) { return 0; }
+int64_t pconv_matmul_i8_workspace(int64_t m, int64_t n, int64_t k)
+{
+    return sizes_fit(m, n, k) ? matmul_i8_part_bytes(m, n, k) : 0;
+}
 
 int pconv_matmul_i8(const int8_t *a_dev, int64_t a_stride, const float *a_scale, const int8_t *b_dev, int64_t b_stride,
                     const float *b_scale, const float *bias_dev, void *y_dev, int64_t y_stride, pconv_dtype y_dtype,
-                    int64_t m, int64_t n, int64_t k, int fuse_relu, void *, int64_t, void *hip_stream)
+                    int64_t m, int64_t n, int64_t k, int fuse_relu, void *work, int64_t work_bytes, void *hip_stream)
 {
     const char *who = "pconv_matmul_i8";
     I8Product p;
@@ -122,13 +134,14 @@ int pconv_matmul_i8(const int8_t *a_dev, int64_t a_stride, const float *a_scale,
     if (m == 0 || n == 0) return PCONV_OK;
     if (!a_scale || (k && !a_dev)) return invalid(who, "null pointer argument");
     if (!stride_fits(m, k, a_stride)) return invalid(who, "rows must lie at least their length apart");
+    if (const int rc = check_work(who, work, work_bytes, pconv_matmul_i8_workspace(m, n, k))) return rc;
     p.a = a_dev; p.lda = a_stride; p.sa = a_scale;
-    return launch_matmul_i8(p, hip_stream);
+    return launch_matmul_i8(p, work, hip_stream);
 }
 
-int64_t pconv_linear_i8_workspace(int64_t m, int64_t, int64_t k, pconv_dtype)
+int64_t pconv_linear_i8_workspace(int64_t m, int64_t n, int64_t k, pconv_dtype)
 {
-    return m > 0 && k >= 0 && m <= kMaxRows && k <= kMaxK ? round16(4 * m) + m * round16(k) : 0;
+    return sizes_fit(m, n, k) ? round16(4 * m) + m * round16(k) + matmul_i8_part_bytes(m, n, k) : 0;
 }
 
 int pconv_linear_i8(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, const int8_t *w_dev, int64_t w_stride,
@@ -142,15 +155,13 @@ int pconv_linear_i8(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, co
     if (m == 0 || n == 0) return PCONV_OK;
     if (k && !x_dev) return invalid(who, "null pointer argument");
     if (!stride_fits(m, k, x_stride)) return invalid(who, "rows must lie at least their length apart");
-    const int64_t need = pconv_linear_i8_workspace(m, n, k, x_dtype);
-    if (need > 0 && (!work || work_bytes < need)) return invalid(who, "the work space is too small");
-    if (reinterpret_cast<uintptr_t>(work) % 16 != 0) return invalid(who, "the work space must be aligned to 16 bytes");
+    if (const int rc = check_work(who, work, work_bytes, pconv_linear_i8_workspace(m, n, k, x_dtype))) return rc;
     float *const scale = static_cast<float *>(work);
     int8_t *const q = static_cast<int8_t *>(work) + round16(4 * m);
     const int64_t ldq = round16(k);
     if (const int rc = launch_quantize_rows(x_dev, x_stride, x_dtype == PCONV_BF16, m, k, q, ldq, ldq, scale, hip_stream)) return rc;
     p.a = q; p.lda = ldq; p.sa = scale;
-    return launch_matmul_i8(p, hip_stream);
+    return launch_matmul_i8(p, q + m * ldq, hip_stream);
 }
 
 int64_t pconv_grad_workspace(int64_t num)
