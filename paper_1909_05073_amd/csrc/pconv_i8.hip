@@ -9,6 +9,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "pconv_internal.h"
 #include "pconv_ops.h"
@@ -123,20 +124,26 @@ __device__ __forceinline__ Vec<T> load_part(const T *row, int64_t at, int64_t co
     return v;
 }
 
-// The same elements quantised, to q; [cols, q_cols) is filled with zeros.
 template <typename T>
-__device__ __forceinline__ void store_part(const Vec<T> &v, const RowScale &r, int8_t *row, int64_t at, int64_t q_cols)
+__device__ __forceinline__ void quantize_part(const Vec<T> &v, const RowScale &r, uint32_t (&w)[Vec<T>::N / 4])
 {
-    constexpr int N = Vec<T>::N;
-    uint32_t w[N / 4];
 #pragma unroll
-    for (int j = 0; j < N / 4; ++j) {
+    for (int j = 0; j < Vec<T>::N / 4; ++j) {
         if (r.mode == 0)
             w[j] = pack4(quantize(v.at(4 * j), r), quantize(v.at(4 * j + 1), r), quantize(v.at(4 * j + 2), r), quantize(v.at(4 * j + 3), r));
         else
             w[j] = pack4(quantize_rare(v.at(4 * j), r), quantize_rare(v.at(4 * j + 1), r), quantize_rare(v.at(4 * j + 2), r),
                          quantize_rare(v.at(4 * j + 3), r));
     }
+}
+
+// The same elements quantised, to q; [cols, q_cols) is filled with zeros.
+template <typename T>
+__device__ __forceinline__ void store_part(const Vec<T> &v, const RowScale &r, int8_t *row, int64_t at, int64_t q_cols)
+{
+    constexpr int N = Vec<T>::N;
+    uint32_t w[N / 4];
+    quantize_part(v, r, w);
     if (at + N <= q_cols) {
         __builtin_memcpy(row + at, w, N);
     } else {
@@ -219,7 +226,7 @@ __device__ __forceinline__ Channels channels_at(const I8Product &p, int n)
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int at = min(n + i, p.n - 1);
+            const int at = min(n + i, p.n - 1);          // (what lies beyond the last channel is not stored)
             c.scale[i] = p.sb[at];
             if (p.bias) c.bias[i] = p.bias[at];
         }
@@ -228,26 +235,67 @@ __device__ __forceinline__ Channels channels_at(const I8Product &p, int n)
     return c;
 }
 
-__device__ __forceinline__ void finish(const I8Product &p, int m, int n, v4i acc, float sa, const Channels &c)
+__device__ __forceinline__ f4 values_of(const I8Product &p, v4i acc, float sa, const Channels &c)
 {
-    if (m >= p.m || n >= p.n) return;
     f4 v;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         v[i] = float(acc[i]) * (sa * c.scale[i]) + c.bias[i];
         if (p.relu) v[i] = v[i] < 0.0f ? 0.0f : v[i];
     }
-    const int have = min(4, p.n - n);
-    const int64_t to = int64_t(m) * p.ldy + n;
-    if (p.y_bf16) {
-        __bf16 *y = static_cast<__bf16 *>(p.y) + to;
-        const b4 w = __builtin_convertvector(v, b4);
-        if (have == 4) __builtin_memcpy(y, &w, 8);
-        else for (int i = 0; i < have; ++i) y[i] = w[i];
+    return v;
+}
+
+template <typename Y, int N, typename V>
+__device__ __forceinline__ void store_channels(const I8Product &p, int m, int n, V v)
+{
+    Y *y = static_cast<Y *>(p.y) + (int64_t(m) * p.ldy + n);
+    if (n + N <= p.n) {
+        __builtin_memcpy(y, &v, N * sizeof(Y));
     } else {
-        float *y = static_cast<float *>(p.y) + to;
-        if (have == 4) __builtin_memcpy(y, &v, 16);
-        else for (int i = 0; i < have; ++i) y[i] = v[i];
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (n + i < p.n) y[i] = v[i];
+    }
+}
+
+// How a wave's channels are dealt to the first operand's rows: a lane gets four of each matrix instruction's sixteen, and Deal::G
+// instructions' fours are neighbours, so that 16 bytes are stored at once and four lanes store 64 (fp32: 4 channels,
+// bf16: 8).  row(j, r): channel of row r of instruction j; first(j, g): first of the four that lanes 16 g .. hold.
+template <typename Y> struct Deal;
+template <> struct Deal<float> {
+    static constexpr int SH = 2;                         // (bits 0, 1 and SH of a row tell eight rows r apart)
+    static __device__ __forceinline__ int row(int j, int r) { return j * 16 + r; }
+    static __device__ __forceinline__ int first(int j, int g) { return j * 16 + g * 4; }
+};
+template <> struct Deal<__bf16> {
+    static constexpr int SH = 3;
+    static __device__ __forceinline__ int row(int j, int r) { return (j >> 1) * 32 + (r >> 2) * 8 + (j & 1) * 4 + (r & 3); }
+    static __device__ __forceinline__ int first(int j, int g) { return (j >> 1) * 32 + g * 8 + (j & 1) * 4; }
+};
+
+// Rows m + 16 i of y, the NT * 16 channels from n0 on; the lane has `lane & 15` in m and its group in `g`.
+template <typename Y, int MT, int NT>
+__device__ __forceinline__ void store_tile(const I8Product &p, int m, int n0, int g, const v4i (&acc)[MT][NT], const float (&sa)[MT])
+{
+    static_assert(NT % 2 == 0, "");
+#pragma unroll
+    for (int j = 0; j < NT; j += 2) {
+        const int n = n0 + Deal<Y>::first(j, g), n2 = n0 + Deal<Y>::first(j + 1, g);
+        if (n >= p.n) continue;
+        const Channels c = channels_at(p, n), c2 = channels_at(p, n2);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            if (m + 16 * i >= p.m) continue;
+            const f4 v = values_of(p, acc[i][j], sa[i], c), w = values_of(p, acc[i][j + 1], sa[i], c2);
+            if (sizeof(Y) == 4) {
+                store_channels<float, 4>(p, m + 16 * i, n, v);
+                if (n2 < p.n) store_channels<float, 4>(p, m + 16 * i, n2, w);
+            } else {
+                const b8 o = __builtin_convertvector(__builtin_shufflevector(v, w, 0, 1, 2, 3, 4, 5, 6, 7), b8);
+                store_channels<__bf16, 8>(p, m + 16 * i, n, o);
+            }
+        }
     }
 }
 
@@ -284,17 +332,14 @@ __device__ __forceinline__ void tile_at(unsigned id, unsigned tiles_m, unsigned 
 // is left of k behind the last whole stage goes through registers, and so does everything where rows do not begin at
 // multiples of 16 bytes (DMA = false; one stage ahead).
 //
-// A wave's channels are dealt to the matrix instructions so that a lane holds 4 * NG neighbouring ones.
-//
 // `splits` workgroups share a tile, each with its part of k; their sums go to `part` [splits][m][n4], n4 = n rounded up to four.
-template <int BM, int BN, int WM, int WN, int S, bool DMA>
+template <typename Y, int BM, int BN, int WM, int WN, int S, bool DMA>
 __global__ void __launch_bounds__(WM * WN * 64)
 matmul_i8_kernel(const I8Product p, int splits, int *part)
 {
     constexpr int BK = 128, NW = WM * WN, TM = BM / WM, TN = BN / WN, MT = TM / 16, NT = TN / 16;
-    constexpr int NG = NT < 4 ? NT : 4, SH = NG == 4 ? 4 : NG == 2 ? 3 : 2;
     constexpr int PA = BM / 8 / NW, PB = BN / 8 / NW;    // blocks of eight rows that a wave stages
-    static_assert(PA * NW * 8 == BM && PB * NW * 8 == BN && NT % NG == 0, "");
+    static_assert(PA * NW * 8 == BM && PB * NW * 8 == BN, "");
     __shared__ v4i lds[S * (BM + BN) * 8];
     constexpr int STAGE = (BM + BN) * 8;
     const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -309,8 +354,8 @@ matmul_i8_kernel(const I8Product p, int splits, int *part)
     const int s_begin = int(int64_t(stages) * split / splits), s_end = int(int64_t(stages) * (split + 1) / splits);
     const int k_begin = s_begin * BK, k_end = min(s_end * BK, p.k);
 
-    // order of the pieces of a row of weights: bits 0, 1 and SH of the row tell the rows that are read at once apart
-    auto key_b = [](int row) { return (row & 3) | (((row >> SH) & 1) << 2); };
+    // order of the pieces of a row of weights: the rows that are read at once differ in three of their bits
+    auto key_b = [](int row) { return (row & 3) | (((row >> Deal<Y>::SH) & 1) << 2); };
 
     v4i acc[MT][NT];
 #pragma unroll
@@ -330,7 +375,7 @@ matmul_i8_kernel(const I8Product p, int splits, int *part)
             }
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                const int row = wn + (j / NG) * (16 * NG) + (r >> 2) * (4 * NG) + (j % NG) * 4 + (r & 3);
+                const int row = wn + Deal<Y>::row(j, r);
                 b[j] = st[BM * 8 + row * 8 + (piece ^ key_b(row))];
             }
 #pragma unroll
@@ -432,26 +477,22 @@ matmul_i8_kernel(const I8Product p, int splits, int *part)
         }
     }
 
-    const int r = lane & 15;
+    const int m = m0 + wm + (lane & 15), g = lane >> 4;
+    if (splits > 1) {
+        const int64_t n4 = (int64_t(p.n) + 3) / 4 * 4;
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const int n = n0 + wn + (j / NG) * (16 * NG) + (lane >> 4) * (4 * NG) + (j % NG) * 4;
-        if (splits > 1) {
-            const int64_t n4 = (int64_t(p.n) + 3) / 4 * 4;
+        for (int j = 0; j < NT; ++j) {
+            const int n = n0 + wn + Deal<Y>::first(j, g);
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const int m = m0 + wm + i * 16 + r;
-                if (m < p.m && n < p.n) __builtin_memcpy(part + (int64_t(split) * p.m + m) * n4 + n, &acc[i][j], 16);
-            }
-            continue;
+            for (int i = 0; i < MT; ++i)
+                if (m + 16 * i < p.m && n < p.n) __builtin_memcpy(part + (int64_t(split) * p.m + m + 16 * i) * n4 + n, &acc[i][j], 16);
         }
-        const Channels c = channels_at(p, n);
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const int m = m0 + wm + i * 16 + r;
-            finish(p, m, n, acc[i][j], p.sa[min(m, p.m - 1)], c);
-        }
+        return;
     }
+    float sa[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) sa[i] = p.sa[min(m + 16 * i, p.m - 1)];
+    store_tile<Y, MT, NT>(p, m, n0 + wn, g, acc, sa);
 }
 
 // y of the sums of `splits` parts of k; a thread has four channels.
@@ -468,7 +509,118 @@ matmul_i8_join_kernel(const I8Product p, int splits, const int *__restrict__ par
             __builtin_memcpy(&v, part + (int64_t(i) * all + t) * 4, 16);
             s += v;
         }
-        finish(p, m, n, s, p.sa[m], channels_at(p, n));
+        const f4 v = values_of(p, s, p.sa[m], channels_at(p, n));
+        if (p.y_bf16) store_channels<__bf16, 4>(p, m, n, __builtin_convertvector(v, b4));
+        else store_channels<float, 4>(p, m, n, v);
+    }
+}
+
+// The largest value over the 8 or 16 neighbouring lanes that share a row.
+template <int LANES>
+__device__ __forceinline__ uint32_t most_of_lanes(uint32_t v)
+{
+    v = max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0xB1, 0xF, 0xF, true)));       // the other of a pair
+    v = max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x4E, 0xF, 0xF, true)));       // the other pair of four
+    v = max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x141, 0xF, 0xF, true)));      // the other four of eight
+    if (LANES == 16) v = max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x140, 0xF, 0xF, true)));
+    return v;
+}
+
+// Short rows (k up to kThinK): all of k of 16 * MT rows of activations lies in LDS, so that there is no loop of stages and one read of
+// the activations; where they come as floats (T) they are quantised on their way there and never leave the chip.
+// The weights, which every workgroup reads and the level-2 caches hold, go to the registers directly.  Four waves share
+// the rows and take groups of 64 channels in turn.  blockIdx.y: a part of the channels, a multiple of 64 (`part_n`).
+//
+// LANES lanes quantise a row, KEEP vectors of 16 bytes each.
+constexpr int kThinK = 512;
+
+template <typename T, typename Y, int MT, int LANES, int KEEP>
+__global__ void __launch_bounds__(256)
+linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, int part_n)
+{
+    constexpr int BM = 16 * MT, NT = 4;
+    extern __shared__ v4i thin_lds[];                    // BM rows of `pieces` times 16 bytes, and the scales of the rows
+    const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+    const int m0 = int(blockIdx.x) * BM, pieces = (p.k + 127) / 128 * 8;
+    float *const scales = reinterpret_cast<float *>(thin_lds + BM * pieces);
+    if (sizeof(T) == 1) {
+        for (int at = int(threadIdx.x); at < BM * pieces; at += 256) {
+            const int row = at / pieces, c = at - row * pieces;
+            thin_lds[row * pieces + (c ^ (row & 7))] =
+                load16(reinterpret_cast<const int8_t *>(x) + int64_t(min(m0 + row, p.m - 1)) * ldx, c * 16, p.k);
+        }
+        for (int row = int(threadIdx.x); row < BM; row += 256) scales[row] = p.sa[min(m0 + row, p.m - 1)];
+    } else {
+        using V = Vec<std::conditional_t<sizeof(T) == 1, float, T>>;
+        using E = std::conditional_t<sizeof(T) == 1, float, T>;
+        constexpr int N = V::N, AT_ONCE = 64 / LANES, PASSES = BM / 4 / AT_ONCE;
+        const int sub = lane % LANES;
+        V v[PASSES][KEEP];
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) {
+            const int row = wave * (BM / 4) + i * AT_ONCE + lane / LANES;
+            const E *from = reinterpret_cast<const E *>(x) + int64_t(min(m0 + row, p.m - 1)) * ldx;
+#pragma unroll
+            for (int q = 0; q < KEEP; ++q) v[i][q] = load_part(from, (q * LANES + sub) * N, p.k);
+        }
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) {
+            const int row = wave * (BM / 4) + i * AT_ONCE + lane / LANES;
+            uint32_t most = 0;
+#pragma unroll
+            for (int q = 0; q < KEEP; ++q) most = most_of(v[i][q], most);
+            const RowScale s = row_scale(most_of_lanes<LANES>(most));
+            if (sub == 0) scales[row] = s.scale;
+#pragma unroll
+            for (int q = 0; q < KEEP; ++q) {
+                const int byte = (q * LANES + sub) * N, c = byte / 16;
+                uint32_t w[N / 4];
+                quantize_part(v[i][q], s, w);
+                if (c < pieces) __builtin_memcpy(reinterpret_cast<int8_t *>(thin_lds + row * pieces + (c ^ (row & 7))) + byte % 16, w, N);
+            }
+        }
+    }
+    __syncthreads();
+
+    const int r = lane & 15, g = lane >> 4, n_end = min(p.n, int(blockIdx.y + 1) * part_n);
+    for (int n0 = int(blockIdx.y) * part_n + wave * 64; n0 < n_end; n0 += 256) {
+        const int8_t *b[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) b[j] = p.b + int64_t(min(n0 + Deal<Y>::row(j, r), p.n - 1)) * p.ldb;
+        v4i acc[MT][NT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j] = v4i{0, 0, 0, 0};
+        auto step = [&](const v4i (&vb)[NT], int k0) {
+            v4i va[MT];
+            const int c = k0 / 16 + g;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) va[i] = thin_lds[(i * 16 + r) * pieces + (c ^ (r & 7))];
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb[j], va[i], acc[i][j], 0, 0, 0);
+        };
+        auto fetch = [&](v4i (&vb)[NT], int k0) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                if (k0 + 64 <= p.k) __builtin_memcpy(&vb[j], b[j] + k0 + g * 16, 16);
+                else vb[j] = load16(b[j], k0 + g * 16, p.k);
+            }
+        };
+        v4i now[NT], next[NT];
+        if (p.k > 0) fetch(now, 0);
+        for (int k0 = 0; k0 < p.k; k0 += 64) {
+            if (k0 + 64 < p.k) fetch(next, k0 + 64);
+            step(now, k0);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) now[j] = next[j];
+        }
+        float sa[MT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) sa[i] = scales[i * 16 + r];
+        store_tile<Y, MT, NT>(p, m0 + r, n0, g, acc, sa);
     }
 }
 
@@ -509,7 +661,10 @@ matmul_i8_rows_kernel(const I8Product p)
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) s += lds[w][i][lane];
         const int m = i * 16 + (lane & 15), n = n0 + (lane >> 4) * 4;
-        finish(p, m, n, s, p.sa[min(m, p.m - 1)], channels_at(p, n));
+        if (m >= p.m || n >= p.n) continue;
+        const f4 v = values_of(p, s, p.sa[m], channels_at(p, n));
+        if (p.y_bf16) store_channels<__bf16, 4>(p, m, n, __builtin_convertvector(v, b4));
+        else store_channels<float, 4>(p, m, n, v);
     }
 }
 
@@ -561,17 +716,58 @@ template <int BM, int BN, int WM, int WN, int S>
 void launch_tiles(const I8Product &p, int splits, int *part, bool dma, hipStream_t st)
 {
     const unsigned grid = unsigned(((int64_t(p.m) + BM - 1) / BM) * ((int64_t(p.n) + BN - 1) / BN) * splits);
-    if (dma) hipLaunchKernelGGL((matmul_i8_kernel<BM, BN, WM, WN, S, true>), dim3(grid), dim3(WM * WN * 64), 0, st, p, splits, part);
-    else hipLaunchKernelGGL((matmul_i8_kernel<BM, BN, WM, WN, 2, false>), dim3(grid), dim3(WM * WN * 64), 0, st, p, splits, part);
+#define PCONV_LAUNCH(Y, STAGES, DMA) \
+    hipLaunchKernelGGL((matmul_i8_kernel<Y, BM, BN, WM, WN, STAGES, DMA>), dim3(grid), dim3(WM * WN * 64), 0, st, p, splits, part)
+    if (p.y_bf16) { if (dma) PCONV_LAUNCH(__bf16, S, true); else PCONV_LAUNCH(__bf16, 2, false); }
+    else { if (dma) PCONV_LAUNCH(float, S, true); else PCONV_LAUNCH(float, 2, false); }
+#undef PCONV_LAUNCH
 }
 
 constexpr int64_t kRowsM = 16;                           // matmul_i8_rows_kernel serves up to so many rows
 
+// Rows of T (int8_t: quantised already, with their scales in p) times weights, k up to kThinK.
+template <typename T, int LANES, int KEEP>
+int launch_thin(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
+{
+    const int64_t big = (int64_t(p.m) + 63) / 64, groups = (int64_t(p.n) + 255) / 256;
+    const int mt = big * groups >= 512 ? 4 : 2;
+    const int64_t tiles = (int64_t(p.m) + 16 * mt - 1) / (16 * mt);
+    const int64_t parts = std::min<int64_t>(groups, std::max<int64_t>(1, 1024 / tiles));
+    const int part_n = int((groups + parts - 1) / parts * 256);
+    if (tiles >= int64_t(1) << 24) { set_error("pconv_matmul_i8: too many workgroups"); return PCONV_UNSUPPORTED; }
+    const dim3 grid(unsigned(tiles), unsigned((int64_t(p.n) + part_n - 1) / part_n));
+    const size_t lds = size_t(16 * mt) * ((p.k + 127) / 128 * 128 + 4);
+#define PCONV_LAUNCH(Y, MT) hipLaunchKernelGGL((linear_i8_thin_kernel<T, Y, MT, LANES, KEEP>), grid, dim3(256), lds, st, p, x, ldx, part_n)
+    if (p.y_bf16) { if (mt == 4) PCONV_LAUNCH(__bf16, 4); else PCONV_LAUNCH(__bf16, 2); }
+    else { if (mt == 4) PCONV_LAUNCH(float, 4); else PCONV_LAUNCH(float, 2); }
+#undef PCONV_LAUNCH
+    return check_launch("pconv_linear_i8 (short rows)");
+}
+
 }  // namespace
+
+bool linear_i8_thin(int64_t m, int64_t n, int64_t k) { return m > kRowsM && k <= kThinK; }
+
+int launch_linear_i8_thin(const I8Product &p, const void *x, int64_t ldx, int bf16, void *stream)
+{
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (bf16) {
+        const __bf16 *const at = static_cast<const __bf16 *>(x);
+        if (p.k <= 64) return launch_thin<__bf16, 8, 1>(p, at, ldx, st);
+        if (p.k <= 128) return launch_thin<__bf16, 16, 1>(p, at, ldx, st);
+        if (p.k <= 256) return launch_thin<__bf16, 16, 2>(p, at, ldx, st);
+        return launch_thin<__bf16, 16, 4>(p, at, ldx, st);
+    }
+    const float *const at = static_cast<const float *>(x);
+    if (p.k <= 64) return launch_thin<float, 16, 1>(p, at, ldx, st);
+    if (p.k <= 128) return launch_thin<float, 16, 2>(p, at, ldx, st);
+    if (p.k <= 256) return launch_thin<float, 16, 4>(p, at, ldx, st);
+    return launch_thin<float, 16, 8>(p, at, ldx, st);
+}
 
 int64_t matmul_i8_part_bytes(int64_t m, int64_t n, int64_t k)
 {
-    if (m <= kRowsM) return 0;
+    if (m <= kRowsM || linear_i8_thin(m, n, k)) return 0;
     const Cut c = cut_of(m, n, k);
     return c.splits > 1 ? c.splits * m * ((n + 3) / 4 * 4) * 4 : 0;
 }
@@ -583,6 +779,7 @@ int launch_matmul_i8(const I8Product &p, void *part, void *stream)
         hipLaunchKernelGGL((matmul_i8_rows_kernel<1, 8>), dim3(unsigned((p.n + 15) / 16)), dim3(512), 0, st, p);
         return check_launch("pconv_matmul_i8 (few rows)");
     }
+    if (linear_i8_thin(p.m, p.n, p.k)) return launch_thin<int8_t, 8, 1>(p, p.a, p.lda, st);
     const Cut c = cut_of(p.m, p.n, p.k);
     const int64_t tiles = ((int64_t(p.m) + kTileM[c.tile] - 1) / kTileM[c.tile]) * ((int64_t(p.n) + kTileN[c.tile] - 1) / kTileN[c.tile]);
     if (tiles * c.splits >= int64_t(1) << 23) { set_error("pconv_matmul_i8: too many workgroups"); return PCONV_UNSUPPORTED; }
