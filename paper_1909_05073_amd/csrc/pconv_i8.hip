@@ -36,69 +36,49 @@ int check_launch(const char *what)
 
 // The largest magnitude travels as the bits of |x|: ordered like the values, infinity above all numbers and NaN above it.
 struct RowScale {
-    float scale, inv;
-    int mode;                                            // 0: by the reciprocal, 1: tiny scales, by division, 2: all zeros
+    float scale;                                         // what is handed out: NaN where the row holds an infinity or a NaN
+    float step, inv, lift;                               // scale * lift, its reciprocal, and a power of two
+    uint32_t mask;                                       // 0: all of the row is 0
 };
 
 __device__ __forceinline__ RowScale row_scale(uint32_t most)
 {
     RowScale r;
-    const float amax = __uint_as_float(most);
-    if (most >= 0x7F800000u) {
-        r.scale = __uint_as_float(0x7FC00000u); r.inv = 0.0f; r.mode = 2;
-        return r;
-    }
-    r.scale = amax / 127.0f;
-    r.mode = r.scale >= 0x1p-100f ? 0 : r.scale > 0.0f ? 1 : 2;
-    r.inv = r.mode == 0 ? 1.0f / r.scale : 0.0f;
+    const bool bad = most >= 0x7F800000u;
+    const float s = bad ? 0.0f : __uint_as_float(most) / 127.0f;
+    r.scale = bad ? __uint_as_float(0x7FC00000u) : s;
+    r.lift = s < 0x1p-60f ? 0x1p64f : 1.0f;
+    r.step = s * r.lift;
+    r.inv = s > 0.0f ? 1.0f / r.step : 0.0f;
+    r.mask = s > 0.0f ? 0xFFFFFFFFu : 0u;
     return r;
 }
 
 // The nearest whole number of the nearest fp32 number of x / scale, in the low byte.  The correctly rounded quotient comes
-// from the correctly rounded reciprocal by two corrections with the exact remainder (Markstein, 1990): five
-// operations for a division's eleven.  That needs remainders that are no denormals, hence the lower limit of mode 0;
-// quotients so small that theirs are denormal all round to 0.  Adding 1.5 * 2^23 rounds to a whole number in
-// the low bits, ties to even.
+// from the correctly rounded reciprocal by two corrections with the exact remainder (Markstein, 1990): five operations for a
+// division's eleven.  Small rows are lifted by a power of two first, so that a remainder that decides is no denormal.  A
+// scale that is itself a denormal is rounded to few bits; quotients may pass 127 then and are cut.  Adding 1.5 * 2^23
+// rounds to a whole number in the low bits, ties to even.
 __device__ __forceinline__ uint32_t quantize(float x, const RowScale &r)
 {
+    x *= r.lift;
     float t = x * r.inv;
-    t = __builtin_fmaf(__builtin_fmaf(-t, r.scale, x), r.inv, t);
-    t = __builtin_fmaf(__builtin_fmaf(-t, r.scale, x), r.inv, t);
-    return __float_as_uint(t + 12582912.0f);
+    t = __builtin_fmaf(__builtin_fmaf(-t, r.step, x), r.inv, t);
+    t = __builtin_fmaf(__builtin_fmaf(-t, r.step, x), r.inv, t);
+    return __float_as_uint(__builtin_amdgcn_fmed3f(t, -127.0f, 127.0f) + 12582912.0f);
 }
 
-// The rare rows: a scale so small that it is itself rounded to few bits, so that quotients may pass 127.
-__device__ __forceinline__ uint32_t quantize_rare(float x, const RowScale &r)
-{
-    const float t = r.mode == 1 ? fminf(fmaxf(x / r.scale, -127.0f), 127.0f) : 0.0f;
-    return __float_as_uint(t + 12582912.0f);
-}
-
-__device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
-{
-    const uint32_t ab = __builtin_amdgcn_perm(b, a, 0x0C0C0400u), cd = __builtin_amdgcn_perm(d, c, 0x04000C0Cu);
-    return ab | cd;
-}
-
-// 16 bytes of a row of activations as floats
+// 16 bytes of a row of activations
 template <typename T> struct Vec;
 template <> struct Vec<float> {
     static constexpr int N = 4;
     f4 v;
-    __device__ __forceinline__ void load(const float *p) { __builtin_memcpy(&v, p, 16); }
     __device__ __forceinline__ float at(int i) const { return v[i]; }
-    __device__ __forceinline__ void zero() { v = f4{0, 0, 0, 0}; }
-    __device__ __forceinline__ void put(int i, float x) { v[i] = x; }
-    static __device__ __forceinline__ float one(const float *p) { return *p; }
 };
 template <> struct Vec<__bf16> {
     static constexpr int N = 8;
     b8 v;
-    __device__ __forceinline__ void load(const __bf16 *p) { __builtin_memcpy(&v, p, 16); }
     __device__ __forceinline__ float at(int i) const { return float(v[i]); }
-    __device__ __forceinline__ void zero() { v = b8{}; }
-    __device__ __forceinline__ void put(int i, float x) { v[i] = __bf16(x); }
-    static __device__ __forceinline__ float one(const __bf16 *p) { return float(*p); }
 };
 
 template <typename T>
@@ -109,58 +89,111 @@ __device__ __forceinline__ uint32_t most_of(const Vec<T> &v, uint32_t most)
     return most;
 }
 
-// Elements [at, at + N) of a row of `cols`: the last ones one by one, beyond the end zero.
-template <typename T>
-__device__ __forceinline__ Vec<T> load_part(const T *row, int64_t at, int64_t cols)
+// The `size` (< 16) bytes that a row of `len` bytes has from `at` on, the rest zero: cut out of the row's last 16 bytes.
+__device__ __forceinline__ v4i load_end(const void *row, int64_t at, int64_t len)
 {
-    Vec<T> v;
-    if (at + Vec<T>::N <= cols) {
-        v.load(row + at);
+    uint64_t lo = 0, hi = 0;
+    const uint8_t *p = static_cast<const uint8_t *>(row);
+    if (len >= 16) {
+        uint64_t w[2];
+        __builtin_memcpy(w, p + len - 16, 16);
+        const int bits = 8 * int(at + 16 - len);         // 8 .. 120
+        lo = bits < 64 ? (w[0] >> bits) | (w[1] << (64 - bits)) : w[1] >> (bits - 64);
+        hi = bits < 64 ? w[1] >> bits : 0;
     } else {
-        v.zero();
-        for (int i = 0; i < Vec<T>::N; ++i)
-            if (at + i < cols) v.put(i, Vec<T>::one(row + at + i));
+#pragma unroll 1
+        for (int i = 0; i < int(len); ++i) {             // (at is 0)
+            const uint64_t v = uint64_t(p[i]) << (8 * (i & 7));
+            if (i < 8) lo |= v; else hi |= v;
+        }
     }
+    return v4i{int(lo), int(lo >> 32), int(hi), int(hi >> 32)};
+}
+
+// Elements [at, at + N) of a row of `cols`; beyond its end zero.
+template <typename T>
+__device__ __forceinline__ Vec<T> load_vec(const T *row, int64_t at, int64_t cols)
+{
+    v4i w = {0, 0, 0, 0};
+    if (__builtin_expect(at + Vec<T>::N <= cols, 1)) __builtin_memcpy(&w, row + at, 16);
+    else if (__builtin_expect(at < cols, 0)) w = load_end(row, at * int(sizeof(T)), cols * int(sizeof(T)));
+    Vec<T> v;
+    __builtin_memcpy(&v, &w, 16);
     return v;
 }
 
+// The vectors sub, sub + LANES, .. of a row: KEEP of them.  (One piece of code for the row's end, not KEEP.)
+template <typename T, int LANES, int KEEP, bool EXACT = false>
+__device__ __forceinline__ void load_row(const T *row, int sub, int64_t cols, Vec<T> (&v)[KEEP])
+{
+    constexpr int N = Vec<T>::N;
+#pragma unroll
+    for (int i = 0; i < KEEP; ++i) {
+        const int64_t at = (int64_t(i) * LANES + sub) * N;
+        v4i w = {0, 0, 0, 0};
+        if (at + N <= cols) __builtin_memcpy(&w, row + at, 16);
+        __builtin_memcpy(&v[i], &w, 16);
+    }
+    const int64_t last = cols / N;
+    if (!EXACT && __builtin_expect(cols % N != 0, 0) && last < KEEP * LANES) {
+        const v4i w = load_end(row, last * 16, cols * int(sizeof(T)));
+#pragma unroll
+        for (int i = 0; i < KEEP; ++i)
+            if (i * LANES + sub == last) __builtin_memcpy(&v[i], &w, 16);
+    }
+}
+
 template <typename T>
-__device__ __forceinline__ void quantize_part(const Vec<T> &v, const RowScale &r, uint32_t (&w)[Vec<T>::N / 4])
+__device__ __forceinline__ void quantize_vec(const Vec<T> &v, const RowScale &r, uint32_t (&w)[Vec<T>::N / 4])
 {
 #pragma unroll
     for (int j = 0; j < Vec<T>::N / 4; ++j) {
-        if (r.mode == 0)
-            w[j] = pack4(quantize(v.at(4 * j), r), quantize(v.at(4 * j + 1), r), quantize(v.at(4 * j + 2), r), quantize(v.at(4 * j + 3), r));
-        else
-            w[j] = pack4(quantize_rare(v.at(4 * j), r), quantize_rare(v.at(4 * j + 1), r), quantize_rare(v.at(4 * j + 2), r),
-                         quantize_rare(v.at(4 * j + 3), r));
+        uint32_t q[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = quantize(v.at(4 * j + i), r);
+        w[j] = (__builtin_amdgcn_perm(q[1], q[0], 0x0C0C0400u) | __builtin_amdgcn_perm(q[3], q[2], 0x04000C0Cu)) & r.mask;
     }
 }
 
-// The same elements quantised, to q; [cols, q_cols) is filled with zeros.
+// The same elements quantised, to a row of q_cols bytes.
 template <typename T>
-__device__ __forceinline__ void store_part(const Vec<T> &v, const RowScale &r, int8_t *row, int64_t at, int64_t q_cols)
+__device__ __forceinline__ void store_vec(const Vec<T> &v, const RowScale &r, int8_t *row, int64_t at, int64_t q_cols)
 {
     constexpr int N = Vec<T>::N;
     uint32_t w[N / 4];
-    quantize_part(v, r, w);
-    if (at + N <= q_cols) {
+    quantize_vec(v, r, w);
+    if (__builtin_expect(at + N <= q_cols, 1)) {
         __builtin_memcpy(row + at, w, N);
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (at + i < q_cols) row[at + i] = int8_t(w[i / 4] >> (8 * (i & 3)));
+    } else if (__builtin_expect(at < q_cols, 0)) {
+        uint64_t all = w[0];
+        if (N == 8) all |= uint64_t(w[N / 4 - 1]) << 32;
+#pragma unroll 1
+        for (int64_t i = at; i < q_cols; ++i, all >>= 8) row[i] = int8_t(all);
     }
 }
 
+// The largest value over the 8 or 16 neighbouring lanes that share a row.
+template <int LANES>
+__device__ __forceinline__ uint32_t most_of_lanes(uint32_t v)
+{
+    v = max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0xB1, 0xF, 0xF, true)));       // the other of a pair
+    v = max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x4E, 0xF, 0xF, true)));       // the other pair of four
+    v = max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x141, 0xF, 0xF, true)));      // the other four of eight
+    if (LANES >= 16) v = max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x140, 0xF, 0xF, true)));
+    if (LANES >= 32) v = max(v, uint32_t(__shfl_xor(int(v), 16)));
+    if (LANES >= 64) v = max(v, uint32_t(__shfl_xor(int(v), 32)));
+    return v;
+}
+
 // TPR threads of a workgroup share a row; each keeps its first KEEP vectors of 16 bytes in registers between finding the
-// row's scale and quantising, and reads what lies beyond (from a cache) twice.
-template <typename T, int TPR, int THREADS>
+// row's scale and quantising, and reads what lies beyond (from a cache) twice.  [cols, q_cols) is filled with zeros.
+// Code that runs is kept short: a launch of one wave's work a SIMD spends its time on fetching instructions.
+template <typename T, int TPR, int KEEP, int THREADS>
 __global__ void __launch_bounds__(THREADS)
 quantize_rows_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int64_t cols, int8_t *__restrict__ q, int64_t ldq,
                      int64_t q_cols, float *__restrict__ scale)
 {
-    constexpr int N = Vec<T>::N, KEEP = 4, RPW = THREADS / TPR;
+    constexpr int N = Vec<T>::N, RPW = THREADS / TPR;
     __shared__ uint32_t lds[THREADS / 64];
     const int sub = int(threadIdx.x) % TPR;
     const int64_t groups = (rows + RPW - 1) / RPW;
@@ -170,14 +203,11 @@ quantize_rows_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int64_t
         const T *row = x + (live ? r : rows - 1) * ldx;
         Vec<T> v[KEEP];
         uint32_t most = 0;
-#pragma unroll
-        for (int i = 0; i < KEEP; ++i) v[i] = load_part(row, (int64_t(i) * TPR + sub) * N, cols);
+        load_row<T, TPR, KEEP>(row, sub, cols, v);
 #pragma unroll
         for (int i = 0; i < KEEP; ++i) most = most_of(v[i], most);
-#pragma unroll 4
-        for (int64_t at = (int64_t(KEEP) * TPR + sub) * N; at < cols; at += TPR * N) most = most_of(load_part(row, at, cols), most);
-#pragma unroll
-        for (int d = (TPR < 64 ? TPR : 64) / 2; d; d >>= 1) most = max(most, uint32_t(__shfl_xor(int(most), d)));
+        for (int64_t at = (int64_t(KEEP) * TPR + sub) * N; at < cols; at += TPR * N) most = most_of(load_vec(row, at, cols), most);
+        most = most_of_lanes<(TPR < 64 ? TPR : 64)>(most);
         if (TPR > 64) {
             __syncthreads();
             if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = most;
@@ -190,9 +220,9 @@ quantize_rows_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int64_t
         if (!live) continue;
         int8_t *qrow = q + r * ldq;
 #pragma unroll
-        for (int i = 0; i < KEEP; ++i) store_part(v[i], s, qrow, (int64_t(i) * TPR + sub) * N, q_cols);
+        for (int i = 0; i < KEEP; ++i) store_vec(v[i], s, qrow, (int64_t(i) * TPR + sub) * N, q_cols);
         for (int64_t at = (int64_t(KEEP) * TPR + sub) * N; at < q_cols; at += TPR * N)
-            store_part(load_part(row, at, cols), s, qrow, at, q_cols);
+            store_vec(load_vec(row, at, cols), s, qrow, at, q_cols);
         if (sub == 0) scale[r] = s.scale;
     }
 }
@@ -200,27 +230,25 @@ quantize_rows_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int64_t
 // ---- the product --------------------------------------------------------------------------------------------------------
 
 // 16 bytes of a row that has `len` bytes, from `at` on; beyond its end zero.
+template <bool EXACT = false>
 __device__ __forceinline__ v4i load16(const int8_t *row, int at, int len)
 {
     v4i v = {0, 0, 0, 0};
-    if (at + 16 <= len) {
-        __builtin_memcpy(&v, row + at, 16);
-    } else if (at < len) {
-        uint32_t w[4] = {0, 0, 0, 0};
-        for (int i = 0; i < 15; ++i)
-            if (at + i < len) w[i >> 2] |= uint32_t(uint8_t(row[at + i])) << (8 * (i & 3));
-        v = v4i{int(w[0]), int(w[1]), int(w[2]), int(w[3])};
-    }
+    if (__builtin_expect(at + 16 <= len, 1)) __builtin_memcpy(&v, row + at, 16);
+    else if (!EXACT && __builtin_expect(at < len, 0)) v = load_end(row, at, len);
     return v;
 }
 
 // Four neighbouring channels of one row of y, from n on.  ReLU keeps NaN.
 struct Channels { f4 scale, bias; };
 
+// EXACT (here and below): sizes are such that nothing ends inside what a lane reads or writes at once.
+template <bool EXACT = false>
 __device__ __forceinline__ Channels channels_at(const I8Product &p, int n)
 {
     Channels c;
-    if (n + 4 <= p.n) {
+    if (EXACT || __builtin_expect(n + 4 <= p.n, 1)) {
+        if (EXACT) n = min(n, p.n - 4);
         __builtin_memcpy(&c.scale, p.sb + n, 16);
         if (p.bias) __builtin_memcpy(&c.bias, p.bias + n, 16);
     } else {
@@ -246,11 +274,11 @@ __device__ __forceinline__ f4 values_of(const I8Product &p, v4i acc, float sa, c
     return v;
 }
 
-template <typename Y, int N, typename V>
+template <typename Y, int N, bool EXACT = false, typename V>
 __device__ __forceinline__ void store_channels(const I8Product &p, int m, int n, V v)
 {
     Y *y = static_cast<Y *>(p.y) + (int64_t(m) * p.ldy + n);
-    if (n + N <= p.n) {
+    if (EXACT || __builtin_expect(n + N <= p.n, 1)) {
         __builtin_memcpy(y, &v, N * sizeof(Y));
     } else {
 #pragma unroll
@@ -274,26 +302,34 @@ template <> struct Deal<__bf16> {
     static __device__ __forceinline__ int first(int j, int g) { return (j >> 1) * 32 + g * 8 + (j & 1) * 4; }
 };
 
-// Rows m + 16 i of y, the NT * 16 channels from n0 on; the lane has `lane & 15` in m and its group in `g`.
-template <typename Y, int MT, int NT>
-__device__ __forceinline__ void store_tile(const I8Product &p, int m, int n0, int g, const v4i (&acc)[MT][NT], const float (&sa)[MT])
+// Rows m + 16 i of y, the NT * 16 channels from n0 on; the lane has `lane & 15` in m and its group in `g`.  Scales and biases are
+// read before anything is stored: behind a store they would be waited for one by one.
+template <typename Y, int NT, bool EXACT = false>
+__device__ __forceinline__ void load_channels(const I8Product &p, int n0, int g, Channels (&c)[NT])
+{
+#pragma unroll
+    for (int j = 0; j < NT; ++j) c[j] = channels_at<EXACT>(p, n0 + Deal<Y>::first(j, g));
+}
+
+template <typename Y, int MT, int NT, bool EXACT = false>
+__device__ __forceinline__ void store_tile(const I8Product &p, int m, int n0, int g, const v4i (&acc)[MT][NT], const float (&sa)[MT],
+                                           const Channels (&c)[NT])
 {
     static_assert(NT % 2 == 0, "");
 #pragma unroll
-    for (int j = 0; j < NT; j += 2) {
-        const int n = n0 + Deal<Y>::first(j, g), n2 = n0 + Deal<Y>::first(j + 1, g);
-        if (n >= p.n) continue;
-        const Channels c = channels_at(p, n), c2 = channels_at(p, n2);
+    for (int i = 0; i < MT; ++i) {
+        if (m + 16 * i >= p.m) continue;
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            if (m + 16 * i >= p.m) continue;
-            const f4 v = values_of(p, acc[i][j], sa[i], c), w = values_of(p, acc[i][j + 1], sa[i], c2);
+        for (int j = 0; j < NT; j += 2) {
+            const int n = n0 + Deal<Y>::first(j, g), n2 = n0 + Deal<Y>::first(j + 1, g);
+            if (n >= p.n) continue;
+            const f4 v = values_of(p, acc[i][j], sa[i], c[j]), w = values_of(p, acc[i][j + 1], sa[i], c[j + 1]);
             if (sizeof(Y) == 4) {
-                store_channels<float, 4>(p, m + 16 * i, n, v);
-                if (n2 < p.n) store_channels<float, 4>(p, m + 16 * i, n2, w);
+                store_channels<float, 4, EXACT>(p, m + 16 * i, n, v);
+                if (n2 < p.n) store_channels<float, 4, EXACT>(p, m + 16 * i, n2, w);
             } else {
                 const b8 o = __builtin_convertvector(__builtin_shufflevector(v, w, 0, 1, 2, 3, 4, 5, 6, 7), b8);
-                store_channels<__bf16, 8>(p, m + 16 * i, n, o);
+                store_channels<__bf16, 8, EXACT>(p, m + 16 * i, n, o);
             }
         }
     }
@@ -492,7 +528,9 @@ matmul_i8_kernel(const I8Product p, int splits, int *part)
     float sa[MT];
 #pragma unroll
     for (int i = 0; i < MT; ++i) sa[i] = p.sa[min(m + 16 * i, p.m - 1)];
-    store_tile<Y, MT, NT>(p, m, n0 + wn, g, acc, sa);
+    Channels c[NT];
+    load_channels<Y, NT>(p, n0 + wn, g, c);
+    store_tile<Y, MT, NT>(p, m, n0 + wn, g, acc, sa, c);
 }
 
 // y of the sums of `splits` parts of k; a thread has four channels.
@@ -515,112 +553,120 @@ matmul_i8_join_kernel(const I8Product p, int splits, const int *__restrict__ par
     }
 }
 
-// The largest value over the 8 or 16 neighbouring lanes that share a row.
-template <int LANES>
-__device__ __forceinline__ uint32_t most_of_lanes(uint32_t v)
-{
-    v = max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0xB1, 0xF, 0xF, true)));       // the other of a pair
-    v = max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x4E, 0xF, 0xF, true)));       // the other pair of four
-    v = max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x141, 0xF, 0xF, true)));      // the other four of eight
-    if (LANES == 16) v = max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x140, 0xF, 0xF, true)));
-    return v;
-}
-
 // Short rows (k up to kThinK): all of k of 16 * MT rows of activations lies in LDS, so that there is no loop of stages and one read of
 // the activations; where they come as floats (T) they are quantised on their way there and never leave the chip.
-// The weights, which every workgroup reads and the level-2 caches hold, go to the registers directly.  Four waves share
-// the rows and take groups of 64 channels in turn.  blockIdx.y: a part of the channels, a multiple of 64 (`part_n`).
-//
-// LANES lanes quantise a row, KEEP vectors of 16 bytes each.
+// The weights, which every workgroup reads and the level-2 caches hold, go to the registers directly, all KS steps of 64 bytes
+// of the first channels before the activations are waited for.  Four waves share the rows and take groups of 32 channels
+// in turn.  blockIdx.y: a part of the channels, a multiple of 32 (`part_n`).
 constexpr int kThinK = 512;
 
-template <typename T, typename Y, int MT, int LANES, int KEEP>
+template <typename T, typename Y, int MT, int KS, bool EXACT>
 __global__ void __launch_bounds__(256)
 linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, int part_n)
 {
-    constexpr int BM = 16 * MT, NT = 4;
-    extern __shared__ v4i thin_lds[];                    // BM rows of `pieces` times 16 bytes, and the scales of the rows
+    constexpr int BM = 16 * MT, NT = 2, PIECES = KS < 2 ? 8 : KS * 4;
+    __shared__ v4i lds[BM * PIECES];
+    __shared__ float scales[BM];
     const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
-    const int m0 = int(blockIdx.x) * BM, pieces = (p.k + 127) / 128 * 8;
-    float *const scales = reinterpret_cast<float *>(thin_lds + BM * pieces);
-    if (sizeof(T) == 1) {
-        for (int at = int(threadIdx.x); at < BM * pieces; at += 256) {
-            const int row = at / pieces, c = at - row * pieces;
-            thin_lds[row * pieces + (c ^ (row & 7))] =
-                load16(reinterpret_cast<const int8_t *>(x) + int64_t(min(m0 + row, p.m - 1)) * ldx, c * 16, p.k);
-        }
-        for (int row = int(threadIdx.x); row < BM; row += 256) scales[row] = p.sa[min(m0 + row, p.m - 1)];
-    } else {
-        using V = Vec<std::conditional_t<sizeof(T) == 1, float, T>>;
-        using E = std::conditional_t<sizeof(T) == 1, float, T>;
-        constexpr int N = V::N, AT_ONCE = 64 / LANES, PASSES = BM / 4 / AT_ONCE;
-        const int sub = lane % LANES;
-        V v[PASSES][KEEP];
+    const int m0 = int(blockIdx.x) * BM, r = lane & 15, g = lane >> 4;
+
+    const int n_end = min(p.n, int(blockIdx.y + 1) * part_n);
+    bool first = true;
+    float sa[MT];
+    for (int n0 = int(blockIdx.y) * part_n + wave * 32; first || n0 < n_end; n0 += 128) {
+        v4i vb[KS][NT];
+        Channels ch[NT];
+        auto fetch = [&]() {                             // (also behind the last channel, for nothing, so that there is no branch)
+            const int8_t *b[NT];
 #pragma unroll
-        for (int i = 0; i < PASSES; ++i) {
-            const int row = wave * (BM / 4) + i * AT_ONCE + lane / LANES;
-            const E *from = reinterpret_cast<const E *>(x) + int64_t(min(m0 + row, p.m - 1)) * ldx;
+            for (int j = 0; j < NT; ++j) b[j] = p.b + int64_t(min(n0 + Deal<Y>::row(j, r), p.n - 1)) * p.ldb;
 #pragma unroll
-            for (int q = 0; q < KEEP; ++q) v[i][q] = load_part(from, (q * LANES + sub) * N, p.k);
-        }
+            for (int s = 0; s < KS; ++s)
+                if ((EXACT && s == 0) || s * 64 + 64 <= p.k) {
 #pragma unroll
-        for (int i = 0; i < PASSES; ++i) {
-            const int row = wave * (BM / 4) + i * AT_ONCE + lane / LANES;
-            uint32_t most = 0;
+                    for (int j = 0; j < NT; ++j) __builtin_memcpy(&vb[s][j], b[j] + s * 64 + g * 16, 16);
+                }
+            if (!EXACT && p.k % 64 != 0) {
 #pragma unroll
-            for (int q = 0; q < KEEP; ++q) most = most_of(v[i][q], most);
-            const RowScale s = row_scale(most_of_lanes<LANES>(most));
-            if (sub == 0) scales[row] = s.scale;
+                for (int j = 0; j < NT; ++j) {
+                    const v4i end = load16(b[j], p.k / 64 * 64 + g * 16, p.k);
 #pragma unroll
-            for (int q = 0; q < KEEP; ++q) {
-                const int byte = (q * LANES + sub) * N, c = byte / 16;
-                uint32_t w[N / 4];
-                quantize_part(v[i][q], s, w);
-                if (c < pieces) __builtin_memcpy(reinterpret_cast<int8_t *>(thin_lds + row * pieces + (c ^ (row & 7))) + byte % 16, w, N);
+                    for (int s = 0; s < KS; ++s)
+                        if (s == p.k / 64) vb[s][j] = end;
+                }
+            }
+            load_channels<Y, NT, EXACT>(p, n0, g, ch);
+        };
+        if (!first) {
+            fetch();
+        } else if constexpr (sizeof(T) == 1) {
+            constexpr int EACH = BM * PIECES / 256;
+            v4i v[EACH];
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                const int at = i * 256 + int(threadIdx.x), row = at / PIECES, c = at % PIECES;
+                v[i] = load16<EXACT>(x + int64_t(min(m0 + row, p.m - 1)) * ldx, c * 16, p.k);
+            }
+            fetch();
+            if (threadIdx.x < BM) scales[threadIdx.x] = p.sa[min(m0 + int(threadIdx.x), p.m - 1)];
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                const int at = i * 256 + int(threadIdx.x), row = at / PIECES, c = at % PIECES;
+                lds[row * PIECES + (c ^ (row & 7))] = v[i];
+            }
+        } else {
+            // LANES lanes quantise a row, KEEP vectors of 16 bytes each
+            constexpr int N = Vec<T>::N, VECS = KS * 64 / N, LANES = VECS < 16 ? VECS : 16, KEEP = VECS / LANES;
+            constexpr int AT_ONCE = 64 / LANES, PASSES = BM / 4 / AT_ONCE;
+            const int sub = lane % LANES;
+            Vec<T> v[PASSES][KEEP];
+#pragma unroll
+            for (int i = 0; i < PASSES; ++i) {
+                const int row = wave * (BM / 4) + i * AT_ONCE + lane / LANES;
+                const T *from = x + int64_t(min(m0 + row, p.m - 1)) * ldx;
+                load_row<T, LANES, KEEP, EXACT>(from, sub, p.k, v[i]);
+            }
+            fetch();
+#pragma unroll
+            for (int i = 0; i < PASSES; ++i) {
+                const int row = wave * (BM / 4) + i * AT_ONCE + lane / LANES;
+                uint32_t most = 0;
+#pragma unroll
+                for (int q = 0; q < KEEP; ++q) most = most_of(v[i][q], most);
+                const RowScale s = row_scale(most_of_lanes<LANES>(most));
+                if (sub == 0) scales[row] = s.scale;
+#pragma unroll
+                for (int q = 0; q < KEEP; ++q) {
+                    const int byte = (q * LANES + sub) * N, c = byte / 16;
+                    uint32_t w[N / 4];
+                    quantize_vec(v[i][q], s, w);
+                    __builtin_memcpy(reinterpret_cast<int8_t *>(lds + row * PIECES + (c ^ (row & 7))) + byte % 16, w, N);
+                }
             }
         }
-    }
-    __syncthreads();
-
-    const int r = lane & 15, g = lane >> 4, n_end = min(p.n, int(blockIdx.y + 1) * part_n);
-    for (int n0 = int(blockIdx.y) * part_n + wave * 64; n0 < n_end; n0 += 256) {
-        const int8_t *b[NT];
+        if (first) {
+            __syncthreads();
 #pragma unroll
-        for (int j = 0; j < NT; ++j) b[j] = p.b + int64_t(min(n0 + Deal<Y>::row(j, r), p.n - 1)) * p.ldb;
+            for (int i = 0; i < MT; ++i) sa[i] = scales[i * 16 + r];
+            first = false;
+        }
         v4i acc[MT][NT];
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < NT; ++j) acc[i][j] = v4i{0, 0, 0, 0};
-        auto step = [&](const v4i (&vb)[NT], int k0) {
-            v4i va[MT];
-            const int c = k0 / 16 + g;
 #pragma unroll
-            for (int i = 0; i < MT; ++i) va[i] = thin_lds[(i * 16 + r) * pieces + (c ^ (r & 7))];
+        for (int s = 0; s < KS; ++s) {
+            if ((!EXACT || s > 0) && s * 64 >= p.k) continue;
+            v4i va[MT];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) va[i] = lds[(i * 16 + r) * PIECES + ((s * 4 + g) ^ (r & 7))];
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb[j], va[i], acc[i][j], 0, 0, 0);
-        };
-        auto fetch = [&](v4i (&vb)[NT], int k0) {
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                if (k0 + 64 <= p.k) __builtin_memcpy(&vb[j], b[j] + k0 + g * 16, 16);
-                else vb[j] = load16(b[j], k0 + g * 16, p.k);
-            }
-        };
-        v4i now[NT], next[NT];
-        if (p.k > 0) fetch(now, 0);
-        for (int k0 = 0; k0 < p.k; k0 += 64) {
-            if (k0 + 64 < p.k) fetch(next, k0 + 64);
-            step(now, k0);
-#pragma unroll
-            for (int j = 0; j < NT; ++j) now[j] = next[j];
+                for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb[s][j], va[i], acc[i][j], 0, 0, 0);
         }
-        float sa[MT];
-#pragma unroll
-        for (int i = 0; i < MT; ++i) sa[i] = scales[i * 16 + r];
-        store_tile<Y, MT, NT>(p, m0 + r, n0, g, acc, sa);
+        store_tile<Y, MT, NT, EXACT>(p, m0 + r, n0, g, acc, sa, ch);
     }
 }
 
@@ -675,19 +721,23 @@ int launch_quantize_rows(const void *x, int64_t ldx, int bf16, int64_t rows, int
 {
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const int64_t vecs = (q_cols + (bf16 ? 7 : 3)) / (bf16 ? 8 : 4);
-#define PCONV_LAUNCH(TPR, THREADS)                                                                                             \
+#define PCONV_LAUNCH(TPR, KEEP, THREADS)                                                                                       \
     do {                                                                                                                       \
         const unsigned grid = unsigned(std::min<int64_t>((rows + (THREADS / TPR) - 1) / (THREADS / TPR), 1 << 20));            \
-        if (bf16) hipLaunchKernelGGL((quantize_rows_kernel<__bf16, TPR, THREADS>), dim3(grid), dim3(THREADS), 0, st,           \
+        if (bf16) hipLaunchKernelGGL((quantize_rows_kernel<__bf16, TPR, KEEP, THREADS>), dim3(grid), dim3(THREADS), 0, st,     \
                                      static_cast<const __bf16 *>(x), ldx, rows, cols, q, ldq, q_cols, scale);                  \
-        else hipLaunchKernelGGL((quantize_rows_kernel<float, TPR, THREADS>), dim3(grid), dim3(THREADS), 0, st,                 \
+        else hipLaunchKernelGGL((quantize_rows_kernel<float, TPR, KEEP, THREADS>), dim3(grid), dim3(THREADS), 0, st,           \
                                 static_cast<const float *>(x), ldx, rows, cols, q, ldq, q_cols, scale);                        \
     } while (0)
-    if (vecs <= 8) PCONV_LAUNCH(8, 256);
-    else if (vecs <= 64) PCONV_LAUNCH(16, 256);
-    else if (vecs <= 256) PCONV_LAUNCH(64, 256);
-    else if (vecs <= 2048) PCONV_LAUNCH(256, 256);
-    else PCONV_LAUNCH(1024, 1024);
+    if (vecs <= 8) PCONV_LAUNCH(8, 1, 256);
+    else if (vecs <= 16) PCONV_LAUNCH(16, 1, 256);
+    else if (vecs <= 32) PCONV_LAUNCH(16, 2, 256);
+    else if (vecs <= 64) PCONV_LAUNCH(16, 4, 256);
+    else if (vecs <= 256) PCONV_LAUNCH(64, 4, 256);
+    else if (vecs <= 512) PCONV_LAUNCH(256, 2, 256);
+    else if (vecs <= 1024) PCONV_LAUNCH(256, 4, 256);
+    else if (vecs <= 4096) PCONV_LAUNCH(1024, 4, 1024);
+    else PCONV_LAUNCH(1024, 8, 1024);
 #undef PCONV_LAUNCH
     return check_launch("pconv_quantize_rows");
 }
@@ -726,22 +776,32 @@ void launch_tiles(const I8Product &p, int splits, int *part, bool dma, hipStream
 constexpr int64_t kRowsM = 16;                           // matmul_i8_rows_kernel serves up to so many rows
 
 // Rows of T (int8_t: quantised already, with their scales in p) times weights, k up to kThinK.
-template <typename T, int LANES, int KEEP>
-int launch_thin(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
+template <typename T, int KS>
+int launch_thin_steps(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
 {
-    const int64_t big = (int64_t(p.m) + 63) / 64, groups = (int64_t(p.n) + 255) / 256;
-    const int mt = big * groups >= 512 ? 4 : 2;
+    const int64_t groups = (int64_t(p.n) + 127) / 128;
+    const bool exact = p.k > 0 && p.k % 64 == 0 && p.n % 8 == 0;
+    const int mt = exact && (int64_t(p.m) + 63) / 64 * groups >= 512 ? 4 : 2;
     const int64_t tiles = (int64_t(p.m) + 16 * mt - 1) / (16 * mt);
     const int64_t parts = std::min<int64_t>(groups, std::max<int64_t>(1, 1024 / tiles));
-    const int part_n = int((groups + parts - 1) / parts * 256);
+    const int part_n = int((groups + parts - 1) / parts * 128);
     if (tiles >= int64_t(1) << 24) { set_error("pconv_matmul_i8: too many workgroups"); return PCONV_UNSUPPORTED; }
     const dim3 grid(unsigned(tiles), unsigned((int64_t(p.n) + part_n - 1) / part_n));
-    const size_t lds = size_t(16 * mt) * ((p.k + 127) / 128 * 128 + 4);
-#define PCONV_LAUNCH(Y, MT) hipLaunchKernelGGL((linear_i8_thin_kernel<T, Y, MT, LANES, KEEP>), grid, dim3(256), lds, st, p, x, ldx, part_n)
-    if (p.y_bf16) { if (mt == 4) PCONV_LAUNCH(__bf16, 4); else PCONV_LAUNCH(__bf16, 2); }
-    else { if (mt == 4) PCONV_LAUNCH(float, 4); else PCONV_LAUNCH(float, 2); }
+#define PCONV_LAUNCH(Y, MT, EXACT) \
+    hipLaunchKernelGGL((linear_i8_thin_kernel<T, Y, MT, KS, EXACT>), grid, dim3(256), 0, st, p, x, ldx, part_n)
+    if (p.y_bf16) { if (mt == 4) PCONV_LAUNCH(__bf16, 4, true); else if (exact) PCONV_LAUNCH(__bf16, 2, true); else PCONV_LAUNCH(__bf16, 2, false); }
+    else { if (mt == 4) PCONV_LAUNCH(float, 4, true); else if (exact) PCONV_LAUNCH(float, 2, true); else PCONV_LAUNCH(float, 2, false); }
 #undef PCONV_LAUNCH
     return check_launch("pconv_linear_i8 (short rows)");
+}
+
+template <typename T>
+int launch_thin(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
+{
+    if (p.k <= 64) return launch_thin_steps<T, 1>(p, x, ldx, st);
+    if (p.k <= 128) return launch_thin_steps<T, 2>(p, x, ldx, st);
+    if (p.k <= 256) return launch_thin_steps<T, 4>(p, x, ldx, st);
+    return launch_thin_steps<T, 8>(p, x, ldx, st);
 }
 
 }  // namespace
@@ -751,18 +811,7 @@ bool linear_i8_thin(int64_t m, int64_t n, int64_t k) { return m > kRowsM && k <=
 int launch_linear_i8_thin(const I8Product &p, const void *x, int64_t ldx, int bf16, void *stream)
 {
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (bf16) {
-        const __bf16 *const at = static_cast<const __bf16 *>(x);
-        if (p.k <= 64) return launch_thin<__bf16, 8, 1>(p, at, ldx, st);
-        if (p.k <= 128) return launch_thin<__bf16, 16, 1>(p, at, ldx, st);
-        if (p.k <= 256) return launch_thin<__bf16, 16, 2>(p, at, ldx, st);
-        return launch_thin<__bf16, 16, 4>(p, at, ldx, st);
-    }
-    const float *const at = static_cast<const float *>(x);
-    if (p.k <= 64) return launch_thin<float, 16, 1>(p, at, ldx, st);
-    if (p.k <= 128) return launch_thin<float, 16, 2>(p, at, ldx, st);
-    if (p.k <= 256) return launch_thin<float, 16, 4>(p, at, ldx, st);
-    return launch_thin<float, 16, 8>(p, at, ldx, st);
+    return bf16 ? launch_thin(p, static_cast<const __bf16 *>(x), ldx, st) : launch_thin(p, static_cast<const float *>(x), ldx, st);
 }
 
 int64_t matmul_i8_part_bytes(int64_t m, int64_t n, int64_t k)
@@ -779,7 +828,7 @@ int launch_matmul_i8(const I8Product &p, void *part, void *stream)
         hipLaunchKernelGGL((matmul_i8_rows_kernel<1, 8>), dim3(unsigned((p.n + 15) / 16)), dim3(512), 0, st, p);
         return check_launch("pconv_matmul_i8 (few rows)");
     }
-    if (linear_i8_thin(p.m, p.n, p.k)) return launch_thin<int8_t, 8, 1>(p, p.a, p.lda, st);
+    if (linear_i8_thin(p.m, p.n, p.k)) return launch_thin(p, p.a, p.lda, st);
     const Cut c = cut_of(p.m, p.n, p.k);
     const int64_t tiles = ((int64_t(p.m) + kTileM[c.tile] - 1) / kTileM[c.tile]) * ((int64_t(p.n) + kTileN[c.tile] - 1) / kTileN[c.tile]);
     if (tiles * c.splits >= int64_t(1) << 23) { set_error("pconv_matmul_i8: too many workgroups"); return PCONV_UNSUPPORTED; }
