@@ -232,7 +232,7 @@ int pconv_quantize_rows(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype
 /* pconv_matmul_i8 - y [m][n] of a [m][k] and b [n][k], both 8-bit, with a_scale [m], b_scale [n] and bias [n] (or NULL).
  * y is fp32, or bf16 rounded to nearest even.  `work`: device memory of at least pconv_matmul_i8_workspace bytes (mostly 0),
  * aligned to 16 bytes, used in stream order until the call's work is done, its contents are lost.
- * m and n up to 2^31 - 1, k up to 131071 (where 32 bits hold any sum).
+ * m and n up to 2^30, k up to 131071 (where 32 bits hold any sum).
  * Errors: PCONV_INVALID_ARG (null pointers, sizes or strides out of range, too little work space), PCONV_UNSUPPORTED,
  * PCONV_HIP_ERROR (launch failed). */
 int64_t pconv_matmul_i8_workspace(int64_t m, int64_t n, int64_t k);

@@ -8,6 +8,7 @@ present, calls fail loudly.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -457,20 +458,29 @@ def _type_of(t, what):
     raise ValueError(f"{what} must be float32 or bfloat16")
 
 
+_current_device = None
+
+
 def _device_index(*tensors) -> int:
     """The one device that the tensors (or None) are on, which has to be torch's current one."""
-    import torch
-    at = -1
+    global _current_device
+    if _current_device is None:
+        import torch
+        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    at = None
     for t in tensors:
         if t is None:
             continue
-        if not t.is_cuda:
+        i = t.get_device()                               # (-1 on the host)
+        if i < 0:
             raise ValueError("all tensors must be CUDA tensors")
-        i = t.get_device()
-        if at >= 0 and i != at:
+        if at is None:
+            at = i
+        elif i != at:
             raise ValueError("all tensors must be on one device")
-        at = i
-    if at >= 0 and at != torch.cuda.current_device():
+    if at is None:
+        return -1
+    if at != _current_device():
         raise ValueError("the tensors' device must be the current one")
     return at
 
@@ -506,12 +516,22 @@ def _prod(sizes) -> int:
     return n
 
 
+@functools.lru_cache(maxsize=4096)
+def _linear_i8_workspace(m: int, n: int, k: int, x_type: int) -> int:
+    return lib().pconv_linear_i8_workspace(m, n, k, x_type)
+
+
+@functools.lru_cache(maxsize=4096)
+def _matmul_i8_workspace(m: int, n: int, k: int) -> int:
+    return lib().pconv_matmul_i8_workspace(m, n, k)
+
+
 def _scratch(size: int, like):
     """Work space out of torch's pool for a call on the current stream."""
     import torch
     if torch.cuda.is_current_stream_capturing() and not _graph_pool_serves(like.device):
         raise RuntimeError("the stream is being captured by others than torch: call the pconv_... function with work space of your own")
-    return torch.empty(size, dtype=torch.uint8, device=like.device)
+    return like.new_empty(size, dtype=torch.uint8)
 
 
 def _per_channel(t, n, what):
@@ -523,11 +543,10 @@ def _per_channel(t, n, what):
 
 def _output(out, shape, dtype, like):
     """(tensor, elements from row to row) for a result of that shape."""
-    import torch
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=like.device)
-    elif out.dtype != dtype or out.shape != torch.Size(shape):
-        raise ValueError(f"out must be {dtype} of shape {tuple(shape)}")
+        return like.new_empty(shape, dtype=dtype), shape[-1]
+    if out.dtype != dtype or tuple(out.shape) != shape:
+        raise ValueError(f"out must be {dtype} of shape {shape}")
     return out, _rows(out, "out")[2]
 
 
@@ -602,7 +621,7 @@ def matmul_i8(a, a_scale, b, b_scale, bias=None, relu: bool = False, out_dtype=N
     sa, sb = _per_channel(a_scale, m, "a_scale"), _per_channel(b_scale, n, "b_scale")
     bp = _per_channel(bias, n, "bias") if bias is not None else None
     L = _lib or lib()
-    size = L.pconv_matmul_i8_workspace(m, n, k)
+    size = _matmul_i8_workspace(m, n, k)
     work = _scratch(size, a) if size > 0 else None
     rc = L.pconv_matmul_i8(a.data_ptr() or None, a_step, sa or None, b.data_ptr() or None, b_step, sb or None, bp or None,
                            y.data_ptr() or None, y_step, y_type, m, n, k, 1 if relu else 0,
@@ -633,7 +652,7 @@ def linear_i8(x, w, w_scale, bias=None, relu: bool = False, out_dtype=None, out=
     sw = _per_channel(w_scale, n, "w_scale")
     bp = _per_channel(bias, n, "bias") if bias is not None else None
     L = _lib or lib()
-    size = L.pconv_linear_i8_workspace(m, n, k, x_type)
+    size = _linear_i8_workspace(m, n, k, x_type)
     work = _scratch(size, x) if size > 0 else None
     rc = L.pconv_linear_i8(x.data_ptr() or None, x_step, x_type, w.data_ptr() or None, w_step, sw or None, bp or None,
                            y.data_ptr() or None, y_step, y_type, m, n, k, 1 if relu else 0,

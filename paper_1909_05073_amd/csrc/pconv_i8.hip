@@ -20,6 +20,7 @@ namespace {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+typedef uint16_t u2 __attribute__((ext_vector_type(2)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef __bf16 b4 __attribute__((ext_vector_type(4)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
@@ -39,6 +40,7 @@ struct RowScale {
     float scale;                                         // what is handed out: NaN where the row holds an infinity or a NaN
     float step, inv, lift;                               // scale * lift, its reciprocal, and a power of two
     uint32_t mask;                                       // 0: all of the row is 0
+    bool lifts;                                          // a row of the wave is lifted
 };
 
 __device__ __forceinline__ RowScale row_scale(uint32_t most)
@@ -51,21 +53,25 @@ __device__ __forceinline__ RowScale row_scale(uint32_t most)
     r.step = s * r.lift;
     r.inv = s > 0.0f ? 1.0f / r.step : 0.0f;
     r.mask = s > 0.0f ? 0xFFFFFFFFu : 0u;
+    r.lifts = __builtin_amdgcn_ballot_w64(s > 0.0f && s < 0x1p-60f) != 0;
     return r;
 }
 
 // The nearest whole number of the nearest fp32 number of x / scale, in the low byte.  The correctly rounded quotient comes
 // from the correctly rounded reciprocal by two corrections with the exact remainder (Markstein, 1990): five operations for a
-// division's eleven.  Small rows are lifted by a power of two first, so that a remainder that decides is no denormal.  A
-// scale that is itself a denormal is rounded to few bits; quotients may pass 127 then and are cut.  Adding 1.5 * 2^23
-// rounds to a whole number in the low bits, ties to even.
+// division's eleven.  Adding 1.5 * 2^23 rounds to a whole number in the low bits, ties to even.
+//
+// LIFT, for waves that hold a row of small values: those rows are lifted by a power of two first, so that a remainder that
+// decides is no denormal; a scale that is itself a denormal is rounded to few bits, and quotients that pass 127 are cut.
+template <bool LIFT>
 __device__ __forceinline__ uint32_t quantize(float x, const RowScale &r)
 {
-    x *= r.lift;
+    if (LIFT) x *= r.lift;
     float t = x * r.inv;
     t = __builtin_fmaf(__builtin_fmaf(-t, r.step, x), r.inv, t);
     t = __builtin_fmaf(__builtin_fmaf(-t, r.step, x), r.inv, t);
-    return __float_as_uint(__builtin_amdgcn_fmed3f(t, -127.0f, 127.0f) + 12582912.0f);
+    if (LIFT) t = __builtin_amdgcn_fmed3f(t, -127.0f, 127.0f);
+    return __float_as_uint(t + 12582912.0f);
 }
 
 // 16 bytes of a row of activations
@@ -81,12 +87,22 @@ template <> struct Vec<__bf16> {
     __device__ __forceinline__ float at(int i) const { return float(v[i]); }
 };
 
-template <typename T>
-__device__ __forceinline__ uint32_t most_of(const Vec<T> &v, uint32_t most)
+// (The bits of |x| as a float's; bf16 values two at a time.)
+__device__ __forceinline__ uint32_t most_of(const Vec<float> &v, uint32_t most)
 {
 #pragma unroll
-    for (int i = 0; i < Vec<T>::N; ++i) most = max(most, __float_as_uint(v.at(i)) & 0x7FFFFFFFu);
+    for (int i = 0; i < 4; ++i) most = max(most, __float_as_uint(v.v[i]) & 0x7FFFFFFFu);
     return most;
+}
+
+__device__ __forceinline__ uint32_t most_of(const Vec<__bf16> &v, uint32_t most)
+{
+    v4u w;
+    __builtin_memcpy(&w, &v.v, 16);
+    u2 m = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u2, uint32_t(w[i] & 0x7FFF7FFFu)));
+    return max(most, uint32_t(max(m.x, m.y)) << 16);
 }
 
 // The `size` (< 16) bytes that a row of `len` bytes has from `at` on, the rest zero: cut out of the row's last 16 bytes.
@@ -143,16 +159,23 @@ __device__ __forceinline__ void load_row(const T *row, int sub, int64_t cols, Ve
     }
 }
 
-template <typename T>
-__device__ __forceinline__ void quantize_vec(const Vec<T> &v, const RowScale &r, uint32_t (&w)[Vec<T>::N / 4])
+template <bool LIFT, typename T>
+__device__ __forceinline__ void quantize_as(const Vec<T> &v, const RowScale &r, uint32_t (&w)[Vec<T>::N / 4])
 {
 #pragma unroll
     for (int j = 0; j < Vec<T>::N / 4; ++j) {
         uint32_t q[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = quantize(v.at(4 * j + i), r);
+        for (int i = 0; i < 4; ++i) q[i] = quantize<LIFT>(v.at(4 * j + i), r);
         w[j] = (__builtin_amdgcn_perm(q[1], q[0], 0x0C0C0400u) | __builtin_amdgcn_perm(q[3], q[2], 0x04000C0Cu)) & r.mask;
     }
+}
+
+template <typename T>
+__device__ __forceinline__ void quantize_vec(const Vec<T> &v, const RowScale &r, uint32_t (&w)[Vec<T>::N / 4])
+{
+    if (__builtin_expect(r.lifts, 0)) quantize_as<true>(v, r, w);
+    else quantize_as<false>(v, r, w);
 }
 
 // The same elements quantised, to a row of q_cols bytes.
@@ -560,8 +583,8 @@ matmul_i8_join_kernel(const I8Product p, int splits, const int *__restrict__ par
 // in turn.  blockIdx.y: a part of the channels, a multiple of 32 (`part_n`).
 constexpr int kThinK = 512;
 
-template <typename T, typename Y, int MT, int KS, bool EXACT>
-__global__ void __launch_bounds__(256)
+template <typename T, typename Y, int MT, int KS, bool EXACT, int W>
+__global__ void __launch_bounds__(W * 64)
 linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, int part_n)
 {
     constexpr int BM = 16 * MT, NT = 2, PIECES = KS < 2 ? 8 : KS * 4;
@@ -571,85 +594,81 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
     const int m0 = int(blockIdx.x) * BM, r = lane & 15, g = lane >> 4;
 
     const int n_end = min(p.n, int(blockIdx.y + 1) * part_n);
-    bool first = true;
+    int n0 = int(blockIdx.y) * part_n + wave * 32;
+    v4i vb[KS][NT];
+    Channels ch[NT];
+    auto fetch = [&](int n0) {                           // (also behind the last channel, for nothing, so that there is no branch)
+        const int8_t *b[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) b[j] = p.b + int64_t(min(n0 + Deal<Y>::row(j, r), p.n - 1)) * p.ldb;
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+            if ((EXACT && s == 0) || s * 64 + 64 <= p.k) {
+#pragma unroll
+                for (int j = 0; j < NT; ++j) __builtin_memcpy(&vb[s][j], b[j] + s * 64 + g * 16, 16);
+            }
+        if (!EXACT && p.k % 64 != 0) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const v4i end = load16(b[j], p.k / 64 * 64 + g * 16, p.k);
+#pragma unroll
+                for (int s = 0; s < KS; ++s)
+                    if (s == p.k / 64) vb[s][j] = end;
+            }
+        }
+        load_channels<Y, NT, EXACT>(p, n0, g, ch);
+    };
+    if constexpr (sizeof(T) == 1) {
+        constexpr int EACH = BM * PIECES / (W * 64);
+        v4i v[EACH];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int at = i * (W * 64) + int(threadIdx.x), row = at / PIECES, c = at % PIECES;
+            v[i] = load16<EXACT>(x + int64_t(min(m0 + row, p.m - 1)) * ldx, c * 16, p.k);
+        }
+        fetch(n0);
+        if (threadIdx.x < BM) scales[threadIdx.x] = p.sa[min(m0 + int(threadIdx.x), p.m - 1)];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int at = i * (W * 64) + int(threadIdx.x), row = at / PIECES, c = at % PIECES;
+            lds[row * PIECES + (c ^ (row & 7))] = v[i];
+        }
+    } else {
+        // LANES lanes quantise a row, KEEP vectors of 16 bytes each
+        constexpr int N = Vec<T>::N, VECS = KS * 64 / N, LANES = VECS < 16 ? VECS : 16, KEEP = VECS / LANES;
+        constexpr int AT_ONCE = 64 / LANES, PASSES = BM / W / AT_ONCE;
+        static_assert(PASSES * AT_ONCE * W == BM, "");
+        const int sub = lane % LANES;
+        Vec<T> v[PASSES][KEEP];
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) {
+            const int row = wave * (BM / W) + i * AT_ONCE + lane / LANES;
+            const T *from = x + int64_t(min(m0 + row, p.m - 1)) * ldx;
+            load_row<T, LANES, KEEP, EXACT>(from, sub, p.k, v[i]);
+        }
+        fetch(n0);
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) {
+            const int row = wave * (BM / W) + i * AT_ONCE + lane / LANES;
+            uint32_t most = 0;
+#pragma unroll
+            for (int q = 0; q < KEEP; ++q) most = most_of(v[i][q], most);
+            const RowScale s = row_scale(most_of_lanes<LANES>(most));
+            if (sub == 0) scales[row] = s.scale;
+#pragma unroll
+            for (int q = 0; q < KEEP; ++q) {
+                const int byte = (q * LANES + sub) * N, c = byte / 16;
+                uint32_t w[N / 4];
+                quantize_vec(v[i][q], s, w);
+                __builtin_memcpy(reinterpret_cast<int8_t *>(lds + row * PIECES + (c ^ (row & 7))) + byte % 16, w, N);
+            }
+        }
+    }
+    __syncthreads();
     float sa[MT];
-    for (int n0 = int(blockIdx.y) * part_n + wave * 32; first || n0 < n_end; n0 += 128) {
-        v4i vb[KS][NT];
-        Channels ch[NT];
-        auto fetch = [&]() {                             // (also behind the last channel, for nothing, so that there is no branch)
-            const int8_t *b[NT];
 #pragma unroll
-            for (int j = 0; j < NT; ++j) b[j] = p.b + int64_t(min(n0 + Deal<Y>::row(j, r), p.n - 1)) * p.ldb;
-#pragma unroll
-            for (int s = 0; s < KS; ++s)
-                if ((EXACT && s == 0) || s * 64 + 64 <= p.k) {
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) __builtin_memcpy(&vb[s][j], b[j] + s * 64 + g * 16, 16);
-                }
-            if (!EXACT && p.k % 64 != 0) {
-#pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    const v4i end = load16(b[j], p.k / 64 * 64 + g * 16, p.k);
-#pragma unroll
-                    for (int s = 0; s < KS; ++s)
-                        if (s == p.k / 64) vb[s][j] = end;
-                }
-            }
-            load_channels<Y, NT, EXACT>(p, n0, g, ch);
-        };
-        if (!first) {
-            fetch();
-        } else if constexpr (sizeof(T) == 1) {
-            constexpr int EACH = BM * PIECES / 256;
-            v4i v[EACH];
-#pragma unroll
-            for (int i = 0; i < EACH; ++i) {
-                const int at = i * 256 + int(threadIdx.x), row = at / PIECES, c = at % PIECES;
-                v[i] = load16<EXACT>(x + int64_t(min(m0 + row, p.m - 1)) * ldx, c * 16, p.k);
-            }
-            fetch();
-            if (threadIdx.x < BM) scales[threadIdx.x] = p.sa[min(m0 + int(threadIdx.x), p.m - 1)];
-#pragma unroll
-            for (int i = 0; i < EACH; ++i) {
-                const int at = i * 256 + int(threadIdx.x), row = at / PIECES, c = at % PIECES;
-                lds[row * PIECES + (c ^ (row & 7))] = v[i];
-            }
-        } else {
-            // LANES lanes quantise a row, KEEP vectors of 16 bytes each
-            constexpr int N = Vec<T>::N, VECS = KS * 64 / N, LANES = VECS < 16 ? VECS : 16, KEEP = VECS / LANES;
-            constexpr int AT_ONCE = 64 / LANES, PASSES = BM / 4 / AT_ONCE;
-            const int sub = lane % LANES;
-            Vec<T> v[PASSES][KEEP];
-#pragma unroll
-            for (int i = 0; i < PASSES; ++i) {
-                const int row = wave * (BM / 4) + i * AT_ONCE + lane / LANES;
-                const T *from = x + int64_t(min(m0 + row, p.m - 1)) * ldx;
-                load_row<T, LANES, KEEP, EXACT>(from, sub, p.k, v[i]);
-            }
-            fetch();
-#pragma unroll
-            for (int i = 0; i < PASSES; ++i) {
-                const int row = wave * (BM / 4) + i * AT_ONCE + lane / LANES;
-                uint32_t most = 0;
-#pragma unroll
-                for (int q = 0; q < KEEP; ++q) most = most_of(v[i][q], most);
-                const RowScale s = row_scale(most_of_lanes<LANES>(most));
-                if (sub == 0) scales[row] = s.scale;
-#pragma unroll
-                for (int q = 0; q < KEEP; ++q) {
-                    const int byte = (q * LANES + sub) * N, c = byte / 16;
-                    uint32_t w[N / 4];
-                    quantize_vec(v[i][q], s, w);
-                    __builtin_memcpy(reinterpret_cast<int8_t *>(lds + row * PIECES + (c ^ (row & 7))) + byte % 16, w, N);
-                }
-            }
-        }
-        if (first) {
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < MT; ++i) sa[i] = scales[i * 16 + r];
-            first = false;
-        }
+    for (int i = 0; i < MT; ++i) sa[i] = scales[i * 16 + r];
+    for (; n0 < n_end; n0 += W * 32) {
         v4i acc[MT][NT];
 #pragma unroll
         for (int i = 0; i < MT; ++i)
@@ -666,52 +685,112 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
 #pragma unroll
                 for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb[s][j], va[i], acc[i][j], 0, 0, 0);
         }
-        store_tile<Y, MT, NT, EXACT>(p, m0 + r, n0, g, acc, sa, ch);
+        // what comes next is read before the stores: behind them it would wait for them
+        Channels now[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) now[j] = ch[j];
+        if (n0 + W * 32 < n_end) fetch(n0 + W * 32);
+        store_tile<Y, MT, NT, EXACT>(p, m0 + r, n0, g, acc, sa, now);
     }
 }
 
-// Few rows: 16 channels a workgroup, whose waves share the length of k in steps of 256 bytes and add their sums in LDS.
-template <int MT, int WAVES>
-__global__ void __launch_bounds__(WAVES * 64)
-matmul_i8_rows_kernel(const I8Product p)
+// Few rows (up to 16): 16 channels a workgroup, whose waves share the length of k in turns of 256 bytes and add their sums in LDS.
+// Reading the weights is all of it; a wave has the next turn's under way while it multiplies.  T is int8_t, or
+// the rows come as floats, up to kFusedRows elements, and every workgroup quantises all of them to LDS while its first weights
+// are on their way: less than a launch for it takes.
+constexpr int kRowsM = 16, kFusedRows = 32768;
+
+template <typename T>
+__global__ void __launch_bounds__(512)
+linear_i8_rows_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx)
 {
-    __shared__ v4i lds[WAVES][MT][64];
-    const int lane = int(threadIdx.x) & 63, wave = int(threadIdx.x) >> 6;
-    const int n0 = int(blockIdx.x) * 16;
-    const int8_t *b = p.b + int64_t(min(n0 + (lane & 15), p.n - 1)) * p.ldb;
-    const int8_t *a[MT];
+    constexpr int WAVES = 8, TURN = 256;
+    constexpr bool FUSED = sizeof(T) > 1;
+    extern __shared__ v4i rows_lds[];                    // quantised rows, `pitch` bytes from one to the next
+    __shared__ v4i sums[WAVES][64];
+    __shared__ uint32_t mosts[WAVES];
+    __shared__ float scales[kRowsM];
+    const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), r = lane & 15, g = lane >> 4;
+    const int n0 = int(blockIdx.x) * 16, pitch = (p.k + TURN - 1) / TURN * TURN + 16;
+    const int8_t *const b = p.b + int64_t(min(n0 + r, p.n - 1)) * p.ldb;
+    const int whole = p.k / TURN * TURN;
+    v4i vb[4];
+    auto fetch = [&](v4i (&v)[4], int k0) {
 #pragma unroll
-    for (int i = 0; i < MT; ++i) a[i] = p.a + int64_t(min(i * 16 + (lane & 15), p.m - 1)) * p.lda;
-    v4i acc[MT];
+        for (int s = 0; s < 4; ++s) __builtin_memcpy(&v[s], b + k0 + s * 64 + g * 16, 16);
+    };
+    int k0 = wave * TURN;
+    if (k0 < whole) fetch(vb, k0);
+    int8_t *const q = reinterpret_cast<int8_t *>(rows_lds);
+    if constexpr (FUSED) {
+        constexpr int N = Vec<T>::N, KEEP = 4, THREADS = WAVES * 64;
+        const int sub = int(threadIdx.x);
+        for (int m = 0; m < p.m; ++m) {
+            const T *row = x + int64_t(m) * ldx;
+            Vec<T> v[KEEP];
+            load_row<T, THREADS, KEEP>(row, sub, p.k, v);
+            uint32_t most = 0;
 #pragma unroll
-    for (int i = 0; i < MT; ++i) acc[i] = v4i{0, 0, 0, 0};
-    for (int k0 = wave * 256; k0 < p.k; k0 += WAVES * 256) {
-        v4i vb[4], va[4][MT];
-        const int at = k0 + (lane >> 4) * 16;
+            for (int i = 0; i < KEEP; ++i) most = most_of(v[i], most);
+#pragma unroll 4
+            for (int at = (KEEP * THREADS + sub) * N; at < p.k; at += THREADS * N) most = most_of(load_vec(row, at, p.k), most);
+            most = most_of_lanes<64>(most);
+            if (lane == 0) mosts[wave] = most;
+            __syncthreads();
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            vb[s] = load16(b, at + s * 64, p.k);
+            for (int i = 0; i < WAVES; ++i) most = max(most, mosts[i]);
+            const RowScale s = row_scale(most);
+            int8_t *to = q + m * pitch;
 #pragma unroll
-            for (int i = 0; i < MT; ++i) va[s][i] = load16(a[i], at + s * 64, p.k);
+            for (int i = 0; i < KEEP; ++i) {
+                const int at = (i * THREADS + sub) * N;
+                uint32_t w[N / 4];
+                quantize_vec(v[i], s, w);
+                if (at < p.k) __builtin_memcpy(to + at, w, N);
+            }
+            for (int at = (KEEP * THREADS + sub) * N; at < p.k; at += THREADS * N) {
+                uint32_t w[N / 4];
+                quantize_vec(load_vec(row, at, p.k), s, w);
+                __builtin_memcpy(to + at, w, N);
+            }
+            if (sub == 0) scales[m] = s.scale;
+            __syncthreads();
         }
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
-#pragma unroll
-            for (int i = 0; i < MT; ++i) acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb[s], va[s][i], acc[i], 0, 0, 0);
     }
+    const int8_t *const a = FUSED ? q + min(r, p.m - 1) * pitch : p.a + int64_t(min(r, p.m - 1)) * p.lda;
+    v4i acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    while (k0 < whole) {
+        v4i va[4], next[4];
+        const int k1 = k0 + WAVES * TURN;
 #pragma unroll
-    for (int i = 0; i < MT; ++i) lds[wave][i][lane] = acc[i];
+        for (int s = 0; s < 4; ++s) __builtin_memcpy(&va[s], a + k0 + s * 64 + g * 16, 16);
+        if (k1 < whole) fetch(next, k1);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) acc[s & 1] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb[s], va[s], acc[s & 1], 0, 0, 0);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) vb[s] = next[s];
+        k0 = k1;
+    }
+    if (whole < p.k && whole / TURN % WAVES == wave) {   // the last turn is no whole one
+        for (int s = whole; s < p.k; s += 64) {
+            const v4i w = load16(b, s + g * 16, p.k);
+            v4i v;
+            if (FUSED) __builtin_memcpy(&v, a + s + g * 16, 16);   // (beyond k the weights are zeros)
+            else v = load16(a, s + g * 16, p.k);
+            acc[0] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, v, acc[0], 0, 0, 0);
+        }
+    }
+    sums[wave][lane] = acc[0] + acc[1];
     __syncthreads();
-    for (int i = wave; i < MT; i += WAVES) {
-        v4i s = lds[0][i][lane];
+    if (wave) return;
+    v4i s = sums[0][lane];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) s += lds[w][i][lane];
-        const int m = i * 16 + (lane & 15), n = n0 + (lane >> 4) * 4;
-        if (m >= p.m || n >= p.n) continue;
-        const f4 v = values_of(p, s, p.sa[m], channels_at(p, n));
-        if (p.y_bf16) store_channels<__bf16, 4>(p, m, n, __builtin_convertvector(v, b4));
-        else store_channels<float, 4>(p, m, n, v);
-    }
+    for (int w = 1; w < WAVES; ++w) s += sums[w][lane];
+    const int n = n0 + g * 4;
+    if (r >= p.m || n >= p.n) return;
+    const f4 v = values_of(p, s, FUSED ? scales[r] : p.sa[r], channels_at(p, n));
+    if (p.y_bf16) store_channels<__bf16, 4>(p, r, n, __builtin_convertvector(v, b4));
+    else store_channels<float, 4>(p, r, n, v);
 }
 
 }  // namespace
@@ -744,7 +823,7 @@ int launch_quantize_rows(const void *x, int64_t ldx, int bf16, int64_t rows, int
 
 namespace {
 
-// How a product of more rows than matmul_i8_rows_kernel serves is cut up: the tile (an index into launch_tiles) and over how
+// How a product of more rows than linear_i8_rows_kernel serves is cut up: the tile (an index into launch_tiles) and over how
 // many workgroups the length of k is split.
 struct Cut { int tile, splits; };
 
@@ -773,24 +852,31 @@ void launch_tiles(const I8Product &p, int splits, int *part, bool dma, hipStream
 #undef PCONV_LAUNCH
 }
 
-constexpr int64_t kRowsM = 16;                           // matmul_i8_rows_kernel serves up to so many rows
+template <typename T>
+int launch_rows(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
+{
+    const size_t lds = sizeof(T) > 1 ? size_t(p.m) * ((p.k + 255) / 256 * 256 + 16) : 0;
+    hipLaunchKernelGGL((linear_i8_rows_kernel<T>), dim3(unsigned((int64_t(p.n) + 15) / 16)), dim3(512), lds, st, p, x, ldx);
+    return check_launch("pconv_linear_i8 (few rows)");
+}
 
 // Rows of T (int8_t: quantised already, with their scales in p) times weights, k up to kThinK.
 template <typename T, int KS>
 int launch_thin_steps(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
 {
-    const int64_t groups = (int64_t(p.n) + 127) / 128;
+    // Eight waves and 64 rows: 1568x512 -> 2048 12.4 us, with four waves and 32 rows 14.9; more parts than make 512 workgroups do not
+    // pay (every part quantises the rows again).  Rows or channels that end inside a load: four waves and 32 rows.
     const bool exact = p.k > 0 && p.k % 64 == 0 && p.n % 8 == 0;
-    const int mt = exact && (int64_t(p.m) + 63) / 64 * groups >= 512 ? 4 : 2;
-    const int64_t tiles = (int64_t(p.m) + 16 * mt - 1) / (16 * mt);
-    const int64_t parts = std::min<int64_t>(groups, std::max<int64_t>(1, 1024 / tiles));
-    const int part_n = int((groups + parts - 1) / parts * 128);
-    if (tiles >= int64_t(1) << 24) { set_error("pconv_matmul_i8: too many workgroups"); return PCONV_UNSUPPORTED; }
+    const int rows = exact ? 64 : 32, channels = exact ? 256 : 128;
+    const int64_t tiles = (int64_t(p.m) + rows - 1) / rows, groups = (int64_t(p.n) + channels - 1) / channels;
+    const int64_t parts = std::min<int64_t>(groups, std::max<int64_t>(1, 512 / tiles));
+    const int part_n = int((groups + parts - 1) / parts * channels);
+    if (tiles >= int64_t(1) << 23) { set_error("pconv_matmul_i8: too many workgroups"); return PCONV_UNSUPPORTED; }
     const dim3 grid(unsigned(tiles), unsigned((int64_t(p.n) + part_n - 1) / part_n));
-#define PCONV_LAUNCH(Y, MT, EXACT) \
-    hipLaunchKernelGGL((linear_i8_thin_kernel<T, Y, MT, KS, EXACT>), grid, dim3(256), 0, st, p, x, ldx, part_n)
-    if (p.y_bf16) { if (mt == 4) PCONV_LAUNCH(__bf16, 4, true); else if (exact) PCONV_LAUNCH(__bf16, 2, true); else PCONV_LAUNCH(__bf16, 2, false); }
-    else { if (mt == 4) PCONV_LAUNCH(float, 4, true); else if (exact) PCONV_LAUNCH(float, 2, true); else PCONV_LAUNCH(float, 2, false); }
+#define PCONV_LAUNCH(Y, MT, EXACT, W) \
+    hipLaunchKernelGGL((linear_i8_thin_kernel<T, Y, MT, KS, EXACT, W>), grid, dim3(W * 64), 0, st, p, x, ldx, part_n)
+    if (p.y_bf16) { if (exact) PCONV_LAUNCH(__bf16, 4, true, 8); else PCONV_LAUNCH(__bf16, 2, false, 4); }
+    else { if (exact) PCONV_LAUNCH(float, 4, true, 8); else PCONV_LAUNCH(float, 2, false, 4); }
 #undef PCONV_LAUNCH
     return check_launch("pconv_linear_i8 (short rows)");
 }
@@ -806,17 +892,20 @@ int launch_thin(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
 
 }  // namespace
 
-bool linear_i8_thin(int64_t m, int64_t n, int64_t k) { return m > kRowsM && k <= kThinK; }
+static bool thin(int64_t m, int64_t k) { return m > kRowsM && k <= kThinK; }
 
-int launch_linear_i8_thin(const I8Product &p, const void *x, int64_t ldx, int bf16, void *stream)
+bool linear_i8_fused(int64_t m, int64_t n, int64_t k) { return m <= kRowsM ? m * k <= kFusedRows : thin(m, k); }
+
+int launch_linear_i8_fused(const I8Product &p, const void *x, int64_t ldx, int bf16, void *stream)
 {
     const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (p.m <= kRowsM) return bf16 ? launch_rows(p, static_cast<const __bf16 *>(x), ldx, st) : launch_rows(p, static_cast<const float *>(x), ldx, st);
     return bf16 ? launch_thin(p, static_cast<const __bf16 *>(x), ldx, st) : launch_thin(p, static_cast<const float *>(x), ldx, st);
 }
 
 int64_t matmul_i8_part_bytes(int64_t m, int64_t n, int64_t k)
 {
-    if (m <= kRowsM || linear_i8_thin(m, n, k)) return 0;
+    if (m <= kRowsM || thin(m, k)) return 0;
     const Cut c = cut_of(m, n, k);
     return c.splits > 1 ? c.splits * m * ((n + 3) / 4 * 4) * 4 : 0;
 }
@@ -824,11 +913,8 @@ int64_t matmul_i8_part_bytes(int64_t m, int64_t n, int64_t k)
 int launch_matmul_i8(const I8Product &p, void *part, void *stream)
 {
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (p.m <= kRowsM) {
-        hipLaunchKernelGGL((matmul_i8_rows_kernel<1, 8>), dim3(unsigned((p.n + 15) / 16)), dim3(512), 0, st, p);
-        return check_launch("pconv_matmul_i8 (few rows)");
-    }
-    if (linear_i8_thin(p.m, p.n, p.k)) return launch_thin(p, p.a, p.lda, st);
+    if (p.m <= kRowsM) return launch_rows(p, p.a, p.lda, st);
+    if (thin(p.m, p.k)) return launch_thin(p, p.a, p.lda, st);
     const Cut c = cut_of(p.m, p.n, p.k);
     const int64_t tiles = ((int64_t(p.m) + kTileM[c.tile] - 1) / kTileM[c.tile]) * ((int64_t(p.n) + kTileN[c.tile] - 1) / kTileN[c.tile]);
     if (tiles * c.splits >= int64_t(1) << 23) { set_error("pconv_matmul_i8: too many workgroups"); return PCONV_UNSUPPORTED; }

@@ -24,9 +24,9 @@ int launch_quantize_rows(const void *x, int64_t ldx, int bf16, int64_t rows, int
 // bytes of work space (sums of parts of k) that the product takes, and the product
 int64_t matmul_i8_part_bytes(int64_t m, int64_t n, int64_t k);
 int launch_matmul_i8(const I8Product &p, void *part, void *stream);
-// Whether rows are so short that their activations are quantised within the product, and that product (p.a, lda, sa unused).
-bool linear_i8_thin(int64_t m, int64_t n, int64_t k);
-int launch_linear_i8_thin(const I8Product &p, const void *x, int64_t ldx, int bf16, void *stream);
+// Whether rows are so few or so short that they are quantised within the product, and that product (p.a, lda, sa unused).
+bool linear_i8_fused(int64_t m, int64_t n, int64_t k);
+int launch_linear_i8_fused(const I8Product &p, const void *x, int64_t ldx, int bf16, void *stream);
 
 // Up to kGradTensors tensors travel in the arguments of one launch (4 KiB).
 constexpr int kGradTensors = 160, kGradChunk = 16384, kGradBlocks = 2048;

@@ -12,7 +12,7 @@ using namespace pconv;
 
 namespace {
 
-constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1, kMaxK = 131071;
+constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1, kMaxSide = int64_t(1) << 30, kMaxK = 131071;
 constexpr int64_t kMaxTensors = 1 << 24, kMaxElements = int64_t(1) << 45;    // fewer than 2^32 chunks together
 
 int invalid(const char *who, const char *what)
@@ -27,7 +27,7 @@ int64_t round16(int64_t v) { return (v + 15) / 16 * 16; }
 // rows of `len` elements that lie `stride` apart: within the range of a byte offset in 64 bits
 bool stride_fits(int64_t rows, int64_t len, int64_t stride) { return stride >= len && stride <= (int64_t(1) << 58) / (rows > 0 ? rows : 1); }
 
-bool sizes_fit(int64_t m, int64_t n, int64_t k) { return m > 0 && n > 0 && k >= 0 && m <= kMaxRows && n <= kMaxRows && k <= kMaxK; }
+bool sizes_fit(int64_t m, int64_t n, int64_t k) { return m > 0 && n > 0 && k >= 0 && m <= kMaxSide && n <= kMaxSide && k <= kMaxK; }
 
 int check_work(const char *who, const void *work, int64_t have, int64_t need)
 {
@@ -40,7 +40,7 @@ int check_work(const char *who, const void *work, int64_t have, int64_t need)
 int check_product(const char *who, const int8_t *b, int64_t ldb, const float *sb, const float *bias, void *y, int64_t ldy, int y_dtype,
                   int64_t m, int64_t n, int64_t k, int relu, I8Product &p)
 {
-    if (m < 0 || n < 0 || k < 0 || m > kMaxRows || n > kMaxRows) return invalid(who, "m and n must be 0 .. 2^31 - 1");
+    if (m < 0 || n < 0 || k < 0 || m > kMaxSide || n > kMaxSide) return invalid(who, "m and n must be 0 .. 2^30");
     if (k > kMaxK) return invalid(who, "k must be 0 .. 131071");
     if (!is_dtype(y_dtype)) return invalid(who, "unknown dtype of y");
     if (m == 0 || n == 0) return PCONV_OK;
@@ -141,7 +141,7 @@ int pconv_matmul_i8(const int8_t *a_dev, int64_t a_stride, const float *a_scale,
 
 int64_t pconv_linear_i8_workspace(int64_t m, int64_t n, int64_t k, pconv_dtype)
 {
-    return sizes_fit(m, n, k) && !linear_i8_thin(m, n, k) ? round16(4 * m) + m * round16(k) + matmul_i8_part_bytes(m, n, k) : 0;
+    return sizes_fit(m, n, k) && !linear_i8_fused(m, n, k) ? round16(4 * m) + m * round16(k) + matmul_i8_part_bytes(m, n, k) : 0;
 }
 
 int pconv_linear_i8(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, const int8_t *w_dev, int64_t w_stride,
@@ -156,7 +156,7 @@ int pconv_linear_i8(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, co
     if (k && !x_dev) return invalid(who, "null pointer argument");
     if (!stride_fits(m, k, x_stride)) return invalid(who, "rows must lie at least their length apart");
     if (const int rc = check_work(who, work, work_bytes, pconv_linear_i8_workspace(m, n, k, x_dtype))) return rc;
-    if (linear_i8_thin(m, n, k)) return launch_linear_i8_thin(p, x_dev, x_stride, x_dtype == PCONV_BF16, hip_stream);
+    if (linear_i8_fused(m, n, k)) return launch_linear_i8_fused(p, x_dev, x_stride, x_dtype == PCONV_BF16, hip_stream);
     float *const scale = static_cast<float *>(work);
     int8_t *const q = static_cast<int8_t *>(work) + round16(4 * m);
     const int64_t ldq = round16(k);

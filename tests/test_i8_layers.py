@@ -402,6 +402,7 @@ def c_calls():
     yield "apart", lambda: P.pconv_quantize_rows(p, 7, "f32", 2, 8, p, 8, p)
     yield "apart", lambda: P.pconv_quantize_rows(p, 8, "f32", 2, 8, p, 7, p)
     yield "apart", lambda: P.pconv_quantize_rows(p, 1 << 60, "f32", 2, 8, p, 8, p)
+    yield "m and n", lambda: P.pconv_matmul_i8(p, 16, p, p, 16, p, 0, p, 4, "f32", 4, (1 << 30) + 1, 16)
     yield "k must", lambda: P.pconv_matmul_i8(p, 1 << 18, p, p, 1 << 18, p, 0, p, 4, "f32", 4, 4, 131072)
     yield "m and n", lambda: P.pconv_matmul_i8(p, 16, p, p, 16, p, 0, p, 4, "f32", 1 << 31, 4, 16)
     yield "m and n", lambda: P.pconv_matmul_i8(p, 16, p, p, 16, p, 0, p, 4, "f32", 4, -4, 16)
@@ -413,13 +414,13 @@ def c_calls():
         args[i] = 0
         a, sa, b, sb, y = args
         yield "null", lambda a=a, sa=sa, b=b, sb=sb, y=y: P.pconv_matmul_i8(a, 16, sa, b, 16, sb, 0, y, 4, "f32", 4, 4, 16)
-    need = P.pconv_linear_i8_workspace(400, 40, 160)
-    assert need >= 400 * 160
-    yield "work space", lambda: P.pconv_linear_i8(p, 160, "f32", p, 160, p, 0, p, 40, "f32", 400, 40, 160, False, p, need - 1)
-    yield "work space", lambda: P.pconv_linear_i8(p, 160, "f32", p, 160, p, 0, p, 40, "f32", 400, 40, 160, False, 0, need)
-    yield "work space", lambda: P.pconv_linear_i8(p, 160, "f32", p, 160, p, 0, p, 40, "f32", 400, 40, 160, False, p + 8, need)
-    yield "null", lambda: P.pconv_linear_i8(0, 160, "f32", p, 160, p, 0, p, 40, "f32", 400, 40, 160, False, p, need)
-    yield "apart", lambda: P.pconv_linear_i8(p, 159, "f32", p, 160, p, 0, p, 40, "f32", 400, 40, 160, False, p, need)
+    need = P.pconv_linear_i8_workspace(400, 40, 1600)
+    assert need >= 400 * 1600
+    yield "work space", lambda: P.pconv_linear_i8(p, 1600, "f32", p, 1600, p, 0, p, 40, "f32", 400, 40, 1600, False, p, need - 1)
+    yield "work space", lambda: P.pconv_linear_i8(p, 1600, "f32", p, 1600, p, 0, p, 40, "f32", 400, 40, 1600, False, 0, need)
+    yield "work space", lambda: P.pconv_linear_i8(p, 1600, "f32", p, 1600, p, 0, p, 40, "f32", 400, 40, 1600, False, p + 8, need)
+    yield "null", lambda: P.pconv_linear_i8(0, 1600, "f32", p, 1600, p, 0, p, 40, "f32", 400, 40, 1600, False, p, need)
+    yield "apart", lambda: P.pconv_linear_i8(p, 1599, "f32", p, 1600, p, 0, p, 40, "f32", 400, 40, 1600, False, p, need)
 
 
 def test_c_entries_refuse_what_they_cannot_run():
