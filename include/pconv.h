@@ -231,18 +231,20 @@ int pconv_quantize_rows(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype
 
 /* pconv_matmul_i8 - y [m][n] of a [m][k] and b [n][k], both 8-bit, with a_scale [m], b_scale [n] and bias [n] (or NULL).
  * y is fp32, or bf16 rounded to nearest even.  `work`: device memory of at least pconv_matmul_i8_workspace bytes (mostly 0),
- * aligned to 16 bytes, used in stream order until the call's work is done, its contents are lost.
+ * aligned to 16 bytes, used in stream order until the call's work is done, its contents are lost.  rows_at_16: whether the
+ * rows of a and b all begin at multiples of 16 bytes and lie at most 8 MiB apart; with 0 the size is enough for any rows.
  * m and n up to 2^30, k up to 131071 (where 32 bits hold any sum).
  * Errors: PCONV_INVALID_ARG (null pointers, sizes or strides out of range, too little work space), PCONV_UNSUPPORTED,
  * PCONV_HIP_ERROR (launch failed). */
-int64_t pconv_matmul_i8_workspace(int64_t m, int64_t n, int64_t k);
+int64_t pconv_matmul_i8_workspace(int64_t m, int64_t n, int64_t k, int rows_at_16);
 int pconv_matmul_i8(const int8_t *a_dev, int64_t a_stride, const float *a_scale, const int8_t *b_dev, int64_t b_stride,
                     const float *b_scale, const float *bias_dev, void *y_dev, int64_t y_stride, pconv_dtype y_dtype,
                     int64_t m, int64_t n, int64_t k, int fuse_relu, void *work, int64_t work_bytes, void *hip_stream);
 
 /* pconv_linear_i8 - pconv_quantize_rows of x [m][k] and pconv_matmul_i8 with the weights w [n][k], in one call and with
- * the same results.  The quantised activations stay in the work space, or on the chip where the call is small. */
-int64_t pconv_linear_i8_workspace(int64_t m, int64_t n, int64_t k, pconv_dtype x_dtype);
+ * the same results.  The quantised activations stay in the work space, or on the chip where rows are few or short.
+ * rows_at_16: as above, of the rows of w. */
+int64_t pconv_linear_i8_workspace(int64_t m, int64_t n, int64_t k, int rows_at_16);
 int pconv_linear_i8(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, const int8_t *w_dev, int64_t w_stride,
                     const float *w_scale, const float *bias_dev, void *y_dev, int64_t y_stride, pconv_dtype y_dtype,
                     int64_t m, int64_t n, int64_t k, int fuse_relu, void *work, int64_t work_bytes, void *hip_stream);

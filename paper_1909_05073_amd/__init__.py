@@ -110,7 +110,7 @@ def lib():
     L.pconv_quantize_rows.restype = ip
     L.pconv_quantize_rows.argtypes = [vp, i64, ip, i64, i64, vp, i64, vp, vp]
     L.pconv_matmul_i8_workspace.restype = i64
-    L.pconv_matmul_i8_workspace.argtypes = [i64, i64, i64]
+    L.pconv_matmul_i8_workspace.argtypes = [i64, i64, i64, ip]
     L.pconv_matmul_i8.restype = ip
     L.pconv_matmul_i8.argtypes = [vp, i64, vp, vp, i64, vp, vp, vp, i64, ip, i64, i64, i64, ip, vp, i64, vp]
     L.pconv_linear_i8_workspace.restype = i64
@@ -516,16 +516,6 @@ def _prod(sizes) -> int:
     return n
 
 
-@functools.lru_cache(maxsize=4096)
-def _linear_i8_workspace(m: int, n: int, k: int, x_type: int) -> int:
-    return lib().pconv_linear_i8_workspace(m, n, k, x_type)
-
-
-@functools.lru_cache(maxsize=4096)
-def _matmul_i8_workspace(m: int, n: int, k: int) -> int:
-    return lib().pconv_matmul_i8_workspace(m, n, k)
-
-
 def _scratch(size: int, like):
     """Work space out of torch's pool for a call on the current stream."""
     import torch
@@ -557,8 +547,8 @@ def pconv_quantize_rows(x_ptr: int, x_stride: int, x_dtype, rows: int, cols: int
                                      scale_ptr or None, stream or None))
 
 
-def pconv_matmul_i8_workspace(m: int, n: int, k: int) -> int:
-    return lib().pconv_matmul_i8_workspace(m, n, k)
+def pconv_matmul_i8_workspace(m: int, n: int, k: int, rows_at_16: bool = False) -> int:
+    return lib().pconv_matmul_i8_workspace(m, n, k, int(bool(rows_at_16)))
 
 
 def pconv_matmul_i8(a_ptr: int, a_stride: int, a_scale: int, b_ptr: int, b_stride: int, b_scale: int, bias_ptr, y_ptr: int,
@@ -570,8 +560,8 @@ def pconv_matmul_i8(a_ptr: int, a_stride: int, a_scale: int, b_ptr: int, b_strid
                                  work or None, work_bytes, stream or None))
 
 
-def pconv_linear_i8_workspace(m: int, n: int, k: int, x_dtype=F32) -> int:
-    return lib().pconv_linear_i8_workspace(m, n, k, _DTYPE[x_dtype])
+def pconv_linear_i8_workspace(m: int, n: int, k: int, rows_at_16: bool = False) -> int:
+    return lib().pconv_linear_i8_workspace(m, n, k, int(bool(rows_at_16)))
 
 
 def pconv_linear_i8(x_ptr: int, x_stride: int, x_dtype, w_ptr: int, w_stride: int, w_scale: int, bias_ptr, y_ptr: int,
@@ -581,6 +571,15 @@ def pconv_linear_i8(x_ptr: int, x_stride: int, x_dtype, w_ptr: int, w_stride: in
     _check(lib().pconv_linear_i8(x_ptr or None, x_stride, _DTYPE[x_dtype], w_ptr or None, w_stride, w_scale or None,
                                  bias_ptr or None, y_ptr or None, y_stride, _DTYPE[y_dtype], m, n, k, int(bool(fuse_relu)),
                                  work or None, work_bytes, stream or None))
+
+
+# (remembered by sizes: a call of the library costs 0.7 us)
+_linear_i8_workspace = functools.lru_cache(maxsize=4096)(pconv_linear_i8_workspace)
+_matmul_i8_workspace = functools.lru_cache(maxsize=4096)(pconv_matmul_i8_workspace)
+
+
+def _at_16(ptr: int, step: int) -> bool:
+    return (ptr | step) & 15 == 0 and step <= 1 << 23
 
 
 def quantize_rows(x):
@@ -621,9 +620,10 @@ def matmul_i8(a, a_scale, b, b_scale, bias=None, relu: bool = False, out_dtype=N
     sa, sb = _per_channel(a_scale, m, "a_scale"), _per_channel(b_scale, n, "b_scale")
     bp = _per_channel(bias, n, "bias") if bias is not None else None
     L = _lib or lib()
-    size = _matmul_i8_workspace(m, n, k)
+    a_ptr, b_ptr = a.data_ptr(), b.data_ptr()
+    size = _matmul_i8_workspace(m, n, k, _at_16(a_ptr, a_step) and _at_16(b_ptr, b_step))
     work = _scratch(size, a) if size > 0 else None
-    rc = L.pconv_matmul_i8(a.data_ptr() or None, a_step, sa or None, b.data_ptr() or None, b_step, sb or None, bp or None,
+    rc = L.pconv_matmul_i8(a_ptr or None, a_step, sa or None, b_ptr or None, b_step, sb or None, bp or None,
                            y.data_ptr() or None, y_step, y_type, m, n, k, 1 if relu else 0,
                            work.data_ptr() if work is not None else None, size, _stream(index))
     if rc != OK:
@@ -652,9 +652,10 @@ def linear_i8(x, w, w_scale, bias=None, relu: bool = False, out_dtype=None, out=
     sw = _per_channel(w_scale, n, "w_scale")
     bp = _per_channel(bias, n, "bias") if bias is not None else None
     L = _lib or lib()
-    size = _linear_i8_workspace(m, n, k, x_type)
+    w_ptr = w.data_ptr()
+    size = _linear_i8_workspace(m, n, k, _at_16(w_ptr, w_step))
     work = _scratch(size, x) if size > 0 else None
-    rc = L.pconv_linear_i8(x.data_ptr() or None, x_step, x_type, w.data_ptr() or None, w_step, sw or None, bp or None,
+    rc = L.pconv_linear_i8(x.data_ptr() or None, x_step, x_type, w_ptr or None, w_step, sw or None, bp or None,
                            y.data_ptr() or None, y_step, y_type, m, n, k, 1 if relu else 0,
                            work.data_ptr() if work is not None else None, size, _stream(index))
     if rc != OK:

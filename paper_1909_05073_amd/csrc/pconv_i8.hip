@@ -364,10 +364,11 @@ __device__ __forceinline__ v4u buffer_at(const int8_t *p)
     v4u r;
     r.x = __builtin_amdgcn_readfirstlane(uint32_t(at));
     r.y = __builtin_amdgcn_readfirstlane(uint32_t(at >> 32) & 0xFFFFu);
-    r.z = 0xFFFFFFFFu;
+    r.z = 0xFFFF0000u;
     r.w = 0x00020000u;
     return r;
 }
+constexpr uint32_t kNowhere = 0xFFFFFFF0u;               // an offset beyond any buffer: nothing is read, LDS gets zeros
 
 // Which tile a workgroup computes.  Workgroups go round the 8 XCDs, each of which has a level-2 cache of its own: an XCD gets
 // a run of tiles, and a run goes down GROUP tiles of rows before it goes on to the next tile of channels, so that the tiles that
@@ -386,13 +387,13 @@ __device__ __forceinline__ void tile_at(unsigned id, unsigned tiles_m, unsigned 
 // LDS.  A row of a stage is eight pieces of 16 bytes, stored in an order that depends on the row so that the eight rows that are
 // read at once lie in different banks.
 //
-// DMA: stages go from memory to LDS past the registers, S - 1 of them ahead of the one that is multiplied; a wave waits for its own
-// loads of the next stage, and the barrier then tells it that everybody's are there and that the stage before is read.  What
-// is left of k behind the last whole stage goes through registers, and so does everything where rows do not begin at
-// multiples of 16 bytes (DMA = false; one stage ahead).
+// Stages go from memory to LDS past the registers, S - 1 of them ahead of the one that is multiplied; a wave waits for its own
+// loads of the next stage, and the barrier then tells it that everybody's are there and that the stage before is read.  In
+// the last stage the pieces behind the end of k are zeros; only where k ends inside a piece does that stage go through registers.
+// Rows begin at multiples of 16 bytes (realign_kernel sees to it).
 //
 // `splits` workgroups share a tile, each with its part of k; their sums go to `part` [splits][m][n4], n4 = n rounded up to four.
-template <typename Y, int BM, int BN, int WM, int WN, int S, bool DMA>
+template <typename Y, int BM, int BN, int WM, int WN, int S>
 __global__ void __launch_bounds__(WM * WN * 64)
 matmul_i8_kernel(const I8Product p, int splits, int *part)
 {
@@ -444,96 +445,64 @@ matmul_i8_kernel(const I8Product p, int splits, int *part)
         }
     };
 
-    // through registers: a thread fetches the pieces at its place in every block of eight rows
-    v4i ra[PA], rb[PB];
-    auto fetch = [&](int k0) {
-        const int at = k0 + (lane & 7) * 16;
+    const v4u at_a = buffer_at(p.a + int64_t(m0) * p.lda + k_begin), at_b = buffer_at(p.b + int64_t(n0) * p.ldb + k_begin);
+    uint32_t off_a[PA], off_b[PB];
+    int col_a[PA], col_b[PB];                            // where a lane's piece begins in a stage
 #pragma unroll
-        for (int i = 0; i < PA; ++i) {
-            const int row = min(m0 + (i * NW + wave) * 8 + (lane >> 3), p.m - 1);
-            ra[i] = load16(p.a + int64_t(row) * p.lda, at, k_end);
-        }
+    for (int i = 0; i < PA; ++i) {
+        const int row = (i * NW + wave) * 8 + (lane >> 3);
+        col_a[i] = ((lane & 7) ^ (row & 7)) * 16;
+        off_a[i] = uint32_t(min(row, p.m - 1 - m0)) * uint32_t(p.lda) + uint32_t(col_a[i]);
+    }
 #pragma unroll
-        for (int i = 0; i < PB; ++i) {
-            const int row = min(n0 + (i * NW + wave) * 8 + (lane >> 3), p.n - 1);
-            rb[i] = load16(p.b + int64_t(row) * p.ldb, at, k_end);
-        }
+    for (int i = 0; i < PB; ++i) {
+        const int row = (i * NW + wave) * 8 + (lane >> 3);
+        col_b[i] = ((lane & 7) ^ key_b(row)) * 16;
+        off_b[i] = uint32_t(min(row, p.n - 1 - n0)) * uint32_t(p.ldb) + uint32_t(col_b[i]);
+    }
+    const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds)) + uint32_t(wave) * 1024u;
+    // (written as assembly so that the compiler does not wait for these loads before every read of LDS)
+    const int length = k_end - k_begin, whole = length / BK, rest = length % BK;
+    const int count = whole + (rest > 0 && rest % 16 == 0 ? 1 : 0);
+    auto stage = [&](int s) {
+        const uint32_t to = base + uint32_t(s % S) * uint32_t(STAGE * 16), k0 = uint32_t(s) * BK;
+        const int have = s < whole ? BK : rest;
+#pragma unroll
+        for (int i = 0; i < PA; ++i)
+            asm volatile("s_mov_b32 m0, %1\n s_nop 0\n buffer_load_dwordx4 %0, %2, %3 offen lds"
+                         ::"v"(col_a[i] < have ? off_a[i] : kNowhere), "s"(to + uint32_t(i * NW * 1024)), "s"(at_a), "s"(k0) : "memory");
+#pragma unroll
+        for (int i = 0; i < PB; ++i)
+            asm volatile("s_mov_b32 m0, %1\n s_nop 0\n buffer_load_dwordx4 %0, %2, %3 offen lds"
+                         ::"v"(col_b[i] < have ? off_b[i] : kNowhere), "s"(to + uint32_t(BM * 128 + i * NW * 1024)), "s"(at_b), "s"(k0) : "memory");
     };
-    auto store = [&](v4i *st) {
+    constexpr int L = PA + PB;
+    static_assert((S - 2) * L <= 63, "");
 #pragma unroll
-        for (int i = 0; i < PA; ++i) {
-            const int row = (i * NW + wave) * 8 + (lane >> 3);
-            st[row * 8 + ((lane & 7) ^ (row & 7))] = ra[i];
-        }
-#pragma unroll
-        for (int i = 0; i < PB; ++i) {
-            const int row = (i * NW + wave) * 8 + (lane >> 3);
-            st[BM * 8 + row * 8 + ((lane & 7) ^ key_b(row))] = rb[i];
-        }
-    };
-
-    if (DMA) {
-        const v4u at_a = buffer_at(p.a + int64_t(m0) * p.lda + k_begin), at_b = buffer_at(p.b + int64_t(n0) * p.ldb + k_begin);
-        uint32_t off_a[PA], off_b[PB];
-#pragma unroll
-        for (int i = 0; i < PA; ++i) {
-            const int row = (i * NW + wave) * 8 + (lane >> 3);
-            off_a[i] = uint32_t(min(row, p.m - 1 - m0)) * uint32_t(p.lda) + uint32_t(((lane & 7) ^ (row & 7)) * 16);
-        }
-#pragma unroll
-        for (int i = 0; i < PB; ++i) {
-            const int row = (i * NW + wave) * 8 + (lane >> 3);
-            off_b[i] = uint32_t(min(row, p.n - 1 - n0)) * uint32_t(p.ldb) + uint32_t(((lane & 7) ^ key_b(row)) * 16);
-        }
-        const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds)) + uint32_t(wave) * 1024u;
-        // (written as assembly so that the compiler does not wait for these loads before every read of LDS)
-        auto stage = [&](int s) {
-            const uint32_t to = base + uint32_t(s % S) * uint32_t(STAGE * 16), k0 = uint32_t(s) * BK;
-#pragma unroll
-            for (int i = 0; i < PA; ++i)
-                asm volatile("s_mov_b32 m0, %1\n s_nop 0\n buffer_load_dwordx4 %0, %2, %3 offen lds"
-                             ::"v"(off_a[i]), "s"(to + uint32_t(i * NW * 1024)), "s"(at_a), "s"(k0) : "memory");
-#pragma unroll
-            for (int i = 0; i < PB; ++i)
-                asm volatile("s_mov_b32 m0, %1\n s_nop 0\n buffer_load_dwordx4 %0, %2, %3 offen lds"
-                             ::"v"(off_b[i]), "s"(to + uint32_t(BM * 128 + i * NW * 1024)), "s"(at_b), "s"(k0) : "memory");
-        };
-        constexpr int L = PA + PB;
-        static_assert((S - 2) * L <= 63, "");
-        const int whole = (k_end - k_begin) / BK;
-#pragma unroll
-        for (int s = 0; s < S - 1; ++s)
-            if (s < whole) stage(s);
-        for (int s = 0; s < whole; ++s) {
+    for (int s = 0; s < S - 1; ++s)
+        if (s < count) stage(s);
+    const int all = count + (rest % 16 != 0 ? 1 : 0);
+#pragma unroll 1
+    for (int s = 0; s < all; ++s) {
+        if (s < count) {
             // the loads of stage s are done when at most those of the stages behind it are under way
-            const int behind = min(S - 2, whole - 1 - s);
+            const int behind = min(S - 2, count - 1 - s);
             if (behind == S - 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n s_barrier" ::"n"((S - 2) * L) : "memory");
             else if (S > 3 && behind == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n s_barrier" ::"n"(L) : "memory");
             else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n s_barrier" ::: "memory");
-            if (s + S - 1 < whole) stage(s + S - 1);
-            multiply(lds + (s % S) * STAGE);
-        }
-        if (k_begin + whole * BK < k_end) {
-            fetch(k_begin + whole * BK);
-            __syncthreads();
-            store(lds);
-            __syncthreads();
-            multiply(lds);
-        }
-    } else {
-        if (k_begin < k_end) {
-            fetch(k_begin);
-            store(lds);
-        }
-        __syncthreads();
-        int buf = 0;
-        for (int k0 = k_begin; k0 < k_end; k0 += BK, buf ^= 1) {
-            const bool more = k0 + BK < k_end;
-            if (more) fetch(k0 + BK);
-            multiply(lds + buf * STAGE);
-            if (more) store(lds + (buf ^ 1) * STAGE);
+            if (s + S - 1 < count) stage(s + S - 1);
+        } else {                                         // k ends inside a piece
+            v4i *const to = lds + (s % S) * STAGE + wave * 64 + lane;
+#pragma unroll 1
+            for (int i = 0; i < PA + PB; ++i) {
+                const bool b = i >= PA;
+                const int at = ((b ? i - PA : i) * NW + wave) * 8 + (lane >> 3), key = b ? key_b(at) : at & 7;
+                const int8_t *row = b ? p.b + int64_t(min(n0 + at, p.n - 1)) * p.ldb : p.a + int64_t(min(m0 + at, p.m - 1)) * p.lda;
+                to[i * NW * 64] = load16(row, k_begin + whole * BK + ((lane & 7) ^ key) * 16, k_end);
+            }
             __syncthreads();
         }
+        multiply(lds + (s % S) * STAGE);
     }
 
     const int m = m0 + wm + (lane & 15), g = lane >> 4;
@@ -554,6 +523,21 @@ matmul_i8_kernel(const I8Product p, int splits, int *part)
     Channels c[NT];
     load_channels<Y, NT>(p, n0 + wn, g, c);
     store_tile<Y, MT, NT>(p, m, n0 + wn, g, acc, sa, c);
+}
+
+// Rows to multiples of 16 bytes, zeros behind their ends; blockIdx.y: which of two matrices.
+struct Realign { const int8_t *from[2]; int8_t *to[2]; int64_t ld[2]; int rows[2]; int k, pieces; };
+
+__global__ void __launch_bounds__(256)
+realign_kernel(const Realign a)
+{
+    const int i = int(blockIdx.y);
+    const int64_t all = int64_t(a.rows[i]) * a.pieces;
+    for (int64_t t = int64_t(blockIdx.x) * 256 + threadIdx.x; t < all; t += int64_t(gridDim.x) * 256) {
+        const int64_t row = t / a.pieces;
+        const v4i v = load16(a.from[i] + row * a.ld[i], int(t - row * a.pieces) * 16, a.k);
+        __builtin_memcpy(a.to[i] + t * 16, &v, 16);
+    }
 }
 
 // y of the sums of `splits` parts of k; a thread has four channels.
@@ -584,7 +568,7 @@ matmul_i8_join_kernel(const I8Product p, int splits, const int *__restrict__ par
 constexpr int kThinK = 512;
 
 template <typename T, typename Y, int MT, int KS, bool EXACT, int W>
-__global__ void __launch_bounds__(W * 64)
+__global__ void __launch_bounds__(W * 64, KS <= 4 ? 4 : 2)
 linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, int part_n)
 {
     constexpr int BM = 16 * MT, NT = 2, PIECES = KS < 2 ? 8 : KS * 4;
@@ -596,7 +580,6 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
     const int n_end = min(p.n, int(blockIdx.y + 1) * part_n);
     int n0 = int(blockIdx.y) * part_n + wave * 32;
     v4i vb[KS][NT];
-    Channels ch[NT];
     auto fetch = [&](int n0) {                           // (also behind the last channel, for nothing, so that there is no branch)
         const int8_t *b[NT];
 #pragma unroll
@@ -616,7 +599,6 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
                     if (s == p.k / 64) vb[s][j] = end;
             }
         }
-        load_channels<Y, NT, EXACT>(p, n0, g, ch);
     };
     if constexpr (sizeof(T) == 1) {
         constexpr int EACH = BM * PIECES / (W * 64);
@@ -685,12 +667,11 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
 #pragma unroll
                 for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb[s][j], va[i], acc[i][j], 0, 0, 0);
         }
-        // what comes next is read before the stores: behind them it would wait for them
-        Channels now[NT];
-#pragma unroll
-        for (int j = 0; j < NT; ++j) now[j] = ch[j];
+        Channels ch[NT];
+        load_channels<Y, NT, EXACT>(p, n0, g, ch);
+        // the next weights are read before the stores: behind them they would wait for them
         if (n0 + W * 32 < n_end) fetch(n0 + W * 32);
-        store_tile<Y, MT, NT, EXACT>(p, m0 + r, n0, g, acc, sa, now);
+        store_tile<Y, MT, NT, EXACT>(p, m0 + r, n0, g, acc, sa, ch);
     }
 }
 
@@ -827,29 +808,34 @@ namespace {
 // many workgroups the length of k is split.
 struct Cut { int tile, splits; };
 
-constexpr int kTileM[] = {32, 64, 128, 256}, kTileN[] = {128, 128, 128, 256};
+constexpr int kTiles = 4, kTileM[kTiles] = {32, 64, 128, 256}, kTileN[kTiles] = {128, 128, 128, 256};
+constexpr int64_t kUnits = 256;                          // compute units
 
+// The cheapest by a count of cycles: a compute unit takes its tiles one after the other, a stage of a tile at the rate of the
+// matrix units (half of their peak) or of what 40 bytes a cycle bring from the level-2 cache, whichever is slower.
+// Joining the parts of k is one more launch and reads and writes the sums.
 Cut cut_of(int64_t m, int64_t n, int64_t k)
 {
-    const auto tiles = [&](int t) { return ((m + kTileM[t] - 1) / kTileM[t]) * ((n + kTileN[t] - 1) / kTileN[t]); };
-    Cut c{m <= 32 ? 0 : m <= 64 ? 1 : 2, 1};
-    if (tiles(3) >= 256) c.tile = 3;
-    else if (c.tile == 2 && tiles(2) < 256 && tiles(1) >= 2 * tiles(2) && tiles(1) <= 512) c.tile = 1;
+    constexpr int64_t stage_cycles[kTiles] = {512, 614, 1100, 4096}, start = 4000, join = 9000;
     const int64_t stages = (k + 127) / 128;
-    if (tiles(c.tile) <= 128 && stages >= 8)
-        c.splits = int(std::min<int64_t>(std::min<int64_t>(256 / tiles(c.tile), stages / 4), 32));
-    return c;
+    Cut best{0, 1};
+    double least = 0;
+    for (int t = 0; t < kTiles; ++t)
+        for (int64_t s = 1; s == 1 || (s <= 32 && s * 4 <= stages); s *= 2) {
+            const int64_t tiles = ((m + kTileM[t] - 1) / kTileM[t]) * ((n + kTileN[t] - 1) / kTileN[t]);
+            double c = double((tiles * s + kUnits - 1) / kUnits) * double((stages + s - 1) / s) * double(stage_cycles[t]) + start;
+            if (s > 1) c += join + double(s) * double(m) * double(n) * 8 / 2000;
+            if ((t == 0 && s == 1) || c < least || (c == least && s == 1)) { least = c; best = Cut{t, int(s)}; }
+        }
+    return best;
 }
 
 template <int BM, int BN, int WM, int WN, int S>
-void launch_tiles(const I8Product &p, int splits, int *part, bool dma, hipStream_t st)
+void launch_tiles(const I8Product &p, int splits, int *part, hipStream_t st)
 {
     const unsigned grid = unsigned(((int64_t(p.m) + BM - 1) / BM) * ((int64_t(p.n) + BN - 1) / BN) * splits);
-#define PCONV_LAUNCH(Y, STAGES, DMA) \
-    hipLaunchKernelGGL((matmul_i8_kernel<Y, BM, BN, WM, WN, STAGES, DMA>), dim3(grid), dim3(WM * WN * 64), 0, st, p, splits, part)
-    if (p.y_bf16) { if (dma) PCONV_LAUNCH(__bf16, S, true); else PCONV_LAUNCH(__bf16, 2, false); }
-    else { if (dma) PCONV_LAUNCH(float, S, true); else PCONV_LAUNCH(float, 2, false); }
-#undef PCONV_LAUNCH
+    if (p.y_bf16) hipLaunchKernelGGL((matmul_i8_kernel<__bf16, BM, BN, WM, WN, S>), dim3(grid), dim3(WM * WN * 64), 0, st, p, splits, part);
+    else hipLaunchKernelGGL((matmul_i8_kernel<float, BM, BN, WM, WN, S>), dim3(grid), dim3(WM * WN * 64), 0, st, p, splits, part);
 }
 
 template <typename T>
@@ -903,29 +889,50 @@ int launch_linear_i8_fused(const I8Product &p, const void *x, int64_t ldx, int b
     return bf16 ? launch_thin(p, static_cast<const __bf16 *>(x), ldx, st) : launch_thin(p, static_cast<const float *>(x), ldx, st);
 }
 
-int64_t matmul_i8_part_bytes(int64_t m, int64_t n, int64_t k)
+bool rows_at_16(const int8_t *at, int64_t ld) { return reinterpret_cast<uintptr_t>(at) % 16 == 0 && ld % 16 == 0 && ld <= 1 << 23; }
+
+int64_t matmul_i8_work_bytes(int64_t m, int64_t n, int64_t k, bool a_at_16, bool b_at_16)
 {
     if (m <= kRowsM || thin(m, k)) return 0;
     const Cut c = cut_of(m, n, k);
-    return c.splits > 1 ? c.splits * m * ((n + 3) / 4 * 4) * 4 : 0;
+    const int64_t row = (k + 15) / 16 * 16;
+    return (a_at_16 ? 0 : m * row) + (b_at_16 ? 0 : n * row) + (c.splits > 1 ? c.splits * m * ((n + 3) / 4 * 4) * 4 : 0);
 }
 
-int launch_matmul_i8(const I8Product &p, void *part, void *stream)
+int launch_matmul_i8(const I8Product &product, void *work, void *stream)
 {
     const hipStream_t st = static_cast<hipStream_t>(stream);
+    I8Product p = product;
     if (p.m <= kRowsM) return launch_rows(p, p.a, p.lda, st);
     if (thin(p.m, p.k)) return launch_thin(p, p.a, p.lda, st);
     const Cut c = cut_of(p.m, p.n, p.k);
     const int64_t tiles = ((int64_t(p.m) + kTileM[c.tile] - 1) / kTileM[c.tile]) * ((int64_t(p.n) + kTileN[c.tile] - 1) / kTileN[c.tile]);
     if (tiles * c.splits >= int64_t(1) << 23) { set_error("pconv_matmul_i8: too many workgroups"); return PCONV_UNSUPPORTED; }
-    // rows at multiples of 16 bytes, a tile's rows within 32 bits
-    const auto fits = [](const int8_t *at, int64_t ld) { return reinterpret_cast<uintptr_t>(at) % 16 == 0 && ld % 16 == 0 && ld <= 1 << 23; };
-    const bool dma = fits(p.a, p.lda) && fits(p.b, p.ldb);
-    int *const sums = static_cast<int *>(part);
-    if (c.tile == 0) launch_tiles<32, 128, 1, 4, 4>(p, c.splits, sums, dma, st);
-    else if (c.tile == 1) launch_tiles<64, 128, 2, 2, 3>(p, c.splits, sums, dma, st);
-    else if (c.tile == 2) launch_tiles<128, 128, 2, 2, 2>(p, c.splits, sums, dma, st);
-    else launch_tiles<256, 256, 2, 4, 2>(p, c.splits, sums, dma, st);
+    int8_t *at = static_cast<int8_t *>(work);
+    Realign r{};
+    r.k = p.k; r.pieces = (p.k + 15) / 16;
+    unsigned moved = 0;
+    const auto move = [&](const int8_t *&from, int64_t &ld, int rows) {
+        if (rows_at_16(from, ld)) return;
+        r.from[moved] = from; r.to[moved] = at; r.ld[moved] = ld; r.rows[moved] = rows;
+        ++moved;
+        from = at; ld = int64_t(r.pieces) * 16;
+        at += rows * ld;
+    };
+    move(p.a, p.lda, p.m);
+    move(p.b, p.ldb, p.n);
+    if (moved) {
+        const int64_t most = int64_t(std::max(r.rows[0], r.rows[1])) * r.pieces;
+        hipLaunchKernelGGL(realign_kernel, dim3(unsigned(std::min<int64_t>((most + 255) / 256, 1 << 16)), moved), dim3(256), 0, st, r);
+        if (const int rc = check_launch("pconv_matmul_i8 (aligning rows)")) return rc;
+    }
+    int *const sums = reinterpret_cast<int *>(at);
+    // (tiles of 128 rows: four stages where a compute unit has one workgroup, two where it has two)
+    if (c.tile == 0) launch_tiles<32, 128, 1, 4, 4>(p, c.splits, sums, st);
+    else if (c.tile == 1) launch_tiles<64, 128, 2, 2, 3>(p, c.splits, sums, st);
+    else if (c.tile == 2 && tiles * c.splits <= kUnits) launch_tiles<128, 128, 2, 2, 4>(p, c.splits, sums, st);
+    else if (c.tile == 2) launch_tiles<128, 128, 2, 2, 2>(p, c.splits, sums, st);
+    else launch_tiles<256, 256, 2, 4, 2>(p, c.splits, sums, st);
     if (const int rc = check_launch("pconv_matmul_i8")) return rc;
     if (c.splits == 1) return PCONV_OK;
     const int64_t quads = (int64_t(p.n) + 3) / 4 * p.m;

@@ -21,9 +21,11 @@ struct I8Product {
 // Launchers: arguments checked, sizes not 0.  They return a pconv_status.
 int launch_quantize_rows(const void *x, int64_t ldx, int bf16, int64_t rows, int64_t cols, int8_t *q, int64_t ldq,
                          int64_t q_cols, float *scale, void *stream);
-// bytes of work space (sums of parts of k) that the product takes, and the product
-int64_t matmul_i8_part_bytes(int64_t m, int64_t n, int64_t k);
-int launch_matmul_i8(const I8Product &p, void *part, void *stream);
+// Whether rows begin at multiples of 16 bytes (and a tile's lie within 32 bits); the work space of a product (copies of
+// operands whose rows do not, sums of parts of k), and the product.
+bool rows_at_16(const int8_t *at, int64_t ld);
+int64_t matmul_i8_work_bytes(int64_t m, int64_t n, int64_t k, bool a_at_16, bool b_at_16);
+int launch_matmul_i8(const I8Product &p, void *work, void *stream);
 // Whether rows are so few or so short that they are quantised within the product, and that product (p.a, lda, sa unused).
 bool linear_i8_fused(int64_t m, int64_t n, int64_t k);
 int launch_linear_i8_fused(const I8Product &p, const void *x, int64_t ldx, int bf16, void *stream);

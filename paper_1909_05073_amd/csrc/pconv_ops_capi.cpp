@@ -119,9 +119,9 @@ int pconv_quantize_rows(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype
     return launch_quantize_rows(x_dev, x_stride, x_dtype == PCONV_BF16, rows, cols, q_dev, q_stride, cols, scale_dev, hip_stream);
 }
 
-int64_t pconv_matmul_i8_workspace(int64_t m, int64_t n, int64_t k)
+int64_t pconv_matmul_i8_workspace(int64_t m, int64_t n, int64_t k, int rows_at_16)
 {
-    return sizes_fit(m, n, k) ? matmul_i8_part_bytes(m, n, k) : 0;
+    return sizes_fit(m, n, k) ? matmul_i8_work_bytes(m, n, k, rows_at_16 != 0, rows_at_16 != 0) : 0;
 }
 
 int pconv_matmul_i8(const int8_t *a_dev, int64_t a_stride, const float *a_scale, const int8_t *b_dev, int64_t b_stride,
@@ -134,14 +134,14 @@ int pconv_matmul_i8(const int8_t *a_dev, int64_t a_stride, const float *a_scale,
     if (m == 0 || n == 0) return PCONV_OK;
     if (!a_scale || (k && !a_dev)) return invalid(who, "null pointer argument");
     if (!stride_fits(m, k, a_stride)) return invalid(who, "rows must lie at least their length apart");
-    if (const int rc = check_work(who, work, work_bytes, pconv_matmul_i8_workspace(m, n, k))) return rc;
+    if (const int rc = check_work(who, work, work_bytes, matmul_i8_work_bytes(m, n, k, rows_at_16(a_dev, a_stride), rows_at_16(b_dev, b_stride)))) return rc;
     p.a = a_dev; p.lda = a_stride; p.sa = a_scale;
     return launch_matmul_i8(p, work, hip_stream);
 }
 
-int64_t pconv_linear_i8_workspace(int64_t m, int64_t n, int64_t k, pconv_dtype)
+int64_t pconv_linear_i8_workspace(int64_t m, int64_t n, int64_t k, int rows_at_16)
 {
-    return sizes_fit(m, n, k) && !linear_i8_fused(m, n, k) ? round16(4 * m) + m * round16(k) + matmul_i8_part_bytes(m, n, k) : 0;
+    return sizes_fit(m, n, k) && !linear_i8_fused(m, n, k) ? round16(4 * m) + m * round16(k) + matmul_i8_work_bytes(m, n, k, true, rows_at_16 != 0) : 0;
 }
 
 int pconv_linear_i8(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, const int8_t *w_dev, int64_t w_stride,
@@ -155,7 +155,7 @@ int pconv_linear_i8(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, co
     if (m == 0 || n == 0) return PCONV_OK;
     if (k && !x_dev) return invalid(who, "null pointer argument");
     if (!stride_fits(m, k, x_stride)) return invalid(who, "rows must lie at least their length apart");
-    if (const int rc = check_work(who, work, work_bytes, pconv_linear_i8_workspace(m, n, k, x_dtype))) return rc;
+    if (const int rc = check_work(who, work, work_bytes, pconv_linear_i8_workspace(m, n, k, rows_at_16(w_dev, w_stride)))) return rc;
     if (linear_i8_fused(m, n, k)) return launch_linear_i8_fused(p, x_dev, x_stride, x_dtype == PCONV_BF16, hip_stream);
     float *const scale = static_cast<float *>(work);
     int8_t *const q = static_cast<int8_t *>(work) + round16(4 * m);
