@@ -30,21 +30,25 @@ int launch_matmul_i8(const I8Product &p, void *work, void *stream);
 bool linear_i8_fused(int64_t m, int64_t n, int64_t k);
 int launch_linear_i8_fused(const I8Product &p, const void *x, int64_t ldx, int bf16, void *stream);
 
-// Up to kGradTensors tensors travel in the arguments of one launch (4 KiB).
-constexpr int kGradTensors = 160, kGradChunk = 16384, kGradBlocks = 2048;
+// Up to kGradTensors tensors travel in the arguments of one launch (4 KiB), cut into chunks of 1 << `log2` elements.
+constexpr int kGradTensors = 160, kGradBlocks = 2048;
+constexpr int kGradLog2 = 14, kGradLog2Few = 12, kGradLog2One = 10;          // many elements, few, a launch of one workgroup
 struct GradTable {
     const void *in[kGradTensors];
     void *out[kGradTensors];
     uint32_t start[kGradTensors];      // first chunk of the tensor (ascending)
     uint16_t last[kGradTensors];       // elements of its last chunk, less one
     uint16_t types[kGradTensors];      // bit 0: input bf16, bit 1: output bf16
-    int32_t count;
+    int32_t count, log2;
     uint32_t chunks;
+    uint32_t passing;                  // the first pass reads chunks below this one past the caches (the second all, with `passing`)
 };
 int launch_grad_norm(const GradTable &t, unsigned blocks, double *partials, void *stream);
 int launch_grad_total(const double *partials, unsigned count, double *total, float *norm, void *stream);
-int launch_grad_scale(const GradTable &t, unsigned blocks, const double *partials, unsigned count, float max_norm, float eps,
-                      float *norm, void *stream);
+int launch_grad_scale(const GradTable &t, const double *partials, unsigned count, bool passing, float max_norm, float eps, float *norm,
+                      void *stream);
+// few elements: all of it by one workgroup
+int launch_grad_clip_one(const GradTable &t, float max_norm, float eps, float *norm, void *stream);
 
 }  // namespace pconv
 

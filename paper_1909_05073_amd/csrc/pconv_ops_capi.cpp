@@ -50,24 +50,75 @@ int check_product(const char *who, const int8_t *b, int64_t ldb, const float *sb
     return PCONV_OK;
 }
 
-// A table of up to kGradTensors of the tensors from `at` on, which moves there; false where there are none left.
-bool next_table(const void *const *in, void *const *out, const int64_t *counts, const int32_t *types, const int32_t *out_types,
-                int64_t num, int64_t &at, GradTable &t)
+// The tensors that are clipped together, and how they are cut up.
+struct Grads {
+    const void *const *in;
+    void *const *out;
+    const int64_t *counts;
+    const int32_t *types, *out_types;
+    int64_t num;
+    int log2;              // elements of a chunk
+    int64_t chunks;        // all of them
+    int64_t kept;          // bytes of the last gradients that are left in the caches; less than 0: of all
+
+    int64_t tables() const { return (num + kGradTensors - 1) / kGradTensors; }
+};
+
+constexpr int64_t kKeptBytes = int64_t(192) << 20, kCachedBytes = int64_t(256) << 20;
+
+Grads grads_of(const void *const *in, void *const *out, const int64_t *counts, const int32_t *types, const int32_t *out_types, int64_t num)
 {
-    t.count = 0; t.chunks = 0;
-    for (; at < num && t.count < kGradTensors; ++at) {
-        const int64_t n = counts[at];
-        if (n == 0) continue;
-        const int64_t chunks = (n + kGradChunk - 1) / kGradChunk;
-        const int i = t.count++;
-        t.in[i] = in[at];
-        t.out[i] = out ? out[at] : nullptr;
-        t.start[i] = t.chunks;
-        t.last[i] = uint16_t((n - 1) % kGradChunk);
-        t.types[i] = uint16_t((types[at] == PCONV_BF16 ? 1 : 0) | (out && out_types[at] == PCONV_BF16 ? 2 : 0));
-        t.chunks += uint32_t(chunks);
+    Grads g{in, out, counts, types, out_types, num, 0, 0, -1};
+    int64_t elements = 0, bytes = 0, ones = 0, few = 0, many = 0;
+    for (int64_t i = 0; i < num; ++i) {
+        const int64_t n = counts[i];
+        elements += n;
+        bytes += n * ((types[i] == PCONV_BF16 ? 2 : 4) + (!out || out[i] == in[i] ? 0 : out_types[i] == PCONV_BF16 ? 2 : 4));
+        ones += (n + (1 << kGradLog2One) - 1) >> kGradLog2One;
+        few += (n + (1 << kGradLog2Few) - 1) >> kGradLog2Few;
+        many += (n + (1 << kGradLog2) - 1) >> kGradLog2;
     }
-    return t.count > 0;
+    // One workgroup for up to two chunks a wave (a launch less on the host: 2.4 us); chunks of 4096 elements while
+    // those of 16384 would not be one for each compute unit (where they are, finding a chunk's tensor costs more than it gives).
+    if (out && num <= kGradTensors && ones <= 32) { g.log2 = kGradLog2One; g.chunks = ones; }
+    else if (elements < int64_t(256) << kGradLog2) { g.log2 = kGradLog2Few; g.chunks = few; }
+    else { g.log2 = kGradLog2; g.chunks = many; }
+    if (out && bytes > kCachedBytes) g.kept = kKeptBytes;
+    return g;
+}
+
+// The table of tensors [kGradTensors * i, ..); false where they are all empty.  `behind`: bytes of the gradients behind them.
+bool table_of(const Grads &g, int64_t i, int64_t behind, GradTable &t)
+{
+    const int64_t begin = i * kGradTensors, end = std::min<int64_t>(begin + kGradTensors, g.num);
+    t.count = 0; t.chunks = 0; t.passing = 0; t.log2 = g.log2;
+    for (int64_t at = begin; at < end; ++at) {
+        const int64_t n = g.counts[at];
+        if (n == 0) continue;
+        const int k = t.count++;
+        t.in[k] = g.in[at];
+        t.out[k] = g.out ? g.out[at] : nullptr;
+        t.start[k] = t.chunks;
+        t.last[k] = uint16_t((n - 1) & ((int64_t(1) << g.log2) - 1));
+        t.types[k] = uint16_t((g.types[at] == PCONV_BF16 ? 1 : 0) | (g.out && g.out_types[at] == PCONV_BF16 ? 2 : 0));
+        t.chunks += uint32_t((n + (int64_t(1) << g.log2) - 1) >> g.log2);
+    }
+    if (g.kept < 0 || t.count == 0) return t.count > 0;
+    t.passing = t.chunks;
+    for (int k = t.count - 1; k >= 0 && behind < g.kept; --k) {          // from the last: the chunks that are kept
+        const int64_t each = int64_t(t.types[k] & 1 ? 2 : 4) << g.log2, have = (k + 1 < t.count ? t.start[k + 1] : t.chunks) - t.start[k];
+        const int64_t keep = std::min(have, (g.kept - behind + each - 1) / each);
+        t.passing -= uint32_t(keep);
+        behind += keep * each;
+    }
+    return true;
+}
+
+int64_t table_bytes(const Grads &g, int64_t i)
+{
+    int64_t b = 0;
+    for (int64_t at = i * kGradTensors; at < std::min<int64_t>((i + 1) * kGradTensors, g.num); ++at) b += g.counts[at] * (g.types[at] == PCONV_BF16 ? 2 : 4);
+    return b;
 }
 
 int check_grads(const char *who, const void *const *in, const int64_t *counts, const int32_t *types, int64_t num, float *norm,
@@ -88,17 +139,21 @@ int check_grads(const char *who, const void *const *in, const int64_t *counts, c
 }
 
 // The sums of squares of all tables, to work[1 ..]; how many there are.
-int sum_squares(const void *const *in, const int64_t *counts, const int32_t *types, int64_t num, double *work, void *stream,
-                unsigned &sums, int &tables)
+int sum_squares(const Grads &g, double *work, void *stream, unsigned &sums)
 {
-    const int64_t most = (num + kGradTensors - 1) / kGradTensors;
-    const unsigned cap = most <= 1 ? unsigned(kGradBlocks) : unsigned(std::max<int64_t>(64, kGradBlocks / most));
-    sums = 0; tables = 0;
-    GradTable t;
-    for (int64_t at = 0; next_table(in, nullptr, counts, types, nullptr, num, at, t); ++tables) {
-        const unsigned blocks = std::min(t.chunks, cap);
-        if (const int rc = launch_grad_norm(t, blocks, work + 1 + sums, stream)) return rc;
-        sums += blocks;
+    const unsigned cap = unsigned(std::max<int64_t>(64, kGradBlocks / std::max<int64_t>(1, g.tables())));
+    int64_t behind = 0;
+    if (g.kept >= 0)
+        for (int64_t i = 1; i < g.tables(); ++i) behind += table_bytes(g, i);
+    sums = 0;
+    for (int64_t i = 0; i < g.tables(); ++i) {
+        GradTable t;
+        if (table_of(g, i, behind, t)) {
+            const unsigned blocks = std::min(t.chunks, cap);
+            if (const int rc = launch_grad_norm(t, blocks, work + 1 + sums, stream)) return rc;
+            sums += blocks;
+        }
+        if (g.kept >= 0 && i + 1 < g.tables()) behind -= table_bytes(g, i + 1);
     }
     return PCONV_OK;
 }
@@ -177,8 +232,8 @@ int pconv_grad_norm(const void *const *grads, const int64_t *counts, const int32
 {
     if (const int rc = check_grads("pconv_grad_norm", grads, counts, dtypes, num, norm_dev, work, work_bytes)) return rc;
     double *const sums = static_cast<double *>(work);
-    unsigned count; int tables;
-    if (const int rc = sum_squares(grads, counts, dtypes, num, sums, hip_stream, count, tables)) return rc;
+    unsigned count;
+    if (const int rc = sum_squares(grads_of(grads, nullptr, counts, dtypes, nullptr, num), sums, hip_stream, count)) return rc;
     return launch_grad_total(sums + 1, count, sums, norm_dev, hip_stream);
 }
 
@@ -197,18 +252,25 @@ int pconv_clip_grads(const void *const *grads, void *const *outs, const int64_t 
         if (reinterpret_cast<uintptr_t>(outs[i]) % (out_dtypes[i] == PCONV_BF16 ? 2 : 4) != 0) return invalid(who, "an output must be aligned to its type");
         if (counts[i] && outs[i] == grads[i] && out_dtypes[i] != dtypes[i]) return invalid(who, "an output in its gradient's place must have its type");
     }
-    double *const sums = static_cast<double *>(work);
-    unsigned count; int tables;
-    if (const int rc = sum_squares(grads, counts, dtypes, num, sums, hip_stream, count, tables)) return rc;
-    const double *from = sums + 1;
-    if (tables != 1) {                                   // (none: the norm of nothing is 0)
-        if (const int rc = launch_grad_total(from, count, sums, norm_dev, hip_stream)) return rc;
-        from = sums; count = 1;
-    }
+    const Grads g = grads_of(grads, outs, counts, dtypes, out_dtypes, num);
     GradTable t;
-    for (int64_t at = 0; next_table(grads, outs, counts, dtypes, out_dtypes, num, at, t);) {
-        const unsigned blocks = std::min(t.chunks, unsigned(kGradBlocks));
-        if (const int rc = launch_grad_scale(t, blocks, from, count, max_norm, eps, tables == 1 ? norm_dev : nullptr, hip_stream)) return rc;
+    if (g.log2 == kGradLog2One && g.chunks > 0) {
+        (void)table_of(g, 0, 0, t);
+        return launch_grad_clip_one(t, max_norm, eps, norm_dev, hip_stream);
+    }
+    double *const sums = static_cast<double *>(work);
+    unsigned count;
+    if (const int rc = sum_squares(g, sums, hip_stream, count)) return rc;
+    // Every workgroup of the second pass adds the partial sums by itself; with several tables or many workgroups one launch for it takes
+    // less.  (Also for nothing at all: the norm is 0.)
+    const bool total = g.tables() != 1 || count == 0 || g.chunks > 2 * kGradBlocks;
+    if (total)
+        if (const int rc = launch_grad_total(sums + 1, count, sums, norm_dev, hip_stream)) return rc;
+    int64_t behind = 0;
+    for (int64_t i = g.tables() - 1; i >= 0; --i) {
+        if (table_of(g, i, behind, t))
+            if (const int rc = launch_grad_scale(t, total ? sums : sums + 1, total ? 1 : count, g.kept >= 0, max_norm, eps, total ? nullptr : norm_dev, hip_stream)) return rc;
+        if (g.kept >= 0) behind += table_bytes(g, i);
     }
     return PCONV_OK;
 }
