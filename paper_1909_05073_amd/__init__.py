@@ -449,13 +449,18 @@ def maxpool2x2(x, layout="nchw"):
 
 # ---- layers in 8-bit integers ------------------------------------------------------------
 
+_types = {}                                          # torch's types to the library's; filled by the first call
+
+
 def _type_of(t, what):
-    import torch
-    if t.dtype == torch.float32:
-        return F32
-    if t.dtype == torch.bfloat16:
-        return BF16
-    raise ValueError(f"{what} must be float32 or bfloat16")
+    code = _types.get(t.dtype)
+    if code is None:
+        import torch
+        _types.update({torch.float32: F32, torch.bfloat16: BF16})
+        code = _types.get(t.dtype)
+        if code is None:
+            raise ValueError(f"{what} must be float32 or bfloat16")
+    return code
 
 
 _current_device = None
@@ -487,26 +492,27 @@ def _device_index(*tensors) -> int:
 
 def _rows(t, what):
     """(rows, columns, elements from row to row) of a tensor [..., columns] whose rows can be walked with one stride."""
-    if t.dim() < 1:
-        raise ValueError(f"{what} must have at least one dimension")
-    if t.dim() != 2:
-        if t.dim() > 2 and not t.is_contiguous():
-            try:
-                t = t.view(-1, t.shape[-1])
-            except RuntimeError:
-                raise ValueError(f"the rows of {what} must lie one stride apart") from None
-        else:
-            k = t.shape[-1]
-            if t.dim() == 1 and k > 1 and t.stride(0) != 1:
-                raise ValueError(f"{what} must be contiguous along its last dimension")
-            return (t.numel() // k if k else _prod(t.shape[:-1])), k, k
-    m, k = t.shape
+    shape = t.shape
+    if len(shape) != 2:
+        if not shape:
+            raise ValueError(f"{what} must have at least one dimension")
+        k = shape[-1]
+        if t.is_contiguous():
+            return (t.numel() // k if k else _prod(shape[:-1])), k, k
+        try:
+            t = t.view(-1, k)
+        except RuntimeError:
+            raise ValueError(f"the rows of {what} must lie one stride apart") from None
+        shape = t.shape
+    m, k = shape
     step, one = t.stride()
-    if k > 1 and one != 1:
+    if one != 1 and k > 1:
         raise ValueError(f"{what} must be contiguous along its last dimension")
-    if m > 1 and step < k:
-        raise ValueError(f"the rows of {what} must not overlap")
-    return m, k, max(step, k)
+    if step < k:
+        if m > 1:
+            raise ValueError(f"the rows of {what} must not overlap")
+        step = k
+    return m, k, step
 
 
 def _prod(sizes) -> int:
@@ -528,15 +534,15 @@ def _per_channel(t, n, what):
     import torch
     if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{what} must be {n} contiguous float32 numbers")
-    return t.data_ptr()
+    return t.data_ptr() or None
 
 
 def _output(out, shape, dtype, like):
     """(tensor, elements from row to row) for a result of that shape."""
     if out is None:
         return like.new_empty(shape, dtype=dtype), shape[-1]
-    if out.dtype != dtype or tuple(out.shape) != shape:
-        raise ValueError(f"out must be {dtype} of shape {shape}")
+    if out.dtype != dtype or out.shape != shape:
+        raise ValueError(f"out must be {dtype} of shape {tuple(shape)}")
     return out, _rows(out, "out")[2]
 
 
@@ -590,10 +596,10 @@ def quantize_rows(x):
     dtype = _type_of(x, "x")
     index = _device_index(x)
     m, k, step = _rows(x, "x")
-    lead = tuple(x.shape[:-1])
+    lead = x.shape[:-1]
     wide = (k + 15) // 16 * 16
-    q = torch.empty(lead + (wide,), dtype=torch.int8, device=x.device)
-    scale = torch.empty(lead, dtype=torch.float32, device=x.device)
+    q = x.new_empty(lead + (wide,), dtype=torch.int8)
+    scale = x.new_empty(lead, dtype=torch.float32)
     rc = (_lib or lib()).pconv_quantize_rows(x.data_ptr() or None, step, dtype, m, k, q.data_ptr() or None, wide,
                                              scale.data_ptr() or None, _stream(index))
     if rc != OK:
@@ -615,17 +621,16 @@ def matmul_i8(a, a_scale, b, b_scale, bias=None, relu: bool = False, out_dtype=N
         raise ValueError("a and b must have rows of one length")
     if out_dtype is None:
         out_dtype = out.dtype if out is not None else torch.float32
-    y, y_step = _output(out, tuple(a.shape[:-1]) + (n,), out_dtype, a)
+    y, y_step = _output(out, a.shape[:-1] + (n,), out_dtype, a)
     y_type = _type_of(y, "out")
     sa, sb = _per_channel(a_scale, m, "a_scale"), _per_channel(b_scale, n, "b_scale")
     bp = _per_channel(bias, n, "bias") if bias is not None else None
-    L = _lib or lib()
     a_ptr, b_ptr = a.data_ptr(), b.data_ptr()
     size = _matmul_i8_workspace(m, n, k, _at_16(a_ptr, a_step) and _at_16(b_ptr, b_step))
-    work = _scratch(size, a) if size > 0 else None
-    rc = L.pconv_matmul_i8(a_ptr or None, a_step, sa or None, b_ptr or None, b_step, sb or None, bp or None,
-                           y.data_ptr() or None, y_step, y_type, m, n, k, 1 if relu else 0,
-                           work.data_ptr() if work is not None else None, size, _stream(index))
+    work = _scratch(size, a) if size else None
+    rc = (_lib or lib()).pconv_matmul_i8(a_ptr or None, a_step, sa, b_ptr or None, b_step, sb, bp, y.data_ptr() or None, y_step,
+                                         y_type, m, n, k, 1 if relu else 0, work.data_ptr() if size else None, size,
+                                         _stream(index))
     if rc != OK:
         _check(rc)
     return y
@@ -645,19 +650,19 @@ def linear_i8(x, w, w_scale, bias=None, relu: bool = False, out_dtype=None, out=
     n, kw, w_step = _rows(w, "w")
     if k != kw:
         raise ValueError("x and w must have rows of one length")
-    if out_dtype is None:
-        out_dtype = out.dtype if out is not None else x.dtype
-    y, y_step = _output(out, tuple(x.shape[:-1]) + (n,), out_dtype, x)
-    y_type = _type_of(y, "out")
+    if out is None and out_dtype is None:
+        y, y_step, y_type = x.new_empty(x.shape[:-1] + (n,)), n, x_type
+    else:
+        y, y_step = _output(out, x.shape[:-1] + (n,), out_dtype or out.dtype, x)
+        y_type = _type_of(y, "out")
     sw = _per_channel(w_scale, n, "w_scale")
     bp = _per_channel(bias, n, "bias") if bias is not None else None
-    L = _lib or lib()
     w_ptr = w.data_ptr()
     size = _linear_i8_workspace(m, n, k, _at_16(w_ptr, w_step))
-    work = _scratch(size, x) if size > 0 else None
-    rc = L.pconv_linear_i8(x.data_ptr() or None, x_step, x_type, w_ptr or None, w_step, sw or None, bp or None,
-                           y.data_ptr() or None, y_step, y_type, m, n, k, 1 if relu else 0,
-                           work.data_ptr() if work is not None else None, size, _stream(index))
+    work = _scratch(size, x) if size else None
+    rc = (_lib or lib()).pconv_linear_i8(x.data_ptr() or None, x_step, x_type, w_ptr or None, w_step, sw, bp,
+                                         y.data_ptr() or None, y_step, y_type, m, n, k, 1 if relu else 0,
+                                         work.data_ptr() if size else None, size, _stream(index))
     if rc != OK:
         _check(rc)
     return y
