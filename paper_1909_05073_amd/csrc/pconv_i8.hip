@@ -383,7 +383,21 @@ __device__ __forceinline__ void tile_at(unsigned id, unsigned tiles_m, unsigned 
     tn = in / rows;
 }
 
-// Tiles of BM rows of y and BN channels, WM x WN waves.  128 bytes of k of all the tile's rows are a stage; S stages lie in
+// Waits until at most `behind` (0 .. MOST) stages of L loads each of this wave are under way and its reads of LDS are done, and for
+// the other waves of the workgroup to get there.
+template <int MOST, int L>
+__device__ __forceinline__ void wait_for_stages(int behind)
+{
+    if constexpr (MOST > 0) {
+        if (behind == MOST) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n s_barrier" ::"n"(MOST * L) : "memory");
+        else wait_for_stages<MOST - 1, L>(behind);
+    } else {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n s_barrier" ::: "memory");
+    }
+}
+
+// Tiles of BM rows of y and BN channels, WM x WN waves, and KG such sets of waves that take the stages in turn (a stage takes a wave 0.4 us of
+// waiting for one thing after the other, however far ahead it is loaded).  128 bytes of k of all the tile's rows are a stage; S stages lie in
 // LDS.  A row of a stage is eight pieces of 16 bytes, stored in an order that depends on the row so that the eight rows that are
 // read at once lie in different banks.
 //
@@ -393,16 +407,18 @@ __device__ __forceinline__ void tile_at(unsigned id, unsigned tiles_m, unsigned 
 // Rows begin at multiples of 16 bytes (realign_kernel sees to it).
 //
 // `splits` workgroups share a tile, each with its part of k; their sums go to `part` [splits][m][n4], n4 = n rounded up to four.
-template <typename Y, int BM, int BN, int WM, int WN, int S>
-__global__ void __launch_bounds__(WM * WN * 64)
+template <typename Y, int BM, int BN, int WM, int WN, int S, int KG>
+__global__ void __launch_bounds__(KG * WM * WN * 64)
 matmul_i8_kernel(const I8Product p, int splits, int *part)
 {
     constexpr int BK = 128, NW = WM * WN, TM = BM / WM, TN = BN / WN, MT = TM / 16, NT = TN / 16;
     constexpr int PA = BM / 8 / NW, PB = BN / 8 / NW;    // blocks of eight rows that a wave stages
     static_assert(PA * NW * 8 == BM && PB * NW * 8 == BN, "");
-    __shared__ v4i lds[S * (BM + BN) * 8];
-    constexpr int STAGE = (BM + BN) * 8;
-    const int tid = int(threadIdx.x), lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    constexpr int STAGE = (BM + BN) * 8, SUMS = NW * MT * NT * 64;       // (of one set of waves)
+    __shared__ v4i lds[S * KG * STAGE];
+    static_assert(KG == 1 || (KG - 1) * SUMS <= S * KG * STAGE, "");
+    const int lane = int(threadIdx.x) & 63, set = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / (NW * 64));
+    const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6) % NW;
     const unsigned tiles_n = unsigned(p.n + BN - 1) / BN, tiles_m = unsigned(p.m + BM - 1) / BM;
     unsigned tm, tn;
     tile_at(blockIdx.x / unsigned(splits), tiles_m, tiles_n, tm, tn);
@@ -460,12 +476,14 @@ matmul_i8_kernel(const I8Product p, int splits, int *part)
         col_b[i] = ((lane & 7) ^ key_b(row)) * 16;
         off_b[i] = uint32_t(min(row, p.n - 1 - n0)) * uint32_t(p.ldb) + uint32_t(col_b[i]);
     }
-    const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds)) + uint32_t(wave) * 1024u;
+    const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds)) + uint32_t(set) * uint32_t(STAGE * 16) + uint32_t(wave) * 1024u;
     // (written as assembly so that the compiler does not wait for these loads before every read of LDS)
     const int length = k_end - k_begin, whole = length / BK, rest = length % BK;
     const int count = whole + (rest > 0 && rest % 16 == 0 ? 1 : 0);
-    auto stage = [&](int s) {
-        const uint32_t to = base + uint32_t(s % S) * uint32_t(STAGE * 16), k0 = uint32_t(s) * BK;
+    // stage `turn` of this set is stage turn * KG + set of all
+    auto stage = [&](int turn) {
+        const int s = turn * KG + set;
+        const uint32_t to = base + uint32_t(turn % S) * uint32_t(KG * STAGE * 16), k0 = uint32_t(s) * BK;
         const int have = s < whole ? BK : rest;
 #pragma unroll
         for (int i = 0; i < PA; ++i)
@@ -478,31 +496,50 @@ matmul_i8_kernel(const I8Product p, int splits, int *part)
     };
     constexpr int L = PA + PB;
     static_assert((S - 2) * L <= 63, "");
+    const int mine = (count - set + KG - 1) / KG;        // whole stages of this set (count >= 0, so at least 0)
+    const bool ragged = rest % 16 != 0;                  // k ends inside a piece: one more stage, through registers
+    const int all = count + (ragged ? 1 : 0), turns = (all + KG - 1) / KG;
 #pragma unroll
-    for (int s = 0; s < S - 1; ++s)
-        if (s < count) stage(s);
-    const int all = count + (rest % 16 != 0 ? 1 : 0);
+    for (int t = 0; t < S - 1; ++t)
+        if (t < mine) stage(t);
 #pragma unroll 1
-    for (int s = 0; s < all; ++s) {
-        if (s < count) {
-            // the loads of stage s are done when at most those of the stages behind it are under way
-            const int behind = min(S - 2, count - 1 - s);
-            if (behind == S - 2) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n s_barrier" ::"n"((S - 2) * L) : "memory");
-            else if (S > 3 && behind == 1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n s_barrier" ::"n"(L) : "memory");
-            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n s_barrier" ::: "memory");
-            if (s + S - 1 < count) stage(s + S - 1);
-        } else {                                         // k ends inside a piece
-            v4i *const to = lds + (s % S) * STAGE + wave * 64 + lane;
+    for (int t = 0; t < turns; ++t) {
+        // the loads of this turn are done when at most those of the turns behind it are under way
+        wait_for_stages<S - 2, L>(min(S - 2, max(0, mine - 1 - t)));
+        if (t + S - 1 < mine) stage(t + S - 1);
+        const v4i *const st = lds + ((t % S) * KG + set) * STAGE;
+        if (ragged && t == count / KG) {
+            if (set == count % KG) {
+                v4i *const to = lds + ((t % S) * KG + set) * STAGE + wave * 64 + lane;
 #pragma unroll 1
-            for (int i = 0; i < PA + PB; ++i) {
-                const bool b = i >= PA;
-                const int at = ((b ? i - PA : i) * NW + wave) * 8 + (lane >> 3), key = b ? key_b(at) : at & 7;
-                const int8_t *row = b ? p.b + int64_t(min(n0 + at, p.n - 1)) * p.ldb : p.a + int64_t(min(m0 + at, p.m - 1)) * p.lda;
-                to[i * NW * 64] = load16(row, k_begin + whole * BK + ((lane & 7) ^ key) * 16, k_end);
+                for (int i = 0; i < PA + PB; ++i) {
+                    const bool b = i >= PA;
+                    const int at = ((b ? i - PA : i) * NW + wave) * 8 + (lane >> 3), key = b ? key_b(at) : at & 7;
+                    const int8_t *row = b ? p.b + int64_t(min(n0 + at, p.n - 1)) * p.ldb : p.a + int64_t(min(m0 + at, p.m - 1)) * p.lda;
+                    to[i * NW * 64] = load16(row, k_begin + whole * BK + ((lane & 7) ^ key) * 16, k_end);
+                }
             }
             __syncthreads();
         }
-        multiply(lds + (s % S) * STAGE);
+        if (KG == 1 || t * KG + set < all) multiply(st);
+    }
+    if constexpr (KG > 1) {                              // the sets' sums come together
+        __syncthreads();
+        v4i *const to = lds + wave * (MT * NT * 64) + lane;
+        if (set > 0) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) to[(set - 1) * SUMS + (i * NT + j) * 64] = acc[i][j];
+        }
+        __syncthreads();
+        if (set > 0) return;
+#pragma unroll
+        for (int q = 0; q < KG - 1; ++q)
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] += to[q * SUMS + (i * NT + j) * 64];
     }
 
     const int m = m0 + wm + (lane & 15), g = lane >> 4;
@@ -679,7 +716,7 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
 // Reading the weights is all of it; a wave has the next turn's under way while it multiplies.  T is int8_t, or
 // the rows come as floats, up to kFusedRows elements, and every workgroup quantises all of them to LDS while its first weights
 // are on their way: less than a launch for it takes.
-constexpr int kRowsM = 16, kFusedRows = 32768;
+constexpr int kRowsM = 16, kFusedRows = 32768, kRowsMost = 131072;
 
 template <typename T>
 __global__ void __launch_bounds__(512)
@@ -704,9 +741,10 @@ linear_i8_rows_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx)
     if (k0 < whole) fetch(vb, k0);
     int8_t *const q = reinterpret_cast<int8_t *>(rows_lds);
     if constexpr (FUSED) {
-        constexpr int N = Vec<T>::N, KEEP = 4, THREADS = WAVES * 64;
-        const int sub = int(threadIdx.x);
-        for (int m = 0; m < p.m; ++m) {
+        constexpr int N = Vec<T>::N, KEEP = 4;
+        // row m by THREADS threads, all of the workgroup or a wave
+        auto quantize_row = [&](int m, int sub, auto threads) {
+            constexpr int THREADS = decltype(threads)::value;
             const T *row = x + int64_t(m) * ldx;
             Vec<T> v[KEEP];
             load_row<T, THREADS, KEEP>(row, sub, p.k, v);
@@ -716,10 +754,13 @@ linear_i8_rows_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx)
 #pragma unroll 4
             for (int at = (KEEP * THREADS + sub) * N; at < p.k; at += THREADS * N) most = most_of(load_vec(row, at, p.k), most);
             most = most_of_lanes<64>(most);
-            if (lane == 0) mosts[wave] = most;
-            __syncthreads();
+            if (THREADS > 64) {
+                __syncthreads();                         // (the maxima of the row before are read)
+                if (lane == 0) mosts[wave] = most;
+                __syncthreads();
 #pragma unroll
-            for (int i = 0; i < WAVES; ++i) most = max(most, mosts[i]);
+                for (int i = 0; i < WAVES; ++i) most = max(most, mosts[i]);
+            }
             const RowScale s = row_scale(most);
             int8_t *to = q + m * pitch;
 #pragma unroll
@@ -729,14 +770,22 @@ linear_i8_rows_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx)
                 quantize_vec(v[i], s, w);
                 if (at < p.k) __builtin_memcpy(to + at, w, N);
             }
+#pragma unroll 2
             for (int at = (KEEP * THREADS + sub) * N; at < p.k; at += THREADS * N) {
                 uint32_t w[N / 4];
                 quantize_vec(load_vec(row, at, p.k), s, w);
                 __builtin_memcpy(to + at, w, N);
             }
             if (sub == 0) scales[m] = s.scale;
-            __syncthreads();
+        };
+        // Long rows one after the other by all waves, else a row a wave: 2 rows of 25088 24.9 us; 16 rows of 512 19.2 us the
+        // first way, 4.6 the second; 2 rows of 256 4.7 and 3.4.
+        if (p.m < 4 && p.k > 64 * KEEP * N) {
+            for (int m = 0; m < p.m; ++m) quantize_row(m, int(threadIdx.x), std::integral_constant<int, WAVES * 64>());
+        } else {
+            for (int m = wave; m < p.m; m += WAVES) quantize_row(m, lane, std::integral_constant<int, 64>());
         }
+        __syncthreads();
     }
     const int8_t *const a = FUSED ? q + min(r, p.m - 1) * pitch : p.a + int64_t(min(r, p.m - 1)) * p.lda;
     v4i acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
@@ -830,12 +879,12 @@ Cut cut_of(int64_t m, int64_t n, int64_t k)
     return best;
 }
 
-template <int BM, int BN, int WM, int WN, int S>
+template <int BM, int BN, int WM, int WN, int S, int KG>
 void launch_tiles(const I8Product &p, int splits, int *part, hipStream_t st)
 {
     const unsigned grid = unsigned(((int64_t(p.m) + BM - 1) / BM) * ((int64_t(p.n) + BN - 1) / BN) * splits);
-    if (p.y_bf16) hipLaunchKernelGGL((matmul_i8_kernel<__bf16, BM, BN, WM, WN, S>), dim3(grid), dim3(WM * WN * 64), 0, st, p, splits, part);
-    else hipLaunchKernelGGL((matmul_i8_kernel<float, BM, BN, WM, WN, S>), dim3(grid), dim3(WM * WN * 64), 0, st, p, splits, part);
+    if (p.y_bf16) hipLaunchKernelGGL((matmul_i8_kernel<__bf16, BM, BN, WM, WN, S, KG>), dim3(grid), dim3(KG * WM * WN * 64), 0, st, p, splits, part);
+    else hipLaunchKernelGGL((matmul_i8_kernel<float, BM, BN, WM, WN, S, KG>), dim3(grid), dim3(KG * WM * WN * 64), 0, st, p, splits, part);
 }
 
 template <typename T>
@@ -878,14 +927,17 @@ int launch_thin(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
 
 }  // namespace
 
+// The kernel for few rows up to kRowsMost activations: each of its workgroups reads all of them (16 rows of 25088: 33.5 us, in tiles
+// 28.6; 4 rows 26.6 and 28.1; 16 rows of 4096 10.0 and 12.2).
+static bool few(int64_t m, int64_t k) { return m <= kRowsM && m * k <= kRowsMost; }
 static bool thin(int64_t m, int64_t k) { return m > kRowsM && k <= kThinK; }
 
-bool linear_i8_fused(int64_t m, int64_t n, int64_t k) { return m <= kRowsM ? m * k <= kFusedRows : thin(m, k); }
+bool linear_i8_fused(int64_t m, int64_t, int64_t k) { return m <= kRowsM ? m * k <= kFusedRows : thin(m, k); }
 
 int launch_linear_i8_fused(const I8Product &p, const void *x, int64_t ldx, int bf16, void *stream)
 {
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (p.m <= kRowsM) return bf16 ? launch_rows(p, static_cast<const __bf16 *>(x), ldx, st) : launch_rows(p, static_cast<const float *>(x), ldx, st);
+    if (few(p.m, p.k)) return bf16 ? launch_rows(p, static_cast<const __bf16 *>(x), ldx, st) : launch_rows(p, static_cast<const float *>(x), ldx, st);
     return bf16 ? launch_thin(p, static_cast<const __bf16 *>(x), ldx, st) : launch_thin(p, static_cast<const float *>(x), ldx, st);
 }
 
@@ -893,7 +945,7 @@ bool rows_at_16(const int8_t *at, int64_t ld) { return reinterpret_cast<uintptr_
 
 int64_t matmul_i8_work_bytes(int64_t m, int64_t n, int64_t k, bool a_at_16, bool b_at_16)
 {
-    if (m <= kRowsM || thin(m, k)) return 0;
+    if (few(m, k) || thin(m, k)) return 0;
     const Cut c = cut_of(m, n, k);
     const int64_t row = (k + 15) / 16 * 16;
     return (a_at_16 ? 0 : m * row) + (b_at_16 ? 0 : n * row) + (c.splits > 1 ? c.splits * m * ((n + 3) / 4 * 4) * 4 : 0);
@@ -903,7 +955,7 @@ int launch_matmul_i8(const I8Product &product, void *work, void *stream)
 {
     const hipStream_t st = static_cast<hipStream_t>(stream);
     I8Product p = product;
-    if (p.m <= kRowsM) return launch_rows(p, p.a, p.lda, st);
+    if (few(p.m, p.k)) return launch_rows(p, p.a, p.lda, st);
     if (thin(p.m, p.k)) return launch_thin(p, p.a, p.lda, st);
     const Cut c = cut_of(p.m, p.n, p.k);
     const int64_t tiles = ((int64_t(p.m) + kTileM[c.tile] - 1) / kTileM[c.tile]) * ((int64_t(p.n) + kTileN[c.tile] - 1) / kTileN[c.tile]);
@@ -927,12 +979,15 @@ int launch_matmul_i8(const I8Product &product, void *work, void *stream)
         if (const int rc = check_launch("pconv_matmul_i8 (aligning rows)")) return rc;
     }
     int *const sums = reinterpret_cast<int *>(at);
-    // (tiles of 128 rows: four stages where a compute unit has one workgroup, two where it has two)
-    if (c.tile == 0) launch_tiles<32, 128, 1, 4, 4>(p, c.splits, sums, st);
-    else if (c.tile == 1) launch_tiles<64, 128, 2, 2, 3>(p, c.splits, sums, st);
-    else if (c.tile == 2 && tiles * c.splits <= kUnits) launch_tiles<128, 128, 2, 2, 4>(p, c.splits, sums, st);
-    else if (c.tile == 2) launch_tiles<128, 128, 2, 2, 2>(p, c.splits, sums, st);
-    else launch_tiles<256, 256, 2, 4, 2>(p, c.splits, sums, st);
+    // as many stages as LDS holds where a compute unit has one workgroup (17x2048 -> 1000: 8.6 us with four stages), else room for two
+    const bool deep = tiles * c.splits <= kUnits;
+    if (c.tile == 0 && deep) launch_tiles<32, 128, 1, 4, 4, 2>(p, c.splits, sums, st);
+    else if (c.tile == 0) launch_tiles<32, 128, 1, 4, 4, 1>(p, c.splits, sums, st);
+    else if (c.tile == 1 && deep) launch_tiles<64, 128, 2, 2, 3, 2>(p, c.splits, sums, st);
+    else if (c.tile == 1) launch_tiles<64, 128, 2, 2, 3, 1>(p, c.splits, sums, st);
+    else if (c.tile == 2 && deep) launch_tiles<128, 128, 2, 2, 2, 2>(p, c.splits, sums, st);
+    else if (c.tile == 2) launch_tiles<128, 128, 2, 2, 2, 1>(p, c.splits, sums, st);
+    else launch_tiles<256, 256, 2, 4, 2, 1>(p, c.splits, sums, st);
     if (const int rc = check_launch("pconv_matmul_i8")) return rc;
     if (c.splits == 1) return PCONV_OK;
     const int64_t quads = (int64_t(p.n) + 3) / 4 * p.m;
