@@ -265,6 +265,25 @@ __device__ __forceinline__ v4i load16(const int8_t *row, int at, int len)
 // Four neighbouring channels of one row of y, from n on.  ReLU keeps NaN.
 struct Channels { f4 scale, bias; };
 
+// 16 bytes at an address of any alignment, as the five words that hold them.  (A load of 16 bytes that is not aligned to a word takes 2.6 times one that
+// is: 6x17360 -> 562 31 us and 16.)  No word is read that holds none of the bytes.
+__device__ __forceinline__ v4i load16_loose(const int8_t *p)
+{
+    const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p)) & 3u;
+    const int8_t *const q = p - off;
+    typedef v4i Words __attribute__((aligned(4)));
+    const v4i w = *reinterpret_cast<const Words *>(q);
+    const uint32_t last = *reinterpret_cast<const uint32_t *>(q + (off ? 16 : 12));
+    v4i v;
+    v[0] = int(__builtin_amdgcn_alignbyte(uint32_t(w[1]), uint32_t(w[0]), off));
+    v[1] = int(__builtin_amdgcn_alignbyte(uint32_t(w[2]), uint32_t(w[1]), off));
+    v[2] = int(__builtin_amdgcn_alignbyte(uint32_t(w[3]), uint32_t(w[2]), off));
+    v[3] = int(__builtin_amdgcn_alignbyte(last, uint32_t(w[3]), off));
+    return v;
+}
+
+__device__ __forceinline__ bool rows_at_words(const int8_t *p, int64_t ld) { return ((reinterpret_cast<uintptr_t>(p) | uint64_t(ld)) & 3u) == 0; }
+
 // EXACT (here and below): sizes are such that nothing ends inside what a lane reads or writes at once.
 template <bool EXACT = false>
 __device__ __forceinline__ Channels channels_at(const I8Product &p, int n)
@@ -616,17 +635,27 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
 
     const int n_end = min(p.n, int(blockIdx.y + 1) * part_n);
     int n0 = int(blockIdx.y) * part_n + wave * 32;
+    const bool words = EXACT || rows_at_words(p.b, p.ldb);
     v4i vb[KS][NT];
     auto fetch = [&](int n0) {                           // (also behind the last channel, for nothing, so that there is no branch)
         const int8_t *b[NT];
 #pragma unroll
         for (int j = 0; j < NT; ++j) b[j] = p.b + int64_t(min(n0 + Deal<Y>::row(j, r), p.n - 1)) * p.ldb;
+        if (EXACT || words) {
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
-            if ((EXACT && s == 0) || s * 64 + 64 <= p.k) {
+            for (int s = 0; s < KS; ++s)
+                if ((EXACT && s == 0) || s * 64 + 64 <= p.k) {
 #pragma unroll
-                for (int j = 0; j < NT; ++j) __builtin_memcpy(&vb[s][j], b[j] + s * 64 + g * 16, 16);
-            }
+                    for (int j = 0; j < NT; ++j) __builtin_memcpy(&vb[s][j], b[j] + s * 64 + g * 16, 16);
+                }
+        } else {
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+                if (s * 64 + 64 <= p.k) {
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) vb[s][j] = load16_loose(b[j] + s * 64 + g * 16);
+                }
+        }
         if (!EXACT && p.k % 64 != 0) {
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
@@ -733,9 +762,15 @@ linear_i8_rows_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx)
     const int8_t *const b = p.b + int64_t(min(n0 + r, p.n - 1)) * p.ldb;
     const int whole = p.k / TURN * TURN;
     v4i vb[4];
+    const bool words = rows_at_words(p.b, p.ldb);
     auto fetch = [&](v4i (&v)[4], int k0) {
+        if (words) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s) __builtin_memcpy(&v[s], b + k0 + s * 64 + g * 16, 16);
+            for (int s = 0; s < 4; ++s) __builtin_memcpy(&v[s], b + k0 + s * 64 + g * 16, 16);
+        } else {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) v[s] = load16_loose(b + k0 + s * 64 + g * 16);
+        }
     };
     int k0 = wave * TURN;
     if (k0 < whole) fetch(vb, k0);
@@ -802,13 +837,17 @@ linear_i8_rows_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx)
         k0 = k1;
     }
     if (whole < p.k && whole / TURN % WAVES == wave) {   // the last turn is no whole one
-        for (int s = whole; s < p.k; s += 64) {
-            const v4i w = load16(b, s + g * 16, p.k);
-            v4i v;
-            if (FUSED) __builtin_memcpy(&v, a + s + g * 16, 16);   // (beyond k the weights are zeros)
-            else v = load16(a, s + g * 16, p.k);
-            acc[0] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, v, acc[0], 0, 0, 0);
+        v4i va[4];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const int at = whole + s * 64 + g * 16;
+            vb[s] = load16(b, at, p.k);
+            // (what lies in LDS beyond k meets weights of zero)
+            if (FUSED) __builtin_memcpy(&va[s], a + at, 16);
+            else va[s] = load16(a, at, p.k);
         }
+#pragma unroll
+        for (int s = 0; s < 4; ++s) acc[s & 1] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb[s], va[s], acc[s & 1], 0, 0, 0);
     }
     sums[wave][lane] = acc[0] + acc[1];
     __syncthreads();
@@ -838,6 +877,7 @@ int launch_quantize_rows(const void *x, int64_t ldx, int bf16, int64_t rows, int
         else hipLaunchKernelGGL((quantize_rows_kernel<float, TPR, KEEP, THREADS>), dim3(grid), dim3(THREADS), 0, st,           \
                                 static_cast<const float *>(x), ldx, rows, cols, q, ldq, q_cols, scale);                        \
     } while (0)
+    // (1024 threads for a row of 1244 vectors: 7962 rows 107 us, with 256 55; 300 rows 7.8 and 5.5)
     if (vecs <= 8) PCONV_LAUNCH(8, 1, 256);
     else if (vecs <= 16) PCONV_LAUNCH(16, 1, 256);
     else if (vecs <= 32) PCONV_LAUNCH(16, 2, 256);
@@ -845,6 +885,7 @@ int launch_quantize_rows(const void *x, int64_t ldx, int bf16, int64_t rows, int
     else if (vecs <= 256) PCONV_LAUNCH(64, 4, 256);
     else if (vecs <= 512) PCONV_LAUNCH(256, 2, 256);
     else if (vecs <= 1024) PCONV_LAUNCH(256, 4, 256);
+    else if (vecs <= 2048 && rows >= 128) PCONV_LAUNCH(256, 8, 256);
     else if (vecs <= 4096) PCONV_LAUNCH(1024, 4, 1024);
     else PCONV_LAUNCH(1024, 8, 1024);
 #undef PCONV_LAUNCH
@@ -891,7 +932,8 @@ template <typename T>
 int launch_rows(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
 {
     const size_t lds = sizeof(T) > 1 ? size_t(p.m) * ((p.k + 255) / 256 * 256 + 16) : 0;
-    hipLaunchKernelGGL((linear_i8_rows_kernel<T>), dim3(unsigned((int64_t(p.n) + 15) / 16)), dim3(512), lds, st, p, x, ldx);
+    const unsigned grid = unsigned((int64_t(p.n) + 15) / 16);
+    hipLaunchKernelGGL((linear_i8_rows_kernel<T>), dim3(grid), dim3(512), lds, st, p, x, ldx);
     return check_launch("pconv_linear_i8 (few rows)");
 }
 
@@ -901,7 +943,7 @@ int launch_thin_steps(const I8Product &p, const T *x, int64_t ldx, hipStream_t s
 {
     // Eight waves and 64 rows: 1568x512 -> 2048 12.4 us, with four waves and 32 rows 14.9; more parts than make 512 workgroups do not
     // pay (every part quantises the rows again).  Rows or channels that end inside a load: four waves and 32 rows.
-    const bool exact = p.k > 0 && p.k % 64 == 0 && p.n % 8 == 0;
+    const bool exact = p.k > 0 && p.k % 64 == 0 && p.n % 8 == 0 && p.ldb % 4 == 0 && reinterpret_cast<uintptr_t>(p.b) % 4 == 0;
     const int rows = exact ? 64 : 32, channels = exact ? 256 : 128;
     const int64_t tiles = (int64_t(p.m) + rows - 1) / rows, groups = (int64_t(p.n) + channels - 1) / channels;
     const int64_t parts = std::min<int64_t>(groups, std::max<int64_t>(1, 512 / tiles));
