@@ -16,6 +16,8 @@
 
 namespace pconv {
 
+bool rows_at_16(const int8_t *at, int64_t ld) { return reinterpret_cast<uintptr_t>(at) % 16 == 0 && ld % 16 == 0 && ld <= 1 << 23; }
+
 namespace {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
@@ -616,18 +618,185 @@ matmul_i8_join_kernel(const I8Product p, int splits, const int *__restrict__ par
     }
 }
 
-// Short rows (k up to kThinK): all of k of 16 * MT rows of activations lies in LDS, so that there is no loop of stages and one read of
-// the activations; where they come as floats (T) they are quantised on their way there and never leave the chip.
-// The weights, which every workgroup reads and the level-2 caches hold, go to the registers directly, all KS steps of 64 bytes
-// of the first channels before the activations are waited for.  Four waves share the rows and take groups of 32 channels
-// in turn.  blockIdx.y: a part of the channels, a multiple of 32 (`part_n`).
+// Short rows (k up to kThinK): all of k of BM rows of activations lies in LDS, so that there is no loop of stages and one read of the
+// activations; where they come as floats they are quantised on their way there and never leave the chip.
 constexpr int kThinK = 512;
 
-template <typename T, typename Y, int MT, int KS, bool EXACT, int W>
-__global__ void __launch_bounds__(W * 64, KS <= 4 ? 4 : 2)
+// LDS holds rows of PIECES times 16 bytes, whose order makes the 16 lanes that are read at once differ in their places modulo 256 bytes.
+template <int KS> struct ThinLds {
+    static constexpr int PIECES = KS < 2 ? 8 : KS * 4, KEY = PIECES < 16 ? 7 : 15;
+    static __device__ __forceinline__ int at(int row, int piece) { return row * PIECES + (piece ^ (row & KEY)); }
+};
+
+// Quantising BM rows of up to KS * 64 elements by W waves: LANES lanes a row, KEEP vectors of 16 bytes each.
+template <typename T, int KS, int W, int BM> struct ThinRows {
+    static constexpr int N = Vec<T>::N, VECS = KS * 64 / N, LANES = VECS < 16 ? VECS : 16, KEEP = VECS / LANES;
+    static constexpr int AT_ONCE = 64 / LANES, PASSES = BM / W / AT_ONCE;
+    static_assert(PASSES * AT_ONCE * W == BM, "");
+
+    template <bool EXACT>
+    static __device__ __forceinline__ void load(const T *x, int64_t ldx, int m0, int m, int k, int wave, int lane, Vec<T> (&v)[PASSES][KEEP])
+    {
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) {
+            const int row = wave * (BM / W) + i * AT_ONCE + lane / LANES;
+            load_row<T, LANES, KEEP, EXACT>(x + int64_t(min(m0 + row, m - 1)) * ldx, lane % LANES, k, v[i]);
+        }
+    }
+
+    static __device__ __forceinline__ void store(const Vec<T> (&v)[PASSES][KEEP], int wave, int lane, v4i *lds, float *scales)
+    {
+#pragma unroll
+        for (int i = 0; i < PASSES; ++i) {
+            const int row = wave * (BM / W) + i * AT_ONCE + lane / LANES;
+            uint32_t most = 0;
+#pragma unroll
+            for (int q = 0; q < KEEP; ++q) most = most_of(v[i][q], most);
+            const RowScale s = row_scale(most_of_lanes<LANES>(most));
+            if (lane % LANES == 0) scales[row] = s.scale;
+#pragma unroll
+            for (int q = 0; q < KEEP; ++q) {
+                const int byte = (q * LANES + lane % LANES) * N;
+                uint32_t w[N / 4];
+                quantize_vec(v[i][q], s, w);
+                __builtin_memcpy(reinterpret_cast<int8_t *>(lds + ThinLds<KS>::at(row, byte / 16)) + byte % 16, w, N);
+            }
+        }
+    }
+};
+
+// Waits until at most `behind` (0 .. MOST) groups of L loads each of this wave are under way.
+template <int MOST, int L>
+__device__ __forceinline__ void wait_for_loads(int behind)
+{
+    if constexpr (MOST > 0) {
+        if (behind >= MOST) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(MOST * L) : "memory");
+        else wait_for_loads<MOST - 1, L>(behind);
+    } else {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    }
+}
+
+// Short rows in whole steps: k a multiple of 64, n of 8, the rows of the weights at multiples of 16 bytes.  Eight waves share
+// 64 rows and take groups of 32 channels in turn; blockIdx.y: a part of the channels, a multiple of 256 (`part_n`).  The weights, which
+// every workgroup reads and the level-2 caches hold, come in steps of 64 bytes of k of a group's channels, past the registers to a ring of
+// D steps in LDS that is the wave's own: no barrier, and four lanes read 64 bytes of a row together (read as the matrix
+// instruction wants them, no two lanes do, and a quarter of the cache's rate is all there is).
+template <typename T, typename Y, int KS>
+__global__ void __launch_bounds__(512, KS <= 4 ? 4 : 2)
 linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, int part_n)
 {
-    constexpr int BM = 16 * MT, NT = 2, PIECES = KS < 2 ? 8 : KS * 4;
+    constexpr int MT = 4, W = 8, BM = 16 * MT, NT = 2, D = KS == 8 ? 6 : 3, STEP = 32 * 4;
+    __shared__ v4i lds[BM * ThinLds<KS>::PIECES];
+    __shared__ v4i ring[W][D * STEP];
+    __shared__ float scales[BM];
+    const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
+    const int m0 = int(blockIdx.x) * BM, r = lane & 15, g = lane >> 4, steps = p.k / 64;
+    int n0 = int(blockIdx.y) * part_n + wave * 32;
+    const int n_end = min(p.n, int(blockIdx.y + 1) * part_n);
+
+    // order of the four pieces of a row of a step (see ThinLds)
+    auto key = [](int row) { return (0x78 >> (((row >> Deal<Y>::SH) & 3) * 2)) & 3; };
+    const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(ring[wave]));
+    int next_n = n0, next_step = 0, issued = 0;          // what is read next, and how many steps have been
+    v4u at_b = {0, 0, 0, 0};
+    uint32_t off[2] = {0, 0};
+    auto aim = [&]() {
+        at_b = buffer_at(p.b + int64_t(next_n) * p.ldb);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int row = i * 16 + (lane >> 2);
+            off[i] = uint32_t(min(row, p.n - 1 - next_n)) * uint32_t(p.ldb) + uint32_t(((lane & 3) ^ key(row)) * 16);
+        }
+    };
+    auto issue = [&]() {
+        if (next_n >= n_end) return;
+        const uint32_t to = base + uint32_t(issued % D) * uint32_t(STEP * 16);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            asm volatile("s_mov_b32 m0, %1\n s_nop 0\n buffer_load_dwordx4 %0, %2, %3 offen lds"
+                         ::"v"(off[i]), "s"(to + uint32_t(i * 1024)), "s"(at_b), "s"(uint32_t(next_step) * 64u) : "memory");
+        ++issued;
+        if (++next_step == steps) {
+            next_step = 0;
+            next_n += W * 32;
+            if (next_n < n_end) aim();
+        }
+    };
+    auto start = [&]() {
+        if (next_n < n_end) aim();
+#pragma unroll 1
+        for (int i = 0; i < D - 1; ++i) issue();
+    };
+
+    if constexpr (sizeof(T) == 1) {
+        constexpr int PIECES = ThinLds<KS>::PIECES, EACH = BM * PIECES / (W * 64);
+        v4i v[EACH];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int at = i * (W * 64) + int(threadIdx.x);
+            v[i] = load16<true>(x + int64_t(min(m0 + at / PIECES, p.m - 1)) * ldx, at % PIECES * 16, p.k);
+        }
+        start();
+        if (threadIdx.x < BM) scales[threadIdx.x] = p.sa[min(m0 + int(threadIdx.x), p.m - 1)];
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int at = i * (W * 64) + int(threadIdx.x);
+            lds[ThinLds<KS>::at(at / PIECES, at % PIECES)] = v[i];
+        }
+    } else {
+        Vec<T> v[ThinRows<T, KS, W, BM>::PASSES][ThinRows<T, KS, W, BM>::KEEP];
+        ThinRows<T, KS, W, BM>::template load<true>(x, ldx, m0, p.m, p.k, wave, lane, v);
+        start();
+        ThinRows<T, KS, W, BM>::store(v, wave, lane, lds, scales);
+    }
+    __syncthreads();
+    float sa[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) sa[i] = scales[i * 16 + r];
+    int landed = 0;                                      // steps that are known to be in LDS
+    for (int c = 0; n0 < n_end; n0 += W * 32) {
+        v4i acc[MT][NT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j] = v4i{0, 0, 0, 0};
+#pragma unroll 1
+        for (int s = 0; s < steps; ++s, ++c) {
+            if (c >= landed) wait_for_loads<D - 2, 2>(issued - 1 - c);
+            // (the step that this one overwrites has been multiplied)
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            issue();
+            const v4i *const st = ring[wave] + (c % D) * STEP;
+            v4i va[MT], vb[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const int row = Deal<Y>::row(j, r);
+                vb[j] = st[row * 4 + (g ^ key(row))];
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i) va[i] = lds[ThinLds<KS>::at(i * 16 + r, s * 4 + g)];
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb[j], va[i], acc[i][j], 0, 0, 0);
+        }
+        Channels ch[NT];
+        load_channels<Y, NT, true>(p, n0, g, ch);
+        // what is under way is waited for before the stores: waiting for it behind them would be waiting for them
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        landed = issued;
+        store_tile<Y, MT, NT, true>(p, m0 + r, n0, g, acc, sa, ch);
+    }
+}
+
+// Short rows that end inside a step, or channels inside a store, or weights whose rows do not begin at multiples of 16 bytes: four waves, 32 rows,
+// the weights go to the registers directly, all KS steps of the first channels before the activations are waited for.
+template <typename T, typename Y, int KS>
+__global__ void __launch_bounds__(256, KS <= 2 ? 4 : 2)
+linear_i8_thin_ragged_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, int part_n)
+{
+    constexpr int MT = 2, W = 4, BM = 16 * MT, NT = 2, PIECES = ThinLds<KS>::PIECES;
     __shared__ v4i lds[BM * PIECES];
     __shared__ float scales[BM];
     const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
@@ -635,16 +804,16 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
 
     const int n_end = min(p.n, int(blockIdx.y + 1) * part_n);
     int n0 = int(blockIdx.y) * part_n + wave * 32;
-    const bool words = EXACT || rows_at_words(p.b, p.ldb);
+    const bool words = rows_at_words(p.b, p.ldb);
     v4i vb[KS][NT];
     auto fetch = [&](int n0) {                           // (also behind the last channel, for nothing, so that there is no branch)
         const int8_t *b[NT];
 #pragma unroll
         for (int j = 0; j < NT; ++j) b[j] = p.b + int64_t(min(n0 + Deal<Y>::row(j, r), p.n - 1)) * p.ldb;
-        if (EXACT || words) {
+        if (words) {
 #pragma unroll
             for (int s = 0; s < KS; ++s)
-                if ((EXACT && s == 0) || s * 64 + 64 <= p.k) {
+                if (s * 64 + 64 <= p.k) {
 #pragma unroll
                     for (int j = 0; j < NT; ++j) __builtin_memcpy(&vb[s][j], b[j] + s * 64 + g * 16, 16);
                 }
@@ -656,7 +825,7 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
                     for (int j = 0; j < NT; ++j) vb[s][j] = load16_loose(b[j] + s * 64 + g * 16);
                 }
         }
-        if (!EXACT && p.k % 64 != 0) {
+        if (p.k % 64 != 0) {
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
                 const v4i end = load16(b[j], p.k / 64 * 64 + g * 16, p.k);
@@ -672,45 +841,20 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
             const int at = i * (W * 64) + int(threadIdx.x), row = at / PIECES, c = at % PIECES;
-            v[i] = load16<EXACT>(x + int64_t(min(m0 + row, p.m - 1)) * ldx, c * 16, p.k);
+            v[i] = load16(x + int64_t(min(m0 + row, p.m - 1)) * ldx, c * 16, p.k);
         }
         fetch(n0);
         if (threadIdx.x < BM) scales[threadIdx.x] = p.sa[min(m0 + int(threadIdx.x), p.m - 1)];
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
             const int at = i * (W * 64) + int(threadIdx.x), row = at / PIECES, c = at % PIECES;
-            lds[row * PIECES + (c ^ (row & 7))] = v[i];
+            lds[ThinLds<KS>::at(row, c)] = v[i];
         }
     } else {
-        // LANES lanes quantise a row, KEEP vectors of 16 bytes each
-        constexpr int N = Vec<T>::N, VECS = KS * 64 / N, LANES = VECS < 16 ? VECS : 16, KEEP = VECS / LANES;
-        constexpr int AT_ONCE = 64 / LANES, PASSES = BM / W / AT_ONCE;
-        static_assert(PASSES * AT_ONCE * W == BM, "");
-        const int sub = lane % LANES;
-        Vec<T> v[PASSES][KEEP];
-#pragma unroll
-        for (int i = 0; i < PASSES; ++i) {
-            const int row = wave * (BM / W) + i * AT_ONCE + lane / LANES;
-            const T *from = x + int64_t(min(m0 + row, p.m - 1)) * ldx;
-            load_row<T, LANES, KEEP, EXACT>(from, sub, p.k, v[i]);
-        }
+        Vec<T> v[ThinRows<T, KS, W, BM>::PASSES][ThinRows<T, KS, W, BM>::KEEP];
+        ThinRows<T, KS, W, BM>::template load<false>(x, ldx, m0, p.m, p.k, wave, lane, v);
         fetch(n0);
-#pragma unroll
-        for (int i = 0; i < PASSES; ++i) {
-            const int row = wave * (BM / W) + i * AT_ONCE + lane / LANES;
-            uint32_t most = 0;
-#pragma unroll
-            for (int q = 0; q < KEEP; ++q) most = most_of(v[i][q], most);
-            const RowScale s = row_scale(most_of_lanes<LANES>(most));
-            if (sub == 0) scales[row] = s.scale;
-#pragma unroll
-            for (int q = 0; q < KEEP; ++q) {
-                const int byte = (q * LANES + sub) * N, c = byte / 16;
-                uint32_t w[N / 4];
-                quantize_vec(v[i][q], s, w);
-                __builtin_memcpy(reinterpret_cast<int8_t *>(lds + row * PIECES + (c ^ (row & 7))) + byte % 16, w, N);
-            }
-        }
+        ThinRows<T, KS, W, BM>::store(v, wave, lane, lds, scales);
     }
     __syncthreads();
     float sa[MT];
@@ -724,20 +868,20 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
             for (int j = 0; j < NT; ++j) acc[i][j] = v4i{0, 0, 0, 0};
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-            if ((!EXACT || s > 0) && s * 64 >= p.k) continue;
+            if (s * 64 >= p.k) continue;
             v4i va[MT];
 #pragma unroll
-            for (int i = 0; i < MT; ++i) va[i] = lds[(i * 16 + r) * PIECES + ((s * 4 + g) ^ (r & 7))];
+            for (int i = 0; i < MT; ++i) va[i] = lds[ThinLds<KS>::at(i * 16 + r, s * 4 + g)];
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
                 for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb[s][j], va[i], acc[i][j], 0, 0, 0);
         }
         Channels ch[NT];
-        load_channels<Y, NT, EXACT>(p, n0, g, ch);
+        load_channels<Y, NT>(p, n0, g, ch);
         // the next weights are read before the stores: behind them they would wait for them
         if (n0 + W * 32 < n_end) fetch(n0 + W * 32);
-        store_tile<Y, MT, NT, EXACT>(p, m0 + r, n0, g, acc, sa, ch);
+        store_tile<Y, MT, NT>(p, m0 + r, n0, g, acc, sa, ch);
     }
 }
 
@@ -941,19 +1085,20 @@ int launch_rows(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
 template <typename T, int KS>
 int launch_thin_steps(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
 {
-    // Eight waves and 64 rows: 1568x512 -> 2048 12.4 us, with four waves and 32 rows 14.9; more parts than make 512 workgroups do not
-    // pay (every part quantises the rows again).  Rows or channels that end inside a load: four waves and 32 rows.
-    const bool exact = p.k > 0 && p.k % 64 == 0 && p.n % 8 == 0 && p.ldb % 4 == 0 && reinterpret_cast<uintptr_t>(p.b) % 4 == 0;
+    const bool exact = p.k > 0 && p.k % 64 == 0 && p.n % 8 == 0 && rows_at_16(p.b, p.ldb);
     const int rows = exact ? 64 : 32, channels = exact ? 256 : 128;
     const int64_t tiles = (int64_t(p.m) + rows - 1) / rows, groups = (int64_t(p.n) + channels - 1) / channels;
+    // (every part quantises the rows again: no more of them than make 512 workgroups)
     const int64_t parts = std::min<int64_t>(groups, std::max<int64_t>(1, 512 / tiles));
     const int part_n = int((groups + parts - 1) / parts * channels);
     if (tiles >= int64_t(1) << 23) { set_error("pconv_matmul_i8: too many workgroups"); return PCONV_UNSUPPORTED; }
     const dim3 grid(unsigned(tiles), unsigned((int64_t(p.n) + part_n - 1) / part_n));
-#define PCONV_LAUNCH(Y, MT, EXACT, W) \
-    hipLaunchKernelGGL((linear_i8_thin_kernel<T, Y, MT, KS, EXACT, W>), grid, dim3(W * 64), 0, st, p, x, ldx, part_n)
-    if (p.y_bf16) { if (exact) PCONV_LAUNCH(__bf16, 4, true, 8); else PCONV_LAUNCH(__bf16, 2, false, 4); }
-    else { if (exact) PCONV_LAUNCH(float, 4, true, 8); else PCONV_LAUNCH(float, 2, false, 4); }
+#define PCONV_LAUNCH(Y)                                                                                                        \
+    do {                                                                                                                       \
+        if (exact) hipLaunchKernelGGL((linear_i8_thin_kernel<T, Y, KS>), grid, dim3(512), 0, st, p, x, ldx, part_n);          \
+        else hipLaunchKernelGGL((linear_i8_thin_ragged_kernel<T, Y, KS>), grid, dim3(256), 0, st, p, x, ldx, part_n);          \
+    } while (0)
+    if (p.y_bf16) PCONV_LAUNCH(__bf16); else PCONV_LAUNCH(float);
 #undef PCONV_LAUNCH
     return check_launch("pconv_linear_i8 (short rows)");
 }
@@ -982,8 +1127,6 @@ int launch_linear_i8_fused(const I8Product &p, const void *x, int64_t ldx, int b
     if (few(p.m, p.k)) return bf16 ? launch_rows(p, static_cast<const __bf16 *>(x), ldx, st) : launch_rows(p, static_cast<const float *>(x), ldx, st);
     return bf16 ? launch_thin(p, static_cast<const __bf16 *>(x), ldx, st) : launch_thin(p, static_cast<const float *>(x), ldx, st);
 }
-
-bool rows_at_16(const int8_t *at, int64_t ld) { return reinterpret_cast<uintptr_t>(at) % 16 == 0 && ld % 16 == 0 && ld <= 1 << 23; }
 
 int64_t matmul_i8_work_bytes(int64_t m, int64_t n, int64_t k, bool a_at_16, bool b_at_16)
 {
