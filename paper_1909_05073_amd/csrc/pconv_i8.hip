@@ -678,48 +678,58 @@ __device__ __forceinline__ void wait_for_loads(int behind)
 }
 
 // Short rows in whole steps: k a multiple of 64, n of 8, the rows of the weights at multiples of 16 bytes.  Eight waves share
-// 64 rows and take groups of 32 channels in turn; blockIdx.y: a part of the channels, a multiple of 256 (`part_n`).  The weights, which
-// every workgroup reads and the level-2 caches hold, come in steps of 64 bytes of k of a group's channels, past the registers to a ring of
-// D steps in LDS that is the wave's own: no barrier, and four lanes read 64 bytes of a row together (read as the matrix
-// instruction wants them, no two lanes do, and a quarter of the cache's rate is all there is).
-template <typename T, typename Y, int KS>
+// 64 rows, MH sets of them a part of the rows each, and take groups of 32 channels in turn; blockIdx.y: a part of the channels (`part_n`).
+// The weights, which every workgroup reads and the level-2 caches hold, come in steps of 128 bytes of k (64, where that is all) of a group's
+// channels, past the registers to a ring of D steps in LDS that is the wave's own: no barrier, and eight lanes read
+// 128 bytes of a row together (read as the matrix instruction wants them, no two lanes do, and a quarter of the cache's rate
+// is all there is).
+template <typename T, typename Y, int KS, int MH>
 __global__ void __launch_bounds__(512, KS <= 4 ? 4 : 2)
 linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, int part_n)
 {
-    constexpr int MT = 4, W = 8, BM = 16 * MT, NT = 2, D = KS == 8 ? 6 : 3, STEP = 32 * 4;
+    constexpr int W = 8, BM = 64, MT = 4 / MH, NT = 2, WN = W / MH, HALVES = KS == 1 ? 1 : 2, ROW = 4 * HALVES, STEP = 32 * ROW;
+    constexpr int D = KS == 1 || KS == 8 ? 3 : 2, L = STEP / 64;         // (two workgroups a compute unit but for KS = 8)
+    constexpr int AT_ONCE = 64 / ROW;                    // rows of a step that a load brings
     __shared__ v4i lds[BM * ThinLds<KS>::PIECES];
     __shared__ v4i ring[W][D * STEP];
-    __shared__ float scales[BM];
+    // the scales of the rows lie in the first wave's last step until it is read into
+    float *const scales = reinterpret_cast<float *>(ring[0] + (D - 1) * STEP);
     const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
-    const int m0 = int(blockIdx.x) * BM, r = lane & 15, g = lane >> 4, steps = p.k / 64;
-    int n0 = int(blockIdx.y) * part_n + wave * 32;
-    const int n_end = min(p.n, int(blockIdx.y + 1) * part_n);
+    const int m0 = int(blockIdx.x) * BM, r = lane & 15, g = lane >> 4, steps = (p.k + 64 * HALVES - 1) / (64 * HALVES);
+    int n0 = int(blockIdx.y) * part_n + wave % WN * 32;
+    const int n_end = min(p.n, int(blockIdx.y + 1) * part_n), upper = wave / WN * (MT * 16);
 
-    // order of the four pieces of a row of a step (see ThinLds)
-    auto key = [](int row) { return (0x78 >> (((row >> Deal<Y>::SH) & 3) * 2)) & 3; };
+    // order of the pieces of a row of a step (see ThinLds)
+    auto key = [](int row) {
+        const int q = row >> Deal<Y>::SH;
+        return HALVES == 1 ? (0x78 >> ((q & 3) * 2)) & 3 : (row & 3) | ((q & 1) << 2);
+    };
     const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(ring[wave]));
     int next_n = n0, next_step = 0, issued = 0;          // what is read next, and how many steps have been
     v4u at_b = {0, 0, 0, 0};
-    uint32_t off[2] = {0, 0};
+    uint32_t off[L], end[L];
     auto aim = [&]() {
         at_b = buffer_at(p.b + int64_t(next_n) * p.ldb);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int row = i * 16 + (lane >> 2);
-            off[i] = uint32_t(min(row, p.n - 1 - next_n)) * uint32_t(p.ldb) + uint32_t(((lane & 3) ^ key(row)) * 16);
+        for (int i = 0; i < L; ++i) {
+            const int row = i * AT_ONCE + lane / ROW, col = (lane % ROW ^ key(row)) * 16;
+            off[i] = uint32_t(min(row, p.n - 1 - next_n)) * uint32_t(p.ldb) + uint32_t(col);
+            end[i] = HALVES == 2 && p.k % 128 != 0 && col >= 64 ? kNowhere : off[i];         // (in a last step of 64 bytes)
         }
     };
     auto issue = [&]() {
         if (next_n >= n_end) return;
         const uint32_t to = base + uint32_t(issued % D) * uint32_t(STEP * 16);
+        const bool last = next_step == steps - 1;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < L; ++i)
             asm volatile("s_mov_b32 m0, %1\n s_nop 0\n buffer_load_dwordx4 %0, %2, %3 offen lds"
-                         ::"v"(off[i]), "s"(to + uint32_t(i * 1024)), "s"(at_b), "s"(uint32_t(next_step) * 64u) : "memory");
+                         ::"v"(last ? end[i] : off[i]), "s"(to + uint32_t(i * 1024)), "s"(at_b), "s"(uint32_t(next_step) * uint32_t(64 * HALVES)) : "memory");
         ++issued;
-        if (++next_step == steps) {
+        ++next_step;
+        if (last) {
             next_step = 0;
-            next_n += W * 32;
+            next_n += WN * 32;
             if (next_n < n_end) aim();
         }
     };
@@ -753,9 +763,10 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
     __syncthreads();
     float sa[MT];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) sa[i] = scales[i * 16 + r];
+    for (int i = 0; i < MT; ++i) sa[i] = scales[upper + i * 16 + r];
+    __syncthreads();
     int landed = 0;                                      // steps that are known to be in LDS
-    for (int c = 0; n0 < n_end; n0 += W * 32) {
+    for (int c = 0; n0 < n_end; n0 += WN * 32) {
         v4i acc[MT][NT];
 #pragma unroll
         for (int i = 0; i < MT; ++i)
@@ -763,30 +774,33 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
             for (int j = 0; j < NT; ++j) acc[i][j] = v4i{0, 0, 0, 0};
 #pragma unroll 1
         for (int s = 0; s < steps; ++s, ++c) {
-            if (c >= landed) wait_for_loads<D - 2, 2>(issued - 1 - c);
+            if (c >= landed) wait_for_loads<D - 2, L>(issued - 1 - c);
             // (the step that this one overwrites has been multiplied)
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             issue();
             const v4i *const st = ring[wave] + (c % D) * STEP;
-            v4i va[MT], vb[NT];
 #pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                const int row = Deal<Y>::row(j, r);
-                vb[j] = st[row * 4 + (g ^ key(row))];
+            for (int h = 0; h < HALVES; ++h) {
+                v4i va[MT], vb[NT];
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    const int row = Deal<Y>::row(j, r);
+                    vb[j] = st[row * ROW + ((h * 4 + g) ^ key(row))];
+                }
+#pragma unroll
+                for (int i = 0; i < MT; ++i) va[i] = lds[ThinLds<KS>::at(upper + i * 16 + r, (s * HALVES + h) * 4 + g)];
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb[j], va[i], acc[i][j], 0, 0, 0);
             }
-#pragma unroll
-            for (int i = 0; i < MT; ++i) va[i] = lds[ThinLds<KS>::at(i * 16 + r, s * 4 + g)];
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb[j], va[i], acc[i][j], 0, 0, 0);
         }
         Channels ch[NT];
         load_channels<Y, NT, true>(p, n0, g, ch);
         // what is under way is waited for before the stores: waiting for it behind them would be waiting for them
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         landed = issued;
-        store_tile<Y, MT, NT, true>(p, m0 + r, n0, g, acc, sa, ch);
+        store_tile<Y, MT, NT, true>(p, m0 + upper + r, n0, g, acc, sa, ch);
     }
 }
 
@@ -1086,7 +1100,8 @@ template <typename T, int KS>
 int launch_thin_steps(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
 {
     const bool exact = p.k > 0 && p.k % 64 == 0 && p.n % 8 == 0 && rows_at_16(p.b, p.ldb);
-    const int rows = exact ? 64 : 32, channels = exact ? 256 : 128;
+    const bool narrow = p.n <= 128;                      // half of the waves would have no channels: they take half of the rows
+    const int rows = exact ? 64 : 32, channels = exact && !narrow ? 256 : 128;
     const int64_t tiles = (int64_t(p.m) + rows - 1) / rows, groups = (int64_t(p.n) + channels - 1) / channels;
     // (every part quantises the rows again: no more of them than make 512 workgroups)
     const int64_t parts = std::min<int64_t>(groups, std::max<int64_t>(1, 512 / tiles));
@@ -1095,7 +1110,8 @@ int launch_thin_steps(const I8Product &p, const T *x, int64_t ldx, hipStream_t s
     const dim3 grid(unsigned(tiles), unsigned((int64_t(p.n) + part_n - 1) / part_n));
 #define PCONV_LAUNCH(Y)                                                                                                        \
     do {                                                                                                                       \
-        if (exact) hipLaunchKernelGGL((linear_i8_thin_kernel<T, Y, KS>), grid, dim3(512), 0, st, p, x, ldx, part_n);          \
+        if (exact && narrow) hipLaunchKernelGGL((linear_i8_thin_kernel<T, Y, KS, 2>), grid, dim3(512), 0, st, p, x, ldx, part_n); \
+        else if (exact) hipLaunchKernelGGL((linear_i8_thin_kernel<T, Y, KS, 1>), grid, dim3(512), 0, st, p, x, ldx, part_n);   \
         else hipLaunchKernelGGL((linear_i8_thin_ragged_kernel<T, Y, KS>), grid, dim3(256), 0, st, p, x, ldx, part_n);          \
     } while (0)
     if (p.y_bf16) PCONV_LAUNCH(__bf16); else PCONV_LAUNCH(float);
