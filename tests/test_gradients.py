@@ -269,3 +269,30 @@ def test_wrong_tensors_are_refused():
             call()
     P.GradList([a, b], out=[a, z[2000:3000]]).clip(1.0)  # one in place, one not
     P.GradList([a, a], out=[b, z[2000:3000]]).clip(1.0)  # read twice, written once each
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("in_place", [False, True])
+def test_more_than_the_caches_hold_in_several_launches(in_place):
+    """300 tensors of 256 KiB to 2 MiB, fp32 and bf16: two tables, read and written past the caches, the last part kept there."""
+    import torch
+    rng = np.random.default_rng(9)
+    sizes = [int(n) for n in rng.integers(1 << 16, 1 << 20, 300)]
+    say(f"[case] clip {len(sizes)} tensors, {sum(sizes)} elements, in place {in_place}")
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(4)
+    grads = [torch.randn(n, generator=gen, device="cuda").to(torch.bfloat16 if i % 3 == 0 else torch.float32) for i, n in enumerate(sizes)]
+    want_norm = math.sqrt(math.fsum(float(g.double().square().sum()) for g in grads))
+    factor = 7.0 / (want_norm + 1e-6)
+    want = [g.double() * factor for g in grads]
+    outs = grads if in_place else [torch.full_like(g, float("nan"), dtype=torch.float32) for g in grads]
+    norm = P.clip_grad_norm(grads, 7.0, out=None if in_place else outs)
+    assert abs(float(norm) - want_norm) <= 1.01 * U * want_norm
+    for i, (o, w) in enumerate(zip(outs, want)):
+        tol = 2.02 * U * w.abs() + 2.0 ** -149
+        if o.dtype == torch.bfloat16:
+            tol = tol * 1.01 + 2.0 ** -8 * 1.01 * w.abs() + 2.0 ** -133
+        assert bool(((o.double() - w).abs() <= tol).all()), f"tensor {i}"
+    mine = [torch.ones(3, device="cuda")] + [torch.zeros(1 << 26, device="cuda") for _ in range(2)]
+    mine[2][-1] = 2.0
+    assert abs(float(P.clip_grad_norm(mine, 1.0)) - math.sqrt(7)) <= 3 * U and abs(float(mine[2][-1]) * math.sqrt(7) / 2 - 1) < 1e-6
