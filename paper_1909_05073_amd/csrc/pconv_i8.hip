@@ -900,19 +900,21 @@ linear_i8_thin_ragged_kernel(const I8Product p, const T *__restrict__ x, int64_t
 }
 
 // Few rows (up to 16): 16 channels a workgroup, whose waves share the length of k in turns of 256 bytes and add their sums in LDS.
-// Reading the weights is all of it; a wave has the next turn's under way while it multiplies.  T is int8_t, or
+// Reading the weights is all of it; a wave has the next turns' under way while it multiplies: D > 0, in a ring of its own in LDS, past
+// the registers (rows at multiples of 16 bytes; see linear_i8_thin_kernel), D = 0, in registers.  T is int8_t, or
 // the rows come as floats, up to kFusedRows elements, and every workgroup quantises all of them to LDS while its first weights
 // are on their way: less than a launch for it takes.
 constexpr int kRowsM = 16, kFusedRows = 32768, kRowsMost = 131072;
 
-template <typename T>
+template <typename T, int D, bool LONG>
 __global__ void __launch_bounds__(512)
 linear_i8_rows_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx)
 {
     constexpr int WAVES = 8, TURN = 256;
     constexpr bool FUSED = sizeof(T) > 1;
     extern __shared__ v4i rows_lds[];                    // quantised rows, `pitch` bytes from one to the next
-    __shared__ v4i sums[WAVES][64];
+    constexpr bool RING = D > 0;
+    __shared__ v4i ring[WAVES][RING ? D * 256 : 64];
     __shared__ uint32_t mosts[WAVES];
     __shared__ float scales[kRowsM];
     const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), r = lane & 15, g = lane >> 4;
@@ -931,13 +933,36 @@ linear_i8_rows_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx)
         }
     };
     int k0 = wave * TURN;
-    if (k0 < whole) fetch(vb, k0);
+    // the ring: a turn is 16 rows of 256 bytes, 16 lanes read a row together
+    const v4u at_b = buffer_at(p.b + int64_t(n0) * p.ldb);
+    uint32_t off[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = i * 4 + (lane >> 4);
+        off[i] = uint32_t(min(row, p.n - 1 - n0)) * uint32_t(p.ldb) + uint32_t((lane & 15) ^ row) * 16u;
+    }
+    const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(ring[wave]));
+    const int mine = whole / TURN > wave ? (whole / TURN - wave + WAVES - 1) / WAVES : 0;
+    auto issue = [&](int t) {
+        if (t >= mine) return;
+        const uint32_t to = base + uint32_t(t % (RING ? D : 1)) * 4096u, at = uint32_t(wave + t * WAVES) * uint32_t(TURN);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            asm volatile("s_mov_b32 m0, %1\n s_nop 0\n buffer_load_dwordx4 %0, %2, %3 offen lds"
+                         ::"v"(off[i]), "s"(to + uint32_t(i * 1024)), "s"(at_b), "s"(at) : "memory");
+    };
+    if constexpr (RING) {
+#pragma unroll 1
+        for (int t = 0; t < D; ++t) issue(t);
+    } else {
+        if (k0 < whole) fetch(vb, k0);
+    }
     int8_t *const q = reinterpret_cast<int8_t *>(rows_lds);
     if constexpr (FUSED) {
-        constexpr int N = Vec<T>::N, KEEP = 4;
-        // row m by THREADS threads, all of the workgroup or a wave
-        auto quantize_row = [&](int m, int sub, auto threads) {
-            constexpr int THREADS = decltype(threads)::value;
+        constexpr int N = Vec<T>::N;
+        // row m by THREADS threads, all of the workgroup or a wave, KEEP vectors each in registers
+        auto quantize_row = [&](int m, int sub, auto threads, auto keep) {
+            constexpr int THREADS = decltype(threads)::value, KEEP = decltype(keep)::value;
             const T *row = x + int64_t(m) * ldx;
             Vec<T> v[KEEP];
             load_row<T, THREADS, KEEP>(row, sub, p.k, v);
@@ -959,9 +984,10 @@ linear_i8_rows_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx)
 #pragma unroll
             for (int i = 0; i < KEEP; ++i) {
                 const int at = (i * THREADS + sub) * N;
+                if (at >= p.k) continue;
                 uint32_t w[N / 4];
                 quantize_vec(v[i], s, w);
-                if (at < p.k) __builtin_memcpy(to + at, w, N);
+                __builtin_memcpy(to + at, w, N);
             }
 #pragma unroll 2
             for (int at = (KEEP * THREADS + sub) * N; at < p.k; at += THREADS * N) {
@@ -973,16 +999,34 @@ linear_i8_rows_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx)
         };
         // Long rows one after the other by all waves, else a row a wave: 2 rows of 25088 24.9 us; 16 rows of 512 19.2 us the
         // first way, 4.6 the second; 2 rows of 256 4.7 and 3.4.
-        if (p.m < 4 && p.k > 64 * KEEP * N) {
-            for (int m = 0; m < p.m; ++m) quantize_row(m, int(threadIdx.x), std::integral_constant<int, WAVES * 64>());
+        if (p.m < 4 && p.k > 64 * 4 * N) {
+            for (int m = 0; m < p.m; ++m) quantize_row(m, int(threadIdx.x), std::integral_constant<int, WAVES * 64>(), std::integral_constant<int, LONG ? kFusedRows / (WAVES * 64 * N) : 4>());
         } else {
-            for (int m = wave; m < p.m; m += WAVES) quantize_row(m, lane, std::integral_constant<int, 64>());
+            for (int m = wave; m < p.m; m += WAVES) quantize_row(m, lane, std::integral_constant<int, 64>(), std::integral_constant<int, 4>());
         }
         __syncthreads();
     }
     const int8_t *const a = FUSED ? q + min(r, p.m - 1) * pitch : p.a + int64_t(min(r, p.m - 1)) * p.lda;
     v4i acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-    while (k0 < whole) {
+    if constexpr (RING) {
+#pragma unroll 1
+        for (int t = 0; t < mine; ++t) {
+            wait_for_loads<D - 1, 4>(min(D - 1, mine - 1 - t));
+            const v4i *const st = ring[wave] + (t % D) * 256;
+            const int at = (wave + t * WAVES) * TURN + g * 16;
+            v4i va[4];
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                vb[s] = st[r * 16 + ((s * 4 + g) ^ r)];
+                __builtin_memcpy(&va[s], a + at + s * 64, 16);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // (read, so that it may be overwritten)
+            issue(t + D);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) acc[s & 1] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb[s], va[s], acc[s & 1], 0, 0, 0);
+        }
+    }
+    while (!RING && k0 < whole) {
         v4i va[4], next[4];
         const int k1 = k0 + WAVES * TURN;
 #pragma unroll
@@ -1007,12 +1051,12 @@ linear_i8_rows_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx)
 #pragma unroll
         for (int s = 0; s < 4; ++s) acc[s & 1] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb[s], va[s], acc[s & 1], 0, 0, 0);
     }
-    sums[wave][lane] = acc[0] + acc[1];
+    ring[wave][lane] = acc[0] + acc[1];
     __syncthreads();
     if (wave) return;
-    v4i s = sums[0][lane];
+    v4i s = ring[0][lane];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) s += sums[w][lane];
+    for (int w = 1; w < WAVES; ++w) s += ring[w][lane];
     const int n = n0 + g * 4;
     if (r >= p.m || n >= p.n) return;
     const f4 v = values_of(p, s, FUSED ? scales[r] : p.sa[r], channels_at(p, n));
@@ -1091,7 +1135,20 @@ int launch_rows(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
 {
     const size_t lds = sizeof(T) > 1 ? size_t(p.m) * ((p.k + 255) / 256 * 256 + 16) : 0;
     const unsigned grid = unsigned((int64_t(p.n) + 15) / 16);
-    hipLaunchKernelGGL((linear_i8_rows_kernel<T>), dim3(grid), dim3(512), lds, st, p, x, ldx);
+    // The ring takes 64 KB of LDS: where a compute unit has one workgroup at most, or two fit still (1x25088 -> 1000 18.3 us without it, 12.0;
+    // 2x8192 -> 8192 16.3 and, one workgroup a compute unit with it, 19.6).  There long rows stay in registers between their two
+    // uses (10.9 us; 1x4096 -> 1000 4.8 us with few registers and 5.9).
+    if constexpr (sizeof(T) > 1) {
+        const bool one = int64_t(grid) <= kUnits;
+        if (rows_at_16(p.b, p.ldb) && (one || lds <= 14 * 1024)) {
+            if (one && p.k > kFusedRows / 4 && p.m < 4)
+                hipLaunchKernelGGL((linear_i8_rows_kernel<T, 2, true>), dim3(grid), dim3(512), lds, st, p, x, ldx);
+            else
+                hipLaunchKernelGGL((linear_i8_rows_kernel<T, 2, false>), dim3(grid), dim3(512), lds, st, p, x, ldx);
+            return check_launch("pconv_linear_i8 (few rows)");
+        }
+    }
+    hipLaunchKernelGGL((linear_i8_rows_kernel<T, 0, false>), dim3(grid), dim3(512), lds, st, p, x, ldx);
     return check_launch("pconv_linear_i8 (few rows)");
 }
 
