@@ -777,7 +777,11 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
     for (int i = 0; i < MT; ++i) sa[i] = scales[upper + i * 16 + r];
     __syncthreads();
     int landed = 0;                                      // steps that are known to be in LDS
+    Channels ch[NT];
+    if (n0 < n_end) load_channels<Y, NT, true>(p, n0, g, ch);
     for (int c = 0; n0 < n_end; n0 += WN * 32) {
+        Channels next[NT];
+        load_channels<Y, NT, true>(p, min(n0 + WN * 32, p.n), g, next);
         v4i acc[MT][NT];
 #pragma unroll
         for (int i = 0; i < MT; ++i)
@@ -806,12 +810,14 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
                     for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb[j], va[i], acc[i][j], 0, 0, 0);
             }
         }
-        Channels ch[NT];
-        load_channels<Y, NT, true>(p, n0, g, ch);
         // what is under way is waited for before the stores: waiting for it behind them would be waiting for them
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int j = 0; j < NT; ++j) asm volatile("" : "+v"(next[j].scale), "+v"(next[j].bias));
+        if (issued > landed) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         landed = issued;
         store_tile<Y, MT, NT, true>(p, m0 + upper + r, n0, g, acc, sa, ch);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) ch[j] = next[j];
     }
 }
 
