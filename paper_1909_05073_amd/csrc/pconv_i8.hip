@@ -690,8 +690,7 @@ __device__ __forceinline__ void wait_for_loads(int behind)
 
 // Short rows in whole steps: k a multiple of 64, n of 8, the rows of the weights at multiples of 16 bytes.  Eight waves share
 // 64 rows, MH sets of them a part of the rows each, and take groups of 32 channels in turn; blockIdx.y: a part of the channels (`part_n`).
-// The weights, which every workgroup reads and the level-2 caches hold, come in steps of 128 bytes of k (64, where that is all) of a group's
-// channels, past the registers to a ring of D steps in LDS that is the wave's own: no barrier, and eight lanes read
+// The weights, which every workgroup reads and the level-2 caches hold, come in steps of 128 bytes of k of a group's channels (k up to 64: one step, to the registers), past the registers to a ring of D steps in LDS that is the wave's own: no barrier, and eight lanes read
 // 128 bytes of a row together (read as the matrix instruction wants them, no two lanes do, and a quarter of the cache's rate
 // is all there is).
 template <typename T, typename Y, int KS, int MH>
@@ -699,12 +698,13 @@ __global__ void __launch_bounds__(512, KS <= 4 ? 4 : 2)
 linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, int part_n)
 {
     constexpr int W = 8, BM = 64, MT = 4 / MH, NT = 2, WN = W / MH, HALVES = KS == 1 ? 1 : 2, ROW = 4 * HALVES, STEP = 32 * ROW;
-    constexpr int D = KS == 1 || KS == 8 ? 3 : 2, L = STEP / 64;         // (two workgroups a compute unit but for KS = 8)
+    constexpr bool RING = KS > 1;
+    constexpr int D = KS == 8 ? 3 : RING ? 2 : 1, L = STEP / 64;         // (two workgroups a compute unit but for KS = 8)
     constexpr int AT_ONCE = 64 / ROW;                    // rows of a step that a load brings
     __shared__ v4i lds[BM * ThinLds<KS>::PIECES];
-    __shared__ v4i ring[W][D * STEP];
-    // the scales of the rows lie in the first wave's last step until it is read into
-    float *const scales = reinterpret_cast<float *>(ring[0] + (D - 1) * STEP);
+    __shared__ v4i ring[RING ? W : 1][RING ? D * STEP : 16];
+    // (the scales of the rows: in the first wave's last step until it is read into)
+    float *const scales = reinterpret_cast<float *>(ring[0] + (RING ? D - 1 : 0) * STEP);
     const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
     const int m0 = int(blockIdx.x) * BM, r = lane & 15, g = lane >> 4, steps = (p.k + 64 * HALVES - 1) / (64 * HALVES);
     int n0 = int(blockIdx.y) * part_n + wave % WN * 32;
@@ -715,7 +715,7 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
         const int q = row >> Deal<Y>::SH;
         return HALVES == 1 ? (0x78 >> ((q & 3) * 2)) & 3 : (row & 3) | ((q & 1) << 2);
     };
-    const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(ring[wave]));
+    const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(ring[RING ? wave : 0]));
     int next_n = n0, next_step = 0, issued = 0;          // what is read next, and how many steps have been
     v4u at_b = {0, 0, 0, 0};
     uint32_t off[L], end[L];
@@ -744,7 +744,17 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
             if (next_n < n_end) aim();
         }
     };
+    v4i vb[NT];
+    auto fetch = [&](int n0) {                           // (one step: to the registers)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+            __builtin_memcpy(&vb[j], p.b + int64_t(min(n0 + Deal<Y>::row(j, r), p.n - 1)) * p.ldb + g * 16, 16);
+    };
     auto start = [&]() {
+        if constexpr (!RING) {
+            fetch(n0);
+            return;
+        }
         if (next_n < n_end) aim();
 #pragma unroll 1
         for (int i = 0; i < D - 1; ++i) issue();
@@ -771,32 +781,47 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
         start();
         ThinRows<T, KS, W, BM>::store(v, wave, lane, lds, scales);
     }
+    Channels ch[NT];
+    if (n0 < n_end) load_channels<Y, NT, true>(p, n0, g, ch);
     __syncthreads();
     float sa[MT];
 #pragma unroll
     for (int i = 0; i < MT; ++i) sa[i] = scales[upper + i * 16 + r];
-    __syncthreads();
+    if (RING) __syncthreads();
     int landed = 0;                                      // steps that are known to be in LDS
-    Channels ch[NT];
-    if (n0 < n_end) load_channels<Y, NT, true>(p, n0, g, ch);
     for (int c = 0; n0 < n_end; n0 += WN * 32) {
+        const bool more = n0 + WN * 32 < n_end;
         Channels next[NT];
-        load_channels<Y, NT, true>(p, min(n0 + WN * 32, p.n), g, next);
+        if (more) load_channels<Y, NT, true>(p, n0 + WN * 32, g, next);
         v4i acc[MT][NT];
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < NT; ++j) acc[i][j] = v4i{0, 0, 0, 0};
+        if constexpr (!RING) {
+            v4i va[MT];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) va[i] = lds[ThinLds<KS>::at(upper + i * 16 + r, g)];
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(vb[j], va[i], acc[i][j], 0, 0, 0);
+            if (more) {
+                fetch(n0 + WN * 32);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) asm volatile("" : "+v"(vb[j]));
+            }
+        }
 #pragma unroll 1
-        for (int s = 0; s < steps; ++s, ++c) {
-            if (c >= landed) wait_for_loads<D - 2, L>(issued - 1 - c);
+        for (int s = 0; RING && s < steps; ++s, ++c) {
+            if (c >= landed) wait_for_loads<(RING ? D - 2 : 0), L>(issued - 1 - c);
             // (the step that this one overwrites has been multiplied)
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             issue();
-            const v4i *const st = ring[wave] + (c % D) * STEP;
+            const v4i *const st = ring[RING ? wave : 0] + (c % D) * STEP;
 #pragma unroll
             for (int h = 0; h < HALVES; ++h) {
-                v4i va[MT], vb[NT];
+                v4i va[MT];
 #pragma unroll
                 for (int j = 0; j < NT; ++j) {
                     const int row = Deal<Y>::row(j, r);
@@ -811,8 +836,10 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
             }
         }
         // what is under way is waited for before the stores: waiting for it behind them would be waiting for them
+        if (more) {
 #pragma unroll
-        for (int j = 0; j < NT; ++j) asm volatile("" : "+v"(next[j].scale), "+v"(next[j].bias));
+            for (int j = 0; j < NT; ++j) asm volatile("" : "+v"(next[j].scale), "+v"(next[j].bias));
+        }
         if (issued > landed) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         landed = issued;
         store_tile<Y, MT, NT, true>(p, m0 + upper + r, n0, g, acc, sa, ch);
