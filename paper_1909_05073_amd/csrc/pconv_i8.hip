@@ -396,11 +396,11 @@ __device__ __forceinline__ v4u buffer_at(const int8_t *p)
     v4u r;
     r.x = __builtin_amdgcn_readfirstlane(uint32_t(at));
     r.y = __builtin_amdgcn_readfirstlane(uint32_t(at >> 32) & 0xFFFFu);
-    r.z = 0xFFFF0000u;
+    r.z = 0x90000000u;                                   // (a tile's rows are within 2^31 bytes and a row's length)
     r.w = 0x00020000u;
     return r;
 }
-constexpr uint32_t kNowhere = 0xFFFFFFF0u;               // an offset beyond any buffer: nothing is read, LDS gets zeros
+constexpr uint32_t kNowhere = 0xC0000000u;               // beyond the buffer, whatever is added: nothing is read, LDS gets zeros
 
 // Which tile a workgroup computes.  Workgroups go round the 8 XCDs, each of which has a level-2 cache of its own: an XCD gets
 // a run of tiles, and a run goes down GROUP tiles of rows before it goes on to the next tile of channels, so that the tiles that

@@ -217,6 +217,34 @@ def test_product_and_layer_against_the_formula(m, n, k, dtype):
     check(P.linear_i8(x, wd, sd, relu=not relu, out_dtype=other), want, bound, "linear_i8, no bias")
 
 
+# Lengths that are whole pieces of 16 bytes but no whole stages of 128, by each kernel; few, many and odd channels; k split.
+PIECES = [(20, 64, 192), (20, 24, 320), (100, 256, 448), (130, 520, 192), (70, 128, 384), (17, 8, 64), (33, 1000, 64), (64, 136, 512),
+          (1, 40, 16), (3, 48, 272), (16, 16, 4112), (2, 300, 8208), (1, 9, 24992), (5, 17, 30000),
+          (20, 64, 528), (65, 130, 576), (40, 256, 1104), (300, 300, 2064), (129, 512, 720), (1000, 260, 656), (24, 40, 20016),
+          (2600, 2050, 592), (33, 7, 16400), (10, 100, 13120), (12, 64, 16384)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k", PIECES)
+def test_lengths_that_end_inside_a_stage(m, n, k, dtype):
+    import torch
+    say(f"[case] linear_i8 {m}x{n}x{k} {dtype}")
+    rng = np.random.default_rng(m * 10007 + n * 101 + k)
+    x, values = as_type(make_x(rng, m, k), dtype)
+    w, sb, bias = make_layer8(rng, n, k)
+    q, sa = plain_quantize(values)
+    want, bound = plain_product(q, sa, w, sb, bias, True)
+    # behind the weights lie bytes that would show
+    wide = torch.full((n, k + 64), 101, dtype=torch.int8, device="cuda")
+    wide[:, :k] = dev(w)
+    for b in (dev(w), wide[:, :k]):
+        check(P.linear_i8(x, b, dev(sb), dev(bias), relu=True), want, bound, "linear_i8")
+        a = torch.full((m, k + 16), 99, dtype=torch.int8, device="cuda")
+        a[:, :k] = dev(q.astype(np.int8))
+        check(P.matmul_i8(a[:, :k], dev(sa), b, dev(sb), dev(bias), relu=True, out_dtype=x.dtype), want, bound, "matmul_i8")
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("m,n,k", [(1, 20, 70), (5, 33, 300), (40, 50, 129), (130, 140, 200), (300, 130, 64)])
 @pytest.mark.parametrize("offset,extra", [(0, 16), (0, 1), (1, 0), (3, 6), (16, 48)])
@@ -311,7 +339,7 @@ def test_leading_dimensions_are_rows():
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("m,n,k", [(1030, 24, 48), (40, 24, 48), (3, 24, 48)])
+@pytest.mark.parametrize("m,n,k", [(1030, 24, 48), (40, 24, 48), (3, 24, 48), (40, 24, 600), (3, 24, 600)])
 def test_offsets_beyond_32_bits(m, n, k):
     """Rows of a, of x and of y that lie so far apart that the last ones are beyond 2^32 bytes; rows of b as well."""
     import torch
