@@ -350,18 +350,18 @@ def test_offsets_beyond_32_bits(m, n, k):
     x = make_x(rng, m, k)
     q, sa = plain_quantize(x)
     want, bound = plain_product(q, sa, w, sb, bias, False)
-    room = torch.empty((m - 1) * step + 64, dtype=torch.int8, device="cuda")
+    room = torch.empty((m - 1) * step + k + 64, dtype=torch.int8, device="cuda")
     a = torch.as_strided(room, (m, k), (step, 1))
     a.copy_(dev(q.astype(np.int8)))
     check(P.matmul_i8(a, dev(sa), dev(w), dev(sb), dev(bias)), want, bound, "far rows of a")
     rows = min(n, 24)
     far = (1 << 32) // (rows - 1) // 16 * 16 + 64
-    room = torch.empty((rows - 1) * far + 64, dtype=torch.int8, device="cuda")
+    room = torch.empty((rows - 1) * far + k + 64, dtype=torch.int8, device="cuda")
     b = torch.as_strided(room, (n, k), (far, 1))
     b.copy_(dev(w))
     check(P.matmul_i8(dev(q.astype(np.int8)), dev(sa), b, dev(sb), dev(bias)), want, bound, "far rows of b")
     del room, a, b
-    room = torch.empty((m - 1) * (step // 4) + 64, dtype=torch.float32, device="cuda")
+    room = torch.empty((m - 1) * (step // 4) + k + 64, dtype=torch.float32, device="cuda")
     xs = torch.as_strided(room, (m, k), (step // 4, 1))
     xs.copy_(dev(x))
     check(P.linear_i8(xs, dev(w), dev(sb), dev(bias)), want, bound, "far rows of x")
