@@ -246,6 +246,32 @@ def test_lengths_that_end_inside_a_stage(m, n, k, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("m,n,k", [(7900, 4000, 592), (7900, 4000, 585), (5000, 1030, 1040), (90_000, 72, 560), (40_000, 200, 320), (20_000, 264, 448)])
+def test_many_tiles(m, n, k):
+    """Products whose tiles fill the card, against 64 bits on the card."""
+    import torch
+    say(f"[case] matmul_i8 {m}x{n}x{k}")
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(m + k)
+    x = torch.randn(m, k, generator=gen, device="cuda") * torch.rand(m, 1, generator=gen, device="cuda")
+    w = torch.randint(-127, 128, (n, k), generator=gen, device="cuda", dtype=torch.int8)
+    sb, bias = torch.rand(n, generator=gen, device="cuda"), torch.randn(n, generator=gen, device="cuda")
+    most = x.abs().amax(1, keepdim=True)
+    scale = most / torch.full_like(most, 127.0)
+    q = (x / scale).round()                              # (no row of zeros among these)
+    scaled = (q.double() @ w.double().t()) * scale.double() * sb.double()
+    want = scaled + bias.double()
+    bound = 4 * U * (scaled.abs() + bias.double().abs())
+    got, s = P.quantize_rows(x)
+    assert torch.equal(got.float(), q) and torch.equal(s, scale[:, 0])
+    for dtype in (torch.float32, torch.bfloat16):
+        tol = bound if dtype == torch.float32 else bound * (1 + 2.0 ** -8) + 2.0 ** -8 * want.abs() * (1 + 2.0 ** -8)
+        for y in (P.linear_i8(x, w, sb, bias, out_dtype=dtype), P.matmul_i8(got, s, w, sb, bias, out_dtype=dtype)):
+            assert bool(((y.double() - want).abs() <= tol).all())
+        assert torch.equal(P.linear_i8(x, w, sb, bias, relu=True, out_dtype=dtype), y.clamp(min=0))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("m,n,k", [(1, 20, 70), (5, 33, 300), (40, 50, 129), (130, 140, 200), (300, 130, 64)])
 @pytest.mark.parametrize("offset,extra", [(0, 16), (0, 1), (1, 0), (3, 6), (16, 48)])
 def test_operands_and_outputs_that_lie_apart_and_begin_anywhere(m, n, k, offset, extra):
