@@ -7,7 +7,7 @@
 //
 // Elements that fit the caches beside their outputs are left there.  Of more, the first pass reads past the caches all but the last 192 MB, which the
 // second pass, from the last chunk to the first, finds in the 256 MB memory-side cache; its stores pass the caches too.  138 million fp32
-// elements: first pass 87 us (6.4 TB/s; 129 where the caches were left full of outputs), second 170 us (206 with nothing kept).
+// elements: first pass 87 us (6.4 TB/s; 129 where the caches were left full of outputs), second 186 us (206 with nothing kept).
 #include <hip/hip_runtime.h>
 
 #include "pconv_internal.h"
@@ -226,7 +226,7 @@ grad_scale_kernel(const GradTable t, const double *__restrict__ partials, uint32
         chunk_scale<kThreads, PASSING>(find_chunk(t, t.chunks - 1 - c), f, threadIdx.x);
 }
 
-// Few elements: one workgroup, whose waves take the chunks in turn, does both passes.
+// Few elements: one workgroup, whose waves take the chunks in turn, does both passes (2320 elements 4.9 us, two kernels 3.1 and 3.8).
 __global__ void __launch_bounds__(1024)
 grad_clip_one_kernel(const GradTable t, float max_norm, float eps, float *norm)
 {
