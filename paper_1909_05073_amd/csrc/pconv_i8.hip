@@ -692,7 +692,7 @@ __device__ __forceinline__ void wait_for_loads(int behind)
     }
 }
 
-// Short rows in whole steps: k a multiple of 64, n of 8, the rows of the weights at multiples of 16 bytes.  Eight waves share
+// Short rows in whole pieces: k a multiple of 16, n of 8, the rows of the weights at multiples of 16 bytes.  Eight waves share
 // 64 rows, MH sets of them a part of the rows each, and take groups of 32 channels in turn; blockIdx.y: a part of the channels (`part_n`).
 // The weights, which every workgroup reads and the level-2 caches hold, come in steps of 128 bytes of k of a group's channels (k up to 64: one step, to the registers), past the registers to a ring of D steps in LDS that is the wave's own: no barrier, and eight lanes read
 // 128 bytes of a row together (read as the matrix instruction wants them, no two lanes do, and a quarter of the cache's rate
@@ -710,7 +710,8 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
     // (the scales of the rows: in the first wave's last step until it is read into)
     float *const scales = reinterpret_cast<float *>(ring[0] + (RING ? D - 1 : 0) * STEP);
     const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6);
-    const int m0 = int(blockIdx.x) * BM, r = lane & 15, g = lane >> 4, steps = (p.k + 64 * HALVES - 1) / (64 * HALVES);
+    const int m0 = int(blockIdx.x) * BM, r = lane & 15, g = lane >> 4;
+    const int steps = (p.k + 64 * HALVES - 1) / (64 * HALVES), rest = p.k % (64 * HALVES);
     int n0 = int(blockIdx.y) * part_n + wave % WN * 32;
     const int n_end = min(p.n, int(blockIdx.y + 1) * part_n), upper = wave / WN * (MT * 16);
 
@@ -729,7 +730,7 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
         for (int i = 0; i < L; ++i) {
             const int row = i * AT_ONCE + lane / ROW, col = (lane % ROW ^ key(row)) * 16;
             off[i] = uint32_t(min(row, p.n - 1 - next_n)) * uint32_t(p.ldb) + uint32_t(col);
-            end[i] = HALVES == 2 && p.k % 128 != 0 && col >= 64 ? kNowhere : off[i];         // (in a last step of 64 bytes)
+            end[i] = rest && col >= rest ? kNowhere : off[i];                // (in the last step)
         }
     };
     auto issue = [&]() {
@@ -749,10 +750,11 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
         }
     };
     v4i vb[NT];
+    const int piece = g * 16 < p.k ? g * 16 : 0;         // (behind k the activations are zeros)
     auto fetch = [&](int n0) {                           // (one step: to the registers)
 #pragma unroll
         for (int j = 0; j < NT; ++j)
-            __builtin_memcpy(&vb[j], p.b + int64_t(min(n0 + Deal<Y>::row(j, r), p.n - 1)) * p.ldb + g * 16, 16);
+            __builtin_memcpy(&vb[j], p.b + int64_t(min(n0 + Deal<Y>::row(j, r), p.n - 1)) * p.ldb + piece, 16);
     };
     auto start = [&]() {
         if constexpr (!RING) {
@@ -852,7 +854,7 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
     }
 }
 
-// Short rows that end inside a step, or channels inside a store, or weights whose rows do not begin at multiples of 16 bytes: four waves, 32 rows,
+// Short rows that end inside a piece, or channels inside a store, or weights whose rows do not begin at multiples of 16 bytes: four waves, 32 rows,
 // the weights go to the registers directly, all KS steps of the first channels before the activations are waited for.
 template <typename T, typename Y, int KS>
 __global__ void __launch_bounds__(256, KS <= 2 ? 4 : 2)
@@ -1211,7 +1213,7 @@ int launch_rows(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
 template <typename T, int KS>
 int launch_thin_steps(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
 {
-    const bool exact = p.k > 0 && p.k % 64 == 0 && p.n % 8 == 0 && rows_at_16(p.b, p.ldb);
+    const bool exact = p.k > 0 && p.k % 16 == 0 && p.n % 8 == 0 && rows_at_16(p.b, p.ldb);
     const bool narrow = p.n <= 128;                      // half of the waves would have no channels: they take half of the rows
     const int rows = exact ? 64 : 32, channels = exact && !narrow ? 256 : 128;
     const int64_t tiles = (int64_t(p.m) + rows - 1) / rows, groups = (int64_t(p.n) + channels - 1) / channels;

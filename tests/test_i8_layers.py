@@ -246,6 +246,14 @@ def test_lengths_that_end_inside_a_stage(m, n, k, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k", [16, 32, 48, 80, 96, 112, 144, 176, 208, 240, 272, 336, 400, 432, 496])
+def test_short_rows_of_whole_pieces(k, dtype):
+    for m, n in ((17, 8), (64, 136), (130, 520)):
+        test_lengths_that_end_inside_a_stage(m, n, k, dtype)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("m,n,k", [(7900, 4000, 592), (7900, 4000, 585), (5000, 1030, 1040), (90_000, 72, 560), (40_000, 200, 320), (20_000, 264, 448)])
 def test_many_tiles(m, n, k):
     """Products whose tiles fill the card, against 64 bits on the card."""
