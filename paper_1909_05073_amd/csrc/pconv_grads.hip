@@ -5,9 +5,10 @@
 // tensors' addresses in its arguments, so a step needs no table in device memory.  The tensors are cut into chunks; the workgroups
 // of the first pass take every gridDim-th chunk, those of the second one chunk each.
 //
-// Elements that fit the caches beside their outputs are left there.  Of more, the first pass reads past the caches all but the last 192 MB, which the
-// second pass, from the last chunk to the first, finds in the 256 MB memory-side cache; its stores pass the caches too.  138 million fp32
-// elements: first pass 87 us (6.4 TB/s; 129 where the caches were left full of outputs), second 186 us (206 with nothing kept).
+// Up to 128 MB of elements and outputs are left in the caches (87 MB 25.9 us, 28 with stores past them; 216 MB 73 and 60).  Of
+// more, the first pass reads past the caches all but the last 192 MB, which the second pass, from the last chunk to the first,
+// finds in the 256 MB memory-side cache; its stores pass the caches too.  138 million fp32 elements: first pass 87 us (6.4 TB/s;
+// 129 where the caches were left full of outputs), second 186 us (206 with nothing kept).
 #include <hip/hip_runtime.h>
 
 #include "pconv_internal.h"

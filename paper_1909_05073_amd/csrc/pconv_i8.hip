@@ -1134,12 +1134,17 @@ int launch_quantize_rows(const void *x, int64_t ldx, int bf16, int64_t rows, int
     // Activations that are read once and are more than a part of the caches are read past them, so that they do not push out what the product reads
     // (8992x9184 -> 280: 143 us without, 133).
     const bool passing = rows * cols * (bf16 ? 2 : 4) > int64_t(64) << 20;
+    // Many rows: two a wave, or one with eight vectors a lane, so that more of them is under way (66 vectors, 100000 bf16 rows 59.7 us by a wave
+    // each and 38.4 so, 1000 rows 3.2 and 3.6; 288 vectors, 50000 fp32 rows 76.1 us by 256 threads and 49.7 by a wave, 1000 rows 3.8 and 4.4).
     // (1024 threads for a row of 1244 vectors: 7962 rows 107 us, with 256 55; 300 rows 7.8 and 5.5; of 2296: 8992 rows 116 and 94)
     if (vecs <= 8) PCONV_LAUNCH(8, 1, 256);
     else if (vecs <= 16) PCONV_LAUNCH(16, 1, 256);
     else if (vecs <= 32) PCONV_LAUNCH(16, 2, 256);
     else if (vecs <= 64) PCONV_LAUNCH(16, 4, 256);
+    else if (vecs <= 128 && rows > 4096) PCONV_LAUNCH(32, 4, 256);
+    else if (vecs <= 128) PCONV_LAUNCH(64, 2, 256);
     else if (vecs <= 256) PCONV_LAUNCH(64, 4, 256);
+    else if (vecs <= 512 && rows > 8192) PCONV_LAUNCH(64, 8, 256);
     else if (vecs <= 512) PCONV_LAUNCH(256, 2, 256);
     else if (vecs <= 1024) PCONV_LAUNCH(256, 4, 256);
     else if (vecs <= 2048 && rows >= 128) PCONV_LAUNCH(256, 8, 256);

@@ -64,7 +64,7 @@ struct Grads {
     int64_t tables() const { return (num + kGradTensors - 1) / kGradTensors; }
 };
 
-constexpr int64_t kKeptBytes = int64_t(192) << 20, kCachedBytes = int64_t(256) << 20;
+constexpr int64_t kKeptBytes = int64_t(192) << 20, kCachedBytes = int64_t(128) << 20;
 
 Grads grads_of(const void *const *in, void *const *out, const int64_t *counts, const int32_t *types, const int32_t *out_types, int64_t num)
 {
