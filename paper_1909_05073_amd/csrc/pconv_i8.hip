@@ -635,7 +635,8 @@ matmul_i8_join_kernel(const I8Product p, int splits, const int *__restrict__ par
 
 // Short rows (k up to kThinK): all of k of BM rows of activations lies in LDS, so that there is no loop of stages and one read of the
 // activations; where they come as floats they are quantised on their way there and never leave the chip.
-constexpr int kThinK = 512;
+constexpr int kThinK = 512, kThinLongK = 2048;           // (quantised within the product, and where thin_long() says so)
+constexpr int thin_rows(int ks) { return ks <= 16 ? 64 : 32; }           // rows of a workgroup in whole pieces
 
 // LDS holds rows of PIECES times 16 bytes, whose order makes the 16 lanes that are read at once differ in their places modulo 256 bytes.
 template <int KS> struct ThinLds {
@@ -659,7 +660,7 @@ template <typename T, int KS, int W, int BM> struct ThinRows {
         }
     }
 
-    static __device__ __forceinline__ void store(const Vec<T> (&v)[PASSES][KEEP], int wave, int lane, v4i *lds, float *scales)
+    static __device__ __forceinline__ void store(const Vec<T> (&v)[PASSES][KEEP], int k, int wave, int lane, v4i *lds, float *scales)
     {
 #pragma unroll
         for (int i = 0; i < PASSES; ++i) {
@@ -671,6 +672,7 @@ template <typename T, int KS, int W, int BM> struct ThinRows {
             if (lane % LANES == 0) scales[row] = s.scale;
 #pragma unroll
             for (int q = 0; q < KEEP; ++q) {
+                if (KS > 8 && q * LANES * N >= (k + 127) / 128 * 128) continue;            // (behind the last step)
                 const int byte = (q * LANES + lane % LANES) * N;
                 uint32_t w[N / 4];
                 quantize_vec(v[i][q], s, w);
@@ -701,9 +703,9 @@ template <typename T, typename Y, int KS, int MH>
 __global__ void __launch_bounds__(512, KS <= 4 ? 4 : 2)
 linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, int part_n)
 {
-    constexpr int W = 8, BM = 64, MT = 4 / MH, NT = 2, WN = W / MH, HALVES = KS == 1 ? 1 : 2, ROW = 4 * HALVES, STEP = 32 * ROW;
+    constexpr int W = 8, BM = thin_rows(KS), MT = BM / 16 / MH, NT = 2, WN = W / MH, HALVES = KS == 1 ? 1 : 2, ROW = 4 * HALVES, STEP = 32 * ROW;
     constexpr bool RING = KS > 1;
-    constexpr int D = KS == 8 ? 3 : RING ? 2 : 1, L = STEP / 64;         // (two workgroups a compute unit but for KS = 8)
+    constexpr int D = KS >= 8 ? 3 : RING ? 2 : 1, L = STEP / 64;         // (two workgroups a compute unit but for KS from 8)
     constexpr int AT_ONCE = 64 / ROW;                    // rows of a step that a load brings
     __shared__ v4i lds[BM * ThinLds<KS>::PIECES];
     __shared__ v4i ring[RING ? W : 1][RING ? D * STEP : 16];
@@ -785,7 +787,7 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
         Vec<T> v[ThinRows<T, KS, W, BM>::PASSES][ThinRows<T, KS, W, BM>::KEEP];
         ThinRows<T, KS, W, BM>::template load<true>(x, ldx, m0, p.m, p.k, wave, lane, v);
         start();
-        ThinRows<T, KS, W, BM>::store(v, wave, lane, lds, scales);
+        ThinRows<T, KS, W, BM>::store(v, p.k, wave, lane, lds, scales);
     }
     Channels ch[NT];
     if (n0 < n_end) load_channels<Y, NT, true>(p, n0, g, ch);
@@ -918,7 +920,7 @@ linear_i8_thin_ragged_kernel(const I8Product p, const T *__restrict__ x, int64_t
         Vec<T> v[ThinRows<T, KS, W, BM>::PASSES][ThinRows<T, KS, W, BM>::KEEP];
         ThinRows<T, KS, W, BM>::template load<false>(x, ldx, m0, p.m, p.k, wave, lane, v);
         fetch(n0);
-        ThinRows<T, KS, W, BM>::store(v, wave, lane, lds, scales);
+        ThinRows<T, KS, W, BM>::store(v, p.k, wave, lane, lds, scales);
     }
     __syncthreads();
     float sa[MT];
@@ -1220,10 +1222,10 @@ int launch_thin_steps(const I8Product &p, const T *x, int64_t ldx, hipStream_t s
 {
     const bool exact = p.k > 0 && p.k % 16 == 0 && p.n % 8 == 0 && rows_at_16(p.b, p.ldb);
     const bool narrow = p.n <= 128;                      // half of the waves would have no channels: they take half of the rows
-    const int rows = exact ? 64 : 32, channels = exact && !narrow ? 256 : 128;
+    const int rows = exact ? thin_rows(KS) : 32, channels = exact && !narrow ? 256 : 128;
     const int64_t tiles = (int64_t(p.m) + rows - 1) / rows, groups = (int64_t(p.n) + channels - 1) / channels;
     // (every part quantises the rows again: no more of them than make 512 workgroups)
-    const int64_t parts = std::min<int64_t>(groups, std::max<int64_t>(1, 512 / tiles));
+    const int64_t parts = std::min<int64_t>(groups, std::max<int64_t>(1, (KS <= 8 ? 512 : 256) / tiles));
     const int part_n = int((groups + parts - 1) / parts * channels);
     if (tiles >= int64_t(1) << 23) { set_error("pconv_matmul_i8: too many workgroups"); return PCONV_UNSUPPORTED; }
     const dim3 grid(unsigned(tiles), unsigned((int64_t(p.n) + part_n - 1) / part_n));
@@ -1231,7 +1233,7 @@ int launch_thin_steps(const I8Product &p, const T *x, int64_t ldx, hipStream_t s
     do {                                                                                                                       \
         if (exact && narrow) hipLaunchKernelGGL((linear_i8_thin_kernel<T, Y, KS, 2>), grid, dim3(512), 0, st, p, x, ldx, part_n); \
         else if (exact) hipLaunchKernelGGL((linear_i8_thin_kernel<T, Y, KS, 1>), grid, dim3(512), 0, st, p, x, ldx, part_n);   \
-        else hipLaunchKernelGGL((linear_i8_thin_ragged_kernel<T, Y, KS>), grid, dim3(256), 0, st, p, x, ldx, part_n);          \
+        else if constexpr (KS <= 8) hipLaunchKernelGGL((linear_i8_thin_ragged_kernel<T, Y, KS>), grid, dim3(256), 0, st, p, x, ldx, part_n); \
     } while (0)
     if (p.y_bf16) PCONV_LAUNCH(__bf16); else PCONV_LAUNCH(float);
 #undef PCONV_LAUNCH
@@ -1244,7 +1246,9 @@ int launch_thin(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
     if (p.k <= 64) return launch_thin_steps<T, 1>(p, x, ldx, st);
     if (p.k <= 128) return launch_thin_steps<T, 2>(p, x, ldx, st);
     if (p.k <= 256) return launch_thin_steps<T, 4>(p, x, ldx, st);
-    return launch_thin_steps<T, 8>(p, x, ldx, st);
+    if (p.k <= 512) return launch_thin_steps<T, 8>(p, x, ldx, st);
+    if constexpr (sizeof(T) > 1) return p.k <= 1024 ? launch_thin_steps<T, 16>(p, x, ldx, st) : launch_thin_steps<T, 32>(p, x, ldx, st);
+    return PCONV_UNSUPPORTED;                            // (quantised rows of that length go in tiles)
 }
 
 }  // namespace
@@ -1254,7 +1258,20 @@ int launch_thin(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
 static bool few(int64_t m, int64_t k) { return m <= kRowsM && m * k <= kRowsMost; }
 static bool thin(int64_t m, int64_t k) { return m > kRowsM && k <= kThinK; }
 
-bool linear_i8_fused(int64_t m, int64_t, int64_t k) { return m <= kRowsM ? m * k <= kFusedRows : thin(m, k); }
+// Rows of up to kThinLongK in whole pieces, quantised within the product as short rows are: one launch, no work space (4.9 us less on the
+// host).  The loads, the quantising and the products of a workgroup follow each other and no other one is there to fill in, so that is
+// right for few rounds of workgroups only: 1000x1024 -> 256 fp32 12.8 us, apart 15.3 (the GPU's part 13.0 and 9.9); 16000x768 -> 256 bf16 15 and 22; 50000x1024 -> 256
+// fp32 86 and 71; above 1024 with 32 rows a workgroup 4000x1536 -> 512 bf16 15 and 18.6, 16000x1536 -> 1024 fp32 73 and 57.
+static bool thin_long(int64_t m, int64_t n, int64_t k, bool b_at_16)
+{
+    if (m <= kRowsM || k <= kThinK || k > kThinLongK || k % 16 != 0 || n % 8 != 0 || n > 2048 || !b_at_16) return false;
+    return k <= 1024 ? m <= kUnits * 64 : (m + 31) / 32 * ((n + 255) / 256) <= 2 * kUnits;
+}
+
+bool linear_i8_fused(int64_t m, int64_t n, int64_t k, bool b_at_16)
+{
+    return m <= kRowsM ? m * k <= kFusedRows : thin(m, k) || thin_long(m, n, k, b_at_16);
+}
 
 int launch_linear_i8_fused(const I8Product &p, const void *x, int64_t ldx, int bf16, void *stream)
 {

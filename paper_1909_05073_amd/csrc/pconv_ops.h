@@ -27,7 +27,7 @@ bool rows_at_16(const int8_t *at, int64_t ld);
 int64_t matmul_i8_work_bytes(int64_t m, int64_t n, int64_t k, bool a_at_16, bool b_at_16);
 int launch_matmul_i8(const I8Product &p, void *work, void *stream);
 // Whether rows are so few or so short that they are quantised within the product, and that product (p.a, lda, sa unused).
-bool linear_i8_fused(int64_t m, int64_t n, int64_t k);
+bool linear_i8_fused(int64_t m, int64_t n, int64_t k, bool b_at_16);
 int launch_linear_i8_fused(const I8Product &p, const void *x, int64_t ldx, int bf16, void *stream);
 
 // Up to kGradTensors tensors travel in the arguments of one launch (4 KiB), cut into chunks of 1 << `log2` elements.

@@ -196,7 +196,7 @@ int pconv_matmul_i8(const int8_t *a_dev, int64_t a_stride, const float *a_scale,
 
 int64_t pconv_linear_i8_workspace(int64_t m, int64_t n, int64_t k, int rows_at_16)
 {
-    return sizes_fit(m, n, k) && !linear_i8_fused(m, n, k) ? round16(4 * m) + m * round16(k) + matmul_i8_work_bytes(m, n, k, true, rows_at_16 != 0) : 0;
+    return sizes_fit(m, n, k) && !linear_i8_fused(m, n, k, rows_at_16 != 0) ? round16(4 * m) + m * round16(k) + matmul_i8_work_bytes(m, n, k, true, rows_at_16 != 0) : 0;
 }
 
 int pconv_linear_i8(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, const int8_t *w_dev, int64_t w_stride,
@@ -211,7 +211,7 @@ int pconv_linear_i8(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, co
     if (k && !x_dev) return invalid(who, "null pointer argument");
     if (!stride_fits(m, k, x_stride)) return invalid(who, "rows must lie at least their length apart");
     if (const int rc = check_work(who, work, work_bytes, pconv_linear_i8_workspace(m, n, k, rows_at_16(w_dev, w_stride)))) return rc;
-    if (linear_i8_fused(m, n, k)) return launch_linear_i8_fused(p, x_dev, x_stride, x_dtype == PCONV_BF16, hip_stream);
+    if (linear_i8_fused(m, n, k, rows_at_16(w_dev, w_stride))) return launch_linear_i8_fused(p, x_dev, x_stride, x_dtype == PCONV_BF16, hip_stream);
     float *const scale = static_cast<float *>(work);
     int8_t *const q = static_cast<int8_t *>(work) + round16(4 * m);
     const int64_t ldq = round16(k);
