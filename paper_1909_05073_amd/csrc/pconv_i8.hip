@@ -221,20 +221,66 @@ __device__ __forceinline__ uint32_t most_of_lanes(uint32_t v)
     return v;
 }
 
+// 16 bytes of a row that has `len` bytes, from `at` on; beyond its end zero.
+template <bool EXACT = false>
+__device__ __forceinline__ v4i load16(const int8_t *row, int at, int len)
+{
+    v4i v = {0, 0, 0, 0};
+    if (__builtin_expect(at + 16 <= len, 1)) __builtin_memcpy(&v, row + at, 16);
+    else if (!EXACT && __builtin_expect(at < len, 0)) v = load_end(row, at, len);
+    return v;
+}
+
+// 16 bytes at an address of any alignment, as the five words that hold them.  (A load of 16 bytes that is not aligned to a word takes 2.6 times one that
+// is: 6x17360 -> 562 31 us and 16.)  No word is read that holds none of the bytes.
+__device__ __forceinline__ v4i load16_loose(const int8_t *p)
+{
+    const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p)) & 3u;
+    const int8_t *const q = p - off;
+    typedef v4i Words __attribute__((aligned(4)));
+    const v4i w = *reinterpret_cast<const Words *>(q);
+    const uint32_t last = *reinterpret_cast<const uint32_t *>(q + (off ? 16 : 12));
+    v4i v;
+    v[0] = int(__builtin_amdgcn_alignbyte(uint32_t(w[1]), uint32_t(w[0]), off));
+    v[1] = int(__builtin_amdgcn_alignbyte(uint32_t(w[2]), uint32_t(w[1]), off));
+    v[2] = int(__builtin_amdgcn_alignbyte(uint32_t(w[3]), uint32_t(w[2]), off));
+    v[3] = int(__builtin_amdgcn_alignbyte(last, uint32_t(w[3]), off));
+    return v;
+}
+
+// Rows to multiples of 16 bytes, zeros behind their ends, by `threads` threads.
+__device__ __forceinline__ void realign(const Realign &a, int64_t thread, int64_t threads)
+{
+    const int64_t all = int64_t(a.rows) * a.pieces;
+#pragma unroll 1
+    for (int64_t t = thread; t < all; t += threads) {
+        const int64_t row = t / a.pieces;
+        const int at = int(t - row * a.pieces) * 16;
+        const int8_t *from = a.from + row * a.ld;
+        const v4i v = at + 16 <= a.k ? load16_loose(from + at) : load16(from, at, a.k);
+        __builtin_memcpy(a.to + t * 16, &v, 16);
+    }
+}
+
 // TPR threads of a workgroup share a row; each keeps its first KEEP vectors of 16 bytes in registers between finding the
 // row's scale and quantising, and reads what lies beyond (from a cache) twice.  [cols, q_cols) is filled with zeros.
+// The workgroups from `blocks` on bring the rows of a product's weights to multiples of 16 bytes meanwhile (a launch less).
 // Code that runs is kept short: a launch of one wave's work a SIMD spends its time on fetching instructions.  Bound by memory: 8192x4096
 // bf16 20 us, 5.0 TB/s.
 template <typename T, int TPR, int KEEP, int THREADS, bool PASSING>
 __global__ void __launch_bounds__(THREADS)
 quantize_rows_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int64_t cols, int8_t *__restrict__ q, int64_t ldq,
-                     int64_t q_cols, float *__restrict__ scale)
+                     int64_t q_cols, float *__restrict__ scale, unsigned blocks, const Realign weights)
 {
     constexpr int N = Vec<T>::N, RPW = THREADS / TPR;
     __shared__ uint32_t lds[THREADS / 64];
+    if (__builtin_expect(blockIdx.x >= blocks, 0)) {
+        realign(weights, int64_t(blockIdx.x - blocks) * THREADS + threadIdx.x, int64_t(gridDim.x - blocks) * THREADS);
+        return;
+    }
     const int sub = int(threadIdx.x) % TPR;
     const int64_t groups = (rows + RPW - 1) / RPW;
-    for (int64_t g = blockIdx.x; g < groups; g += gridDim.x) {
+    for (int64_t g = blockIdx.x; g < groups; g += blocks) {
         const int64_t r = g * RPW + int(threadIdx.x) / TPR;
         const bool live = r < rows;
         const T *row = x + (live ? r : rows - 1) * ldx;
@@ -266,35 +312,8 @@ quantize_rows_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int64_t
 
 // ---- the product --------------------------------------------------------------------------------------------------------
 
-// 16 bytes of a row that has `len` bytes, from `at` on; beyond its end zero.
-template <bool EXACT = false>
-__device__ __forceinline__ v4i load16(const int8_t *row, int at, int len)
-{
-    v4i v = {0, 0, 0, 0};
-    if (__builtin_expect(at + 16 <= len, 1)) __builtin_memcpy(&v, row + at, 16);
-    else if (!EXACT && __builtin_expect(at < len, 0)) v = load_end(row, at, len);
-    return v;
-}
-
 // Four neighbouring channels of one row of y, from n on.  ReLU keeps NaN.
 struct Channels { f4 scale, bias; };
-
-// 16 bytes at an address of any alignment, as the five words that hold them.  (A load of 16 bytes that is not aligned to a word takes 2.6 times one that
-// is: 6x17360 -> 562 31 us and 16.)  No word is read that holds none of the bytes.
-__device__ __forceinline__ v4i load16_loose(const int8_t *p)
-{
-    const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p)) & 3u;
-    const int8_t *const q = p - off;
-    typedef v4i Words __attribute__((aligned(4)));
-    const v4i w = *reinterpret_cast<const Words *>(q);
-    const uint32_t last = *reinterpret_cast<const uint32_t *>(q + (off ? 16 : 12));
-    v4i v;
-    v[0] = int(__builtin_amdgcn_alignbyte(uint32_t(w[1]), uint32_t(w[0]), off));
-    v[1] = int(__builtin_amdgcn_alignbyte(uint32_t(w[2]), uint32_t(w[1]), off));
-    v[2] = int(__builtin_amdgcn_alignbyte(uint32_t(w[3]), uint32_t(w[2]), off));
-    v[3] = int(__builtin_amdgcn_alignbyte(last, uint32_t(w[3]), off));
-    return v;
-}
 
 __device__ __forceinline__ bool rows_at_words(const int8_t *p, int64_t ld) { return ((reinterpret_cast<uintptr_t>(p) | uint64_t(ld)) & 3u) == 0; }
 
@@ -598,19 +617,11 @@ matmul_i8_kernel(const I8Product p, int splits, int *part)
     store_tile<Y, MT, NT>(p, m, n0 + wn, g, acc, sa, c);
 }
 
-// Rows to multiples of 16 bytes, zeros behind their ends; blockIdx.y: which of two matrices.
-struct Realign { const int8_t *from[2]; int8_t *to[2]; int64_t ld[2]; int rows[2]; int k, pieces; };
-
+// Rows of one or two matrices to multiples of 16 bytes (blockIdx.y: which).  777x1155 and 1001x1155: 3.9 us.
 __global__ void __launch_bounds__(256)
-realign_kernel(const Realign a)
+realign_kernel(const Realign a0, const Realign a1)
 {
-    const int i = int(blockIdx.y);
-    const int64_t all = int64_t(a.rows[i]) * a.pieces;
-    for (int64_t t = int64_t(blockIdx.x) * 256 + threadIdx.x; t < all; t += int64_t(gridDim.x) * 256) {
-        const int64_t row = t / a.pieces;
-        const v4i v = load16(a.from[i] + row * a.ld[i], int(t - row * a.pieces) * 16, a.k);
-        __builtin_memcpy(a.to[i] + t * 16, &v, 16);
-    }
+    realign(blockIdx.y ? a1 : a0, int64_t(blockIdx.x) * 256 + threadIdx.x, int64_t(gridDim.x) * 256);
 }
 
 // y of the sums of `splits` parts of k; a thread has four channels.
@@ -1119,16 +1130,19 @@ linear_i8_rows_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx)
 }  // namespace
 
 int launch_quantize_rows(const void *x, int64_t ldx, int bf16, int64_t rows, int64_t cols, int8_t *q, int64_t ldq,
-                         int64_t q_cols, float *scale, void *stream)
+                         int64_t q_cols, float *scale, void *stream, const Realign *weights)
 {
     const hipStream_t st = static_cast<hipStream_t>(stream);
     const int64_t vecs = (q_cols + (bf16 ? 7 : 3)) / (bf16 ? 8 : 4);
+    const Realign other = weights ? *weights : Realign{};
+    const int64_t pieces = int64_t(other.rows) * other.pieces;
 #define PCONV_LAUNCH_AS(T, TPR, KEEP, THREADS, PASSING)                                                                        \
-    hipLaunchKernelGGL((quantize_rows_kernel<T, TPR, KEEP, THREADS, PASSING>), dim3(grid), dim3(THREADS), 0, st,               \
-                       static_cast<const T *>(x), ldx, rows, cols, q, ldq, q_cols, scale)
+    hipLaunchKernelGGL((quantize_rows_kernel<T, TPR, KEEP, THREADS, PASSING>), dim3(grid + more), dim3(THREADS), 0, st,        \
+                       static_cast<const T *>(x), ldx, rows, cols, q, ldq, q_cols, scale, grid, other)
 #define PCONV_LAUNCH(TPR, KEEP, THREADS)                                                                                       \
     do {                                                                                                                       \
         const unsigned grid = unsigned(std::min<int64_t>((rows + (THREADS / TPR) - 1) / (THREADS / TPR), 1 << 20));            \
+        const unsigned more = unsigned(std::min<int64_t>((pieces + THREADS - 1) / THREADS, 1 << 16));                          \
         const bool once = passing && vecs <= TPR * KEEP;                                                                       \
         if (bf16) { if (once) PCONV_LAUNCH_AS(__bf16, TPR, KEEP, THREADS, true); else PCONV_LAUNCH_AS(__bf16, TPR, KEEP, THREADS, false); } \
         else { if (once) PCONV_LAUNCH_AS(float, TPR, KEEP, THREADS, true); else PCONV_LAUNCH_AS(float, TPR, KEEP, THREADS, false); } \
@@ -1280,9 +1294,13 @@ int launch_linear_i8_fused(const I8Product &p, const void *x, int64_t ldx, int b
     return bf16 ? launch_thin(p, static_cast<const __bf16 *>(x), ldx, st) : launch_thin(p, static_cast<const float *>(x), ldx, st);
 }
 
+bool matmul_i8_aligns(int64_t m, int64_t k) { return !few(m, k) && !thin(m, k); }
+
+Realign realigned(const int8_t *from, int64_t ld, int rows, int k, int8_t *to) { return Realign{from, to, ld, rows, k, (k + 15) / 16}; }
+
 int64_t matmul_i8_work_bytes(int64_t m, int64_t n, int64_t k, bool a_at_16, bool b_at_16)
 {
-    if (few(m, k) || thin(m, k)) return 0;
+    if (!matmul_i8_aligns(m, k)) return 0;
     const Cut c = cut_of(m, n, k);
     const int64_t row = (k + 15) / 16 * 16;
     return (a_at_16 ? 0 : m * row) + (b_at_16 ? 0 : n * row) + (c.splits > 1 ? c.splits * m * ((n + 3) / 4 * 4) * 4 : 0);
@@ -1298,21 +1316,20 @@ int launch_matmul_i8(const I8Product &product, void *work, void *stream)
     const int64_t tiles = ((int64_t(p.m) + kTileM[c.tile] - 1) / kTileM[c.tile]) * ((int64_t(p.n) + kTileN[c.tile] - 1) / kTileN[c.tile]);
     if (tiles * c.splits >= int64_t(1) << 23) { set_error("pconv_matmul_i8: too many workgroups"); return PCONV_UNSUPPORTED; }
     int8_t *at = static_cast<int8_t *>(work);
-    Realign r{};
-    r.k = p.k; r.pieces = (p.k + 15) / 16;
-    unsigned moved = 0;
+    Realign moved[2] = {};
+    unsigned count = 0;
     const auto move = [&](const int8_t *&from, int64_t &ld, int rows) {
         if (rows_at_16(from, ld)) return;
-        r.from[moved] = from; r.to[moved] = at; r.ld[moved] = ld; r.rows[moved] = rows;
-        ++moved;
-        from = at; ld = int64_t(r.pieces) * 16;
+        moved[count] = realigned(from, ld, rows, p.k, at);
+        from = at;
+        ld = int64_t(moved[count++].pieces) * 16;
         at += rows * ld;
     };
     move(p.a, p.lda, p.m);
     move(p.b, p.ldb, p.n);
-    if (moved) {
-        const int64_t most = int64_t(std::max(r.rows[0], r.rows[1])) * r.pieces;
-        hipLaunchKernelGGL(realign_kernel, dim3(unsigned(std::min<int64_t>((most + 255) / 256, 1 << 16)), moved), dim3(256), 0, st, r);
+    if (count) {
+        const int64_t most = int64_t(std::max(moved[0].rows, moved[1].rows)) * moved[0].pieces;
+        hipLaunchKernelGGL(realign_kernel, dim3(unsigned(std::min<int64_t>((most + 255) / 256, 1 << 16)), count), dim3(256), 0, st, moved[0], moved[1]);
         if (const int rc = check_launch("pconv_matmul_i8 (aligning rows)")) return rc;
     }
     int *const sums = reinterpret_cast<int *>(at);

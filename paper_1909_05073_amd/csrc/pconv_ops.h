@@ -18,13 +18,23 @@ struct I8Product {
     int relu, y_bf16;
 };
 
-// Launchers: arguments checked, sizes not 0.  They return a pconv_status.
+// Rows that begin anywhere, and where they go: rows of `pieces` times 16 bytes, one behind the other.
+struct Realign {
+    const int8_t *from;
+    int8_t *to;
+    int64_t ld;
+    int rows, k, pieces;
+};
+
+// Launchers: arguments checked, sizes not 0.  They return a pconv_status.  `weights` are brought to multiples of 16 bytes by the same launch.
 int launch_quantize_rows(const void *x, int64_t ldx, int bf16, int64_t rows, int64_t cols, int8_t *q, int64_t ldq,
-                         int64_t q_cols, float *scale, void *stream);
+                         int64_t q_cols, float *scale, void *stream, const Realign *weights = nullptr);
 // Whether rows begin at multiples of 16 bytes (and a tile's lie within 32 bits); the work space of a product (copies of
 // operands whose rows do not, sums of parts of k), and the product.
 bool rows_at_16(const int8_t *at, int64_t ld);
 int64_t matmul_i8_work_bytes(int64_t m, int64_t n, int64_t k, bool a_at_16, bool b_at_16);
+bool matmul_i8_aligns(int64_t m, int64_t k);             // whether the product of those sizes reads such rows only
+Realign realigned(const int8_t *from, int64_t ld, int rows, int k, int8_t *to);
 int launch_matmul_i8(const I8Product &p, void *work, void *stream);
 // Whether rows are so few or so short that they are quantised within the product, and that product (p.a, lda, sa unused).
 bool linear_i8_fused(int64_t m, int64_t n, int64_t k, bool b_at_16);

@@ -215,9 +215,13 @@ int pconv_linear_i8(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, co
     float *const scale = static_cast<float *>(work);
     int8_t *const q = static_cast<int8_t *>(work) + round16(4 * m);
     const int64_t ldq = round16(k);
-    if (const int rc = launch_quantize_rows(x_dev, x_stride, x_dtype == PCONV_BF16, m, k, q, ldq, ldq, scale, hip_stream)) return rc;
+    int8_t *rest = q + m * ldq;
+    const bool align = !rows_at_16(w_dev, w_stride) && matmul_i8_aligns(m, k);
+    const Realign weights = align ? realigned(w_dev, w_stride, p.n, p.k, rest) : Realign{};
+    if (const int rc = launch_quantize_rows(x_dev, x_stride, x_dtype == PCONV_BF16, m, k, q, ldq, ldq, scale, hip_stream, align ? &weights : nullptr)) return rc;
     p.a = q; p.lda = ldq; p.sa = scale;
-    return launch_matmul_i8(p, q + m * ldq, hip_stream);
+    if (align) { p.b = rest; p.ldb = ldq; rest += n * ldq; }
+    return launch_matmul_i8(p, rest, hip_stream);
 }
 
 int64_t pconv_grad_workspace(int64_t num)
