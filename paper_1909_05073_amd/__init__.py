@@ -527,7 +527,7 @@ def _scratch(size: int, like):
     import torch
     if torch.cuda.is_current_stream_capturing() and not _graph_pool_serves(like.device):
         raise RuntimeError("the stream is being captured by others than torch: call the pconv_... function with work space of your own")
-    return like.new_empty(size, dtype=torch.uint8)
+    return torch.empty_strided((size,), (1,), dtype=torch.uint8, device=like.device)
 
 
 def _per_channel(t, n, what):
@@ -537,10 +537,19 @@ def _per_channel(t, n, what):
     return t.data_ptr() or None
 
 
-def _output(out, shape, dtype, like):
-    """(tensor, elements from row to row) for a result of that shape."""
+def _empty(lead, m, n, dtype, like):
+    """A new tensor [..., n] of m rows.  (For [m, n] by sizes and steps: 0.5 us less than by its shape.)"""
+    import torch
+    if len(lead) == 1:
+        return torch.empty_strided((m, n), (n or 1, 1), dtype=dtype, device=like.device)
+    return like.new_empty(lead + (n,), dtype=dtype)
+
+
+def _output(out, lead, m, n, dtype, like):
+    """(tensor, elements from row to row) for a result [..., n] of m rows."""
     if out is None:
-        return like.new_empty(shape, dtype=dtype), shape[-1]
+        return _empty(lead, m, n, dtype, like), n
+    shape = lead + (n,)
     if out.dtype != dtype or out.shape != shape:
         raise ValueError(f"out must be {dtype} of shape {tuple(shape)}")
     return out, _rows(out, "out")[2]
@@ -598,8 +607,8 @@ def quantize_rows(x):
     m, k, step = _rows(x, "x")
     lead = x.shape[:-1]
     wide = (k + 15) // 16 * 16
-    q = x.new_empty(lead + (wide,), dtype=torch.int8)
-    scale = x.new_empty(lead, dtype=torch.float32)
+    q = _empty(lead, m, wide, torch.int8, x)
+    scale = torch.empty_strided((m,), (1,), dtype=torch.float32, device=x.device) if len(lead) == 1 else x.new_empty(lead, dtype=torch.float32)
     rc = (_lib or lib()).pconv_quantize_rows(x.data_ptr() or None, step, dtype, m, k, q.data_ptr() or None, wide,
                                              scale.data_ptr() or None, _stream(index))
     if rc != OK:
@@ -621,7 +630,7 @@ def matmul_i8(a, a_scale, b, b_scale, bias=None, relu: bool = False, out_dtype=N
         raise ValueError("a and b must have rows of one length")
     if out_dtype is None:
         out_dtype = out.dtype if out is not None else torch.float32
-    y, y_step = _output(out, a.shape[:-1] + (n,), out_dtype, a)
+    y, y_step = _output(out, a.shape[:-1], m, n, out_dtype, a)
     y_type = _type_of(y, "out")
     sa, sb = _per_channel(a_scale, m, "a_scale"), _per_channel(b_scale, n, "b_scale")
     bp = _per_channel(bias, n, "bias") if bias is not None else None
@@ -651,9 +660,9 @@ def linear_i8(x, w, w_scale, bias=None, relu: bool = False, out_dtype=None, out=
     if k != kw:
         raise ValueError("x and w must have rows of one length")
     if out is None and out_dtype is None:
-        y, y_step, y_type = x.new_empty(x.shape[:-1] + (n,)), n, x_type
+        y, y_step, y_type = x.new_empty(m, n) if x.dim() == 2 else x.new_empty(x.shape[:-1] + (n,)), n, x_type
     else:
-        y, y_step = _output(out, x.shape[:-1] + (n,), out_dtype or out.dtype, x)
+        y, y_step = _output(out, x.shape[:-1], m, n, out_dtype or out.dtype, x)
         y_type = _type_of(y, "out")
     sw = _per_channel(w_scale, n, "w_scale")
     bp = _per_channel(bias, n, "bias") if bias is not None else None
@@ -750,10 +759,10 @@ class GradList:
         if self._num == 0:
             raise ValueError("the list is empty")
         like = self.grads[0]
-        if self._index != torch.cuda.current_device():
+        if self._index != _current_device():
             raise ValueError("the tensors' device must be the current one")
         work = _scratch(self._size, like)
-        return torch.empty((), dtype=torch.float32, device=like.device), work
+        return torch.empty_strided((), (), dtype=torch.float32, device=like.device), work
 
     def norm(self):
         """The 2-norm of all gradients together, a tensor of one fp32 number on their device."""

@@ -476,13 +476,13 @@ def c_calls():
         args[i] = 0
         a, sa, b, sb, y = args
         yield "null", lambda a=a, sa=sa, b=b, sb=sb, y=y: P.pconv_matmul_i8(a, 16, sa, b, 16, sb, 0, y, 4, "f32", 4, 4, 16)
-    need = P.pconv_linear_i8_workspace(400, 40, 1600, True)
-    assert need >= 400 * 1600
-    yield "work space", lambda: P.pconv_linear_i8(p, 1600, "f32", p, 1600, p, 0, p, 40, "f32", 400, 40, 1600, False, p, need - 1)
-    yield "work space", lambda: P.pconv_linear_i8(p, 1600, "f32", p, 1600, p, 0, p, 40, "f32", 400, 40, 1600, False, 0, need)
-    yield "work space", lambda: P.pconv_linear_i8(p, 1600, "f32", p, 1600, p, 0, p, 40, "f32", 400, 40, 1600, False, p + 8, need)
-    yield "null", lambda: P.pconv_linear_i8(0, 1600, "f32", p, 1600, p, 0, p, 40, "f32", 400, 40, 1600, False, p, need)
-    yield "apart", lambda: P.pconv_linear_i8(p, 1599, "f32", p, 1600, p, 0, p, 40, "f32", 400, 40, 1600, False, p, need)
+    need = P.pconv_linear_i8_workspace(400, 40, 2600, True)
+    assert need >= 400 * 2600
+    yield "work space", lambda: P.pconv_linear_i8(p, 2600, "f32", p, 2600, p, 0, p, 40, "f32", 400, 40, 2600, False, p, need - 1)
+    yield "work space", lambda: P.pconv_linear_i8(p, 2600, "f32", p, 2600, p, 0, p, 40, "f32", 400, 40, 2600, False, 0, need)
+    yield "work space", lambda: P.pconv_linear_i8(p, 2600, "f32", p, 2600, p, 0, p, 40, "f32", 400, 40, 2600, False, p + 8, need)
+    yield "null", lambda: P.pconv_linear_i8(0, 2600, "f32", p, 2600, p, 0, p, 40, "f32", 400, 40, 2600, False, p, need)
+    yield "apart", lambda: P.pconv_linear_i8(p, 1599, "f32", p, 2600, p, 0, p, 40, "f32", 400, 40, 2600, False, p, need)
 
 
 def test_c_entries_refuse_what_they_cannot_run():
