@@ -455,7 +455,8 @@ __device__ __forceinline__ void wait_for_stages(int behind)
 //
 // Stages go from memory to LDS past the registers, S - 1 of them ahead of the one that is multiplied; a wave waits for its own
 // loads of the next stage, and the barrier then tells it that everybody's are there and that the stage before is read.  In
-// the last stage the pieces behind the end of k are zeros; only where k ends inside a piece does that stage go through registers.
+// the last stage the pieces behind the end of k are zeros.  Where k ends inside a piece the piece is loaded whole (what lies behind it is
+// still before the next row, so the last rows of all go through registers), and the activations' part behind k is cleared in LDS.
 // Rows begin at multiples of 16 bytes (realign_kernel sees to it).
 //
 // `splits` workgroups share a tile, each with its part of k; their sums go to `part` [splits][m][n4], n4 = n rounded up to four.
@@ -518,23 +519,25 @@ matmul_i8_kernel(const I8Product p, int splits, int *part)
 
     const v4u at_a = buffer_at(p.a + int64_t(m0) * p.lda + k_begin), at_b = buffer_at(p.b + int64_t(n0) * p.ldb + k_begin);
     uint32_t off_a[PA], off_b[PB];
-    int col_a[PA], col_b[PB];                            // where a lane's piece begins in a stage
+    int end_a[PA], end_b[PB];                            // byte of a stage up to which a lane's piece is loaded only if k reaches behind it
 #pragma unroll
     for (int i = 0; i < PA; ++i) {
         const int row = (i * NW + wave) * 8 + (lane >> 3);
-        col_a[i] = ((lane & 7) ^ (row & 7)) * 16;
-        off_a[i] = uint32_t(min(row, p.m - 1 - m0)) * uint32_t(p.lda) + uint32_t(col_a[i]);
+        const int col = ((lane & 7) ^ (row & 7)) * 16;
+        end_a[i] = col + (m0 + row < p.m - 1 ? 0 : 15);
+        off_a[i] = uint32_t(min(row, p.m - 1 - m0)) * uint32_t(p.lda) + uint32_t(col);
     }
 #pragma unroll
     for (int i = 0; i < PB; ++i) {
         const int row = (i * NW + wave) * 8 + (lane >> 3);
-        col_b[i] = ((lane & 7) ^ key_b(row)) * 16;
-        off_b[i] = uint32_t(min(row, p.n - 1 - n0)) * uint32_t(p.ldb) + uint32_t(col_b[i]);
+        const int col = ((lane & 7) ^ key_b(row)) * 16;
+        end_b[i] = col + (n0 + row < p.n - 1 ? 0 : 15);
+        off_b[i] = uint32_t(min(row, p.n - 1 - n0)) * uint32_t(p.ldb) + uint32_t(col);
     }
     const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds)) + uint32_t(set) * uint32_t(STAGE * 16) + uint32_t(wave) * 1024u;
     // (written as assembly so that the compiler does not wait for these loads before every read of LDS)
     const int length = k_end - k_begin, whole = length / BK, rest = length % BK;
-    const int count = whole + (rest > 0 && rest % 16 == 0 ? 1 : 0);
+    const int count = whole + (rest > 0 ? 1 : 0);
     // stage `turn` of this set is stage turn * KG + set of all
     auto stage = [&](int turn) {
         const int s = turn * KG + set;
@@ -543,17 +546,17 @@ matmul_i8_kernel(const I8Product p, int splits, int *part)
 #pragma unroll
         for (int i = 0; i < PA; ++i)
             asm volatile("s_mov_b32 m0, %1\n s_nop 0\n buffer_load_dwordx4 %0, %2, %3 offen lds"
-                         ::"v"(col_a[i] < have ? off_a[i] : kNowhere), "s"(to + uint32_t(i * NW * 1024)), "s"(at_a), "s"(k0) : "memory");
+                         ::"v"(end_a[i] < have ? off_a[i] : kNowhere), "s"(to + uint32_t(i * NW * 1024)), "s"(at_a), "s"(k0) : "memory");
 #pragma unroll
         for (int i = 0; i < PB; ++i)
             asm volatile("s_mov_b32 m0, %1\n s_nop 0\n buffer_load_dwordx4 %0, %2, %3 offen lds"
-                         ::"v"(col_b[i] < have ? off_b[i] : kNowhere), "s"(to + uint32_t(BM * 128 + i * NW * 1024)), "s"(at_b), "s"(k0) : "memory");
+                         ::"v"(end_b[i] < have ? off_b[i] : kNowhere), "s"(to + uint32_t(BM * 128 + i * NW * 1024)), "s"(at_b), "s"(k0) : "memory");
     };
     constexpr int L = PA + PB;
     static_assert((S - 2) * L <= 63, "");
-    const int mine = (count - set + KG - 1) / KG;        // whole stages of this set (count >= 0, so at least 0)
-    const bool ragged = rest % 16 != 0;                  // k ends inside a piece: one more stage, through registers
-    const int all = count + (ragged ? 1 : 0), turns = (all + KG - 1) / KG;
+    const int mine = (count - set + KG - 1) / KG;        // stages of this set (count >= 0, so at least 0)
+    const bool ragged = rest % 16 != 0;                  // k ends inside a piece
+    const int turns = (count + KG - 1) / KG;
 #pragma unroll
     for (int t = 0; t < S - 1; ++t)
         if (t < mine) stage(t);
@@ -562,21 +565,26 @@ matmul_i8_kernel(const I8Product p, int splits, int *part)
         // the loads of this turn are done when at most those of the turns behind it are under way
         wait_for_stages<S - 2, L>(min(S - 2, max(0, mine - 1 - t)));
         if (t + S - 1 < mine) stage(t + S - 1);
-        const v4i *const st = lds + ((t % S) * KG + set) * STAGE;
-        if (ragged && t == count / KG) {
-            if (set == count % KG) {
-                v4i *const to = lds + ((t % S) * KG + set) * STAGE + wave * 64 + lane;
-#pragma unroll 1
-                for (int i = 0; i < PA + PB; ++i) {
-                    const bool b = i >= PA;
-                    const int at = ((b ? i - PA : i) * NW + wave) * 8 + (lane >> 3), key = b ? key_b(at) : at & 7;
-                    const int8_t *row = b ? p.b + int64_t(min(n0 + at, p.n - 1)) * p.ldb : p.a + int64_t(min(m0 + at, p.m - 1)) * p.lda;
-                    to[i * NW * 64] = load16(row, k_begin + whole * BK + ((lane & 7) ^ key) * 16, k_end);
+        v4i *const st = lds + ((t % S) * KG + set) * STAGE;
+        if (ragged && t == whole / KG) {
+            if (set == whole % KG) {
+                const int piece = rest / 16, at = k_begin + whole * BK + piece * 16;
+                for (int row = wave * 64 + lane; row < BM; row += NW * 64) {
+                    v4i v = st[row * 8 + (piece ^ (row & 7))];
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const int bits = max(0, min(32, (rest % 16 - 4 * w) * 8));
+                        v[w] &= int(uint32_t((uint64_t(1) << bits) - 1));
+                    }
+                    if (m0 + row >= p.m - 1) v = load16(p.a + int64_t(p.m - 1) * p.lda, at, k_end);
+                    st[row * 8 + (piece ^ (row & 7))] = v;
                 }
+                for (int row = wave * 64 + lane; row < BN; row += NW * 64)
+                    if (n0 + row >= p.n - 1) st[BM * 8 + row * 8 + (piece ^ key_b(row))] = load16(p.b + int64_t(p.n - 1) * p.ldb, at, k_end);
             }
             __syncthreads();
         }
-        if (KG == 1 || t * KG + set < all) multiply(st);
+        if (KG == 1 || t * KG + set < count) multiply(st);
     }
     if constexpr (KG > 1) {                              // the sets' sums come together
         __syncthreads();

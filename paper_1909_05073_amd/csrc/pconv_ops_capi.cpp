@@ -220,7 +220,7 @@ int pconv_linear_i8(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, co
     const Realign weights = align ? realigned(w_dev, w_stride, p.n, p.k, rest) : Realign{};
     if (const int rc = launch_quantize_rows(x_dev, x_stride, x_dtype == PCONV_BF16, m, k, q, ldq, ldq, scale, hip_stream, align ? &weights : nullptr)) return rc;
     p.a = q; p.lda = ldq; p.sa = scale;
-    if (align) { p.b = rest; p.ldb = ldq; rest += n * ldq; }
+    if (align) { p.b = rest; p.ldb = ldq; p.k = int(ldq); rest += n * ldq; }          // (zeros behind the ends of both)
     return launch_matmul_i8(p, rest, hip_stream);
 }
 

@@ -246,6 +246,31 @@ def test_lengths_that_end_inside_a_stage(m, n, k, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("k", [513, 527, 585, 641, 1023, 1155, 2050, 9001, 20013])
+def test_what_lies_behind_the_rows_does_not_count(k):
+    """Rows at multiples of 16 bytes whose last piece is not theirs alone; the last row ends with the memory."""
+    import torch
+    for m, n in ((17, 5), (32, 128), (33, 129), (64, 300), (130, 520), (1500, 700)):
+        if m * k > 2_000_000:
+            continue
+        say(f"[case] matmul_i8 {m}x{n}x{k}")
+        rng = np.random.default_rng(m * 10007 + n * 101 + k)
+        _, values = as_type(make_x(rng, m, k), "f32")
+        w, sb, bias = make_layer8(rng, n, k)
+        q, sa = plain_quantize(values)
+        want, bound = plain_product(q, sa, w, sb, bias, True)
+        rows = []
+        for t, byte in ((q.astype(np.int8), 99), (w, -101)):
+            step = (k + 15) // 16 * 16 + 16 * (m % 2)
+            flat = torch.full(((len(t) - 1) * step + k,), byte, dtype=torch.int8, device="cuda")
+            rows.append(flat.as_strided((len(t), k), (step, 1)))
+            rows[-1].copy_(dev(t))
+        check(P.matmul_i8(rows[0], dev(sa), rows[1], dev(sb), dev(bias), relu=True), want, bound, "matmul_i8")
+        x = dev(values.astype(np.float32))
+        check(P.linear_i8(x, rows[1], dev(sb), dev(bias), relu=True), want, bound, "linear_i8")
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("k", [16, 32, 48, 80, 96, 112, 144, 176, 208, 240, 272, 336, 400, 432, 496])
 def test_short_rows_of_whole_pieces(k, dtype):
