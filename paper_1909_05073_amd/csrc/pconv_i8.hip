@@ -462,7 +462,7 @@ __device__ __forceinline__ void wait_for_stages(int behind)
 // `splits` workgroups share a tile, each with its part of k; their sums go to `part` [splits][m][n4], n4 = n rounded up to four.
 //
 // Bound by the matrix units and the clock that the card allows them (8192x4096 -> 4096: 126 us, 2.2 POP/s; zeros 113 us), with few
-// rows by memory (32x25088 -> 4096: 22 us, 4.7 TB/s), with few tiles by a stage's latencies (777x1155 -> 1001: 10 us).
+// rows by memory (32x25088 -> 4096: 22 us, 4.7 TB/s), with few tiles by a stage's latencies (777x1155 -> 1001: 8.7 us).
 template <typename Y, int BM, int BN, int WM, int WN, int S, int KG>
 __global__ void __launch_bounds__(KG * WM * WN * 64)
 matmul_i8_kernel(const I8Product p, int splits, int *part)
@@ -625,7 +625,7 @@ matmul_i8_kernel(const I8Product p, int splits, int *part)
     store_tile<Y, MT, NT>(p, m, n0 + wn, g, acc, sa, c);
 }
 
-// Rows of one or two matrices to multiples of 16 bytes (blockIdx.y: which).  777x1155 and 1001x1155: 3.9 us.
+// Rows of one or two matrices to multiples of 16 bytes (blockIdx.y: which).  1001x1155: 3.6 us.
 __global__ void __launch_bounds__(256)
 realign_kernel(const Realign a0, const Realign a1)
 {
@@ -714,10 +714,12 @@ __device__ __forceinline__ void wait_for_loads(int behind)
 }
 
 // Short rows in whole pieces: k a multiple of 16, n of 8, the rows of the weights at multiples of 16 bytes.  Eight waves share
-// 64 rows, MH sets of them a part of the rows each, and take groups of 32 channels in turn; blockIdx.y: a part of the channels (`part_n`).
-// The weights, which every workgroup reads and the level-2 caches hold, come in steps of 128 bytes of k of a group's channels (k up to 64: one step, to the registers), past the registers to a ring of D steps in LDS that is the wave's own: no barrier, and eight lanes read
-// 128 bytes of a row together (read as the matrix instruction wants them, no two lanes do, and a quarter of the cache's rate
-// is all there is).  Bound by memory and a workgroup's start and end: 100352x64 -> 256 bf16 15.5 us, 4.1 TB/s.
+// 64 rows (32 where k passes 1024), MH sets of them a part of the rows each, and take groups of 32 channels in turn; blockIdx.y: a
+// part of the channels (`part_n`).  The weights, which every workgroup reads and the level-2 caches hold, come in steps of 128 bytes
+// of k of a group's channels (k up to 64: one step, to the registers), past the registers to a ring of D steps in LDS that is
+// the wave's own: no barrier, and eight lanes read 128 bytes of a row together (read as the matrix instruction wants them, no two
+// lanes do, and a quarter of the cache's rate is all there is).  Bound by memory and a workgroup's start and end:
+// 100352x64 -> 256 bf16 15.6 us, 4.1 TB/s.
 template <typename T, typename Y, int KS, int MH>
 __global__ void __launch_bounds__(512, KS <= 4 ? 4 : 2)
 linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, int part_n)
