@@ -1075,7 +1075,7 @@ linear_i8_rows_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx)
         if (p.m < 4 && p.k > 64 * 4 * N) {
             for (int m = 0; m < p.m; ++m) quantize_row(m, int(threadIdx.x), std::integral_constant<int, WAVES * 64>(), std::integral_constant<int, LONG ? kFusedRows / (WAVES * 64 * N) : 4>());
         } else {
-            for (int m = wave; m < p.m; m += WAVES) quantize_row(m, lane, std::integral_constant<int, 64>(), std::integral_constant<int, 4>());
+            for (int m = wave; m < p.m; m += WAVES) quantize_row(m, lane, std::integral_constant<int, 64>(), std::integral_constant<int, LONG ? 16 : 4>());
         }
         __syncthreads();
     }
@@ -1225,11 +1225,11 @@ int launch_rows(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
     const unsigned grid = unsigned((int64_t(p.n) + 15) / 16);
     // The ring takes 64 KB of LDS: where a compute unit has one workgroup at most, or two fit still (1x25088 -> 1000 18.3 us without it, 12.0;
     // 2x8192 -> 8192 16.3 and, one workgroup a compute unit with it, 19.6).  There long rows stay in registers between their two
-    // uses (10.9 us; 1x4096 -> 1000 4.8 us with few registers and 5.9).
+    // uses (10.9 us; 1x4096 -> 1000 4.8 us with few registers and 5.9; rows that a wave has, 10x3200 -> 1856 fp32 8.8 and 10.5, 10x1168 7.2 and 6.0).
     if constexpr (sizeof(T) > 1) {
         const bool one = int64_t(grid) <= kUnits;
         if (rows_at_16(p.b, p.ldb) && (one || lds <= 14 * 1024)) {
-            if (one && p.k > kFusedRows / 4 && p.m < 4)
+            if (one && (p.m < 4 ? p.k > kFusedRows / 4 : p.k >= 64 * 10 * Vec<T>::N))
                 hipLaunchKernelGGL((linear_i8_rows_kernel<T, 2, true>), dim3(grid), dim3(512), lds, st, p, x, ldx);
             else
                 hipLaunchKernelGGL((linear_i8_rows_kernel<T, 2, false>), dim3(grid), dim3(512), lds, st, p, x, ldx);

@@ -246,6 +246,14 @@ def test_lengths_that_end_inside_a_stage(m, n, k, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(4, 40, 8192), (8, 33, 4096), (12, 20, 2704), (5, 130, 5136), (6, 7, 5440), (9, 24, 2560), (3, 20, 10000),
+                                   (4, 5000, 8176), (7, 17, 4112)])
+def test_a_few_long_rows(m, n, k, dtype):
+    test_lengths_that_end_inside_a_stage(m, n, k, dtype)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("k", [513, 527, 585, 641, 1023, 1155, 2050, 9001, 20013])
 def test_what_lies_behind_the_rows_does_not_count(k):
     """Rows at multiples of 16 bytes whose last piece is not theirs alone; the last row ends with the memory."""
