@@ -1270,9 +1270,11 @@ int launch_thin(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
     if (p.k <= 64) return launch_thin_steps<T, 1>(p, x, ldx, st);
     if (p.k <= 128) return launch_thin_steps<T, 2>(p, x, ldx, st);
     if (p.k <= 256) return launch_thin_steps<T, 4>(p, x, ldx, st);
-    if (p.k <= 512) return launch_thin_steps<T, 8>(p, x, ldx, st);
-    if constexpr (sizeof(T) > 1) return p.k <= 1024 ? launch_thin_steps<T, 16>(p, x, ldx, st) : launch_thin_steps<T, 32>(p, x, ldx, st);
-    return PCONV_UNSUPPORTED;                            // (quantised rows of that length go in tiles)
+    if constexpr (sizeof(T) > 1) {                       // (quantised rows of more than kThinK go in tiles)
+        if (p.k > 1024) return launch_thin_steps<T, 32>(p, x, ldx, st);
+        if (p.k > kThinK) return launch_thin_steps<T, 16>(p, x, ldx, st);
+    }
+    return launch_thin_steps<T, 8>(p, x, ldx, st);
 }
 
 }  // namespace
