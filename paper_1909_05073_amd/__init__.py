@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
+import operator
 import os
 
 import numpy as np
@@ -707,21 +708,41 @@ def _dense(t) -> bool:
     return True
 
 
+_bytes_of = operator.attrgetter("nbytes")
+
+
 class GradList:
     """The gradients of a network's tensors, to be measured and limited together.
 
     grads: CUDA tensors on one device, fp32 or bf16, each dense (contiguous in some order of its dimensions).  out: where
     the limited gradients go, a tensor of the same shape and strides, fp32 or bf16, for each; without it they are
-    changed in place.  The list keeps the tensors: it is made once for buffers that stay (zero_grad(set_to_none=False)) and
-    again when they are replaced."""
+    changed in place.
+
+    The list keeps the tensors.  Every call looks up where they lie and how many bytes they have, so that tensors that
+    were given other memory (`data`, `set_`, `resize_`) are followed there; a tensor that stays where it is keeps its type
+    and its order of dimensions.  Gradients that are replaced by other tensors, as zero_grad(set_to_none=True), torch's
+    default, does, need a new list: this one goes on limiting the old ones."""
 
     def __init__(self, grads, out=None):
-        grads = list(grads)
-        outs = grads if out is None else list(out)
+        self.grads = list(grads)
+        self.out = self.grads if out is None else list(out)
+        self._lay_out()
+
+    def _places(self):
+        """Address and bytes of every tensor."""
+        import torch
+        places = [*map(torch.Tensor.data_ptr, self.grads), *map(_bytes_of, self.grads)]
+        if self.out is not self.grads:
+            places += [*map(torch.Tensor.data_ptr, self.out), *map(_bytes_of, self.out)]
+        return places
+
+    def _lay_out(self):
+        """Checks the tensors, and writes down where they lie as the library takes it."""
+        self._at = None                                  # (until all of them are found right)
+        grads, outs = self.grads, self.out
         if len(outs) != len(grads):
             raise ValueError("out must hold a tensor for each gradient")
-        self.grads, self.out = grads, outs
-        self._index = _device_index(*grads, *(outs if out is not None else ()))
+        self._index = _device_index(*grads, *(outs if outs is not grads else ()))
         for g, o in zip(grads, outs):
             if not _dense(g):
                 raise ValueError("a gradient must be dense")
@@ -737,6 +758,7 @@ class GradList:
         self._types, self._out_types = (C.c_int32 * num)(*types), (C.c_int32 * num)(*out_types)
         self._refuse_overlaps(types, out_types)
         self._size = lib().pconv_grad_workspace(num)
+        self._at = self._places()
 
     def _refuse_overlaps(self, types, out_types):
         """No output may lie over another one, or over a gradient that is not its own."""
@@ -756,6 +778,8 @@ class GradList:
 
     def _begin(self):
         import torch
+        if self._places() != self._at:
+            self._lay_out()
         if self._num == 0:
             raise ValueError("the list is empty")
         like = self.grads[0]

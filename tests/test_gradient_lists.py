@@ -1,0 +1,131 @@
+"""What a list of gradients keeps from one call to the next, and what it must not: the tensors, not where they lay.
+
+The tests on the host run the binding over a library that only takes notes; those on the card compare with 64 bits under the
+bounds of test_gradients.py."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+import paper_1909_05073_amd as P
+
+from gpu_util import say
+from test_gradients import check, host, plain
+
+
+class FakeLibrary:
+    """Notes what it is given."""
+
+    def __init__(self):
+        self.calls = []
+
+    def pconv_grad_workspace(self, num):
+        return 64
+
+    def pconv_grad_norm(self, grads, counts, types, num, norm, work, size, stream):
+        self.calls.append((list(grads), None, list(counts), list(types), None))
+        return P.OK
+
+    def pconv_clip_grads(self, grads, outs, counts, types, out_types, num, max_norm, eps, norm, work, size, stream):
+        self.calls.append((list(grads), list(outs), list(counts), list(types), list(out_types)))
+        return P.OK
+
+
+@pytest.fixture
+def notes(monkeypatch):
+    """The calls that reach the library, with tensors in host memory."""
+    import torch
+    fake = FakeLibrary()
+    monkeypatch.setattr(P, "_lib", fake)
+    monkeypatch.setattr(P, "_stream", lambda index: None)
+    monkeypatch.setattr(P, "_device_index", lambda *tensors: 0 if tensors else -1)
+    monkeypatch.setattr(P, "_current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    return fake.calls
+
+
+def changes():
+    """(name, what gives a tensor of 60 elements other memory, another size or type)."""
+    import torch
+    yield "data", lambda t: setattr(t, "data", torch.ones(60))
+    yield "set_", lambda t: t.set_(torch.ones(60))
+    yield "grown", lambda t: t.resize_(6000)
+    yield "cut", lambda t: t.resize_(7)
+    yield "first part", lambda t: setattr(t, "data", t.data[:11])
+    yield "storage", lambda t: (t.untyped_storage().resize_(0), t.untyped_storage().resize_(4 * 60))
+    yield "type", lambda t: setattr(t, "data", torch.ones(60, dtype=torch.bfloat16))
+
+
+@pytest.mark.parametrize("which", range(7))
+@pytest.mark.parametrize("side", ["in place", "gradient and output"])
+def test_tensors_with_other_memory_are_seen(notes, which, side):
+    import torch
+    name, change = list(changes())[which]
+    grads = [torch.ones(60), torch.ones(30)]
+    outs = None if side == "in place" else [torch.zeros(60), torch.zeros(30)]
+    plan = P.GradList(grads, outs)
+    plan.clip(1.0)
+    held = [torch.empty(60) for _ in range(8)]           # (so that new memory is other memory)
+    for t in grads[:1] + (outs[:1] if outs else []):
+        change(t)
+    plan.clip(1.0)
+    plan.norm()
+    assert len(held) == 8 and len(notes) == 3
+    for at, to, counts, types, out_types in notes[1:]:
+        assert at == [g.data_ptr() for g in grads] and counts == [g.numel() for g in grads], name
+        assert types == [P.BF16 if g.dtype == torch.bfloat16 else P.F32 for g in grads], name
+        if to is not None:
+            want = outs or grads
+            assert to == [o.data_ptr() for o in want] and out_types == [P.BF16 if o.dtype == torch.bfloat16 else P.F32 for o in want], name
+
+
+def test_other_tensors_in_the_list_are_seen(notes):
+    import torch
+    plan = P.GradList([torch.ones(60), torch.ones(30)])
+    plan.grads[1] = torch.ones(45)
+    plan.clip(1.0)
+    assert notes[0][0] == notes[0][1] == [g.data_ptr() for g in plan.grads] and notes[0][2] == [60, 45]
+
+
+def test_changes_that_no_list_may_have_are_refused_until_they_are_gone(notes):
+    import torch
+    flat = torch.ones(200)
+    grads = [flat[:60], flat[60:120]]
+    plan = P.GradList(grads)
+    was = grads[1].data
+    grads[1].data = flat[59:119]                         # over the first
+    for _ in range(2):
+        with pytest.raises(ValueError, match="overlap"):
+            plan.clip(1.0)
+    grads[1].data = was
+    plan.clip(1.0)
+    assert len(notes) == 1 and notes[0][0] == [flat.data_ptr(), flat.data_ptr() + 240]
+    grads[0].data = flat[:60].double()
+    with pytest.raises(ValueError):
+        plan.norm()
+    assert len(notes) == 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("with_out", [False, True])
+def test_clipping_follows_the_tensors_to_other_memory(with_out):
+    import torch
+    say(f"[case] clip after other memory, out {with_out}")
+    rng = np.random.default_rng(4)
+    fresh = lambda n: torch.from_numpy(rng.standard_normal(n).astype(np.float32)).cuda()
+    grads = [fresh(50_000), fresh(700), fresh(70_000)]
+    outs = [torch.zeros_like(g) for g in grads] if with_out else None
+    plan = P.GradList(grads, outs)
+    plan.clip(1.0)
+    grads[0].data = fresh(50_000)
+    grads[1].set_(fresh(900))
+    grads[2].resize_(90_000).normal_()
+    if with_out:
+        outs[1].resize_(900)
+        outs[2].data = torch.zeros(90_000, device="cuda")
+    else:
+        outs = grads
+    values = [host(g) for g in grads]
+    want_norm, want = plain(values, 2.0)
+    assert abs(float(plan.norm()) - want_norm) <= 1.01 * 2.0 ** -24 * want_norm
+    check(plan.clip(2.0), outs, want_norm, want)
