@@ -556,6 +556,36 @@ def _output(out, lead, m, n, dtype, like):
     return out, _rows(out, "out")[2]
 
 
+def _share(a, b) -> bool:
+    """Whether two runs of rows, (address, rows, bytes of a row, bytes from row to row), have a byte in common."""
+    (at, rows, size, step), (to, others, length, apart) = a, b
+    if not (rows and size and others and length):
+        return False
+    if at >= to + (others - 1) * apart + length or to >= at + (rows - 1) * step + size:
+        return False
+    if rows == 1:
+        step = apart
+    elif others == 1:
+        apart = step
+    # Of the second run's rows the first that ends behind the start of a row of the first run must begin behind its end.
+    # With equal distances only how many rows further it is counts, so that one row stands for all.
+    if step == apart:
+        j = max((at - to - length) // apart + 1, 1 - rows)
+        return j < others and to + j * apart < at + size
+    starts = at + step * np.arange(rows, dtype=np.int64)
+    j = np.maximum((starts - to - length) // apart + 1, 0)
+    return bool(((j < others) & (to + j * apart < starts + size)).any())
+
+
+def _refuse_overlap(out, *inputs):
+    """out and each of the inputs: (tensor or None, rows, columns, elements from row to row)."""
+    run = lambda t, rows, columns, step: (t.data_ptr(), rows, columns * t.element_size(), step * t.element_size())
+    to = run(*out)
+    for i in inputs:
+        if i[0] is not None and _share(to, run(*i)):
+            raise ValueError("out must not overlap an input")
+
+
 def pconv_quantize_rows(x_ptr: int, x_stride: int, x_dtype, rows: int, cols: int, q_ptr: int, q_stride: int,
                         scale_ptr: int, stream: int = 0):
     """Raw-pointer call, one to one with the C entry point."""
@@ -620,7 +650,8 @@ def quantize_rows(x):
 def matmul_i8(a, a_scale, b, b_scale, bias=None, relu: bool = False, out_dtype=None, out=None):
     """a [..., k], b [n, k]: int8 CUDA tensors.  Returns act((a @ b.T) * a_scale[..., None] * b_scale + bias) [..., n].
 
-    a_scale [...], b_scale [n], bias [n]: fp32.  out_dtype: torch.float32 (unless `out` says otherwise) or torch.bfloat16."""
+    a_scale [...], b_scale [n], bias [n]: fp32.  out_dtype: torch.float32 (unless `out` says otherwise) or torch.bfloat16.
+    out: where the result goes; it must not overlap an input (its rows may lie between those of one)."""
     import torch
     if a.dtype != torch.int8 or b.dtype != torch.int8 or b.dim() != 2:
         raise ValueError("a [..., k] and b [n, k] must be int8")
@@ -635,6 +666,8 @@ def matmul_i8(a, a_scale, b, b_scale, bias=None, relu: bool = False, out_dtype=N
     y_type = _type_of(y, "out")
     sa, sb = _per_channel(a_scale, m, "a_scale"), _per_channel(b_scale, n, "b_scale")
     bp = _per_channel(bias, n, "bias") if bias is not None else None
+    if out is not None:
+        _refuse_overlap((y, m, n, y_step), (a, m, k, a_step), (b, n, k, b_step), (a_scale, 1, m, m), (b_scale, 1, n, n), (bias, 1, n, n))
     a_ptr, b_ptr = a.data_ptr(), b.data_ptr()
     size = _matmul_i8_workspace(m, n, k, _at_16(a_ptr, a_step) and _at_16(b_ptr, b_step))
     work = _scratch(size, a) if size else None
@@ -650,7 +683,7 @@ def linear_i8(x, w, w_scale, bias=None, relu: bool = False, out_dtype=None, out=
     """x [..., k]: CUDA tensor, fp32 or bf16; w [n, k] int8 and w_scale [n] as quantize_rows gives them for the weights.
 
     Returns matmul_i8(*quantize_rows(x), w, w_scale, bias, relu) [..., n], of x's type unless `out_dtype` or `out` says
-    otherwise."""
+    otherwise.  out: as there."""
     import torch
     x_type = _type_of(x, "x")
     if w.dtype != torch.int8 or w.dim() != 2:
@@ -667,6 +700,8 @@ def linear_i8(x, w, w_scale, bias=None, relu: bool = False, out_dtype=None, out=
         y_type = _type_of(y, "out")
     sw = _per_channel(w_scale, n, "w_scale")
     bp = _per_channel(bias, n, "bias") if bias is not None else None
+    if out is not None:
+        _refuse_overlap((y, m, n, y_step), (x, m, k, x_step), (w, n, k, w_step), (w_scale, 1, n, n), (bias, 1, n, n))
     w_ptr = w.data_ptr()
     size = _linear_i8_workspace(m, n, k, _at_16(w_ptr, w_step))
     work = _scratch(size, x) if size else None
