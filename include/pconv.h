@@ -256,8 +256,9 @@ int pconv_linear_i8(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, co
  *
  *   norm = sqrt( sum over all tensors and elements of g^2 )        out = g * min(1, max_norm / (norm + eps))
  *
- * Squares are summed in fp64 in a fixed order.  A norm that is NaN makes all outputs NaN, an infinite one makes them 0, and
- * NaN where g is infinite.  A tensor is a plain run of counts[i] >= 0 elements, fp32 or bf16, that begins
+ * Squares are summed in fp64 in a fixed order.  The factor is 1 where max_norm >= norm + eps, both
+ * infinite or both 0 among it: an infinite max_norm limits nothing.  A norm that is NaN makes all outputs NaN; an infinite one
+ * makes them 0 with a finite max_norm, and NaN where g is infinite.  A tensor is a plain run of counts[i] >= 0 elements, fp32 or bf16, that begins
  * anywhere its type may.
  *
  *   grads      host, [num] device pointers (not read where counts[i] == 0)

@@ -135,9 +135,10 @@ struct Factor { float first, then; };
 
 __device__ __forceinline__ Factor factor_of(double total, float max_norm, float eps)
 {
-    const double f = double(max_norm) / (sqrt(total) + double(eps));
-    // (0 / 0, a limit of zero and gradients of zero, is NaN as well: eps keeps it away)
-    if (f >= 1.0) return Factor{1.0f, 1.0f};
+    const double least = sqrt(total) + double(eps);
+    // (also for an infinite norm and limit and for 0 and 0, whose quotients are no numbers; a norm that is NaN goes on)
+    if (double(max_norm) >= least) return Factor{1.0f, 1.0f};
+    const double f = double(max_norm) / least;
     if (f < 0x1p-100) return Factor{0x1p-64f, float(f * 0x1p64)};
     return Factor{1.0f, float(f)};
 }

@@ -129,3 +129,31 @@ def test_clipping_follows_the_tensors_to_other_memory(with_out):
     want_norm, want = plain(values, 2.0)
     assert abs(float(plan.norm()) - want_norm) <= 1.01 * 2.0 ** -24 * want_norm
     check(plan.clip(2.0), outs, want_norm, want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sizes", [[40, 9], [300_000, 77], [50] * 170])
+def test_an_infinite_limit_limits_nothing_and_a_limit_of_zero_leaves_no_nan(sizes):
+    """By one workgroup, in two launches, and with a launch for the total."""
+    import math
+    import torch
+    say(f"[case] clip, infinite norms and limits, norms and limits of zero, {len(sizes)} tensors")
+    make = lambda: [torch.full((n,), 2.0, device="cuda") for n in sizes]
+    for in_place in (True, False):
+        grads = make()
+        grads[0][3] = math.inf
+        want = [g.clone() for g in grads]
+        outs = grads if in_place else [torch.full_like(g, float("nan")) for g in grads]
+        assert math.isinf(float(P.clip_grad_norm(grads, math.inf, out=None if in_place else outs)))
+        assert all(torch.equal(o, w) for o, w in zip(outs, want))
+        grads[1][2] = math.nan                           # what is no number stays none
+        assert math.isnan(float(P.clip_grad_norm(grads, math.inf, out=None if in_place else outs)))
+        assert all(bool(torch.isnan(o).all()) for o in outs)
+        grads = [g.zero_() for g in make()]
+        outs = grads if in_place else [torch.full_like(g, float("nan")) for g in grads]
+        assert float(P.clip_grad_norm(grads, 0.0, eps=0.0, out=None if in_place else outs)) == 0
+        assert all(bool((o == 0).all()) for o in outs)
+        grads = make()
+        outs = grads if in_place else [torch.full_like(g, float("nan")) for g in grads]
+        P.clip_grad_norm(grads, 0.0, eps=0.0, out=None if in_place else outs)
+        assert all(bool((o == 0).all()) for o in outs)
