@@ -27,6 +27,15 @@ typedef float f4 __attribute__((ext_vector_type(4)));
 typedef __bf16 b4 __attribute__((ext_vector_type(4)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 
+// Workgroups of up to 512 threads that one dimension of a launch may have: fewer than 2^32 threads.
+constexpr int64_t kMaxGroups = (int64_t(1) << 23) - 1;
+
+int too_many_groups()
+{
+    set_error("8-bit layers: too many workgroups for one launch");
+    return PCONV_UNSUPPORTED;
+}
+
 int check_launch(const char *what)
 {
     const hipError_t e = hipGetLastError();
@@ -1191,6 +1200,8 @@ struct Cut { int tile, splits; };
 constexpr int kTiles = 4, kTileM[kTiles] = {32, 64, 128, 256}, kTileN[kTiles] = {128, 128, 128, 256};
 constexpr int64_t kUnits = 256;                          // compute units
 
+int64_t tiles_of(const Cut &c, int64_t m, int64_t n) { return ((m + kTileM[c.tile] - 1) / kTileM[c.tile]) * ((n + kTileN[c.tile] - 1) / kTileN[c.tile]); }
+
 // The cheapest by a count of cycles: a compute unit takes its tiles one after the other, a stage of a tile at the rate of the
 // matrix units (half of their peak) or of what 40 bytes a cycle bring from the level-2 cache, whichever is slower.
 // Joining the parts of k is one more launch and reads and writes the sums.
@@ -1202,7 +1213,7 @@ Cut cut_of(int64_t m, int64_t n, int64_t k)
     double least = 0;
     for (int t = 0; t < kTiles; ++t)
         for (int64_t s = 1; s == 1 || (s <= 32 && s * 4 <= stages); s *= 2) {
-            const int64_t tiles = ((m + kTileM[t] - 1) / kTileM[t]) * ((n + kTileN[t] - 1) / kTileN[t]);
+            const int64_t tiles = tiles_of(Cut{t, int(s)}, m, n);
             double c = double((tiles * s + kUnits - 1) / kUnits) * double((stages + s - 1) / s) * double(stage_cycles[t]) + start;
             if (s > 1) c += join + double(s) * double(m) * double(n) * 8 / 2000;
             if ((t == 0 && s == 1) || c < least || (c == least && s == 1)) { least = c; best = Cut{t, int(s)}; }
@@ -1218,11 +1229,14 @@ void launch_tiles(const I8Product &p, int splits, int *part, hipStream_t st)
     else hipLaunchKernelGGL((matmul_i8_kernel<float, BM, BN, WM, WN, S, KG>), dim3(grid), dim3(KG * WM * WN * 64), 0, st, p, splits, part);
 }
 
+int64_t rows_groups(int64_t n) { return (n + 15) / 16; }
+
 template <typename T>
 int launch_rows(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
 {
     const size_t lds = sizeof(T) > 1 ? size_t(p.m) * ((p.k + 255) / 256 * 256 + 16) : 0;
-    const unsigned grid = unsigned((int64_t(p.n) + 15) / 16);
+    if (rows_groups(p.n) > kMaxGroups) return too_many_groups();
+    const unsigned grid = unsigned(rows_groups(p.n));
     // The ring takes 64 KB of LDS: where a compute unit has one workgroup at most, or two fit still (1x25088 -> 1000 18.3 us without it, 12.0;
     // 2x8192 -> 8192 16.3 and, one workgroup a compute unit with it, 19.6).  There long rows stay in registers between their two
     // uses (10.9 us; 1x4096 -> 1000 4.8 us with few registers and 5.9; rows that a wave has, 10x3200 -> 1856 fp32 8.8 and 10.5, 10x1168 7.2 and 6.0).
@@ -1251,7 +1265,7 @@ int launch_thin_steps(const I8Product &p, const T *x, int64_t ldx, hipStream_t s
     // (every part quantises the rows again: no more of them than make 512 workgroups)
     const int64_t parts = std::min<int64_t>(groups, std::max<int64_t>(1, (KS <= 8 ? 512 : 256) / tiles));
     const int part_n = int((groups + parts - 1) / parts * channels);
-    if (tiles >= int64_t(1) << 23) { set_error("pconv_matmul_i8: too many workgroups"); return PCONV_UNSUPPORTED; }
+    if (tiles > kMaxGroups) return too_many_groups();
     const dim3 grid(unsigned(tiles), unsigned((int64_t(p.n) + part_n - 1) / part_n));
 #define PCONV_LAUNCH(Y)                                                                                                        \
     do {                                                                                                                       \
@@ -1306,6 +1320,13 @@ int launch_linear_i8_fused(const I8Product &p, const void *x, int64_t ldx, int b
     return bf16 ? launch_thin(p, static_cast<const __bf16 *>(x), ldx, st) : launch_thin(p, static_cast<const float *>(x), ldx, st);
 }
 
+int check_linear_i8_apart(int64_t m, int64_t n, int64_t k)
+{
+    if (few(m, k)) return rows_groups(n) > kMaxGroups ? too_many_groups() : PCONV_OK;
+    const Cut c = cut_of(m, n, k);
+    return tiles_of(c, m, n) * c.splits > kMaxGroups ? too_many_groups() : PCONV_OK;
+}
+
 bool matmul_i8_aligns(int64_t m, int64_t k) { return !few(m, k) && !thin(m, k); }
 
 Realign realigned(const int8_t *from, int64_t ld, int rows, int k, int8_t *to) { return Realign{from, to, ld, rows, k, (k + 15) / 16}; }
@@ -1325,8 +1346,8 @@ int launch_matmul_i8(const I8Product &product, void *work, void *stream)
     if (few(p.m, p.k)) return launch_rows(p, p.a, p.lda, st);
     if (thin(p.m, p.k)) return launch_thin(p, p.a, p.lda, st);
     const Cut c = cut_of(p.m, p.n, p.k);
-    const int64_t tiles = ((int64_t(p.m) + kTileM[c.tile] - 1) / kTileM[c.tile]) * ((int64_t(p.n) + kTileN[c.tile] - 1) / kTileN[c.tile]);
-    if (tiles * c.splits >= int64_t(1) << 23) { set_error("pconv_matmul_i8: too many workgroups"); return PCONV_UNSUPPORTED; }
+    const int64_t tiles = tiles_of(c, p.m, p.n);
+    if (tiles * c.splits > kMaxGroups) return too_many_groups();
     int8_t *at = static_cast<int8_t *>(work);
     Realign moved[2] = {};
     unsigned count = 0;

@@ -38,6 +38,8 @@ Realign realigned(const int8_t *from, int64_t ld, int rows, int k, int8_t *to);
 int launch_matmul_i8(const I8Product &p, void *work, void *stream);
 // Whether rows are so few or so short that they are quantised within the product, and that product (p.a, lda, sa unused).
 bool linear_i8_fused(int64_t m, int64_t n, int64_t k, bool b_at_16);
+// Whether the product of rows that are quantised by a launch of their own can be launched: asked before that one.
+int check_linear_i8_apart(int64_t m, int64_t n, int64_t k);
 int launch_linear_i8_fused(const I8Product &p, const void *x, int64_t ldx, int bf16, void *stream);
 
 // Up to kGradTensors tensors travel in the arguments of one launch (4 KiB), cut into chunks of 1 << `log2` elements.

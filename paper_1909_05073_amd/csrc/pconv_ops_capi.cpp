@@ -212,6 +212,7 @@ int pconv_linear_i8(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, co
     if (!stride_fits(m, k, x_stride)) return invalid(who, "rows must lie at least their length apart");
     if (const int rc = check_work(who, work, work_bytes, pconv_linear_i8_workspace(m, n, k, rows_at_16(w_dev, w_stride)))) return rc;
     if (linear_i8_fused(m, n, k, rows_at_16(w_dev, w_stride))) return launch_linear_i8_fused(p, x_dev, x_stride, x_dtype == PCONV_BF16, hip_stream);
+    if (const int rc = check_linear_i8_apart(m, n, k)) return rc;
     float *const scale = static_cast<float *>(work);
     int8_t *const q = static_cast<int8_t *>(work) + round16(4 * m);
     const int64_t ldq = round16(k);
