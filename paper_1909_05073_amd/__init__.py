@@ -586,6 +586,12 @@ def _refuse_overlap(out, *inputs):
             raise ValueError("out must not overlap an input")
 
 
+def _changed(tensors):
+    """Tells autograd that the tensors hold other values now, as torch's own calls in place do."""
+    import torch
+    torch.autograd.graph.increment_version(tensors)
+
+
 def pconv_quantize_rows(x_ptr: int, x_stride: int, x_dtype, rows: int, cols: int, q_ptr: int, q_stride: int,
                         scale_ptr: int, stream: int = 0):
     """Raw-pointer call, one to one with the C entry point."""
@@ -676,6 +682,8 @@ def matmul_i8(a, a_scale, b, b_scale, bias=None, relu: bool = False, out_dtype=N
                                          _stream(index))
     if rc != OK:
         _check(rc)
+    if out is not None:
+        _changed((y,))
     return y
 
 
@@ -710,6 +718,8 @@ def linear_i8(x, w, w_scale, bias=None, relu: bool = False, out_dtype=None, out=
                                          work.data_ptr() if size else None, size, _stream(index))
     if rc != OK:
         _check(rc)
+    if out is not None:
+        _changed((y,))
     return y
 
 
@@ -840,6 +850,7 @@ class GradList:
                                               _stream(self._index))
         if rc != OK:
             _check(rc)
+        _changed(self.out)
         return norm
 
 
