@@ -771,7 +771,17 @@ class GradList:
     def __init__(self, grads, out=None):
         self.grads = list(grads)
         self.out = self.grads if out is None else list(out)
+        self._writes = True
         self._lay_out()
+
+    @classmethod
+    def _read_only(cls, grads):
+        """A list whose norm alone is asked for: its tensors may overlap."""
+        made = cls.__new__(cls)
+        made.grads = made.out = list(grads)
+        made._writes = False
+        made._lay_out()
+        return made
 
     def _places(self):
         """Address and bytes of every tensor."""
@@ -801,7 +811,8 @@ class GradList:
         self._in = (C.c_void_p * num)(*(g.data_ptr() for g in grads))
         self._to = (C.c_void_p * num)(*(o.data_ptr() for o in outs))
         self._types, self._out_types = (C.c_int32 * num)(*types), (C.c_int32 * num)(*out_types)
-        self._refuse_overlaps(types, out_types)
+        if self._writes:
+            self._refuse_overlaps(types, out_types)
         self._size = lib().pconv_grad_workspace(num)
         self._at = self._places()
 
@@ -855,8 +866,8 @@ class GradList:
 
 
 def grad_norm(grads):
-    """The 2-norm of all gradients together; see GradList."""
-    return GradList(grads).norm()
+    """The 2-norm of all gradients together; see GradList.  Nothing is written, and the tensors may overlap."""
+    return GradList._read_only(grads).norm()
 
 
 def clip_grad_norm(grads, max_norm: float, eps: float = 1e-6, out=None):

@@ -157,3 +157,26 @@ def test_an_infinite_limit_limits_nothing_and_a_limit_of_zero_leaves_no_nan(size
         outs = grads if in_place else [torch.full_like(g, float("nan")) for g in grads]
         P.clip_grad_norm(grads, 0.0, eps=0.0, out=None if in_place else outs)
         assert all(bool((o == 0).all()) for o in outs)
+
+
+def test_the_norm_alone_takes_tensors_that_overlap(notes):
+    """Nothing is written: every tensor counts, as the formula says."""
+    import torch
+    flat = torch.ones(200)
+    P.grad_norm([flat, flat, flat[50:90]])
+    assert notes[0][0] == [flat.data_ptr(), flat.data_ptr(), flat.data_ptr() + 200] and notes[0][2] == [200, 200, 40]
+    with pytest.raises(ValueError, match="overlap"):
+        P.clip_grad_norm([flat, flat], 1.0)
+    with pytest.raises(ValueError, match="dense"):
+        P.grad_norm([flat[::2]])
+
+
+@pytest.mark.gpu
+def test_the_norm_of_tensors_that_overlap():
+    import math
+    import torch
+    say("[case] grad_norm of tensors that overlap")
+    flat = torch.full((50_000,), 2.0, device="cuda")
+    want = math.sqrt(4.0 * 110_000)
+    assert abs(float(P.grad_norm([flat, flat, flat[10:10_010]])) - want) <= 1.01 * 2.0 ** -24 * want
+    assert bool((flat == 2.0).all())
