@@ -133,7 +133,7 @@ int check_grads(const char *who, const void *const *in, const int64_t *counts, c
         if (counts[i] < 0 || counts[i] > kMaxElements || (total += counts[i]) > kMaxElements) return invalid(who, "counts must be 0 .. 2^45, and so their sum");
         if (counts[i] && !in[i]) return invalid(who, "null pointer of a tensor");
         if (!is_dtype(types[i])) return invalid(who, "unknown dtype of a tensor");
-        if (reinterpret_cast<uintptr_t>(in[i]) % (types[i] == PCONV_BF16 ? 2 : 4) != 0) return invalid(who, "a tensor must be aligned to its type");
+        if (counts[i] && reinterpret_cast<uintptr_t>(in[i]) % (types[i] == PCONV_BF16 ? 2 : 4) != 0) return invalid(who, "a tensor must be aligned to its type");
     }
     return PCONV_OK;
 }
@@ -254,7 +254,7 @@ int pconv_clip_grads(const void *const *grads, void *const *outs, const int64_t 
     for (int64_t i = 0; i < num; ++i) {
         if (counts[i] && !outs[i]) return invalid(who, "null pointer of an output");
         if (!is_dtype(out_dtypes[i])) return invalid(who, "unknown dtype of an output");
-        if (reinterpret_cast<uintptr_t>(outs[i]) % (out_dtypes[i] == PCONV_BF16 ? 2 : 4) != 0) return invalid(who, "an output must be aligned to its type");
+        if (counts[i] && reinterpret_cast<uintptr_t>(outs[i]) % (out_dtypes[i] == PCONV_BF16 ? 2 : 4) != 0) return invalid(who, "an output must be aligned to its type");
         if (counts[i] && outs[i] == grads[i] && out_dtypes[i] != dtypes[i]) return invalid(who, "an output in its gradient's place must have its type");
     }
     const Grads g = grads_of(grads, outs, counts, dtypes, out_dtypes, num);

@@ -180,3 +180,16 @@ def test_the_norm_of_tensors_that_overlap():
     want = math.sqrt(4.0 * 110_000)
     assert abs(float(P.grad_norm([flat, flat, flat[10:10_010]])) - want) <= 1.01 * 2.0 ** -24 * want
     assert bool((flat == 2.0).all())
+
+
+def test_pointers_of_empty_tensors_are_not_looked_at():
+    """The header promises it.  (The calls fail at the tensor behind the empty one, before anything is launched.)"""
+    p, need = 1 << 20, P.pconv_grad_workspace(2)
+    ptrs, i64, i32 = (lambda *v: (C.c_void_p * len(v))(*v)), (lambda *v: (C.c_int64 * len(v))(*v)), (lambda *v: (C.c_int32 * len(v))(*v))
+    for odd in (p + 1, p + 2, None):
+        with pytest.raises(P.PconvError, match="null pointer of a tensor"):
+            P.pconv_grad_norm(ptrs(odd, None), i64(0, 4), i32(0, 0), 2, p, p, need)
+        with pytest.raises(P.PconvError, match="null pointer of an output"):
+            P.pconv_clip_grads(ptrs(odd, p), ptrs(odd, None), i64(0, 4), i32(0, 0), i32(0, 0), 2, 1.0, 0.0, p, p, need)
+        with pytest.raises(P.PconvError, match="null pointer of an output"):
+            P.pconv_clip_grads(ptrs(p, p), ptrs(odd, None), i64(0, 4), i32(0, 0), i32(0, 0), 2, 1.0, 0.0, p, p, need)
