@@ -380,6 +380,18 @@ typedef struct {
 int pconv_debug_plan(const pconv_handle *h, int n, int h_in, int w_in, int stride, pconv_layout layout,
                      int fuse_pool, pconv_plan *out);
 
+/* pconv_debug_i8_plan - how pconv_matmul_i8 would run a product, without launching anything, so that a test of one form of a
+ * kernel can make sure that it gets it; also the product of pconv_linear_i8 where its rows are quantised by a launch of their
+ * own.  PCONV_INVALID_ARG for sizes that are not 1 .. 2^30 (k: 0 .. 131071) or a null pointer. */
+typedef struct {
+    int32_t kernel;            /* 1: few rows, 2: short rows, 3: tiles; the rest is 0 but for tiles     */
+    int32_t tile_m, tile_n;    /* rows and channels of a tile                                           */
+    int32_t sets;              /* sets of waves of a workgroup that take the stages of k in turn        */
+    int32_t splits;            /* workgroups that share a tile, each with a part of k                   */
+} pconv_i8_plan;
+
+int pconv_debug_i8_plan(int64_t m, int64_t n, int64_t k, pconv_i8_plan *out);
+
 /* pconv_debug_set_spin_limit - for tests of the error path: the number of polls after which a
  * wait inside the register-tiled kernel gives up (limit <= 0 restores the default, about half a
  * second).  With limit = 1 every such wait gives up at once: the kernels still run to their end,

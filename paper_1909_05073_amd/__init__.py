@@ -42,6 +42,10 @@ class pconv_plan(C.Structure):
                 ("tail_tiles", C.c_int32), ("flat_shape", C.c_int32), ("lone_patches", C.c_int32), ("lone_cut", C.c_int32)]
 
 
+class pconv_i8_plan(C.Structure):
+    _fields_ = [("kernel", C.c_int32), ("tile_m", C.c_int32), ("tile_n", C.c_int32), ("sets", C.c_int32), ("splits", C.c_int32)]
+
+
 _lib = None
 
 
@@ -118,6 +122,8 @@ def lib():
     L.pconv_linear_i8_workspace.argtypes = [i64, i64, i64, ip]
     L.pconv_linear_i8.restype = ip
     L.pconv_linear_i8.argtypes = [vp, i64, ip, vp, i64, vp, vp, vp, i64, ip, i64, i64, i64, ip, vp, i64, vp]
+    L.pconv_debug_i8_plan.restype = ip
+    L.pconv_debug_i8_plan.argtypes = [i64, i64, i64, vp]
     L.pconv_grad_workspace.restype = i64
     L.pconv_grad_workspace.argtypes = [i64]
     L.pconv_grad_norm.restype = ip
@@ -137,7 +143,7 @@ EXPORTED_SYMBOLS = ["pconv_project", "pconv_pack", "pconv_conv2d", "pconv_conv2d
                     "pconv_set_kernel_policy", "pconv_debug_set_tiling", "pconv_debug_set_flat_shape", "pconv_debug_plan", "pconv_debug_set_spin_limit",
                     "pconv_get_async_error", "pconv_pool2x2_fusion", "pconv_debug_measure_fma_peak",
                     "pconv_quantize_rows", "pconv_matmul_i8", "pconv_matmul_i8_workspace", "pconv_linear_i8",
-                    "pconv_linear_i8_workspace", "pconv_grad_workspace", "pconv_grad_norm", "pconv_clip_grads",
+                    "pconv_linear_i8_workspace", "pconv_debug_i8_plan", "pconv_grad_workspace", "pconv_grad_norm", "pconv_clip_grads",
                     "pconv_last_error"]
 
 
@@ -623,6 +629,12 @@ def pconv_linear_i8(x_ptr: int, x_stride: int, x_dtype, w_ptr: int, w_stride: in
     _check(lib().pconv_linear_i8(x_ptr or None, x_stride, _DTYPE[x_dtype], w_ptr or None, w_stride, w_scale or None,
                                  bias_ptr or None, y_ptr or None, y_stride, _DTYPE[y_dtype], m, n, k, int(bool(fuse_relu)),
                                  work or None, work_bytes, stream or None))
+
+
+def pconv_debug_i8_plan(m: int, n: int, k: int) -> pconv_i8_plan:
+    out = pconv_i8_plan()
+    _check(lib().pconv_debug_i8_plan(m, n, k, C.byref(out)))
+    return out
 
 
 # (remembered by sizes: a call of the library costs 0.7 us)

@@ -1221,6 +1221,10 @@ Cut cut_of(int64_t m, int64_t n, int64_t k)
     return best;
 }
 
+// Sets of waves of a workgroup: two, and as many stages as LDS holds, where a compute unit has one workgroup (17x2048 -> 1000: 8.6 us
+// with four stages), else room for two workgroups.  The largest tile fills a compute unit with one set.
+int sets_of(const Cut &c, int64_t tiles) { return c.tile < 3 && tiles * c.splits <= kUnits ? 2 : 1; }
+
 template <int BM, int BN, int WM, int WN, int S, int KG>
 void launch_tiles(const I8Product &p, int splits, int *part, hipStream_t st)
 {
@@ -1339,6 +1343,14 @@ int64_t matmul_i8_work_bytes(int64_t m, int64_t n, int64_t k, bool a_at_16, bool
     return (a_at_16 ? 0 : m * row) + (b_at_16 ? 0 : n * row) + (c.splits > 1 ? c.splits * m * ((n + 3) / 4 * 4) * 4 : 0);
 }
 
+pconv_i8_plan matmul_i8_plan(int64_t m, int64_t n, int64_t k)
+{
+    if (few(m, k)) return pconv_i8_plan{1, 0, 0, 0, 0};
+    if (thin(m, k)) return pconv_i8_plan{2, 0, 0, 0, 0};
+    const Cut c = cut_of(m, n, k);
+    return pconv_i8_plan{3, kTileM[c.tile], kTileN[c.tile], sets_of(c, tiles_of(c, m, n)), c.splits};
+}
+
 int launch_matmul_i8(const I8Product &product, void *work, void *stream)
 {
     const hipStream_t st = static_cast<hipStream_t>(stream);
@@ -1366,13 +1378,12 @@ int launch_matmul_i8(const I8Product &product, void *work, void *stream)
         if (const int rc = check_launch("pconv_matmul_i8 (aligning rows)")) return rc;
     }
     int *const sums = reinterpret_cast<int *>(at);
-    // as many stages as LDS holds where a compute unit has one workgroup (17x2048 -> 1000: 8.6 us with four stages), else room for two
-    const bool deep = tiles * c.splits <= kUnits;
-    if (c.tile == 0 && deep) launch_tiles<32, 128, 1, 4, 4, 2>(p, c.splits, sums, st);
+    const bool two = sets_of(c, tiles) == 2;
+    if (c.tile == 0 && two) launch_tiles<32, 128, 1, 4, 4, 2>(p, c.splits, sums, st);
     else if (c.tile == 0) launch_tiles<32, 128, 1, 4, 4, 1>(p, c.splits, sums, st);
-    else if (c.tile == 1 && deep) launch_tiles<64, 128, 2, 2, 3, 2>(p, c.splits, sums, st);
+    else if (c.tile == 1 && two) launch_tiles<64, 128, 2, 2, 3, 2>(p, c.splits, sums, st);
     else if (c.tile == 1) launch_tiles<64, 128, 2, 2, 3, 1>(p, c.splits, sums, st);
-    else if (c.tile == 2 && deep) launch_tiles<128, 128, 2, 2, 2, 2>(p, c.splits, sums, st);
+    else if (c.tile == 2 && two) launch_tiles<128, 128, 2, 2, 2, 2>(p, c.splits, sums, st);
     else if (c.tile == 2) launch_tiles<128, 128, 2, 2, 2, 1>(p, c.splits, sums, st);
     else launch_tiles<256, 256, 2, 4, 2, 1>(p, c.splits, sums, st);
     if (const int rc = check_launch("pconv_matmul_i8")) return rc;

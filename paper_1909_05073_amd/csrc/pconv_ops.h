@@ -35,6 +35,7 @@ bool rows_at_16(const int8_t *at, int64_t ld);
 int64_t matmul_i8_work_bytes(int64_t m, int64_t n, int64_t k, bool a_at_16, bool b_at_16);
 bool matmul_i8_aligns(int64_t m, int64_t k);             // whether the product of those sizes reads such rows only
 Realign realigned(const int8_t *from, int64_t ld, int rows, int k, int8_t *to);
+pconv_i8_plan matmul_i8_plan(int64_t m, int64_t n, int64_t k);
 int launch_matmul_i8(const I8Product &p, void *work, void *stream);
 // Whether rows are so few or so short that they are quantised within the product, and that product (p.a, lda, sa unused).
 bool linear_i8_fused(int64_t m, int64_t n, int64_t k, bool b_at_16);

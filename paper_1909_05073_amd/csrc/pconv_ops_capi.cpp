@@ -225,6 +225,14 @@ int pconv_linear_i8(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, co
     return launch_matmul_i8(p, rest, hip_stream);
 }
 
+int pconv_debug_i8_plan(int64_t m, int64_t n, int64_t k, pconv_i8_plan *out)
+{
+    if (!out) return invalid("pconv_debug_i8_plan", "null pointer argument");
+    if (!sizes_fit(m, n, k)) return invalid("pconv_debug_i8_plan", "m and n must be 1 .. 2^30, k 0 .. 131071");
+    *out = matmul_i8_plan(m, n, k);
+    return PCONV_OK;
+}
+
 int64_t pconv_grad_workspace(int64_t num)
 {
     // one sum for the total, and those of the launches: of kGradBlocks workgroups together, at least 64 each
