@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
-import operator
+import importlib
 import os
 
 import numpy as np
@@ -583,6 +583,20 @@ def _share(a, b) -> bool:
     return bool(((j < others) & (to + j * apart < starts + size)).any())
 
 
+_tensors_module = None
+
+
+def _tensor_list_calls():
+    """csrc/pconv_tensors.cpp, what is asked of many tensors at once (built as lib() is)."""
+    global _tensors_module
+    if _tensors_module is None:
+        import torch                                     # noqa: F401  (its libraries, which the module needs)
+        if not os.path.exists(_build.TENSORS):
+            _build.build_tensors()
+        _tensors_module = importlib.import_module("._tensors", __name__)
+    return _tensors_module
+
+
 def _refuse_overlap(out, *inputs):
     """out and each of the inputs: (tensor or None, rows, columns, elements from row to row)."""
     run = lambda t, rows, columns, step: (t.data_ptr(), rows, columns * t.element_size(), step * t.element_size())
@@ -590,18 +604,6 @@ def _refuse_overlap(out, *inputs):
     for i in inputs:
         if i[0] is not None and _share(to, run(*i)):
             raise ValueError("out must not overlap an input")
-
-
-_increment_version = None
-
-
-def _changed(tensors):
-    """Tells autograd that the tensors (a list) hold other values now, as torch's own calls in place do."""
-    global _increment_version
-    if _increment_version is None:
-        import torch
-        _increment_version = getattr(torch._C, "_increment_version", None) or torch.autograd.graph.increment_version
-    _increment_version(tensors)
 
 
 def pconv_quantize_rows(x_ptr: int, x_stride: int, x_dtype, rows: int, cols: int, q_ptr: int, q_stride: int,
@@ -701,7 +703,7 @@ def matmul_i8(a, a_scale, b, b_scale, bias=None, relu: bool = False, out_dtype=N
     if rc != OK:
         _check(rc)
     if out is not None:
-        _changed([y])
+        _tensor_list_calls().changed([y])
     return y
 
 
@@ -737,7 +739,7 @@ def linear_i8(x, w, w_scale, bias=None, relu: bool = False, out_dtype=None, out=
     if rc != OK:
         _check(rc)
     if out is not None:
-        _changed([y])
+        _tensor_list_calls().changed([y])
     return y
 
 
@@ -771,9 +773,6 @@ def _dense(t) -> bool:
     return True
 
 
-_bytes_of = operator.attrgetter("nbytes")
-
-
 class GradList:
     """The gradients of a network's tensors, to be measured and limited together.
 
@@ -781,10 +780,9 @@ class GradList:
     the limited gradients go, a tensor of the same shape and strides, fp32 or bf16, for each; without it they are
     changed in place.
 
-    The list keeps the tensors.  Every call looks up where they lie and how many bytes they have, so that tensors that
-    were given other memory (`data`, `set_`, `resize_`) are followed there; a tensor that stays where it is keeps its type
-    and its order of dimensions.  Gradients that are replaced by other tensors, as zero_grad(set_to_none=True), torch's
-    default, does, need a new list: this one goes on limiting the old ones."""
+    The list keeps the tensors.  Every call looks whether one of them was given other memory, sizes or another type (`data`,
+    `set_`, `resize_`), and follows it there.  Gradients that are replaced by other tensors, as
+    zero_grad(set_to_none=True), torch's default, does, need a new list: this one goes on limiting the old ones."""
 
     def __init__(self, grads, out=None):
         self.grads = list(grads)
@@ -801,18 +799,9 @@ class GradList:
         made._lay_out()
         return made
 
-    def _places(self):
-        """Address and bytes of every tensor.  (Looked up by every call: 0.1 us a tensor.)"""
-        grads, outs, address_of = self.grads, self.out, self._address_of
-        if outs is grads:
-            return [*map(address_of, grads), *map(_bytes_of, grads)]
-        return [*map(address_of, grads), *map(_bytes_of, grads), *map(address_of, outs), *map(_bytes_of, outs)]
-
     def _lay_out(self):
         """Checks the tensors, and writes down where they lie as the library takes it."""
-        import torch
         self._at = None                                  # (until all of them are found right)
-        self._address_of = torch.Tensor.data_ptr
         grads, outs = self.grads, self.out
         if len(outs) != len(grads):
             raise ValueError("out must hold a tensor for each gradient")
@@ -833,7 +822,8 @@ class GradList:
         if self._writes:
             self._refuse_overlaps(types, out_types)
         self._size = lib().pconv_grad_workspace(num)
-        self._at = self._places()
+        self._tensors = _tensor_list_calls()
+        self._at = self._tensors.places(grads, outs)
 
     def _refuse_overlaps(self, types, out_types):
         """No output may lie over another one, or over a gradient that is not its own."""
@@ -853,7 +843,7 @@ class GradList:
 
     def _begin(self):
         import torch
-        if self._places() != self._at:
+        if self._tensors.places(self.grads, self.out) != self._at:
             self._lay_out()
         if self._num == 0:
             raise ValueError("the list is empty")
@@ -880,7 +870,7 @@ class GradList:
                                               _stream(self._index))
         if rc != OK:
             _check(rc)
-        _changed(self.out)
+        self._tensors.changed(self.out)
         return norm
 
 

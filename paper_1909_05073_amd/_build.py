@@ -1,12 +1,16 @@
-"""Build the HIP library in-tree: paper_1909_05073_amd/libpconv.so (gfx950 only)."""
+"""Build in-tree the HIP library, paper_1909_05073_amd/libpconv.so (gfx950 only), and the binding's look at torch's tensors,
+_tensors.so (host code)."""
+import importlib.util
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpconv.so")
+TENSORS = os.path.join(HERE, "_tensors.so")
 SOURCES = ["pconv_capi.cpp", "pconv_pack.cpp", "pconv_kernels.hip", "pconv_tiled.hip", "pconv_lone.hip",
            "pconv_mfma.hip", "pconv_mfma_flat.hip", "pconv_ops_capi.cpp", "pconv_i8.hip", "pconv_grads.hip"]
 
@@ -37,7 +41,20 @@ def _run(cmd):
         raise RuntimeError("build step failed: " + " ".join(cmd))
 
 
+def build_tensors(verbose: bool = False) -> str:
+    torch = importlib.util.find_spec("torch").submodule_search_locations[0]
+    # (torch's libraries are in the process already when it is loaded)
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-isystem", os.path.join(torch, "include"),
+           "-isystem", os.path.join(torch, "include", "torch", "csrc", "api", "include"), "-isystem", sysconfig.get_paths()["include"],
+           os.path.join(CSRC, "pconv_tensors.cpp"), "-o", TENSORS, "-L", os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    if verbose:
+        print(" ".join(cmd))
+    _run(cmd)
+    return TENSORS
+
+
 def build(verbose: bool = False) -> str:
+    build_tensors(verbose)
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     objs = []
     gen_dir = os.path.join(HERE, "_build", "gen")

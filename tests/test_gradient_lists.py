@@ -54,9 +54,10 @@ def changes():
     yield "first part", lambda t: setattr(t, "data", t.data[:11])
     yield "storage", lambda t: (t.untyped_storage().resize_(0), t.untyped_storage().resize_(4 * 60))
     yield "type", lambda t: setattr(t, "data", torch.ones(60, dtype=torch.bfloat16))
+    yield "type of the same bytes", lambda t: setattr(t, "data", t.data.view(torch.bfloat16))
 
 
-@pytest.mark.parametrize("which", range(7))
+@pytest.mark.parametrize("which", range(8))
 @pytest.mark.parametrize("side", ["in place", "gradient and output"])
 def test_tensors_with_other_memory_are_seen(notes, which, side):
     import torch
@@ -77,6 +78,29 @@ def test_tensors_with_other_memory_are_seen(notes, which, side):
         if to is not None:
             want = outs or grads
             assert to == [o.data_ptr() for o in want] and out_types == [P.BF16 if o.dtype == torch.bfloat16 else P.F32 for o in want], name
+
+
+def test_another_order_of_dimensions_than_the_outputs_is_seen(notes):
+    import torch
+    grads, outs = [torch.ones(6, 10)], [torch.zeros(6, 10)]
+    plan = P.GradList(grads, outs)
+    grads[0].t_()
+    with pytest.raises(ValueError, match="shape and the strides"):
+        plan.clip(1.0)
+    outs[0].t_()
+    plan.clip(1.0)
+    assert len(notes) == 1
+
+
+def test_what_is_no_tensor_is_refused(notes):
+    import torch
+    plan = P.GradList([torch.ones(5)])
+    plan.grads[0] = None
+    for call in (plan.norm, lambda: P._tensor_list_calls().places((torch.ones(2),)), lambda: P._tensor_list_calls().places([3]),
+                 lambda: P._tensor_list_calls().changed(torch.ones(2)), lambda: P._tensor_list_calls().changed([torch.ones(2), None])):
+        with pytest.raises(TypeError):
+            call()
+    assert notes == []
 
 
 def test_other_tensors_in_the_list_are_seen(notes):
