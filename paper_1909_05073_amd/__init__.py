@@ -1,4 +1,4 @@
-"""Thin Python binding of the PCONV HIP library (argument marshalling only).
+"""Thin Python binding of the PCONV HIP library (argument marshalling and checks only).
 
 Every step of the path - analysis, reorder, compact storage (pconv_pack) and the sparse
 convolution (pconv_conv2d) - runs inside libpconv.so; PyTorch appears only as the owner of
@@ -455,6 +455,8 @@ def maxpool2x2(x, layout="nchw"):
 
 
 # ---- layers in 8-bit integers ------------------------------------------------------------
+#
+# They serve networks that are trained: nothing is recorded for autograd, and results ask for no gradient whatever the inputs do.
 
 _types = {}                                          # torch's types to the library's; filled by the first call
 
@@ -657,7 +659,7 @@ def _at_16(ptr: int, step: int) -> bool:
 def quantize_rows(x):
     """x: CUDA tensor [..., k], fp32 or bf16.  Returns (q [..., k] int8, scale [...] fp32): x is about q * scale[..., None].
 
-    The rows of q lie a multiple of 16 bytes apart, as matmul_i8 and linear_i8 read them fastest."""
+    The rows of q lie a multiple of 16 bytes apart, as matmul_i8 and linear_i8 read them fastest.  Nothing is recorded for autograd."""
     import torch
     dtype = _type_of(x, "x")
     index = _device_index(x)
@@ -677,7 +679,8 @@ def matmul_i8(a, a_scale, b, b_scale, bias=None, relu: bool = False, out_dtype=N
     """a [..., k], b [n, k]: int8 CUDA tensors.  Returns act((a @ b.T) * a_scale[..., None] * b_scale + bias) [..., n].
 
     a_scale [...], b_scale [n], bias [n]: fp32.  out_dtype: torch.float32 (unless `out` says otherwise) or torch.bfloat16.
-    out: where the result goes; it must not overlap an input (its rows may lie between those of one)."""
+    out: where the result goes; it must not overlap an input (its rows may lie between those of one).  Nothing is recorded for
+    autograd."""
     import torch
     if a.dtype != torch.int8 or b.dtype != torch.int8 or b.dim() != 2:
         raise ValueError("a [..., k] and b [n, k] must be int8")
@@ -711,7 +714,7 @@ def linear_i8(x, w, w_scale, bias=None, relu: bool = False, out_dtype=None, out=
     """x [..., k]: CUDA tensor, fp32 or bf16; w [n, k] int8 and w_scale [n] as quantize_rows gives them for the weights.
 
     Returns matmul_i8(*quantize_rows(x), w, w_scale, bias, relu) [..., n], of x's type unless `out_dtype` or `out` says
-    otherwise.  out: as there."""
+    otherwise.  out: as there.  Nothing is recorded for autograd."""
     import torch
     x_type = _type_of(x, "x")
     if w.dtype != torch.int8 or w.dim() != 2:
@@ -782,7 +785,8 @@ class GradList:
 
     The list keeps the tensors.  Every call looks whether one of them was given other memory, sizes or another type (`data`,
     `set_`, `resize_`), and follows it there.  Gradients that are replaced by other tensors, as
-    zero_grad(set_to_none=True), torch's default, does, need a new list: this one goes on limiting the old ones."""
+    zero_grad(set_to_none=True), torch's default, does, need a new list: this one goes on limiting the old ones.  (To make
+    one takes some 1 us a tensor.)"""
 
     def __init__(self, grads, out=None):
         self.grads = list(grads)

@@ -1,14 +1,15 @@
 // The norm of the gradients of many tensors together, and their scaling where it passes a limit.
 //
 // norm = sqrt(sum g^2), out = g * min(1, max_norm / (norm + eps)).  Two passes, because no element can be scaled
-// before the last one is summed; both are bound by memory (three operations an element).  A launch takes the
-// tensors' addresses in its arguments, so a step needs no table in device memory.  The tensors are cut into chunks; the workgroups
-// of the first pass take every gridDim-th chunk, those of the second one chunk each.
+// before the last one is summed; both are bound by memory (three operations an element).  A launch takes the tensors'
+// addresses in its arguments, so a step needs no table in device memory.  The tensors are cut into chunks; the
+// workgroups of the first pass take every gridDim-th chunk, those of the second one chunk each.
 //
-// Up to 128 MB of elements and outputs are left in the caches (87 MB 25.9 us, 28 with stores past them; 216 MB 73 and 60).  Of
-// more, the first pass reads past the caches all but the last 192 MB, which the second pass, from the last chunk to the first,
-// finds in the 256 MB memory-side cache; its stores pass the caches too.  138 million fp32 elements: first pass 87 us (6.4 TB/s;
-// 129 where the caches were left full of outputs), second 186 us (206 with nothing kept).
+// Up to 128 MB of elements and outputs are left in the caches (87 MB 25.9 us, 28 with stores past them; 216 MB 73 and
+// 60).  Of more, the first pass reads past the caches all but the last 192 MB, which the second pass, from the last
+// chunk to the first, finds in the 256 MB memory-side cache; its stores pass the caches too.  138 million fp32
+// elements: first pass 86 us (6.4 TB/s; 129 where the caches were left full of outputs), second 190 us (206 with
+// nothing kept).
 #include <hip/hip_runtime.h>
 
 #include "pconv_internal.h"
@@ -84,8 +85,8 @@ __device__ __forceinline__ void store_at(E *p, V v)
     else __builtin_memcpy(p, &v, sizeof(V));
 }
 
-// Squares are formed and summed in fp64: exact up to the sum's rounding, and no fp32 gradient overflows it.  AT_ONCE vectors of 16
-// bytes are under way together.
+// Squares are formed and summed in fp64: exact up to the sum's rounding, and no fp32 gradient overflows it.  AT_ONCE
+// vectors of 16 bytes are under way together.
 template <int THREADS, typename V, typename E, bool PASSING>
 __device__ __forceinline__ double sum_squares(const E *p, uint32_t n, uint32_t tid)
 {
@@ -228,7 +229,8 @@ grad_scale_kernel(const GradTable t, const double *__restrict__ partials, uint32
         chunk_scale<kThreads, PASSING>(find_chunk(t, t.chunks - 1 - c), f, threadIdx.x);
 }
 
-// Few elements: one workgroup, whose waves take the chunks in turn, does both passes (2320 elements 4.9 us, two kernels 3.1 and 3.8).
+// Few elements: one workgroup, whose waves take the chunks in turn, does both passes (2320 elements 4.7 us, two
+// kernels 3.1 and 3.8).
 __global__ void __launch_bounds__(1024)
 grad_clip_one_kernel(const GradTable t, float max_norm, float eps, float *norm)
 {

@@ -240,8 +240,8 @@ __device__ __forceinline__ v4i load16(const int8_t *row, int at, int len)
     return v;
 }
 
-// 16 bytes at an address of any alignment, as the five words that hold them.  (A load of 16 bytes that is not aligned to a word takes 2.6 times one that
-// is: 6x17360 -> 562 31 us and 16.)  No word is read that holds none of the bytes.
+// 16 bytes at an address of any alignment, as the five words that hold them.  (A load of 16 bytes that is not aligned
+// to a word takes 2.6 times one that is: 6x17360 -> 562 31 us and 16.)  No word is read that holds none of the bytes.
 __device__ __forceinline__ v4i load16_loose(const int8_t *p)
 {
     const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(p)) & 3u;
@@ -271,11 +271,11 @@ __device__ __forceinline__ void realign(const Realign &a, int64_t thread, int64_
     }
 }
 
-// TPR threads of a workgroup share a row; each keeps its first KEEP vectors of 16 bytes in registers between finding the
-// row's scale and quantising, and reads what lies beyond (from a cache) twice.  [cols, q_cols) is filled with zeros.
-// The workgroups from `blocks` on bring the rows of a product's weights to multiples of 16 bytes meanwhile (a launch less).
-// Code that runs is kept short: a launch of one wave's work a SIMD spends its time on fetching instructions.  Bound by memory: 8192x4096
-// bf16 20 us, 5.0 TB/s.
+// TPR threads of a workgroup share a row; each keeps its first KEEP vectors of 16 bytes in registers between finding
+// the row's scale and quantising, and reads what lies beyond (from a cache) twice.  [cols, q_cols) is filled with
+// zeros.  The workgroups from `blocks` on bring the rows of a product's weights to multiples of 16 bytes meanwhile (a
+// launch less).  Code that runs is kept short: a launch of one wave's work a SIMD spends its time on fetching
+// instructions.  Bound by memory: 8192x4096 bf16 20 us, 5.0 TB/s.
 template <typename T, int TPR, int KEEP, int THREADS, bool PASSING>
 __global__ void __launch_bounds__(THREADS)
 quantize_rows_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int64_t cols, int8_t *__restrict__ q, int64_t ldq,
@@ -371,9 +371,10 @@ __device__ __forceinline__ void store_channels(const I8Product &p, int m, int n,
     }
 }
 
-// How a wave's channels are dealt to the first operand's rows: a lane gets four of each matrix instruction's sixteen, and Deal::G
-// instructions' fours are neighbours, so that 16 bytes are stored at once and four lanes store 64 (fp32: 4 channels,
-// bf16: 8).  row(j, r): channel of row r of instruction j; first(j, g): first of the four that lanes 16 g .. hold.
+// How a wave's channels are dealt to the first operand's rows, so that 16 bytes are stored at once and four lanes store
+// 64: a lane gets four of each matrix instruction's sixteen, which are 16 bytes of fp32; of bf16 the fours of two
+// instructions are neighbours.  row(j, r): channel of row r of instruction j; first(j, g): first of the four that lanes
+// 16 g .. hold.
 template <typename Y> struct Deal;
 template <> struct Deal<float> {
     static constexpr int SH = 2;                         // (bits 0, 1 and SH of a row tell eight rows r apart)
@@ -386,8 +387,8 @@ template <> struct Deal<__bf16> {
     static __device__ __forceinline__ int first(int j, int g) { return (j >> 1) * 32 + g * 8 + (j & 1) * 4; }
 };
 
-// Rows m + 16 i of y, the NT * 16 channels from n0 on; the lane has `lane & 15` in m and its group in `g`.  Scales and biases are
-// read before anything is stored: behind a store they would be waited for one by one.
+// Rows m + 16 i of y, the NT * 16 channels from n0 on; the lane has `lane & 15` in m and its group in `g`.  Scales
+// and biases are read before anything is stored: behind a store they would be waited for one by one.
 template <typename Y, int NT, bool EXACT = false>
 __device__ __forceinline__ void load_channels(const I8Product &p, int n0, int g, Channels (&c)[NT])
 {
@@ -431,9 +432,9 @@ __device__ __forceinline__ v4u buffer_at(const int8_t *p)
 }
 constexpr uint32_t kNowhere = 0xC0000000u;               // beyond the buffer, whatever is added: nothing is read, LDS gets zeros
 
-// Which tile a workgroup computes.  Workgroups go round the 8 XCDs, each of which has a level-2 cache of its own: an XCD gets
-// a run of tiles, and a run goes down GROUP tiles of rows before it goes on to the next tile of channels, so that the tiles that
-// run at one time on an XCD share rows of both operands.
+// Which tile a workgroup computes.  Workgroups go round the 8 XCDs, each of which has a level-2 cache of its own: an
+// XCD gets a run of tiles, and a run goes down GROUP tiles of rows before it goes on to the next tile of channels, so
+// that the tiles that run at one time on an XCD share rows of both operands.
 __device__ __forceinline__ void tile_at(unsigned id, unsigned tiles_m, unsigned tiles_n, unsigned &tm, unsigned &tn)
 {
     constexpr unsigned XCDS = 8, GROUP = 8;
@@ -444,8 +445,8 @@ __device__ __forceinline__ void tile_at(unsigned id, unsigned tiles_m, unsigned 
     tn = in / rows;
 }
 
-// Waits until at most `behind` (0 .. MOST) stages of L loads each of this wave are under way and its reads of LDS are done, and for
-// the other waves of the workgroup to get there.
+// Waits until at most `behind` (0 .. MOST) stages of L loads each of this wave are under way and its reads of LDS are
+// done, and for the other waves of the workgroup to get there.
 template <int MOST, int L>
 __device__ __forceinline__ void wait_for_stages(int behind)
 {
@@ -457,21 +458,24 @@ __device__ __forceinline__ void wait_for_stages(int behind)
     }
 }
 
-// Tiles of BM rows of y and BN channels, WM x WN waves, and KG such sets of waves that take the stages in turn (a stage takes a wave 0.4 us of
-// waiting for one thing after the other, however far ahead it is loaded).  128 bytes of k of all the tile's rows are a stage; S stages lie in
-// LDS.  A row of a stage is eight pieces of 16 bytes, stored in an order that depends on the row so that the eight rows that are
-// read at once lie in different banks.
+// Tiles of BM rows of y and BN channels, WM x WN waves, and KG such sets of waves that take the stages in turn (a
+// stage takes a wave 0.4 us of waiting for one thing after the other, however far ahead it is loaded).  128 bytes of
+// k of all the tile's rows are a stage; S stages lie in LDS.  A row of a stage is eight pieces of 16 bytes, stored in
+// an order that depends on the row so that the eight rows that are read at once lie in different banks.
 //
-// Stages go from memory to LDS past the registers, S - 1 of them ahead of the one that is multiplied; a wave waits for its own
-// loads of the next stage, and the barrier then tells it that everybody's are there and that the stage before is read.  In
-// the last stage the pieces behind the end of k are zeros.  Where k ends inside a piece the piece is loaded whole (what lies behind it is
-// still before the next row, so the last rows of all go through registers), and the activations' part behind k is cleared in LDS.
-// Rows begin at multiples of 16 bytes (realign_kernel sees to it).
+// Stages go from memory to LDS past the registers, S - 1 of them ahead of the one that is multiplied; a wave waits
+// for its own loads of the next stage, and the barrier then tells it that everybody's are there and that the stage
+// before is read.  In the last stage the pieces behind the end of k are zeros.  Where k ends inside a piece the piece
+// is loaded whole (what lies behind it is still before the next row, so the last rows of all go through registers),
+// and the activations' part behind k is cleared in LDS.  Rows begin at multiples of 16 bytes (realign_kernel sees to
+// it).
 //
-// `splits` workgroups share a tile, each with its part of k; their sums go to `part` [splits][m][n4], n4 = n rounded up to four.
+// `splits` workgroups share a tile, each with its part of k; their sums go to `part` [splits][m][n4], n4 = n rounded
+// up to four.
 //
-// Bound by the matrix units and the clock that the card allows them (8192x4096 -> 4096: 126 us, 2.2 POP/s; zeros 113 us), with few
-// rows by memory (32x25088 -> 4096: 22 us, 4.7 TB/s), with few tiles by a stage's latencies (777x1155 -> 1001: 8.7 us).
+// Bound by the matrix units, which are busy for half of the cycles, and the clock that the card allows them (8192x4096
+// -> 4096: 123 us, 2.2 POP/s, in runs of 117 to 143; zeros 110 us), with few rows by memory (32x25088 -> 4096: 22 us,
+// 4.7 TB/s), with few tiles by a stage's latencies (777x1155 -> 1001: 8.6 us).
 template <typename Y, int BM, int BN, int WM, int WN, int S, int KG>
 __global__ void __launch_bounds__(KG * WM * WN * 64)
 matmul_i8_kernel(const I8Product p, int splits, int *part)
@@ -528,7 +532,7 @@ matmul_i8_kernel(const I8Product p, int splits, int *part)
 
     const v4u at_a = buffer_at(p.a + int64_t(m0) * p.lda + k_begin), at_b = buffer_at(p.b + int64_t(n0) * p.ldb + k_begin);
     uint32_t off_a[PA], off_b[PB];
-    int end_a[PA], end_b[PB];                            // byte of a stage up to which a lane's piece is loaded only if k reaches behind it
+    int end_a[PA], end_b[PB];                            // (a lane's piece is loaded if k reaches behind this byte of the stage)
 #pragma unroll
     for (int i = 0; i < PA; ++i) {
         const int row = (i * NW + wave) * 8 + (lane >> 3);
@@ -634,7 +638,7 @@ matmul_i8_kernel(const I8Product p, int splits, int *part)
     store_tile<Y, MT, NT>(p, m, n0 + wn, g, acc, sa, c);
 }
 
-// Rows of one or two matrices to multiples of 16 bytes (blockIdx.y: which).  1001x1155: 3.6 us.
+// Rows of one or two matrices to multiples of 16 bytes (blockIdx.y: which).  1001x1155: 3.8 us.
 __global__ void __launch_bounds__(256)
 realign_kernel(const Realign a0, const Realign a1)
 {
@@ -661,12 +665,14 @@ matmul_i8_join_kernel(const I8Product p, int splits, const int *__restrict__ par
     }
 }
 
-// Short rows (k up to kThinK): all of k of BM rows of activations lies in LDS, so that there is no loop of stages and one read of the
-// activations; where they come as floats they are quantised on their way there and never leave the chip.
+// Short rows (k up to kThinK): all of k of BM rows of activations lies in LDS, so that there is no loop of stages and
+// one read of the activations; where they come as floats they are quantised on their way there and never leave the
+// chip.
 constexpr int kThinK = 512, kThinLongK = 2048;           // (quantised within the product, and where thin_long() says so)
 constexpr int thin_rows(int ks) { return ks <= 16 ? 64 : 32; }           // rows of a workgroup in whole pieces
 
-// LDS holds rows of PIECES times 16 bytes, whose order makes the 16 lanes that are read at once differ in their places modulo 256 bytes.
+// LDS holds rows of PIECES times 16 bytes, whose order makes the 16 lanes that are read at once differ in their
+// places modulo 256 bytes.
 template <int KS> struct ThinLds {
     static constexpr int PIECES = KS < 2 ? 8 : KS * 4, KEY = PIECES < 16 ? 7 : 15;
     static __device__ __forceinline__ int at(int row, int piece) { return row * PIECES + (piece ^ (row & KEY)); }
@@ -722,13 +728,14 @@ __device__ __forceinline__ void wait_for_loads(int behind)
     }
 }
 
-// Short rows in whole pieces: k a multiple of 16, n of 8, the rows of the weights at multiples of 16 bytes.  Eight waves share
-// 64 rows (32 where k passes 1024), MH sets of them a part of the rows each, and take groups of 32 channels in turn; blockIdx.y: a
-// part of the channels (`part_n`).  The weights, which every workgroup reads and the level-2 caches hold, come in steps of 128 bytes
-// of k of a group's channels (k up to 64: one step, to the registers), past the registers to a ring of D steps in LDS that is
-// the wave's own: no barrier, and eight lanes read 128 bytes of a row together (read as the matrix instruction wants them, no two
-// lanes do, and a quarter of the cache's rate is all there is).  Bound by memory and a workgroup's start and end:
-// 100352x64 -> 256 bf16 15.6 us, 4.1 TB/s.
+// Short rows in whole pieces: k a multiple of 16, n of 8, the rows of the weights at multiples of 16 bytes.  Eight
+// waves share 64 rows (32 where k passes 1024), MH sets of them a part of the rows each, and take groups of 32
+// channels in turn; blockIdx.y: a part of the channels (`part_n`).  The weights, which every workgroup reads and the
+// level-2 caches hold, come in steps of 128 bytes of k of a group's channels (k up to 64: one step, to the
+// registers), past the registers to a ring of D steps in LDS that is the wave's own: no barrier, and eight lanes read
+// 128 bytes of a row together (read as the matrix instruction wants them, no two lanes do, and a quarter of the
+// cache's rate is all there is).  Bound by memory and a workgroup's start and end: 100352x64 -> 256 bf16 15.6 us, 4.1
+// TB/s.
 template <typename T, typename Y, int KS, int MH>
 __global__ void __launch_bounds__(512, KS <= 4 ? 4 : 2)
 linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, int part_n)
@@ -886,8 +893,9 @@ linear_i8_thin_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, i
     }
 }
 
-// Short rows that end inside a piece, or channels inside a store, or weights whose rows do not begin at multiples of 16 bytes: four waves, 32 rows,
-// the weights go to the registers directly, all KS steps of the first channels before the activations are waited for.
+// Short rows that end inside a piece, or channels inside a store, or weights whose rows do not begin at multiples of
+// 16 bytes: four waves, 32 rows, the weights go to the registers directly, all KS steps of the first channels before
+// the activations are waited for.
 template <typename T, typename Y, int KS>
 __global__ void __launch_bounds__(256, KS <= 2 ? 4 : 2)
 linear_i8_thin_ragged_kernel(const I8Product p, const T *__restrict__ x, int64_t ldx, int part_n)
@@ -981,11 +989,12 @@ linear_i8_thin_ragged_kernel(const I8Product p, const T *__restrict__ x, int64_t
     }
 }
 
-// Few rows (up to 16): 16 channels a workgroup, whose waves share the length of k in turns of 256 bytes and add their sums in LDS.
-// Reading the weights is all of it; a wave has the next turns' under way while it multiplies: D > 0, in a ring of its own in LDS, past
-// the registers (rows at multiples of 16 bytes; see linear_i8_thin_kernel), D = 0, in registers.  T is int8_t, or
-// the rows come as floats, up to kFusedRows elements, and every workgroup quantises all of them to LDS while its first weights
-// are on their way: less than a launch for it takes.  Bound by memory: 1x25088 -> 4096 20.5 us, 5.0 TB/s (LONG), 1x2048 -> 1000 4.4 us.
+// Few rows (up to 16): 16 channels a workgroup, whose waves share the length of k in turns of 256 bytes and add their
+// sums in LDS.  Reading the weights is all of it; a wave has the next turns' under way while it multiplies: D > 0, in
+// a ring of its own in LDS, past the registers (rows at multiples of 16 bytes; see linear_i8_thin_kernel), D = 0, in
+// registers.  T is int8_t, or the rows come as floats, up to kFusedRows elements, and every workgroup quantises all
+// of them to LDS while its first weights are on their way: less than a launch for it takes.  Bound by memory: 1x25088
+// -> 4096 20.5 us, 5.0 TB/s (LONG), 1x2048 -> 1000 4.5 us.
 constexpr int kRowsM = 16, kFusedRows = 32768, kRowsMost = 131072;
 
 template <typename T, int D, bool LONG>
@@ -1166,12 +1175,13 @@ int launch_quantize_rows(const void *x, int64_t ldx, int bf16, int64_t rows, int
         if (bf16) { if (once) PCONV_LAUNCH_AS(__bf16, TPR, KEEP, THREADS, true); else PCONV_LAUNCH_AS(__bf16, TPR, KEEP, THREADS, false); } \
         else { if (once) PCONV_LAUNCH_AS(float, TPR, KEEP, THREADS, true); else PCONV_LAUNCH_AS(float, TPR, KEEP, THREADS, false); } \
     } while (0)
-    // Activations that are read once and are more than a part of the caches are read past them, so that they do not push out what the product reads
-    // (8992x9184 -> 280: 143 us without, 133).
+    // Activations that are read once and are more than a part of the caches are read past them, so that they do not
+    // push out what the product reads (8992x9184 -> 280: 143 us without, 133).
     const bool passing = rows * cols * (bf16 ? 2 : 4) > int64_t(64) << 20;
-    // Many rows: two a wave, or one with eight vectors a lane, so that more of them is under way (66 vectors, 100000 bf16 rows 59.7 us by a wave
-    // each and 38.4 so, 1000 rows 3.2 and 3.6; 288 vectors, 50000 fp32 rows 76.1 us by 256 threads and 49.7 by a wave, 1000 rows 3.8 and 4.4).
-    // (1024 threads for a row of 1244 vectors: 7962 rows 107 us, with 256 55; 300 rows 7.8 and 5.5; of 2296: 8992 rows 116 and 94)
+    // Many rows: two a wave, or one with eight vectors a lane, so that more of them is under way (66 vectors, 100000
+    // bf16 rows 59.7 us by a wave each and 38.4 so, 1000 rows 3.2 and 3.6; 288 vectors, 50000 fp32 rows 76.1 us by
+    // 256 threads and 49.7 by a wave, 1000 rows 3.8 and 4.4).  (1024 threads for a row of 1244 vectors: 7962 rows 107
+    // us, with 256 55; 300 rows 7.8 and 5.5; of 2296: 8992 rows 116 and 94)
     if (vecs <= 8) PCONV_LAUNCH(8, 1, 256);
     else if (vecs <= 16) PCONV_LAUNCH(16, 1, 256);
     else if (vecs <= 32) PCONV_LAUNCH(16, 2, 256);
@@ -1221,8 +1231,9 @@ Cut cut_of(int64_t m, int64_t n, int64_t k)
     return best;
 }
 
-// Sets of waves of a workgroup: two, and as many stages as LDS holds, where a compute unit has one workgroup (17x2048 -> 1000: 8.6 us
-// with four stages), else room for two workgroups.  The largest tile fills a compute unit with one set.
+// Sets of waves of a workgroup: two, and as many stages as LDS holds, where a compute unit has one workgroup (17x2048
+// -> 1000: 8.6 us with four stages), else room for two workgroups.  The largest tile fills a compute unit with one
+// set.
 int sets_of(const Cut &c, int64_t tiles) { return c.tile < 3 && tiles * c.splits <= kUnits ? 2 : 1; }
 
 template <int BM, int BN, int WM, int WN, int S, int KG>
@@ -1241,9 +1252,10 @@ int launch_rows(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
     const size_t lds = sizeof(T) > 1 ? size_t(p.m) * ((p.k + 255) / 256 * 256 + 16) : 0;
     if (rows_groups(p.n) > kMaxGroups) return too_many_groups();
     const unsigned grid = unsigned(rows_groups(p.n));
-    // The ring takes 64 KB of LDS: where a compute unit has one workgroup at most, or two fit still (1x25088 -> 1000 18.3 us without it, 12.0;
-    // 2x8192 -> 8192 16.3 and, one workgroup a compute unit with it, 19.6).  There long rows stay in registers between their two
-    // uses (10.9 us; 1x4096 -> 1000 4.8 us with few registers and 5.9; rows that a wave has, 10x3200 -> 1856 fp32 8.8 and 10.5, 10x1168 7.2 and 6.0).
+    // The ring takes 64 KB of LDS: where a compute unit has one workgroup at most, or two fit still (1x25088 -> 1000
+    // 18.3 us without it, 12.0; 2x8192 -> 8192 16.3 and, one workgroup a compute unit with it, 19.6).  There long
+    // rows stay in registers between their two uses (10.9 us; 1x4096 -> 1000 4.8 us with few registers and 5.9; rows
+    // that a wave has, 10x3200 -> 1856 fp32 8.8 and 10.5, 10x1168 7.2 and 6.0).
     if constexpr (sizeof(T) > 1) {
         const bool one = int64_t(grid) <= kUnits;
         if (rows_at_16(p.b, p.ldb) && (one || lds <= 14 * 1024)) {
@@ -1297,15 +1309,16 @@ int launch_thin(const I8Product &p, const T *x, int64_t ldx, hipStream_t st)
 
 }  // namespace
 
-// The kernel for few rows up to kRowsMost activations: each of its workgroups reads all of them (16 rows of 25088: 33.5 us, in tiles
-// 28.6; 4 rows 26.6 and 28.1; 16 rows of 4096 10.0 and 12.2).
+// The kernel for few rows up to kRowsMost activations: each of its workgroups reads all of them (16 rows of 25088:
+// 33.5 us, in tiles 28.6; 4 rows 26.6 and 28.1; 16 rows of 4096 10.0 and 12.2).
 static bool few(int64_t m, int64_t k) { return m <= kRowsM && m * k <= kRowsMost; }
 static bool thin(int64_t m, int64_t k) { return m > kRowsM && k <= kThinK; }
 
-// Rows of up to kThinLongK in whole pieces, quantised within the product as short rows are: one launch, no work space (4.9 us less on the
-// host).  The loads, the quantising and the products of a workgroup follow each other and no other one is there to fill in, so that is
-// right for few rounds of workgroups only: 1000x1024 -> 256 fp32 12.8 us, apart 15.3 (the GPU's part 13.0 and 9.9); 16000x768 -> 256 bf16 15 and 22; 50000x1024 -> 256
-// fp32 86 and 71; above 1024 with 32 rows a workgroup 4000x1536 -> 512 bf16 15 and 18.6, 16000x1536 -> 1024 fp32 73 and 57.
+// Rows of up to kThinLongK in whole pieces, quantised within the product as short rows are: one launch, no work space
+// (4.9 us less on the host).  The loads, the quantising and the products of a workgroup follow each other and no
+// other one is there to fill in, so that is right for few rounds of workgroups only: 1000x1024 -> 256 fp32 12.8 us,
+// apart 15.3 (the GPU's part 13.0 and 9.9); 16000x768 -> 256 bf16 15 and 22; 50000x1024 -> 256 fp32 86 and 71; above
+// 1024 with 32 rows a workgroup 4000x1536 -> 512 bf16 15 and 18.6, 16000x1536 -> 1024 fp32 73 and 57.
 static bool thin_long(int64_t m, int64_t n, int64_t k, bool b_at_16)
 {
     if (m <= kRowsM || k <= kThinK || k > kThinLongK || k % 16 != 0 || n % 8 != 0 || n > 2048 || !b_at_16) return false;

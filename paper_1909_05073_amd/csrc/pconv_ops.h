@@ -26,7 +26,8 @@ struct Realign {
     int rows, k, pieces;
 };
 
-// Launchers: arguments checked, sizes not 0.  They return a pconv_status.  `weights` are brought to multiples of 16 bytes by the same launch.
+// Launchers: arguments checked, sizes not 0.  They return a pconv_status.  `weights` are brought to multiples of 16
+// bytes by the same launch.
 int launch_quantize_rows(const void *x, int64_t ldx, int bf16, int64_t rows, int64_t cols, int8_t *q, int64_t ldq,
                          int64_t q_cols, float *scale, void *stream, const Realign *weights = nullptr);
 // Whether rows begin at multiples of 16 bytes (and a tile's lie within 32 bits); the work space of a product (copies of
@@ -54,7 +55,7 @@ struct GradTable {
     uint16_t types[kGradTensors];      // bit 0: input bf16, bit 1: output bf16
     int32_t count, log2;
     uint32_t chunks;
-    uint32_t passing;                  // the first pass reads chunks below this one past the caches (the second all, with `passing`)
+    uint32_t passing;                  // the first pass reads the chunks below this one past the caches
 };
 int launch_grad_norm(const GradTable &t, unsigned blocks, double *partials, void *stream);
 int launch_grad_total(const double *partials, unsigned count, double *total, float *norm, void *stream);

@@ -79,7 +79,8 @@ Grads grads_of(const void *const *in, void *const *out, const int64_t *counts, c
         many += (n + (1 << kGradLog2) - 1) >> kGradLog2;
     }
     // One workgroup for up to two chunks a wave (a launch less on the host: 2.4 us); chunks of 4096 elements while
-    // those of 16384 would not be one for each compute unit (where they are, finding a chunk's tensor costs more than it gives).
+    // those of 16384 would not be one for each compute unit (where they are, finding a chunk's tensor costs more than
+    // it gives).
     if (out && num <= kGradTensors && ones <= 32) { g.log2 = kGradLog2One; g.chunks = ones; }
     else if (elements < int64_t(256) << kGradLog2) { g.log2 = kGradLog2Few; g.chunks = few; }
     else { g.log2 = kGradLog2; g.chunks = many; }
@@ -274,8 +275,8 @@ int pconv_clip_grads(const void *const *grads, void *const *outs, const int64_t 
     double *const sums = static_cast<double *>(work);
     unsigned count;
     if (const int rc = sum_squares(g, sums, hip_stream, count)) return rc;
-    // Every workgroup of the second pass adds the partial sums by itself; with several tables or many workgroups one launch for it takes
-    // less.  (Also for nothing at all: the norm is 0.)
+    // Every workgroup of the second pass adds the partial sums by itself; with several tables or many workgroups one
+    // launch for it takes less.  (Also for nothing at all: the norm is 0.)
     const bool total = g.tables() != 1 || count == 0 || g.chunks > 2 * kGradBlocks;
     if (total)
         if (const int rc = launch_grad_total(sums + 1, count, sums, norm_dev, hip_stream)) return rc;

@@ -1,8 +1,10 @@
-// What the binding asks of many of torch's tensors at once; in Python each question takes 0.05 us a tensor, here 0.01.
+// What the binding asks of many of torch's tensors at once; in Python each question takes 0.05 us a tensor, here
+// 0.01.
 //
-// places(list, ..) -> bytes: where the tensors of the lists lie, and as what: for each its address, type, number of dimensions, sizes and
-// steps, as words of 64 bits, so that two calls give equal bytes exactly if nothing of that has changed.  For lists of tensors that
-// are kept from call to call: torch tells nobody that a tensor was given other memory.
+// places(list, ..) -> bytes: where the tensors of the lists lie, and as what: for each its address, type, number of
+// dimensions, sizes and steps, as words of 64 bits, so that two calls give equal bytes exactly if nothing of that has
+// changed.  For lists of tensors that are kept from call to call: torch tells nobody that a tensor was given other
+// memory.
 //
 // changed(list): autograd is told that the tensors hold other values now, as torch's own calls in place do.
 #include <Python.h>
