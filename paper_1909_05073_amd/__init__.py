@@ -695,7 +695,7 @@ def matmul_i8(a, a_scale, b, b_scale, bias=None, relu: bool = False, out_dtype=N
     y_type = _type_of(y, "out")
     sa, sb = _per_channel(a_scale, m, "a_scale"), _per_channel(b_scale, n, "b_scale")
     bp = _per_channel(bias, n, "bias") if bias is not None else None
-    if out is not None:
+    if out is not None and not _tensor_list_calls().apart(y, a, b, a_scale, b_scale, bias):
         _refuse_overlap((y, m, n, y_step), (a, m, k, a_step), (b, n, k, b_step), (a_scale, 1, m, m), (b_scale, 1, n, n), (bias, 1, n, n))
     a_ptr, b_ptr = a.data_ptr(), b.data_ptr()
     size = _matmul_i8_workspace(m, n, k, _at_16(a_ptr, a_step) and _at_16(b_ptr, b_step))
@@ -731,7 +731,7 @@ def linear_i8(x, w, w_scale, bias=None, relu: bool = False, out_dtype=None, out=
         y_type = _type_of(y, "out")
     sw = _per_channel(w_scale, n, "w_scale")
     bp = _per_channel(bias, n, "bias") if bias is not None else None
-    if out is not None:
+    if out is not None and not _tensor_list_calls().apart(y, x, w, w_scale, bias):
         _refuse_overlap((y, m, n, y_step), (x, m, k, x_step), (w, n, k, w_step), (w_scale, 1, n, n), (bias, 1, n, n))
     w_ptr = w.data_ptr()
     size = _linear_i8_workspace(m, n, k, _at_16(w_ptr, w_step))

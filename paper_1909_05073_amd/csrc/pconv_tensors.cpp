@@ -7,6 +7,9 @@
 // memory.
 //
 // changed(list): autograd is told that the tensors hold other values now, as torch's own calls in place do.
+//
+// apart(tensor, tensor or None, ..) -> bool: whether the first shares no byte with the others because the runs of memory from
+// their first elements to their last ones share none.
 #include <Python.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -74,7 +77,41 @@ PyObject *changed(PyObject *, PyObject *list)
     Py_RETURN_NONE;
 }
 
-PyMethodDef methods[] = {{"places", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(places)), METH_FASTCALL, nullptr},
+// [first byte, behind the last one); of an empty tensor nothing.
+struct Run { uintptr_t from, to; };
+
+Run run_of(const at::Tensor &t)
+{
+    if (t.numel() == 0) return Run{0, 0};
+    int64_t last = 0;
+    for (int64_t d = 0; d < t.dim(); ++d) last += (t.size(d) - 1) * t.stride(d);
+    const uintptr_t from = reinterpret_cast<uintptr_t>(t.const_data_ptr());
+    return Run{from, from + uintptr_t(last + 1) * uintptr_t(t.itemsize())};
+}
+
+PyObject *apart(PyObject *, PyObject *const *args, Py_ssize_t count)
+{
+    try {
+        Run first{0, 0};
+        for (Py_ssize_t i = 0; i < count; ++i) {
+            if (i > 0 && args[i] == Py_None) continue;
+            if (!THPVariable_Check(args[i])) {
+                PyErr_SetString(PyExc_TypeError, "tensors are wanted");
+                return nullptr;
+            }
+            const Run r = run_of(THPVariable_Unpack(args[i]));
+            if (i == 0) first = r;
+            else if (r.from < first.to && first.from < r.to) Py_RETURN_FALSE;
+        }
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+    Py_RETURN_TRUE;
+}
+
+PyMethodDef methods[] = {{"apart", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(apart)), METH_FASTCALL, nullptr},
+                         {"places", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(places)), METH_FASTCALL, nullptr},
                          {"changed", changed, METH_O, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

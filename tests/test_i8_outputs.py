@@ -134,3 +134,17 @@ def test_outputs_between_the_rows_of_the_activations():
         assert torch.equal(room[:, :k], was)
     with pytest.raises(ValueError, match="overlap"):
         P.linear_i8(room[:, :k], w, sb, bias, out=room[:, k - n:k])
+
+
+def test_runs_of_memory_that_share_no_byte_are_apart():
+    import torch
+    apart = P._tensor_list_calls().apart
+    flat = torch.zeros(100)
+    out = flat[20:40].view(4, 5)
+    assert apart(out, flat[:20], None, flat[40:], torch.zeros(7), flat[20:20])
+    assert not apart(out, flat[:21]) and not apart(out, None, flat[39:]) and not apart(out, out) and not apart(out, flat.view(torch.int8)[159:160])
+    assert apart(flat[:80].view(4, 20)[:, 5:10], flat[70:]) and not apart(flat[:80].view(4, 20)[:, 5:10], flat[69:70])
+    assert apart(out[:0], flat) and apart(flat[:0], flat)
+    for wrong in ((out, 3), (None, out)):
+        with pytest.raises(TypeError):
+            apart(*wrong)
