@@ -249,6 +249,52 @@ int pconv_linear_i8(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, co
                     const float *w_scale, const float *bias_dev, void *y_dev, int64_t y_stride, pconv_dtype y_dtype,
                     int64_t m, int64_t n, int64_t k, int fuse_relu, void *work, int64_t work_bytes, void *hip_stream);
 
+/* ---- layers in 4-bit floats ----------------------------------------------------------------------
+ *
+ * The same layers with weights of half the bytes.  32 neighbouring values of a row are a block, which has one power of two as
+ * its scale:
+ *
+ *   scale[r][b] = 2^X,  X = floor(log2(max_k |x[r][k]|)) - 2 over the k of block b, cut to -127 .. 127
+ *   q[r][k]     = the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives to x[r][k] / scale[r][b], ties to the even code
+ *   y[r][o]     = act( sum_b scale[r][b] w_scale[o][b] sum_(k in b) q[r][k] * w[o][k]  + bias[o] )
+ *
+ * A value's code is its place in that list, plus 8 where it is negative (also for a negative value that becomes 0); the lower half of
+ * a byte holds the first of two.  A row is ceil(k / 32) blocks of 16 bytes, zeros behind its k values.  A scale is a byte,
+ * X + 127, 255 standing for NaN; scales lie in slabs of 8 blocks, [ceil(k / 256)][rows][8]; behind a row's last block
+ * pconv_quantize_mx4 writes zeros, and the products take whatever is there.
+ * A block of zeros has scale byte 0; one that holds an infinity or a NaN has 255 and zeros, so that all the row's outputs are
+ * NaN.  Sums are fp32, those of parts of k that workgroups share added in a fixed order: the same bits from run to run.
+ *
+ * Rows of q begin at multiples of 16 bytes and lie a multiple of 16 bytes apart, at least their length and at most 8 MiB; a slab
+ * lies a multiple of 8 bytes, at least 8 for each row, behind the one before it, and begins at a multiple of 8 bytes.  Rows of x
+ * and y as above.  A size of 0 is legal.  All calls are asynchronous on hip_stream, allocate nothing, keep nothing from one
+ * call to the next.  Outputs must not overlap inputs.  A call whose size needs more than 2^32 threads gives PCONV_UNSUPPORTED.
+ *
+ * pconv_quantize_mx4 - q and scale of x [rows][cols], fp32 or bf16; weights by the same call, one row for each output channel.
+ * q_stride and slab_stride in bytes; cols up to 2^24. */
+int pconv_quantize_mx4(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, int64_t rows, int64_t cols,
+                       uint8_t *q_dev, int64_t q_stride, uint8_t *scale_dev, int64_t slab_stride, void *hip_stream);
+
+/* pconv_matmul_mx4 - y [m][n] of a [m][blocks] and b [n][blocks] with their scales, and bias [n] (or NULL); y is fp32, or bf16
+ * rounded to nearest even.  Strides of a, b and their slabs in bytes, of y in elements.  `work`: device memory of at
+ * least pconv_matmul_mx4_workspace bytes (often 0), aligned to 16 bytes, used in stream order until the call's work is done, its
+ * contents are lost.  m and n up to 2^30, blocks up to 2^19.
+ * Errors: PCONV_INVALID_ARG (null pointers, sizes, strides or alignments out of range, too little work space),
+ * PCONV_UNSUPPORTED, PCONV_HIP_ERROR (launch failed). */
+int64_t pconv_matmul_mx4_workspace(int64_t m, int64_t n, int64_t blocks);
+int pconv_matmul_mx4(const uint8_t *a_dev, int64_t a_stride, const uint8_t *a_scale, int64_t a_slab, const uint8_t *b_dev,
+                     int64_t b_stride, const uint8_t *b_scale, int64_t b_slab, const float *bias_dev, void *y_dev,
+                     int64_t y_stride, pconv_dtype y_dtype, int64_t m, int64_t n, int64_t blocks, int fuse_relu, void *work,
+                     int64_t work_bytes, void *hip_stream);
+
+/* pconv_linear_mx4 - pconv_quantize_mx4 of x [m][k] and pconv_matmul_mx4 with the weights w [n][ceil(k / 32)], in one call; k up
+ * to 2^24.  The quantised activations stay in the work space, or on the chip. */
+int64_t pconv_linear_mx4_workspace(int64_t m, int64_t n, int64_t k);
+int pconv_linear_mx4(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, const uint8_t *w_dev, int64_t w_stride,
+                     const uint8_t *w_scale, int64_t w_slab, const float *bias_dev, void *y_dev, int64_t y_stride,
+                     pconv_dtype y_dtype, int64_t m, int64_t n, int64_t k, int fuse_relu, void *work, int64_t work_bytes,
+                     void *hip_stream);
+
 /* ---- gradients of a training step ---------------------------------------------------------------
  *
  * Pruning (pconv_project between the steps of a training loop) moves weights at once; the gradients of the next step are
@@ -391,6 +437,12 @@ typedef struct {
 } pconv_i8_plan;
 
 int pconv_debug_i8_plan(int64_t m, int64_t n, int64_t k, pconv_i8_plan *out);
+
+/* pconv_debug_mx4_plan - the same of pconv_matmul_mx4: kernel 1 (few rows) or 2 (tiles).  PCONV_INVALID_ARG for sizes that
+ * are not 1 .. 2^30 (blocks: 0 .. 2^19) or a null pointer. */
+typedef struct { int32_t kernel, tile_m, tile_n, sets, splits; } pconv_mx4_plan;
+
+int pconv_debug_mx4_plan(int64_t m, int64_t n, int64_t blocks, pconv_mx4_plan *out);
 
 /* pconv_debug_set_spin_limit - for tests of the error path: the number of polls after which a
  * wait inside the register-tiled kernel gives up (limit <= 0 restores the default, about half a

@@ -46,6 +46,10 @@ class pconv_i8_plan(C.Structure):
     _fields_ = [("kernel", C.c_int32), ("tile_m", C.c_int32), ("tile_n", C.c_int32), ("sets", C.c_int32), ("splits", C.c_int32)]
 
 
+class pconv_mx4_plan(C.Structure):
+    _fields_ = [("kernel", C.c_int32), ("tile_m", C.c_int32), ("tile_n", C.c_int32), ("sets", C.c_int32), ("splits", C.c_int32)]
+
+
 _lib = None
 
 
@@ -124,6 +128,18 @@ def lib():
     L.pconv_linear_i8.argtypes = [vp, i64, ip, vp, i64, vp, vp, vp, i64, ip, i64, i64, i64, ip, vp, i64, vp]
     L.pconv_debug_i8_plan.restype = ip
     L.pconv_debug_i8_plan.argtypes = [i64, i64, i64, vp]
+    L.pconv_quantize_mx4.restype = ip
+    L.pconv_quantize_mx4.argtypes = [vp, i64, ip, i64, i64, vp, i64, vp, i64, vp]
+    L.pconv_matmul_mx4_workspace.restype = i64
+    L.pconv_matmul_mx4_workspace.argtypes = [i64, i64, i64]
+    L.pconv_matmul_mx4.restype = ip
+    L.pconv_matmul_mx4.argtypes = [vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, i64, ip, i64, i64, i64, ip, vp, i64, vp]
+    L.pconv_linear_mx4_workspace.restype = i64
+    L.pconv_linear_mx4_workspace.argtypes = [i64, i64, i64]
+    L.pconv_linear_mx4.restype = ip
+    L.pconv_linear_mx4.argtypes = [vp, i64, ip, vp, i64, vp, i64, vp, vp, i64, ip, i64, i64, i64, ip, vp, i64, vp]
+    L.pconv_debug_mx4_plan.restype = ip
+    L.pconv_debug_mx4_plan.argtypes = [i64, i64, i64, vp]
     L.pconv_grad_workspace.restype = i64
     L.pconv_grad_workspace.argtypes = [i64]
     L.pconv_grad_norm.restype = ip
@@ -143,7 +159,9 @@ EXPORTED_SYMBOLS = ["pconv_project", "pconv_pack", "pconv_conv2d", "pconv_conv2d
                     "pconv_set_kernel_policy", "pconv_debug_set_tiling", "pconv_debug_set_flat_shape", "pconv_debug_plan", "pconv_debug_set_spin_limit",
                     "pconv_get_async_error", "pconv_pool2x2_fusion", "pconv_debug_measure_fma_peak",
                     "pconv_quantize_rows", "pconv_matmul_i8", "pconv_matmul_i8_workspace", "pconv_linear_i8",
-                    "pconv_linear_i8_workspace", "pconv_debug_i8_plan", "pconv_grad_workspace", "pconv_grad_norm", "pconv_clip_grads",
+                    "pconv_linear_i8_workspace", "pconv_debug_i8_plan",
+                    "pconv_quantize_mx4", "pconv_matmul_mx4", "pconv_matmul_mx4_workspace", "pconv_linear_mx4",
+                    "pconv_linear_mx4_workspace", "pconv_debug_mx4_plan", "pconv_grad_workspace", "pconv_grad_norm", "pconv_clip_grads",
                     "pconv_last_error"]
 
 
@@ -739,6 +757,157 @@ def linear_i8(x, w, w_scale, bias=None, relu: bool = False, out_dtype=None, out=
     rc = (_lib or lib()).pconv_linear_i8(x.data_ptr() or None, x_step, x_type, w_ptr or None, w_step, sw, bp,
                                          y.data_ptr() or None, y_step, y_type, m, n, k, 1 if relu else 0,
                                          work.data_ptr() if size else None, size, _stream(index))
+    if rc != OK:
+        _check(rc)
+    if out is not None:
+        _tensor_list_calls().changed([y])
+    return y
+
+
+# ---- layers in 4-bit floats --------------------------------------------------------------
+#
+# As the 8-bit layers: they serve networks that are trained, nothing is recorded for autograd.
+
+def pconv_quantize_mx4(x_ptr: int, x_stride: int, x_dtype, rows: int, cols: int, q_ptr: int, q_stride: int, scale_ptr: int,
+                       slab_stride: int, stream: int = 0):
+    """Raw-pointer call, one to one with the C entry point."""
+    _check(lib().pconv_quantize_mx4(x_ptr or None, x_stride, _DTYPE[x_dtype], rows, cols, q_ptr or None, q_stride,
+                                    scale_ptr or None, slab_stride, stream or None))
+
+
+def pconv_matmul_mx4_workspace(m: int, n: int, blocks: int) -> int:
+    return lib().pconv_matmul_mx4_workspace(m, n, blocks)
+
+
+def pconv_matmul_mx4(a_ptr: int, a_stride: int, a_scale: int, a_slab: int, b_ptr: int, b_stride: int, b_scale: int, b_slab: int,
+                     bias_ptr, y_ptr: int, y_stride: int, y_dtype, m: int, n: int, blocks: int, fuse_relu: bool = False,
+                     work: int = 0, work_bytes: int = 0, stream: int = 0):
+    """Raw-pointer call, one to one with the C entry point."""
+    _check(lib().pconv_matmul_mx4(a_ptr or None, a_stride, a_scale or None, a_slab, b_ptr or None, b_stride, b_scale or None, b_slab,
+                                  bias_ptr or None, y_ptr or None, y_stride, _DTYPE[y_dtype], m, n, blocks, int(bool(fuse_relu)),
+                                  work or None, work_bytes, stream or None))
+
+
+def pconv_linear_mx4_workspace(m: int, n: int, k: int) -> int:
+    return lib().pconv_linear_mx4_workspace(m, n, k)
+
+
+def pconv_linear_mx4(x_ptr: int, x_stride: int, x_dtype, w_ptr: int, w_stride: int, w_scale: int, w_slab: int, bias_ptr, y_ptr: int,
+                     y_stride: int, y_dtype, m: int, n: int, k: int, fuse_relu: bool = False, work: int = 0, work_bytes: int = 0,
+                     stream: int = 0):
+    """Raw-pointer call, one to one with the C entry point."""
+    _check(lib().pconv_linear_mx4(x_ptr or None, x_stride, _DTYPE[x_dtype], w_ptr or None, w_stride, w_scale or None, w_slab,
+                                  bias_ptr or None, y_ptr or None, y_stride, _DTYPE[y_dtype], m, n, k, int(bool(fuse_relu)),
+                                  work or None, work_bytes, stream or None))
+
+
+def pconv_debug_mx4_plan(m: int, n: int, blocks: int) -> pconv_mx4_plan:
+    out = pconv_mx4_plan()
+    _check(lib().pconv_debug_mx4_plan(m, n, blocks, C.byref(out)))
+    return out
+
+
+_linear_mx4_workspace = functools.lru_cache(maxsize=4096)(pconv_linear_mx4_workspace)
+_matmul_mx4_workspace = functools.lru_cache(maxsize=4096)(pconv_matmul_mx4_workspace)
+
+
+def _blocks(q, scale, rows_first, what):
+    """(rows, blocks, bytes from row to row, bytes from slab to slab) of 4-bit rows [..., 16 * blocks] and scales [slabs, rows, 8]."""
+    import torch
+    if q.dtype != torch.uint8 or scale.dtype != torch.uint8 or (rows_first and q.dim() != 2):
+        raise ValueError(f"{what} {'[n, 16 * blocks]' if rows_first else '[..., 16 * blocks]'} and its scales must be uint8")
+    m, wide, step = _rows(q, what)
+    if wide % 16:
+        raise ValueError(f"the rows of {what} must be blocks of 16 bytes")
+    slabs = (wide + 127) // 128
+    if scale.shape != (slabs, m, 8):
+        raise ValueError(f"the scales of {what} must have the shape {(slabs, m, 8)}")
+    slab, row, one = scale.stride()
+    if one != 1 or (row != 8 and m > 1):
+        raise ValueError(f"the scales of {what} must be contiguous within a slab")
+    if slab < 8 * m:
+        if slabs > 1:
+            raise ValueError(f"the slabs of the scales of {what} must not overlap")
+        slab = 8 * m
+    # (the step of a single row, or slab, may be anything)
+    return m, wide // 16, step if m > 1 else wide, slab if slabs > 1 else 8 * m
+
+
+def quantize_mx4(x):
+    """x: CUDA tensor [..., k], fp32 or bf16.  Returns (q [..., 16 * blocks] uint8, scale [slabs, rows, 8] uint8), 32 values of k a block and
+    8 blocks a slab; see include/pconv.h.  rows: of all leading dimensions together.  Nothing is recorded for autograd."""
+    import torch
+    dtype = _type_of(x, "x")
+    index = _device_index(x)
+    m, k, step = _rows(x, "x")
+    wide = (k + 31) // 32 * 16
+    q = _empty(x.shape[:-1], m, wide, torch.uint8, x)
+    scale = torch.empty_strided(((k + 255) // 256, m, 8), (8 * m or 1, 8, 1), dtype=torch.uint8, device=x.device)
+    rc = (_lib or lib()).pconv_quantize_mx4(x.data_ptr() or None, step, dtype, m, k, q.data_ptr() or None, wide,
+                                            scale.data_ptr() or None, 8 * m, _stream(index))
+    if rc != OK:
+        _check(rc)
+    return q, scale
+
+
+def matmul_mx4(a, a_scale, b, b_scale, bias=None, relu: bool = False, out_dtype=None, out=None):
+    """a [..., 16 * blocks] and b [n, 16 * blocks] with their scales, as quantize_mx4 gives them.  Returns act(a @ b.T + bias) [..., n] of
+    the values that they stand for.
+
+    bias [n]: fp32.  out_dtype: torch.float32 (unless `out` says otherwise) or torch.bfloat16.  out: where the result goes; it
+    must not overlap an input (its rows may lie between those of one).  Nothing is recorded for autograd."""
+    import torch
+    index = _device_index(a, a_scale, b, b_scale, bias, out)
+    m, blocks, a_step, a_slab = _blocks(a, a_scale, False, "a")
+    n, kb, b_step, b_slab = _blocks(b, b_scale, True, "b")
+    if blocks != kb:
+        raise ValueError("a and b must have rows of one length")
+    if out_dtype is None:
+        out_dtype = out.dtype if out is not None else torch.float32
+    y, y_step = _output(out, a.shape[:-1], m, n, out_dtype, a)
+    y_type = _type_of(y, "out")
+    bp = _per_channel(bias, n, "bias") if bias is not None else None
+    if out is not None and not _tensor_list_calls().apart(y, a, b, a_scale, b_scale, bias):
+        slabs = (blocks + 7) // 8
+        _refuse_overlap((y, m, n, y_step), (a, m, 16 * blocks, a_step), (b, n, 16 * blocks, b_step), (a_scale, slabs, 8 * m, a_slab),
+                        (b_scale, slabs, 8 * n, b_slab), (bias, 1, n, n))
+    size = _matmul_mx4_workspace(m, n, blocks)
+    work = _scratch(size, a) if size else None
+    rc = (_lib or lib()).pconv_matmul_mx4(a.data_ptr() or None, a_step, a_scale.data_ptr() or None, a_slab, b.data_ptr() or None, b_step,
+                                          b_scale.data_ptr() or None, b_slab, bp, y.data_ptr() or None, y_step, y_type, m, n, blocks,
+                                          1 if relu else 0, work.data_ptr() if size else None, size, _stream(index))
+    if rc != OK:
+        _check(rc)
+    if out is not None:
+        _tensor_list_calls().changed([y])
+    return y
+
+
+def linear_mx4(x, w, w_scale, bias=None, relu: bool = False, out_dtype=None, out=None):
+    """x [..., k]: CUDA tensor, fp32 or bf16; w [n, 16 * blocks] and w_scale as quantize_mx4 gives them for the weights [n, k].
+
+    Returns matmul_mx4(*quantize_mx4(x), w, w_scale, bias, relu) [..., n], of x's type unless `out_dtype` or `out` says
+    otherwise.  out: as there.  Nothing is recorded for autograd."""
+    x_type = _type_of(x, "x")
+    index = _device_index(x, w, w_scale, bias, out)
+    m, k, x_step = _rows(x, "x")
+    n, blocks, w_step, w_slab = _blocks(w, w_scale, True, "w")
+    if (k + 31) // 32 != blocks:
+        raise ValueError("x and w must have rows of one length")
+    if out is None and out_dtype is None:
+        y, y_step, y_type = x.new_empty(m, n) if x.dim() == 2 else x.new_empty(x.shape[:-1] + (n,)), n, x_type
+    else:
+        y, y_step = _output(out, x.shape[:-1], m, n, out_dtype or out.dtype, x)
+        y_type = _type_of(y, "out")
+    bp = _per_channel(bias, n, "bias") if bias is not None else None
+    if out is not None and not _tensor_list_calls().apart(y, x, w, w_scale, bias):
+        _refuse_overlap((y, m, n, y_step), (x, m, k, x_step), (w, n, 16 * blocks, w_step), (w_scale, (blocks + 7) // 8, 8 * n, w_slab),
+                        (bias, 1, n, n))
+    size = _linear_mx4_workspace(m, n, k)
+    work = _scratch(size, x) if size else None
+    rc = (_lib or lib()).pconv_linear_mx4(x.data_ptr() or None, x_step, x_type, w.data_ptr() or None, w_step, w_scale.data_ptr() or None,
+                                          w_slab, bp, y.data_ptr() or None, y_step, y_type, m, n, k, 1 if relu else 0,
+                                          work.data_ptr() if size else None, size, _stream(index))
     if rc != OK:
         _check(rc)
     if out is not None:

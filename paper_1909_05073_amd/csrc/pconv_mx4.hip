@@ -1,0 +1,480 @@
+// Microscaled 4-bit floats: quantising rows, and products with one power of two as the scale of each 32 values of k.
+//
+//   y[m][n] = act(sum_b 2^(sa[m][b] + sb[n][b] - 254) sum_(k in block b) a[m][k] b[n][k] + bias[n])
+//
+// A block is 16 bytes of a row, which is what a lane of the matrix instruction takes: 16 rows by 4 blocks, each lane a block
+// and the byte of its scale.  The order in which k is summed is free as long as both operands have the same, so lanes
+// 16 g .. take neighbouring blocks in neighbouring steps: their scales are then neighbouring bytes, read together.  The
+// weights are the instruction's first operand and the activations its second, so that a lane ends up with four
+// neighbouring channels of one row of y.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "pconv_internal.h"
+#include "pconv_ops.h"
+#include "pconv_rows.h"
+
+namespace pconv {
+
+namespace {
+
+typedef int v8i __attribute__((ext_vector_type(8)));
+
+int too_many_groups()
+{
+    set_error("4-bit layers: too many workgroups for one launch");
+    return PCONV_UNSUPPORTED;
+}
+
+// ---- quantising rows ---------------------------------------------------------------------------------------------------
+
+// The scale's byte, X + 127, of a block whose largest magnitude has these bits: the exponent less two, at least 0; 255 where
+// the block holds an infinity or a NaN.
+__device__ __forceinline__ uint32_t block_scale(uint32_t most)
+{
+    const uint32_t e = most >> 23;
+    return e >= 255u ? 255u : max(e, 2u) - 2u;
+}
+
+// 2^X as a float (2^-127 is a denormal number, which the conversion takes).
+__device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(byte ? byte << 23 : 0x00400000u); }
+
+// Eight neighbouring values of a row; 4 lanes have a block.
+template <typename T> struct Eight;
+template <> struct Eight<float> {
+    f4 v[2];
+    __device__ __forceinline__ uint32_t most() const
+    {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i / 4][i % 4]) & 0x7FFFFFFFu);
+        return m;
+    }
+    // (the conversion divides by the scale and rounds to the nearest, ties to even, 6 at most)
+    __device__ __forceinline__ uint32_t codes(float s) const
+    {
+        uint32_t w = 0;
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0][0], v[0][1], s, 0);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0][2], v[0][3], s, 1);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[1][0], v[1][1], s, 2);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[1][2], v[1][3], s, 3);
+        return w;
+    }
+};
+template <> struct Eight<__bf16> {
+    b8 v;
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    __device__ __forceinline__ uint32_t most() const
+    {
+        Vec<__bf16> x;
+        x.v = v;
+        return most_of(x, 0);
+    }
+    __device__ __forceinline__ uint32_t codes(float s) const
+    {
+        uint32_t w = 0;
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, b2{v[0], v[1]}, s, 0);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, b2{v[2], v[3]}, s, 1);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, b2{v[4], v[5]}, s, 2);
+        w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, b2{v[6], v[7]}, s, 3);
+        return w;
+    }
+};
+
+// Elements [at, at + 8) of a row of `cols`; beyond its end zero.
+template <typename T>
+__device__ __forceinline__ Eight<T> load_eight(const T *row, int64_t at, int64_t cols)
+{
+    Eight<T> e;
+    if (__builtin_expect(at + 8 <= cols, 1)) {
+        __builtin_memcpy(&e.v, row + at, 8 * sizeof(T));
+    } else {
+        T all[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) all[i] = at + i < cols ? row[at + i] : T(0.0f);
+        __builtin_memcpy(&e.v, all, 8 * sizeof(T));
+    }
+    return e;
+}
+
+// The largest value over the four lanes of a block.
+__device__ __forceinline__ uint32_t most_of_block(uint32_t v)
+{
+    v = max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0xB1, 0xF, 0xF, true)));       // the other of a pair
+    return max(v, uint32_t(__builtin_amdgcn_update_dpp(0, int(v), 0x4E, 0xF, 0xF, true)));    // the other pair of four
+}
+
+// 32 lanes have 256 values of a row, which is a slab: 8 rows a workgroup, `slabs` of them shared by gridDim.y workgroups.
+// Blocks behind the row's last one get scale 0.
+template <typename T>
+__global__ void __launch_bounds__(256)
+quantize_mx4_kernel(const T *__restrict__ x, int64_t ldx, int64_t rows, int64_t cols, int64_t slabs, uint8_t *__restrict__ q,
+                    int64_t ldq, uint8_t *__restrict__ scale, int64_t slab_stride)
+{
+    const int sub = int(threadIdx.x) & 31;
+    for (int64_t r = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5); r < rows; r += int64_t(gridDim.x) * 8) {
+        const T *row = x + r * ldx;
+        for (int64_t s = blockIdx.y; s < slabs; s += gridDim.y) {
+            const int64_t at = s * 256 + sub * 8;
+            const Eight<T> e = load_eight(row, at, cols);
+            const uint32_t byte = block_scale(most_of_block(e.most()));
+            const uint32_t w = byte == 255u ? 0u : e.codes(scale_value(byte));
+            if (at / 32 * 32 < cols) __builtin_memcpy(q + r * ldq + at / 2, &w, 4);
+            if (sub % 4 == 0) scale[s * slab_stride + r * 8 + sub / 4] = uint8_t(byte);
+        }
+    }
+}
+
+// ---- the product --------------------------------------------------------------------------------------------------------
+
+// Four neighbouring channels of one row of y, from n on.  ReLU keeps NaN.
+__device__ __forceinline__ f4 bias_at(const Mx4Product &p, int n)
+{
+    f4 b = {0, 0, 0, 0};
+    if (!p.bias) return b;
+    if (__builtin_expect(n + 4 <= p.n, 1)) {
+        __builtin_memcpy(&b, p.bias + n, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b[i] = p.bias[min(n + i, p.n - 1)];      // (what lies beyond the last channel is not stored)
+    }
+    return b;
+}
+
+__device__ __forceinline__ f4 values_of(const Mx4Product &p, f4 acc, f4 bias)
+{
+    f4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[i] = acc[i] + bias[i];
+        if (p.relu) v[i] = v[i] < 0.0f ? 0.0f : v[i];
+    }
+    return v;
+}
+
+template <typename Y, int N, typename V>
+__device__ __forceinline__ void store_channels(const Mx4Product &p, int m, int n, V v)
+{
+    Y *y = static_cast<Y *>(p.y) + (int64_t(m) * p.ldy + n);
+    if (__builtin_expect(n + N <= p.n, 1)) {
+        __builtin_memcpy(y, &v, N * sizeof(Y));
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (n + i < p.n) y[i] = v[i];
+    }
+}
+
+// acc += the 16 rows of b by the 16 rows of a over 4 blocks; STEP: which of the bytes of sb and sa are the scales.
+template <int STEP>
+__device__ __forceinline__ f4 multiply_blocks(v4i b, v4i a, f4 acc, int sb, int sa)
+{
+    const v8i b8 = __builtin_shufflevector(b, b, 0, 1, 2, 3, -1, -1, -1, -1), a8 = __builtin_shufflevector(a, a, 0, 1, 2, 3, -1, -1, -1, -1);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b8, a8, acc, 4, 4, STEP, sb, STEP, sa);
+}
+
+// Tiles of BM rows of y and BN channels, WM x WN waves, and KG such sets of waves that take the stages in turn.  A slab of
+// all the tile's rows is a stage: 128 bytes of values and 8 of scales a row; S stages lie in LDS.  A row of a stage is
+// eight blocks, stored in an order that depends on the row so that the eight rows that are read at once lie in different
+// banks.
+//
+// Stages go from memory to LDS past the registers, S - 1 of them ahead of the one that is multiplied; a wave waits
+// for its own loads of the next stage, and the barrier then tells it that everybody's are there and that the stage
+// before is read.  In the last stage the blocks behind the end of k are zeros.
+//
+// `splits` workgroups share a tile, each with its part of k; their sums go to `part` [splits][m][n4], n4 = n rounded
+// up to four.
+template <typename Y, int BM, int BN, int WM, int WN, int S, int KG>
+__global__ void __launch_bounds__(KG * WM * WN * 64)
+matmul_mx4_kernel(const Mx4Product p, int splits, float *part)
+{
+    constexpr int NW = WM * WN, TM = BM / WM, TN = BN / WN, MT = TM / 16, NT = TN / 16;
+    constexpr int PA = BM / 8 / NW, PB = BN / 8 / NW;    // pieces of eight rows that a wave stages
+    constexpr int PS = ((BM + BN) / 32 + NW - 1) / NW;   // and of the scales of 32 rows
+    static_assert(PA * NW * 8 == BM && PB * NW * 8 == BN && BM % 32 == 0 && BN % 32 == 0 && NT % 2 == 0, "");
+    constexpr int STAGE = (BM + BN) * 8 + PS * NW * 16, SUMS = NW * MT * NT * 64;        // (in pieces of 16 bytes)
+    __shared__ v4i lds[S * KG * STAGE];
+    static_assert(KG == 1 || (KG - 1) * SUMS <= S * KG * STAGE, "");
+    const int lane = int(threadIdx.x) & 63, set = __builtin_amdgcn_readfirstlane(int(threadIdx.x) / (NW * 64));
+    const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6) % NW;
+    const unsigned tiles_n = unsigned(p.n + BN - 1) / BN, tiles_m = unsigned(p.m + BM - 1) / BM;
+    unsigned tm, tn;
+    tile_at(blockIdx.x / unsigned(splits), tiles_m, tiles_n, tm, tn);
+    const int split = int(blockIdx.x % unsigned(splits));
+    const int m0 = int(tm) * BM, n0 = int(tn) * BN;
+    const int wm = (wave / WN) * TM, wn = (wave % WN) * TN;
+    const int r = lane & 15, g = lane >> 4;
+    // this workgroup's part of k
+    const int stages = (p.blocks + 7) / 8;
+    const int s_begin = int(int64_t(stages) * split / splits), s_end = int(int64_t(stages) * (split + 1) / splits);
+
+    // order of the blocks of a row of weights: the rows that are read at once differ in three of their bits
+    auto key_b = [](int row) { return (row & 3) | (((row >> Deal<Y>::SH) & 1) << 2); };
+
+    f4 acc[MT][NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = f4{0, 0, 0, 0};
+
+    // (`have`: blocks of k from the stage's first on; of one that is not there the scale may be any byte, NaN's too)
+    auto multiply = [&](const v4i *st, int have) {
+        const int mask = 0xFFFF >> max(0, min(16, (2 * g + 2 - have) * 8));
+        const uint16_t *const scales = reinterpret_cast<const uint16_t *>(st + (BM + BN) * 8);
+        int sa[MT], sb[NT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) sa[i] = scales[(wm + i * 16 + r) * 4 + g] & mask;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) sb[j] = scales[(BM + wn + Deal<Y>::row(j, r)) * 4 + g] & mask;
+        auto step = [&](auto kk) {
+            constexpr int KK = decltype(kk)::value;
+            v4i a[MT], b[NT];
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const int row = wm + i * 16 + r;
+                a[i] = st[row * 8 + ((2 * g + KK) ^ (row & 7))];
+            }
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+                const int row = wn + Deal<Y>::row(j, r);
+                b[j] = st[BM * 8 + row * 8 + ((2 * g + KK) ^ key_b(row))];
+            }
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = multiply_blocks<KK>(b[j], a[i], acc[i][j], sb[j], sa[i]);
+        };
+        step(std::integral_constant<int, 0>());
+        step(std::integral_constant<int, 1>());
+    };
+
+    const v4u at_a = buffer_at(reinterpret_cast<const int8_t *>(p.a) + int64_t(m0) * p.lda + int64_t(s_begin) * 128);
+    const v4u at_b = buffer_at(reinterpret_cast<const int8_t *>(p.b) + int64_t(n0) * p.ldb + int64_t(s_begin) * 128);
+    uint32_t off_a[PA], off_b[PB], off_s[PS];
+    int end_a[PA], end_b[PB];                            // (a lane's block is loaded if the stage has it)
+#pragma unroll
+    for (int i = 0; i < PA; ++i) {
+        const int row = (i * NW + wave) * 8 + (lane >> 3);
+        end_a[i] = (lane & 7) ^ (row & 7);
+        off_a[i] = uint32_t(min(row, p.m - 1 - m0)) * uint32_t(p.lda) + uint32_t(end_a[i] * 16);
+    }
+#pragma unroll
+    for (int i = 0; i < PB; ++i) {
+        const int row = (i * NW + wave) * 8 + (lane >> 3);
+        end_b[i] = (lane & 7) ^ key_b(row);
+        off_b[i] = uint32_t(min(row, p.n - 1 - n0)) * uint32_t(p.ldb) + uint32_t(end_b[i] * 16);
+    }
+    // 32 rows of one operand have 256 bytes of scales, a word a lane
+#pragma unroll
+    for (int i = 0; i < PS; ++i) {
+        const int row = (i * NW + wave) * 32 + (lane >> 1);
+        off_s[i] = uint32_t(row < BM ? min(row, p.m - 1 - m0) : min(row - BM, p.n - 1 - n0)) * 8u + uint32_t(lane & 1) * 4u;
+    }
+    const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(lds)) + uint32_t(set) * uint32_t(STAGE * 16);
+    const int count = s_end - s_begin;
+    // (written as assembly so that the compiler does not wait for these loads before every read of LDS)
+    // stage `turn` of this set is stage turn * KG + set of all
+    auto stage = [&](int turn) {
+        const int s = turn * KG + set;
+        const uint32_t to = base + uint32_t(turn % S) * uint32_t(KG * STAGE * 16), k0 = uint32_t(s) * 128u;
+        const int have = p.blocks - (s_begin + s) * 8;
+#pragma unroll
+        for (int i = 0; i < PA; ++i)
+            asm volatile("s_mov_b32 m0, %1\n s_nop 0\n buffer_load_dwordx4 %0, %2, %3 offen lds"
+                         ::"v"(end_a[i] < have ? off_a[i] : kNowhere), "s"(to + uint32_t((i * NW + wave) * 1024)), "s"(at_a), "s"(k0) : "memory");
+#pragma unroll
+        for (int i = 0; i < PB; ++i)
+            asm volatile("s_mov_b32 m0, %1\n s_nop 0\n buffer_load_dwordx4 %0, %2, %3 offen lds"
+                         ::"v"(end_b[i] < have ? off_b[i] : kNowhere), "s"(to + uint32_t(BM * 128 + (i * NW + wave) * 1024)), "s"(at_b), "s"(k0) : "memory");
+#pragma unroll
+        for (int i = 0; i < PS; ++i) {
+            const bool of_a = (i * NW + wave) * 32 < BM;
+            const uint8_t *const from = of_a ? p.sa + int64_t(s_begin + s) * p.slab_a + int64_t(m0) * 8 : p.sb + int64_t(s_begin + s) * p.slab_b + int64_t(n0) * 8;
+            const v4u at_s = buffer_at(reinterpret_cast<const int8_t *>(from));
+            asm volatile("s_mov_b32 m0, %1\n s_nop 0\n buffer_load_dword %0, %2, 0 offen lds"
+                         ::"v"(off_s[i]), "s"(to + uint32_t((BM + BN) * 128 + (i * NW + wave) * 256)), "s"(at_s) : "memory");
+        }
+    };
+    constexpr int L = PA + PB + PS;
+    static_assert((S - 2) * L <= 63, "");
+    const int mine = (count - set + KG - 1) / KG;        // stages of this set (count >= 0, so at least 0)
+    const int turns = (count + KG - 1) / KG;
+#pragma unroll
+    for (int t = 0; t < S - 1; ++t)
+        if (t < mine) stage(t);
+#pragma unroll 1
+    for (int t = 0; t < turns; ++t) {
+        // the loads of this turn are done when at most those of the turns behind it are under way
+        wait_for_stages<S - 2, L>(min(S - 2, max(0, mine - 1 - t)));
+        if (t + S - 1 < mine) stage(t + S - 1);
+        if (KG == 1 || t * KG + set < count) multiply(lds + ((t % S) * KG + set) * STAGE, p.blocks - (s_begin + t * KG + set) * 8);
+    }
+    if constexpr (KG > 1) {                              // the sets' sums come together
+        __syncthreads();
+        f4 *const to = reinterpret_cast<f4 *>(lds) + wave * (MT * NT * 64) + lane;
+        if (set > 0) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) to[(set - 1) * SUMS + (i * NT + j) * 64] = acc[i][j];
+        }
+        __syncthreads();
+        if (set > 0) return;
+#pragma unroll
+        for (int q = 0; q < KG - 1; ++q)
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] += to[q * SUMS + (i * NT + j) * 64];
+    }
+
+    const int m = m0 + wm + r;
+    if (splits > 1) {
+        const int64_t n4 = (int64_t(p.n) + 3) / 4 * 4;
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int n = n0 + wn + Deal<Y>::first(j, g);
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+                if (m + 16 * i < p.m && n < p.n) __builtin_memcpy(part + (int64_t(split) * p.m + m + 16 * i) * n4 + n, &acc[i][j], 16);
+        }
+        return;
+    }
+    f4 bias[NT];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) bias[j] = bias_at(p, n0 + wn + Deal<Y>::first(j, g));
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+        if (m + 16 * i >= p.m) continue;
+#pragma unroll
+        for (int j = 0; j < NT; j += 2) {
+            const int n = n0 + wn + Deal<Y>::first(j, g), n2 = n0 + wn + Deal<Y>::first(j + 1, g);
+            if (n >= p.n) continue;
+            const f4 v = values_of(p, acc[i][j], bias[j]), w = values_of(p, acc[i][j + 1], bias[j + 1]);
+            if (sizeof(Y) == 4) {
+                store_channels<float, 4>(p, m + 16 * i, n, v);
+                if (n2 < p.n) store_channels<float, 4>(p, m + 16 * i, n2, w);
+            } else {
+                const b8 o = __builtin_convertvector(__builtin_shufflevector(v, w, 0, 1, 2, 3, 4, 5, 6, 7), b8);
+                store_channels<__bf16, 8>(p, m + 16 * i, n, o);
+            }
+        }
+    }
+}
+
+// y of the sums of `splits` parts of k; a thread has four channels.
+__global__ void __launch_bounds__(256)
+matmul_mx4_join_kernel(const Mx4Product p, int splits, const float *__restrict__ part)
+{
+    const int64_t quads = (int64_t(p.n) + 3) / 4, all = quads * p.m;
+    for (int64_t t = int64_t(blockIdx.x) * 256 + threadIdx.x; t < all; t += int64_t(gridDim.x) * 256) {
+        const int m = int(t / quads), n = int(t % quads) * 4;
+        f4 s = {0, 0, 0, 0};
+#pragma unroll 4
+        for (int i = 0; i < splits; ++i) {
+            f4 v;
+            __builtin_memcpy(&v, part + (int64_t(i) * all + t) * 4, 16);
+            s += v;
+        }
+        const f4 v = values_of(p, s, bias_at(p, n));
+        if (p.y_bf16) store_channels<__bf16, 4>(p, m, n, __builtin_convertvector(v, b4));
+        else store_channels<float, 4>(p, m, n, v);
+    }
+}
+
+// How a product is cut up: the tile (an index into launch_tiles) and over how many workgroups the length of k is split.
+struct Cut { int tile, splits; };
+
+constexpr int kTiles = 4, kTileM[kTiles] = {32, 64, 128, 256}, kTileN[kTiles] = {128, 128, 128, 256};
+constexpr int64_t kUnits = 256;                          // compute units
+
+int64_t tiles_of(const Cut &c, int64_t m, int64_t n) { return ((m + kTileM[c.tile] - 1) / kTileM[c.tile]) * ((n + kTileN[c.tile] - 1) / kTileN[c.tile]); }
+
+// The cheapest by a count of cycles: a compute unit takes its tiles one after the other, a stage of a tile at the rate of the
+// matrix units (half of their peak) or of what 40 bytes a cycle bring from the level-2 cache, whichever is slower.
+// Joining the parts of k is one more launch and reads and writes the sums.
+Cut cut_of(int64_t m, int64_t n, int64_t blocks)
+{
+    constexpr int64_t stage_cycles[kTiles] = {512, 614, 1100, 4096}, start = 4000, join = 9000;
+    const int64_t stages = (blocks + 7) / 8;
+    Cut best{0, 1};
+    double least = 0;
+    for (int t = 0; t < kTiles; ++t)
+        for (int64_t s = 1; s == 1 || (s <= 32 && s * 4 <= stages); s *= 2) {
+            const int64_t tiles = tiles_of(Cut{t, int(s)}, m, n);
+            double c = double((tiles * s + kUnits - 1) / kUnits) * double((stages + s - 1) / s) * double(stage_cycles[t]) + start;
+            if (s > 1) c += join + double(s) * double(m) * double(n) * 8 / 2000;
+            if ((t == 0 && s == 1) || c < least || (c == least && s == 1)) { least = c; best = Cut{t, int(s)}; }
+        }
+    return best;
+}
+
+// Sets of waves of a workgroup: two where a compute unit has one workgroup, else room for two workgroups.  The largest tile
+// fills a compute unit with one set.
+int sets_of(const Cut &c, int64_t tiles) { return c.tile < 3 && tiles * c.splits <= kUnits ? 2 : 1; }
+
+template <int BM, int BN, int WM, int WN, int S, int KG>
+void launch_tiles(const Mx4Product &p, int splits, float *part, hipStream_t st)
+{
+    const unsigned grid = unsigned(((int64_t(p.m) + BM - 1) / BM) * ((int64_t(p.n) + BN - 1) / BN) * splits);
+    if (p.y_bf16) hipLaunchKernelGGL((matmul_mx4_kernel<__bf16, BM, BN, WM, WN, S, KG>), dim3(grid), dim3(KG * WM * WN * 64), 0, st, p, splits, part);
+    else hipLaunchKernelGGL((matmul_mx4_kernel<float, BM, BN, WM, WN, S, KG>), dim3(grid), dim3(KG * WM * WN * 64), 0, st, p, splits, part);
+}
+
+}  // namespace
+
+int launch_quantize_mx4(const void *x, int64_t ldx, int bf16, int64_t rows, int64_t cols, uint8_t *q, int64_t ldq, uint8_t *scale,
+                        int64_t slab_stride, void *stream)
+{
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const int64_t slabs = (cols + 255) / 256;
+    const unsigned gx = unsigned(std::min<int64_t>((rows + 7) / 8, 1 << 20));
+    const unsigned gy = unsigned(std::min<int64_t>(slabs, std::max<int64_t>(1, 4096 / gx)));
+    if (bf16) hipLaunchKernelGGL(quantize_mx4_kernel<__bf16>, dim3(gx, gy), dim3(256), 0, st, static_cast<const __bf16 *>(x), ldx, rows, cols, slabs, q, ldq, scale, slab_stride);
+    else hipLaunchKernelGGL(quantize_mx4_kernel<float>, dim3(gx, gy), dim3(256), 0, st, static_cast<const float *>(x), ldx, rows, cols, slabs, q, ldq, scale, slab_stride);
+    return check_launch("pconv_quantize_mx4");
+}
+
+int64_t matmul_mx4_work_bytes(int64_t m, int64_t n, int64_t blocks)
+{
+    const Cut c = cut_of(m, n, blocks);
+    return c.splits > 1 ? c.splits * m * ((n + 3) / 4 * 4) * 4 : 0;
+}
+
+int check_matmul_mx4(int64_t m, int64_t n, int64_t blocks)
+{
+    const Cut c = cut_of(m, n, blocks);
+    return tiles_of(c, m, n) * c.splits > kMaxGroups ? too_many_groups() : PCONV_OK;
+}
+
+pconv_mx4_plan matmul_mx4_plan(int64_t m, int64_t n, int64_t blocks)
+{
+    const Cut c = cut_of(m, n, blocks);
+    return pconv_mx4_plan{2, kTileM[c.tile], kTileN[c.tile], sets_of(c, tiles_of(c, m, n)), c.splits};
+}
+
+int launch_matmul_mx4(const Mx4Product &p, void *work, void *stream)
+{
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    const Cut c = cut_of(p.m, p.n, p.blocks);
+    const int64_t tiles = tiles_of(c, p.m, p.n);
+    if (tiles * c.splits > kMaxGroups) return too_many_groups();
+    float *const sums = static_cast<float *>(work);
+    const bool two = sets_of(c, tiles) == 2;
+    if (c.tile == 0 && two) launch_tiles<32, 128, 1, 4, 3, 2>(p, c.splits, sums, st);
+    else if (c.tile == 0) launch_tiles<32, 128, 1, 4, 3, 1>(p, c.splits, sums, st);
+    else if (c.tile == 1 && two) launch_tiles<64, 128, 2, 2, 3, 2>(p, c.splits, sums, st);
+    else if (c.tile == 1) launch_tiles<64, 128, 2, 2, 3, 1>(p, c.splits, sums, st);
+    else if (c.tile == 2 && two) launch_tiles<128, 128, 2, 2, 2, 2>(p, c.splits, sums, st);
+    else if (c.tile == 2) launch_tiles<128, 128, 2, 2, 2, 1>(p, c.splits, sums, st);
+    else launch_tiles<256, 256, 2, 4, 2, 1>(p, c.splits, sums, st);
+    if (const int rc = check_launch("pconv_matmul_mx4")) return rc;
+    if (c.splits == 1) return PCONV_OK;
+    const int64_t quads = (int64_t(p.n) + 3) / 4 * p.m;
+    hipLaunchKernelGGL(matmul_mx4_join_kernel, dim3(unsigned(std::min<int64_t>((quads + 255) / 256, 1 << 16))), dim3(256), 0, st, p, c.splits, sums);
+    return check_launch("pconv_matmul_mx4 (joining the parts of k)");
+}
+
+}  // namespace pconv

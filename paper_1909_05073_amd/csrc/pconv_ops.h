@@ -1,4 +1,4 @@
-// What pconv_ops_capi.cpp and the kernels of the 8-bit layers and the gradients share.
+// What pconv_ops_capi.cpp and the kernels of the 8-bit and 4-bit layers and the gradients share.
 #ifndef PCONV_OPS_H
 #define PCONV_OPS_H
 
@@ -43,6 +43,24 @@ bool linear_i8_fused(int64_t m, int64_t n, int64_t k, bool b_at_16);
 // Whether the product of rows that are quantised by a launch of their own can be launched: asked before that one.
 int check_linear_i8_apart(int64_t m, int64_t n, int64_t k);
 int launch_linear_i8_fused(const I8Product &p, const void *x, int64_t ldx, int bf16, void *stream);
+
+// y [m][n] = act(sum over blocks of 32 of 2^(sa + sb - 254) (a [m][k] . b [n][k]) + bias[n]); rows of 16 bytes a block, scales in
+// slabs of 8 blocks, [slab][row][8]; strides in bytes, that of y in elements.
+struct Mx4Product {
+    const uint8_t *a, *b, *sa, *sb;
+    const float *bias;
+    void *y;
+    int64_t lda, ldb, slab_a, slab_b, ldy;
+    int m, n, blocks;
+    int relu, y_bf16;
+};
+
+int launch_quantize_mx4(const void *x, int64_t ldx, int bf16, int64_t rows, int64_t cols, uint8_t *q, int64_t ldq, uint8_t *scale,
+                        int64_t slab_stride, void *stream);
+int64_t matmul_mx4_work_bytes(int64_t m, int64_t n, int64_t blocks);
+int check_matmul_mx4(int64_t m, int64_t n, int64_t blocks);              // whether the product can be launched
+pconv_mx4_plan matmul_mx4_plan(int64_t m, int64_t n, int64_t blocks);
+int launch_matmul_mx4(const Mx4Product &p, void *work, void *stream);
 
 // Up to kGradTensors tensors travel in the arguments of one launch (4 KiB), cut into chunks of 1 << `log2` elements.
 constexpr int kGradTensors = 160, kGradBlocks = 2048;

@@ -1,4 +1,4 @@
-// extern "C" boundary of the 8-bit layers and the gradients (see include/pconv.h for the contract).
+// extern "C" boundary of the 8-bit and 4-bit layers and the gradients (see include/pconv.h for the contract).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -13,6 +13,7 @@ using namespace pconv;
 namespace {
 
 constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1, kMaxSide = int64_t(1) << 30, kMaxK = 131071;
+constexpr int64_t kMaxBlocks = 1 << 19, kMaxRowBytes = 1 << 23;      // of the 4-bit layers
 constexpr int64_t kMaxTensors = 1 << 24, kMaxElements = int64_t(1) << 45;    // fewer than 2^32 chunks together
 
 int invalid(const char *who, const char *what)
@@ -47,6 +48,34 @@ int check_product(const char *who, const int8_t *b, int64_t ldb, const float *sb
     if (!sb || !y || (k && !b)) return invalid(who, "null pointer argument");
     if (!stride_fits(n, k, ldb) || !stride_fits(m, n, ldy)) return invalid(who, "rows must lie at least their length apart");
     p = I8Product{nullptr, b, nullptr, sb, bias, y, 0, ldb, ldy, int(m), int(n), int(k), relu ? 1 : 0, y_dtype == PCONV_BF16};
+    return PCONV_OK;
+}
+
+// Rows of 4-bit blocks and their scales: within 32 bits where a tile is read.
+int check_blocks(const char *who, const uint8_t *q, int64_t stride, const uint8_t *scale, int64_t slab, int64_t rows, int64_t blocks)
+{
+    if (!q || !scale) return invalid(who, "null pointer argument");
+    if (reinterpret_cast<uintptr_t>(q) % 16 != 0 || stride % 16 != 0) return invalid(who, "rows of 4-bit values must begin at multiples of 16 bytes");
+    if (stride < blocks * 16 || stride > kMaxRowBytes) return invalid(who, "rows of 4-bit values must lie at least their length and at most 8 MiB apart");
+    if (reinterpret_cast<uintptr_t>(scale) % 8 != 0 || slab % 8 != 0) return invalid(who, "slabs of scales must begin at multiples of 8 bytes");
+    if (!stride_fits((blocks + 7) / 8, rows * 8, slab)) return invalid(who, "slabs of scales must lie at least 8 bytes a row apart");
+    return PCONV_OK;
+}
+
+bool mx4_sizes_fit(int64_t m, int64_t n, int64_t blocks) { return m > 0 && n > 0 && blocks >= 0 && m <= kMaxSide && n <= kMaxSide && blocks <= kMaxBlocks; }
+
+// What both products check of their weights and outputs, and the product itself but for its activations.
+int check_product_mx4(const char *who, const uint8_t *b, int64_t ldb, const uint8_t *sb, int64_t slab_b, const float *bias, void *y,
+                      int64_t ldy, int y_dtype, int64_t m, int64_t n, int64_t blocks, int relu, Mx4Product &p)
+{
+    if (m < 0 || n < 0 || m > kMaxSide || n > kMaxSide) return invalid(who, "m and n must be 0 .. 2^30");
+    if (!is_dtype(y_dtype)) return invalid(who, "unknown dtype of y");
+    if (m == 0 || n == 0) return PCONV_OK;
+    if (!y) return invalid(who, "null pointer argument");
+    if (!stride_fits(m, n, ldy)) return invalid(who, "rows must lie at least their length apart");
+    if (blocks)
+        if (const int rc = check_blocks(who, b, ldb, sb, slab_b, n, blocks)) return rc;
+    p = Mx4Product{nullptr, b, nullptr, sb, bias, y, 0, ldb, 0, slab_b, ldy, int(m), int(n), int(blocks), relu ? 1 : 0, y_dtype == PCONV_BF16};
     return PCONV_OK;
 }
 
@@ -231,6 +260,76 @@ int pconv_debug_i8_plan(int64_t m, int64_t n, int64_t k, pconv_i8_plan *out)
     if (!out) return invalid("pconv_debug_i8_plan", "null pointer argument");
     if (!sizes_fit(m, n, k)) return invalid("pconv_debug_i8_plan", "m and n must be 1 .. 2^30, k 0 .. 131071");
     *out = matmul_i8_plan(m, n, k);
+    return PCONV_OK;
+}
+
+int pconv_quantize_mx4(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, int64_t rows, int64_t cols,
+                       uint8_t *q_dev, int64_t q_stride, uint8_t *scale_dev, int64_t slab_stride, void *hip_stream)
+{
+    const char *who = "pconv_quantize_mx4";
+    if (rows < 0 || cols < 0 || rows > kMaxSide || cols > kMaxBlocks * 32) return invalid(who, "rows must be 0 .. 2^30, cols 0 .. 2^24");
+    if (!is_dtype(int(x_dtype))) return invalid(who, "unknown dtype");
+    if (rows == 0 || cols == 0) return PCONV_OK;
+    if (!x_dev) return invalid(who, "null pointer argument");
+    if (!stride_fits(rows, cols, x_stride)) return invalid(who, "rows must lie at least their length apart");
+    if (const int rc = check_blocks(who, q_dev, q_stride, scale_dev, slab_stride, rows, (cols + 31) / 32)) return rc;
+    return launch_quantize_mx4(x_dev, x_stride, x_dtype == PCONV_BF16, rows, cols, q_dev, q_stride, scale_dev, slab_stride, hip_stream);
+}
+
+int64_t pconv_matmul_mx4_workspace(int64_t m, int64_t n, int64_t blocks) { return mx4_sizes_fit(m, n, blocks) ? matmul_mx4_work_bytes(m, n, blocks) : 0; }
+
+int pconv_matmul_mx4(const uint8_t *a_dev, int64_t a_stride, const uint8_t *a_scale, int64_t a_slab, const uint8_t *b_dev,
+                     int64_t b_stride, const uint8_t *b_scale, int64_t b_slab, const float *bias_dev, void *y_dev,
+                     int64_t y_stride, pconv_dtype y_dtype, int64_t m, int64_t n, int64_t blocks, int fuse_relu, void *work,
+                     int64_t work_bytes, void *hip_stream)
+{
+    const char *who = "pconv_matmul_mx4";
+    if (blocks < 0 || blocks > kMaxBlocks) return invalid(who, "blocks must be 0 .. 2^19");
+    Mx4Product p;
+    if (const int rc = check_product_mx4(who, b_dev, b_stride, b_scale, b_slab, bias_dev, y_dev, y_stride, int(y_dtype), m, n, blocks, fuse_relu, p)) return rc;
+    if (m == 0 || n == 0) return PCONV_OK;
+    if (blocks)
+        if (const int rc = check_blocks(who, a_dev, a_stride, a_scale, a_slab, m, blocks)) return rc;
+    if (const int rc = check_work(who, work, work_bytes, matmul_mx4_work_bytes(m, n, blocks))) return rc;
+    p.a = a_dev; p.lda = a_stride; p.sa = a_scale; p.slab_a = a_slab;
+    return launch_matmul_mx4(p, work, hip_stream);
+}
+
+int64_t pconv_linear_mx4_workspace(int64_t m, int64_t n, int64_t k)
+{
+    if (k < 0 || k > kMaxBlocks * 32 || !mx4_sizes_fit(m, n, (k + 31) / 32)) return 0;
+    const int64_t blocks = (k + 31) / 32;
+    return m * blocks * 16 + round16((blocks + 7) / 8 * m * 8) + matmul_mx4_work_bytes(m, n, blocks);
+}
+
+int pconv_linear_mx4(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, const uint8_t *w_dev, int64_t w_stride,
+                     const uint8_t *w_scale, int64_t w_slab, const float *bias_dev, void *y_dev, int64_t y_stride,
+                     pconv_dtype y_dtype, int64_t m, int64_t n, int64_t k, int fuse_relu, void *work, int64_t work_bytes,
+                     void *hip_stream)
+{
+    const char *who = "pconv_linear_mx4";
+    if (!is_dtype(int(x_dtype))) return invalid(who, "unknown dtype of x");
+    if (k < 0 || k > kMaxBlocks * 32) return invalid(who, "k must be 0 .. 2^24");
+    const int64_t blocks = (k + 31) / 32;
+    Mx4Product p;
+    if (const int rc = check_product_mx4(who, w_dev, w_stride, w_scale, w_slab, bias_dev, y_dev, y_stride, int(y_dtype), m, n, blocks, fuse_relu, p)) return rc;
+    if (m == 0 || n == 0) return PCONV_OK;
+    if (k && !x_dev) return invalid(who, "null pointer argument");
+    if (!stride_fits(m, k, x_stride)) return invalid(who, "rows must lie at least their length apart");
+    if (const int rc = check_work(who, work, work_bytes, pconv_linear_mx4_workspace(m, n, k))) return rc;
+    if (const int rc = check_matmul_mx4(m, n, blocks)) return rc;
+    uint8_t *const q = static_cast<uint8_t *>(work), *const scale = q + m * blocks * 16;
+    if (k)
+        if (const int rc = launch_quantize_mx4(x_dev, x_stride, x_dtype == PCONV_BF16, m, k, q, blocks * 16, scale, m * 8, hip_stream)) return rc;
+    p.a = q; p.lda = blocks * 16; p.sa = scale; p.slab_a = m * 8;
+    return launch_matmul_mx4(p, scale + round16((blocks + 7) / 8 * m * 8), hip_stream);
+}
+
+int pconv_debug_mx4_plan(int64_t m, int64_t n, int64_t blocks, pconv_mx4_plan *out)
+{
+    if (!out) return invalid("pconv_debug_mx4_plan", "null pointer argument");
+    if (!mx4_sizes_fit(m, n, blocks)) return invalid("pconv_debug_mx4_plan", "m and n must be 1 .. 2^30, blocks 0 .. 2^19");
+    *out = matmul_mx4_plan(m, n, blocks);
     return PCONV_OK;
 }
 
