@@ -249,6 +249,21 @@ int pconv_linear_i8(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, co
                     const float *w_scale, const float *bias_dev, void *y_dev, int64_t y_stride, pconv_dtype y_dtype,
                     int64_t m, int64_t n, int64_t k, int fuse_relu, void *work, int64_t work_bytes, void *hip_stream);
 
+/* pconv_add_rms_norm_i8 - rows of a residual stream as the layers above read them: added, normalised and quantised in one pass.
+ *
+ *   s[r][k]  = x[r][k] + residual[r][k]
+ *   h[r][k]  = s[r][k] / sqrt(mean_k s[r][k]^2 + eps) * weight[k]
+ *   scale[r] = max_k |h[r][k]| / 127           q[r][k] = h[r][k] / scale[r] to the nearest whole number, ties to even
+ *
+ * The norm is taken of the sums in fp32, squares are summed in fp64; sum [rows][cols], where the sums go, gets them rounded to
+ * the type of x and residual (fp32 or bf16).  residual may be NULL (s = x; sum is NULL then), weight (fp32, [cols]) and sum too.
+ * sum may be x or residual, with the same stride, and must overlap nothing else.  q, scale and odd rows as
+ * pconv_quantize_rows gives them of h: a row that holds an infinity or a NaN has scale NaN and zeros.  eps: a number above 0.
+ * rows and cols up to 2^31 - 1.  Errors as above. */
+int pconv_add_rms_norm_i8(const void *x_dev, int64_t x_stride, const void *residual_dev, int64_t residual_stride, void *sum_dev,
+                          int64_t sum_stride, pconv_dtype dtype, const float *weight_dev, float eps, int64_t rows, int64_t cols,
+                          int8_t *q_dev, int64_t q_stride, float *scale_dev, void *hip_stream);
+
 /* ---- layers in 4-bit floats ----------------------------------------------------------------------
  *
  * The same layers with weights of half the bytes.  32 neighbouring values of a row are a block, which has one power of two as
@@ -323,6 +338,44 @@ int pconv_grad_norm(const void *const *grads, const int64_t *counts, const int32
 int pconv_clip_grads(const void *const *grads, void *const *outs, const int64_t *counts, const int32_t *dtypes,
                      const int32_t *out_dtypes, int64_t num, float max_norm, float eps, float *norm_dev,
                      void *work, int64_t work_bytes, void *hip_stream);
+
+/* ---- distillation -------------------------------------------------------------------------------
+ *
+ * What pruning and few bits lose is trained back towards the unpruned network, the teacher, of which each row has its largest
+ * logits: teacher [rows][top] at the classes [rows][top].  With the student's logits z [rows][v] and a temperature T:
+ *
+ *   p[r][j]    = softmax_j(teacher[r][j] / T) over the entries of row r
+ *   lq[r][u]   = z[r][u] / T - lse[r],  lse[r] = log sum_u exp(z[r][u] / T)
+ *   loss[r]    = T^2 sum_j p[r][j] (log p[r][j] - lq[r][c[r][j]])
+ *   grad[r][u] = w T (exp(lq[r][u]) - sum_(j: c[r][j] = u) p[r][j])          w: what loss[r] counts in the result
+ *
+ * An entry whose class is not 0 .. v - 1 is none, and a teacher's logit of -infinity has p = 0; a row without an entry (or of
+ * such logits alone) has loss 0 and a gradient of zeros.  A class may be named more than once.  p = 0 counts 0 in the loss.
+ * Infinities and NaN otherwise do what the formulas say.  Exponentials and sums within a row are fp32, rows are added in
+ * fp64 in a fixed order; the same bits from run to run.  No gradient goes to the teacher.
+ *
+ *   z, grad    fp32 or bf16 (one type for both);  teacher  fp32 or bf16;  classes  integers of class_bytes 4 or 8 bytes
+ *   strides    elements from row to row, at least the row's length;  rows begin anywhere their type may
+ *   v up to 2^30, top up to 1024, rows up to 2^31 - 1;  T above 0
+ *   mean       0: the result is the sum over the rows (w = 1), else that divided by rows (w = 1 / rows)
+ *   loss_dev   [rows] fp32, receives loss[r];  total_dev  the result, fp32 (or NULL)
+ *   up_dev     fp32, the gradient that comes in: w is multiplied by up_dev[r * up_step], up_step 0 or 1 (NULL: by 1)
+ *
+ * pconv_distill_loss gives loss, total and (unless NULL) lse [rows]; pconv_distill_grad the gradient from that lse;
+ * pconv_distill_loss_grad loss, total and the gradient at once.  Asynchronous on hip_stream, allocate nothing, outputs must not
+ * overlap inputs.  Errors: PCONV_INVALID_ARG, PCONV_HIP_ERROR. */
+int pconv_distill_loss(const void *z_dev, int64_t z_stride, pconv_dtype z_dtype, const void *teacher_dev, int64_t teacher_stride,
+                       pconv_dtype teacher_dtype, const void *classes_dev, int64_t classes_stride, int class_bytes, int64_t rows,
+                       int64_t v, int64_t top, float temperature, int mean, float *loss_dev, float *total_dev, float *lse_dev,
+                       void *hip_stream);
+int pconv_distill_grad(const void *z_dev, int64_t z_stride, pconv_dtype z_dtype, const void *teacher_dev, int64_t teacher_stride,
+                       pconv_dtype teacher_dtype, const void *classes_dev, int64_t classes_stride, int class_bytes, int64_t rows,
+                       int64_t v, int64_t top, float temperature, int mean, const float *lse_dev, const float *up_dev,
+                       int64_t up_step, void *grad_dev, int64_t grad_stride, void *hip_stream);
+int pconv_distill_loss_grad(const void *z_dev, int64_t z_stride, pconv_dtype z_dtype, const void *teacher_dev, int64_t teacher_stride,
+                            pconv_dtype teacher_dtype, const void *classes_dev, int64_t classes_stride, int class_bytes,
+                            int64_t rows, int64_t v, int64_t top, float temperature, int mean, float *loss_dev, float *total_dev,
+                            void *grad_dev, int64_t grad_stride, void *hip_stream);
 
 /* ---- inspection of a handle (tests, benchmarks) --------------------------------------- */
 

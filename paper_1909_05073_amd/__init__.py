@@ -140,6 +140,16 @@ def lib():
     L.pconv_linear_mx4.argtypes = [vp, i64, ip, vp, i64, vp, i64, vp, vp, i64, ip, i64, i64, i64, ip, vp, i64, vp]
     L.pconv_debug_mx4_plan.restype = ip
     L.pconv_debug_mx4_plan.argtypes = [i64, i64, i64, vp]
+    f32 = C.c_float
+    L.pconv_add_rms_norm_i8.restype = ip
+    L.pconv_add_rms_norm_i8.argtypes = [vp, i64, vp, i64, vp, i64, ip, vp, f32, i64, i64, vp, i64, vp, vp]
+    logits = [vp, i64, ip, vp, i64, ip, vp, i64, ip, i64, i64, i64, f32, ip]
+    L.pconv_distill_loss.restype = ip
+    L.pconv_distill_loss.argtypes = logits + [vp, vp, vp, vp]
+    L.pconv_distill_grad.restype = ip
+    L.pconv_distill_grad.argtypes = logits + [vp, vp, i64, vp, i64, vp]
+    L.pconv_distill_loss_grad.restype = ip
+    L.pconv_distill_loss_grad.argtypes = logits + [vp, vp, vp, i64, vp]
     L.pconv_grad_workspace.restype = i64
     L.pconv_grad_workspace.argtypes = [i64]
     L.pconv_grad_norm.restype = ip
@@ -161,7 +171,8 @@ EXPORTED_SYMBOLS = ["pconv_project", "pconv_pack", "pconv_conv2d", "pconv_conv2d
                     "pconv_quantize_rows", "pconv_matmul_i8", "pconv_matmul_i8_workspace", "pconv_linear_i8",
                     "pconv_linear_i8_workspace", "pconv_debug_i8_plan",
                     "pconv_quantize_mx4", "pconv_matmul_mx4", "pconv_matmul_mx4_workspace", "pconv_linear_mx4",
-                    "pconv_linear_mx4_workspace", "pconv_debug_mx4_plan", "pconv_grad_workspace", "pconv_grad_norm", "pconv_clip_grads",
+                    "pconv_linear_mx4_workspace", "pconv_debug_mx4_plan", "pconv_add_rms_norm_i8",
+                    "pconv_distill_loss", "pconv_distill_grad", "pconv_distill_loss_grad", "pconv_grad_workspace", "pconv_grad_norm", "pconv_clip_grads",
                     "pconv_last_error"]
 
 
@@ -764,6 +775,54 @@ def linear_i8(x, w, w_scale, bias=None, relu: bool = False, out_dtype=None, out=
     return y
 
 
+def pconv_add_rms_norm_i8(x_ptr: int, x_stride: int, residual_ptr: int, residual_stride: int, sum_ptr: int, sum_stride: int, dtype,
+                          weight_ptr: int, eps: float, rows: int, cols: int, q_ptr: int, q_stride: int, scale_ptr: int, stream: int = 0):
+    """Raw-pointer call, one to one with the C entry point."""
+    _check(lib().pconv_add_rms_norm_i8(x_ptr or None, x_stride, residual_ptr or None, residual_stride, sum_ptr or None, sum_stride,
+                                       _DTYPE[dtype], weight_ptr or None, eps, rows, cols, q_ptr or None, q_stride, scale_ptr or None,
+                                       stream or None))
+
+
+def add_rms_norm_i8(x, residual=None, weight=None, eps: float = 1e-6, out=None):
+    """x, residual [..., k]: CUDA tensors of one type, fp32 or bf16; weight [k]: fp32.  Returns (q [..., k] int8, scale [...] fp32, s):
+    s = x + residual [..., k], of x's type (x itself without a residual), and q * scale[..., None] is about
+    s / sqrt(mean(s^2) + eps) * weight, the norm taken of the sums before they are rounded.
+
+    The rows of q lie a multiple of 16 bytes apart, as matmul_i8 reads them fastest.  out: where s goes; x or residual, or a
+    tensor that overlaps neither nor weight.  Nothing is recorded for autograd."""
+    import torch
+    dtype = _type_of(x, "x")
+    index = _device_index(x, residual, weight, out)
+    m, k, step = _rows(x, "x")
+    lead = x.shape[:-1]
+    r_ptr = s_ptr = None
+    r_step = s_step = 0
+    s = x
+    if residual is not None:
+        if residual.dtype != x.dtype or residual.shape != x.shape:
+            raise ValueError("residual must have x's type and shape")
+        r_step = _rows(residual, "residual")[2]
+        s, s_step = _output(out, lead, m, k, x.dtype, x)
+        r_ptr, s_ptr = residual.data_ptr() or None, s.data_ptr() or None
+    elif out is not None:
+        raise ValueError("out is for sums: there is no residual")
+    w_ptr = _per_channel(weight, k, "weight") if weight is not None else None
+    if out is not None and not _tensor_list_calls().apart(out, x, residual, weight):
+        to = (s_ptr, s_step if m > 1 else 0)
+        others = [t for t in ((x, m, k, step), (residual, m, k, r_step)) if (t[0].data_ptr() or None, t[3] if m > 1 else 0) != to]
+        _refuse_overlap((s, m, k, s_step), *others, (weight, 1, k, k))
+    wide = (k + 15) // 16 * 16
+    q = _empty(lead, m, wide, torch.int8, x)
+    scale = torch.empty_strided((m,), (1,), dtype=torch.float32, device=x.device) if len(lead) == 1 else x.new_empty(lead, dtype=torch.float32)
+    rc = (_lib or lib()).pconv_add_rms_norm_i8(x.data_ptr() or None, step, r_ptr, r_step, s_ptr, s_step, dtype, w_ptr, eps, m, k,
+                                               q.data_ptr() or None, wide, scale.data_ptr() or None, _stream(index))
+    if rc != OK:
+        _check(rc)
+    if out is not None:
+        _tensor_list_calls().changed([out])
+    return (q if wide == k else q[..., :k]), scale, s
+
+
 # ---- layers in 4-bit floats --------------------------------------------------------------
 #
 # As the 8-bit layers: they serve networks that are trained, nothing is recorded for autograd.
@@ -1055,3 +1114,146 @@ def grad_norm(grads):
 def clip_grad_norm(grads, max_norm: float, eps: float = 1e-6, out=None):
     """Limits the norm of all gradients together, in place unless `out` says otherwise; see GradList.  Returns the norm."""
     return GradList(grads, out).clip(max_norm, eps)
+
+
+# ---- distillation --------------------------------------------------------------------------
+
+def pconv_distill_loss(z_ptr: int, z_stride: int, z_dtype, teacher_ptr: int, teacher_stride: int, teacher_dtype, classes_ptr: int,
+                       classes_stride: int, class_bytes: int, rows: int, v: int, top: int, temperature: float, mean: bool, loss_ptr: int,
+                       total_ptr: int = 0, lse_ptr: int = 0, stream: int = 0):
+    """Raw-pointer call, one to one with the C entry point."""
+    _check(lib().pconv_distill_loss(z_ptr or None, z_stride, _DTYPE[z_dtype], teacher_ptr or None, teacher_stride, _DTYPE[teacher_dtype],
+                                    classes_ptr or None, classes_stride, class_bytes, rows, v, top, temperature, int(bool(mean)),
+                                    loss_ptr or None, total_ptr or None, lse_ptr or None, stream or None))
+
+
+def pconv_distill_grad(z_ptr: int, z_stride: int, z_dtype, teacher_ptr: int, teacher_stride: int, teacher_dtype, classes_ptr: int,
+                       classes_stride: int, class_bytes: int, rows: int, v: int, top: int, temperature: float, mean: bool, lse_ptr: int,
+                       up_ptr: int, up_step: int, grad_ptr: int, grad_stride: int, stream: int = 0):
+    """Raw-pointer call, one to one with the C entry point."""
+    _check(lib().pconv_distill_grad(z_ptr or None, z_stride, _DTYPE[z_dtype], teacher_ptr or None, teacher_stride, _DTYPE[teacher_dtype],
+                                    classes_ptr or None, classes_stride, class_bytes, rows, v, top, temperature, int(bool(mean)),
+                                    lse_ptr or None, up_ptr or None, up_step, grad_ptr or None, grad_stride, stream or None))
+
+
+def pconv_distill_loss_grad(z_ptr: int, z_stride: int, z_dtype, teacher_ptr: int, teacher_stride: int, teacher_dtype, classes_ptr: int,
+                            classes_stride: int, class_bytes: int, rows: int, v: int, top: int, temperature: float, mean: bool,
+                            loss_ptr: int, total_ptr: int, grad_ptr: int, grad_stride: int, stream: int = 0):
+    """Raw-pointer call, one to one with the C entry point."""
+    _check(lib().pconv_distill_loss_grad(z_ptr or None, z_stride, _DTYPE[z_dtype], teacher_ptr or None, teacher_stride, _DTYPE[teacher_dtype],
+                                         classes_ptr or None, classes_stride, class_bytes, rows, v, top, temperature, int(bool(mean)),
+                                         loss_ptr or None, total_ptr or None, grad_ptr or None, grad_stride, stream or None))
+
+
+_REDUCTIONS = ("none", "sum", "mean")
+
+
+def _distill_call(student, teacher, classes, temperature, reduction):
+    """What the calls take alike: (device, rows, classes, the arguments up to `mean`)."""
+    import torch
+    if reduction not in _REDUCTIONS:
+        raise ValueError("reduction must be one of " + ", ".join(_REDUCTIONS))
+    z_type, t_type = _type_of(student, "student"), _type_of(teacher, "teacher")
+    if classes.dtype not in (torch.int64, torch.int32):
+        raise ValueError("classes must be int64 or int32")
+    if teacher.shape != classes.shape or teacher.dim() != student.dim() or teacher.shape[:-1] != student.shape[:-1]:
+        raise ValueError("teacher and classes [..., top] must have the rows of student [..., v]")
+    index = _device_index(student, teacher, classes)
+    m, v, z_step = _rows(student, "student")
+    _, top, t_step = _rows(teacher, "teacher")
+    c_step = _rows(classes, "classes")[2]
+    return index, m, v, (student.data_ptr() or None, z_step, z_type, teacher.data_ptr() or None, t_step, t_type, classes.data_ptr() or None, c_step,
+                         classes.element_size(), m, v, top, float(temperature), 1 if reduction == "mean" else 0)
+
+
+def _distill_losses(student, m, reduction):
+    """(the rows' losses, the result, or None where it is the rows' losses)."""
+    import torch
+    loss = torch.empty_strided((m,), (1,), dtype=torch.float32, device=student.device)
+    return loss, None if reduction == "none" else torch.empty_strided((), (), dtype=torch.float32, device=student.device)
+
+
+def _distill_forward(student, teacher, classes, temperature, reduction, keep):
+    import torch
+    index, m, v, call = _distill_call(student, teacher, classes, temperature, reduction)
+    loss, total = _distill_losses(student, m, reduction)
+    lse = torch.empty_strided((m,), (1,), dtype=torch.float32, device=student.device) if keep else None
+    rc = (_lib or lib()).pconv_distill_loss(*call, loss.data_ptr() or None, total.data_ptr() if total is not None else None,
+                                            (lse.data_ptr() or None) if keep else None, _stream(index))
+    if rc != OK:
+        _check(rc)
+    return (loss.view(student.shape[:-1]) if total is None else total), lse
+
+
+_distill_function = None
+
+
+def _distill_autograd():
+    """The loss as autograd takes it (made when it is first asked for, as torch is loaded then)."""
+    global _distill_function
+    if _distill_function is not None:
+        return _distill_function
+    import torch
+
+    class DistillLoss(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, student, teacher, classes, temperature, reduction):
+            value, lse = _distill_forward(student, teacher, classes, temperature, reduction, True)
+            ctx.save_for_backward(student, teacher, classes, lse)
+            ctx.how = temperature, reduction
+            return value
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, up):
+            student, teacher, classes, lse = ctx.saved_tensors
+            temperature, reduction = ctx.how
+            index, m, v, call = _distill_call(student, teacher, classes, temperature, reduction)
+            up = up.to(torch.float32)
+            if reduction == "none":
+                up = up.reshape(-1).contiguous()
+            grad = _empty(student.shape[:-1], m, v, student.dtype, student)
+            rc = (_lib or lib()).pconv_distill_grad(*call, lse.data_ptr() or None, up.data_ptr() or None, 1 if reduction == "none" else 0,
+                                                    grad.data_ptr() or None, v, _stream(index))
+            if rc != OK:
+                _check(rc)
+            return grad, None, None, None, None
+
+    _distill_function = DistillLoss
+    return DistillLoss
+
+
+def distill_loss(student, teacher, classes, temperature: float = 1.0, reduction: str = "mean"):
+    """student [..., v], teacher [..., top]: logits, CUDA tensors, fp32 or bf16; classes [..., top]: int64 or int32, where the teacher's
+    logits belong (outside 0 .. v - 1: no entry).  Returns T^2 times the divergence of the student's distribution over all classes
+    from the teacher's over its entries, at temperature T: of each row ("none"), their sum, or that divided by the rows
+    ("mean", rows without an entry among them), fp32; see include/pconv.h.
+
+    Recorded for autograd: a gradient goes to the student (of its type), none to the teacher."""
+    import torch
+    if not torch.is_grad_enabled():
+        return _distill_forward(student, teacher, classes, temperature, reduction, False)[0]
+    if teacher.requires_grad:
+        raise ValueError("no gradient goes to the teacher: detach it")
+    if student.requires_grad:
+        return _distill_autograd().apply(student, teacher, classes, temperature, reduction)
+    return _distill_forward(student, teacher, classes, temperature, reduction, False)[0]
+
+
+def distill_loss_grad(student, teacher, classes, temperature: float = 1.0, reduction: str = "mean", out=None):
+    """(distill_loss, its gradient [..., v] with respect to the student), in one pass over the logits; with reduction "none" the gradient of
+    the sum.  For loops that go on from the logits themselves: student.backward(grad).
+
+    out: where the gradient goes, of the student's type; it must not overlap an input.  Nothing is recorded for autograd."""
+    index, m, v, call = _distill_call(student, teacher, classes, temperature, reduction)
+    grad, g_step = _output(out, student.shape[:-1], m, v, student.dtype, student)
+    if out is not None and not _tensor_list_calls().apart(grad, student, teacher, classes):
+        _refuse_overlap((grad, m, v, g_step), (student, m, v, call[1]), (teacher, m, call[11], call[4]), (classes, m, call[11], call[7]))
+    loss, total = _distill_losses(student, m, reduction)
+    rc = (_lib or lib()).pconv_distill_loss_grad(*call, loss.data_ptr() or None, total.data_ptr() if total is not None else None,
+                                                 grad.data_ptr() or None, g_step, _stream(index))
+    if rc != OK:
+        _check(rc)
+    if out is not None:
+        _tensor_list_calls().changed([grad])
+    return (loss.view(student.shape[:-1]) if total is None else total), grad

@@ -12,7 +12,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libpconv.so")
 TENSORS = os.path.join(HERE, "_tensors.so")
 SOURCES = ["pconv_capi.cpp", "pconv_pack.cpp", "pconv_kernels.hip", "pconv_tiled.hip", "pconv_lone.hip",
-           "pconv_mfma.hip", "pconv_mfma_flat.hip", "pconv_ops_capi.cpp", "pconv_i8.hip", "pconv_mx4.hip", "pconv_grads.hip"]
+           "pconv_mfma.hip", "pconv_mfma_flat.hip", "pconv_ops_capi.cpp", "pconv_i8.hip", "pconv_mx4.hip", "pconv_norm.hip",
+           "pconv_distill.hip", "pconv_grads.hip"]
 
 # packed-FP32 instructions are switched off for every device compile of this project
 HIP_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

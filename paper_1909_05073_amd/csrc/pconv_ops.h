@@ -1,4 +1,5 @@
-// What pconv_ops_capi.cpp and the kernels of the 8-bit and 4-bit layers and the gradients share.
+// What pconv_ops_capi.cpp and the kernels of the 8-bit and 4-bit layers, the norm, the distillation and
+// the gradients share.
 #ifndef PCONV_OPS_H
 #define PCONV_OPS_H
 
@@ -61,6 +62,32 @@ int64_t matmul_mx4_work_bytes(int64_t m, int64_t n, int64_t blocks);
 int check_matmul_mx4(int64_t m, int64_t n, int64_t blocks);              // whether the product can be launched
 pconv_mx4_plan matmul_mx4_plan(int64_t m, int64_t n, int64_t blocks);
 int launch_matmul_mx4(const Mx4Product &p, void *work, void *stream);
+
+// s = x + r (r: or null), h = s / sqrt(mean s^2 + eps) * weight (or null), q and scale of h; sum: where s goes (or null).
+struct NormRows {
+    const void *x, *r;
+    void *sum;
+    const float *weight;
+    int8_t *q;
+    float *scale;
+    int64_t ldx, ldr, ldsum, ldq, rows, cols;
+    float eps;
+};
+int launch_add_rms_norm_i8(const NormRows &p, int bf16, void *stream);
+
+// Distillation: student's logits z [rows][v], teacher's t [rows][top] at the classes c.
+struct DistillRows {
+    const void *z, *t, *c;
+    float *loss, *lse;                 // [rows]; lse may be null where the loss is computed
+    const float *up;                   // the gradient that comes in, up_step from row to row; null: 1
+    void *grad;
+    int64_t ldz, ldt, ldc, ldg, rows, up_step;
+    int v, top;
+    float inv_t, t2, factor;           // 1 / T, T^2, T and what the rows are divided by
+    int z_bf16, t_bf16, c_wide;
+};
+int launch_distill(const DistillRows &p, bool loss, bool grad, void *stream);
+int launch_distill_total(const float *loss, int64_t rows, double scale, float *total, void *stream);
 
 // Up to kGradTensors tensors travel in the arguments of one launch (4 KiB), cut into chunks of 1 << `log2` elements.
 constexpr int kGradTensors = 160, kGradBlocks = 2048;

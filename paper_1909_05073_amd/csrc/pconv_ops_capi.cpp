@@ -1,4 +1,4 @@
-// extern "C" boundary of the 8-bit and 4-bit layers and the gradients (see include/pconv.h for the contract).
+// extern "C" boundary of the 8-bit and 4-bit layers, the norm, the distillation and the gradients (see include/pconv.h for the contract).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -13,6 +13,7 @@ using namespace pconv;
 namespace {
 
 constexpr int64_t kMaxRows = (int64_t(1) << 31) - 1, kMaxSide = int64_t(1) << 30, kMaxK = 131071;
+constexpr int64_t kMaxTop = 1024;                                        // entries of a row of the distillation
 constexpr int64_t kMaxBlocks = 1 << 19, kMaxRowBytes = 1 << 23;      // of the 4-bit layers
 constexpr int64_t kMaxTensors = 1 << 24, kMaxElements = int64_t(1) << 45;    // fewer than 2^32 chunks together
 
@@ -77,6 +78,35 @@ int check_product_mx4(const char *who, const uint8_t *b, int64_t ldb, const uint
         if (const int rc = check_blocks(who, b, ldb, sb, slab_b, n, blocks)) return rc;
     p = Mx4Product{nullptr, b, nullptr, sb, bias, y, 0, ldb, 0, slab_b, ldy, int(m), int(n), int(blocks), relu ? 1 : 0, y_dtype == PCONV_BF16};
     return PCONV_OK;
+}
+
+bool at_type(const void *p, int64_t size) { return reinterpret_cast<uintptr_t>(p) % uint64_t(size) == 0; }
+
+// What the calls of the distillation check alike, and what they compute but for their outputs.
+int check_distill(const char *who, const void *z, int64_t ldz, int z_type, const void *t, int64_t ldt, int t_type, const void *c, int64_t ldc,
+                  int class_bytes, int64_t rows, int64_t v, int64_t top, float temperature, int mean, DistillRows &p)
+{
+    if (rows < 0 || rows > kMaxRows || v < 0 || v > kMaxSide) return invalid(who, "rows must be 0 .. 2^31 - 1, v 0 .. 2^30");
+    if (top < 0 || top > kMaxTop) return invalid(who, "top must be 0 .. 1024");
+    if (!is_dtype(z_type) || !is_dtype(t_type)) return invalid(who, "unknown dtype");
+    if (class_bytes != 4 && class_bytes != 8) return invalid(who, "classes must have 4 or 8 bytes");
+    if (!(temperature > 0.0f) || std::isinf(temperature) || std::isinf(1.0f / temperature) || std::isinf(temperature * temperature))
+        return invalid(who, "the temperature must be a number above 0 whose square and reciprocal are numbers");
+    if (rows == 0) return PCONV_OK;
+    if ((v && !z) || (top && (!t || !c))) return invalid(who, "null pointer argument");
+    if (!stride_fits(rows, v, ldz) || !stride_fits(rows, top, ldt) || !stride_fits(rows, top, ldc)) return invalid(who, "rows must lie at least their length apart");
+    if (!at_type(z, z_type == PCONV_BF16 ? 2 : 4) || !at_type(t, t_type == PCONV_BF16 ? 2 : 4) || !at_type(c, class_bytes)) return invalid(who, "rows must be aligned to their type");
+    p = DistillRows{z, t, c, nullptr, nullptr, nullptr, nullptr, ldz, ldt, ldc, 0, rows, 0, int(v), int(top), 1.0f / temperature,
+                    temperature * temperature, float(double(temperature) / (mean ? double(rows) : 1.0)), z_type == PCONV_BF16,
+                    t_type == PCONV_BF16, class_bytes == 8};
+    return PCONV_OK;
+}
+
+int check_grad_rows(const char *who, void *grad, int64_t ldg, int type, int64_t rows, int64_t v)
+{
+    if (v && !grad) return invalid(who, "null pointer argument");
+    if (!stride_fits(rows, v, ldg)) return invalid(who, "rows must lie at least their length apart");
+    return at_type(grad, type == PCONV_BF16 ? 2 : 4) ? PCONV_OK : invalid(who, "rows must be aligned to their type");
 }
 
 // The tensors that are clipped together, and how they are cut up.
@@ -331,6 +361,81 @@ int pconv_debug_mx4_plan(int64_t m, int64_t n, int64_t blocks, pconv_mx4_plan *o
     if (!mx4_sizes_fit(m, n, blocks)) return invalid("pconv_debug_mx4_plan", "m and n must be 1 .. 2^30, blocks 0 .. 2^19");
     *out = matmul_mx4_plan(m, n, blocks);
     return PCONV_OK;
+}
+
+int pconv_add_rms_norm_i8(const void *x_dev, int64_t x_stride, const void *residual_dev, int64_t residual_stride, void *sum_dev,
+                          int64_t sum_stride, pconv_dtype dtype, const float *weight_dev, float eps, int64_t rows, int64_t cols,
+                          int8_t *q_dev, int64_t q_stride, float *scale_dev, void *hip_stream)
+{
+    const char *who = "pconv_add_rms_norm_i8";
+    if (rows < 0 || cols < 0 || rows > kMaxRows || cols > kMaxRows) return invalid(who, "rows and cols must be 0 .. 2^31 - 1");
+    if (!is_dtype(int(dtype))) return invalid(who, "unknown dtype");
+    if (!(eps > 0.0f) || std::isinf(eps)) return invalid(who, "eps must be a number above 0");
+    if (sum_dev && !residual_dev) return invalid(who, "sums are of two operands: there is no residual");
+    if (rows == 0) return PCONV_OK;
+    if (!scale_dev || (cols && (!x_dev || !q_dev))) return invalid(who, "null pointer argument");
+    if (!stride_fits(rows, cols, x_stride) || !stride_fits(rows, cols, q_stride) || (residual_dev && !stride_fits(rows, cols, residual_stride)) ||
+        (sum_dev && !stride_fits(rows, cols, sum_stride)))
+        return invalid(who, "rows must lie at least their length apart");
+    if (sum_dev && rows > 1 && ((sum_dev == x_dev && sum_stride != x_stride) || (sum_dev == residual_dev && sum_stride != residual_stride)))
+        return invalid(who, "sums in an operand's place must have its stride");
+    const int size = dtype == PCONV_BF16 ? 2 : 4;
+    if (!at_type(x_dev, size) || !at_type(residual_dev, size) || !at_type(sum_dev, size) || !at_type(weight_dev, 4)) return invalid(who, "rows must be aligned to their type");
+    return launch_add_rms_norm_i8(NormRows{x_dev, residual_dev, sum_dev, weight_dev, q_dev, scale_dev, x_stride, residual_stride, sum_stride, q_stride,
+                                           rows, cols, eps}, dtype == PCONV_BF16, hip_stream);
+}
+
+int pconv_distill_loss(const void *z_dev, int64_t z_stride, pconv_dtype z_dtype, const void *teacher_dev, int64_t teacher_stride,
+                       pconv_dtype teacher_dtype, const void *classes_dev, int64_t classes_stride, int class_bytes, int64_t rows,
+                       int64_t v, int64_t top, float temperature, int mean, float *loss_dev, float *total_dev, float *lse_dev,
+                       void *hip_stream)
+{
+    const char *who = "pconv_distill_loss";
+    DistillRows p;
+    if (const int rc = check_distill(who, z_dev, z_stride, int(z_dtype), teacher_dev, teacher_stride, int(teacher_dtype), classes_dev, classes_stride,
+                                     class_bytes, rows, v, top, temperature, mean, p)) return rc;
+    if (rows > 0) {
+        if (!loss_dev) return invalid(who, "null pointer argument");
+        p.loss = loss_dev; p.lse = lse_dev;
+        if (const int rc = launch_distill(p, true, false, hip_stream)) return rc;
+    }
+    return total_dev ? launch_distill_total(loss_dev, rows, mean && rows ? 1.0 / double(rows) : 1.0, total_dev, hip_stream) : PCONV_OK;
+}
+
+int pconv_distill_grad(const void *z_dev, int64_t z_stride, pconv_dtype z_dtype, const void *teacher_dev, int64_t teacher_stride,
+                       pconv_dtype teacher_dtype, const void *classes_dev, int64_t classes_stride, int class_bytes, int64_t rows,
+                       int64_t v, int64_t top, float temperature, int mean, const float *lse_dev, const float *up_dev,
+                       int64_t up_step, void *grad_dev, int64_t grad_stride, void *hip_stream)
+{
+    const char *who = "pconv_distill_grad";
+    DistillRows p;
+    if (const int rc = check_distill(who, z_dev, z_stride, int(z_dtype), teacher_dev, teacher_stride, int(teacher_dtype), classes_dev, classes_stride,
+                                     class_bytes, rows, v, top, temperature, mean, p)) return rc;
+    if (up_step != 0 && up_step != 1) return invalid(who, "up_step must be 0 or 1");
+    if (rows == 0) return PCONV_OK;
+    if (!lse_dev) return invalid(who, "null pointer argument");
+    if (const int rc = check_grad_rows(who, grad_dev, grad_stride, int(z_dtype), rows, v)) return rc;
+    if (v == 0) return PCONV_OK;
+    p.lse = const_cast<float *>(lse_dev); p.up = up_dev; p.up_step = up_step; p.grad = grad_dev; p.ldg = grad_stride;
+    return launch_distill(p, false, true, hip_stream);
+}
+
+int pconv_distill_loss_grad(const void *z_dev, int64_t z_stride, pconv_dtype z_dtype, const void *teacher_dev, int64_t teacher_stride,
+                            pconv_dtype teacher_dtype, const void *classes_dev, int64_t classes_stride, int class_bytes,
+                            int64_t rows, int64_t v, int64_t top, float temperature, int mean, float *loss_dev, float *total_dev,
+                            void *grad_dev, int64_t grad_stride, void *hip_stream)
+{
+    const char *who = "pconv_distill_loss_grad";
+    DistillRows p;
+    if (const int rc = check_distill(who, z_dev, z_stride, int(z_dtype), teacher_dev, teacher_stride, int(teacher_dtype), classes_dev, classes_stride,
+                                     class_bytes, rows, v, top, temperature, mean, p)) return rc;
+    if (rows > 0) {
+        if (!loss_dev) return invalid(who, "null pointer argument");
+        if (const int rc = check_grad_rows(who, grad_dev, grad_stride, int(z_dtype), rows, v)) return rc;
+        p.loss = loss_dev; p.grad = grad_dev; p.ldg = grad_stride;
+        if (const int rc = launch_distill(p, true, true, hip_stream)) return rc;
+    }
+    return total_dev ? launch_distill_total(loss_dev, rows, mean && rows ? 1.0 / double(rows) : 1.0, total_dev, hip_stream) : PCONV_OK;
 }
 
 int64_t pconv_grad_workspace(int64_t num)
