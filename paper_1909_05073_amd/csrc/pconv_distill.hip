@@ -37,51 +37,31 @@ struct Running {
     }
 };
 
-// TPR threads that share a row: a wave, or all of a workgroup, which meets at barriers.
-template <int TPR> struct Group {
-    static constexpr int WAVES = TPR / 64;
-    static __device__ __forceinline__ void meet()
-    {
-        if (TPR > 64) {
-            __syncthreads();
-        } else {
-            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-            __builtin_amdgcn_wave_barrier();
-            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+// What the TPR threads of a row, a wave or all of a workgroup, find together; their order depends on nothing.  `room`: a place
+// for each wave, not read any more by a call before.
+template <int TPR>
+__device__ __forceinline__ void join_threads(Running &z, Running &t, Running (*room)[2])
+{
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        z.join(Running{__shfl_xor(z.most, d), __shfl_xor(z.sum, d)});
+        t.join(Running{__shfl_xor(t.most, d), __shfl_xor(t.sum, d)});
+    }
+    if constexpr (TPR > 64) {
+        if ((threadIdx.x & 63) == 0) {
+            room[threadIdx.x >> 6][0] = z;
+            room[threadIdx.x >> 6][1] = t;
+        }
+        __syncthreads();
+        z = room[0][0];
+        t = room[0][1];
+#pragma unroll
+        for (int i = 1; i < TPR / 64; ++i) {
+            z.join(room[i][0]);
+            t.join(room[i][1]);
         }
     }
-    // (`room`: WAVES of them in LDS; nobody reads it any more when the next call begins if a meet() lies between)
-    static __device__ __forceinline__ Running join(Running v, Running *room)
-    {
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) v.join(Running{__shfl_xor(v.most, d), __shfl_xor(v.sum, d)});
-        if (TPR == 64) return v;
-        if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = room[0];
-#pragma unroll
-        for (int i = 1; i < WAVES; ++i) v.join(room[i]);
-        return v;
-    }
-    static __device__ __forceinline__ float add(float v, float *room)
-    {
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-        if (TPR == 64) return v;
-        if ((threadIdx.x & 63) == 0) room[threadIdx.x >> 6] = v;
-        __syncthreads();
-        v = room[0];
-#pragma unroll
-        for (int i = 1; i < WAVES; ++i) v += room[i];
-        return v;
-    }
-};
-
-// What a row's entries leave in LDS, `top` of each.
-struct Entries {
-    float *p, *at;                                       // the teacher's logit over T; the student's at its class
-    int *c;                                              // its class; -1: no entry
-};
+}
 
 __device__ __forceinline__ float teacher_at(const DistillRows &p, int64_t row, int j)
 {
@@ -96,121 +76,167 @@ __device__ __forceinline__ int class_at(const DistillRows &p, int64_t row, int j
     return c >= 0 && c < p.v ? int(c) : -1;
 }
 
-// The entries of a row; log of the sum that their shares were divided by goes to `log_sum` (with the maximum).  Returns whether
-// the row has an entry that counts.
-template <typename T, int TPR>
-__device__ __forceinline__ bool read_entries(const DistillRows &p, const T *z, int64_t row, int sub, Entries e, Running *room, float &log_sum)
+// Vectors first, first + TPR, .. below `whole`, U of them; -infinity in the place of those that are not there.
+template <typename T, int TPR, int U>
+__device__ __forceinline__ void load_vectors(const T *z, int first, int whole, Vec<T> (&v)[U])
 {
-    Running r{-INFINITY, 0.0f};
-    for (int j = sub; j < p.top; j += TPR) {
-        const int c = class_at(p, row, j);
-        const float t = c < 0 ? -INFINITY : teacher_at(p, row, j) * p.inv_t;
-        e.c[j] = c;
-        e.p[j] = t;
-        e.at[j] = c < 0 ? 0.0f : float(z[c]);
-        r.join(Running{t, t == -INFINITY ? 0.0f : 1.0f});
-    }
-    r = Group<TPR>::join(r, room);
-    log_sum = r.base() + __logf(r.sum);
-    const bool some = !(r.most == -INFINITY && r.sum == 0.0f);
-    Group<TPR>::meet();
-    return some;
-}
-
-template <typename T>
-__device__ __forceinline__ void store_grads(const float (&g)[Vec<T>::N], T *row, int64_t at, int64_t cols)
-{
-    constexpr int N = Vec<T>::N;
-    T w[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = T(g[i]);
-    if (__builtin_expect(at + N <= cols, 1)) {
-        __builtin_memcpy(row + at, w, sizeof(w));
-    } else {
+    for (int i = 0; i < U; ++i) {
+        const int k = first + i * TPR;
+        if (k < whole) {
+            __builtin_memcpy(&v[i].v, z + int64_t(k) * Vec<T>::N, 16);
+        } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (at + i < cols) row[at + i] = w[i];
+            for (int e = 0; e < Vec<T>::N; ++e) v[i].v[e] = T(-INFINITY);
+        }
     }
 }
 
-// LOSS: the loss and lse of each row; GRAD: its gradient, from lse where LOSS is false.  TPR threads share a row, which is
-// read again for the gradient; then the classes of the entries are written once more with their shares taken off, each by
-// the first entry that names it.
-template <typename T, int TPR, bool LOSS, bool GRAD>
+// Values stay as they came between their uses: without this bf16 ones are kept as floats too, and 32768 of a workgroup take 221
+// registers.
+template <typename T, int U>
+__device__ __forceinline__ void keep_packed(Vec<T> (&v)[U])
+{
+#pragma unroll
+    for (int i = 0; i < U; ++i) asm volatile("" : "+v"(v[i].v));
+}
+
+// The values of vectors, over T, join what a thread has found.
+template <typename T, int U>
+__device__ __forceinline__ void join_vectors(Running &r, Vec<T> (&v)[U], float inv_t)
+{
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+        for (int e = 0; e < Vec<T>::N; ++e) m = fmaxf(m, v[i].at(e));
+    m = fmaxf(r.most, m * inv_t);
+    const float b = m == -INFINITY ? 0.0f : m;
+    r.sum *= exp_of(r.most - b);
+    keep_packed(v);
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+        for (int e = 0; e < Vec<T>::N; ++e) r.sum += exp_of(__builtin_fmaf(v[i].at(e), inv_t, -b));
+    r.most = m;
+}
+
+// LOSS: the loss and lse of each row; GRAD: its gradient, from lse where LOSS is false.  TPR threads share a row, which they
+// read U vectors of 16 bytes a thread at a time; where both are computed the first U of each stay in registers from the
+// sums to the gradient, and what lies beyond is read twice.  The entries' shares and classes lie in LDS.  The gradient is written as if there were no entries; behind a barrier the first
+// entry that names a class writes it again with the shares of all that name it taken off.
+template <typename T, int TPR, int U, bool LOSS, bool GRAD>
 __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR)
 distill_kernel(const DistillRows p)
 {
-    constexpr int N = Vec<T>::N, THREADS = TPR < 256 ? 256 : TPR, RPW = THREADS / TPR;
+    constexpr int N = Vec<T>::N, THREADS = TPR < 256 ? 256 : TPR, RPW = THREADS / TPR, WAVES = TPR / 64;
     extern __shared__ float entries[];
-    __shared__ Running room_r[2][THREADS / 64];
-    __shared__ float room_f[THREADS / 64];
+    __shared__ Running room[THREADS / 64][2];
+    __shared__ float losses[THREADS / 64];
     const int sub = int(threadIdx.x) % TPR, of = int(threadIdx.x) / TPR;
-    Entries e;
-    e.p = entries + of * 3 * p.top;
-    e.at = e.p + p.top;
-    e.c = reinterpret_cast<int *>(e.at + p.top);
+    const int whole = p.v / N, rest = p.v % N;           // whole vectors of a row; the elements behind them go to a thread each
+    const int fours = (p.top + 3) / 4;
+    float *const share = entries + of * 12 * fours, *const at_class = share + 4 * fours;
+    int *const cls = reinterpret_cast<int *>(at_class + 4 * fours);
+    const auto meet = [] {
+        if constexpr (TPR > 64) {
+            __syncthreads();
+        } else {
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
+        }
+    };
     for (int64_t row = int64_t(blockIdx.x) * RPW + of; row < p.rows; row += int64_t(gridDim.x) * RPW) {
         const T *const z = static_cast<const T *>(p.z) + row * p.ldz;
-        float log_sum;
-        const bool some = read_entries<T, TPR>(p, z, row, sub, e, room_r[0], log_sum);
-        float lse;
+        Vec<T> v[U];
+        load_vectors<T, TPR, U>(z, sub, whole, v);
+        const float last = sub < rest ? float(z[int64_t(whole) * N + sub]) : -INFINITY;
+        // each thread's own entries
+        Running t{-INFINITY, 0.0f}, r{-INFINITY, 0.0f};
+        for (int j = sub; j < 4 * fours; j += TPR) {
+            const int c = j < p.top ? class_at(p, row, j) : -1;
+            const float x = c < 0 ? -INFINITY : teacher_at(p, row, j) * p.inv_t;
+            cls[j] = c;
+            share[j] = x;
+            if (c >= 0) at_class[j] = float(z[c]);
+            t.join(Running{x, x == -INFINITY ? 0.0f : 1.0f});
+        }
         if constexpr (LOSS) {
-            Running r{-INFINITY, 0.0f};
-            for (int64_t at = int64_t(sub) * N; at < p.v; at += TPR * N) {
-                const Vec<T> v = load_vec(z, at, p.v);
-                float x[N], m = -INFINITY;
+            join_vectors<T, U>(r, v, p.inv_t);
+            for (int k = U * TPR + sub; k < whole; k += U * TPR) {
+                Vec<T> w[U];
+                load_vectors<T, TPR, U>(z, k, whole, w);
+                join_vectors<T, U>(r, w, p.inv_t);
+            }
+            if (sub < rest) r.join(Running{last * p.inv_t, last == -INFINITY ? 0.0f : 1.0f});
+        }
+        join_threads<TPR>(r, t, room + of * WAVES);
+        const float lse = LOSS ? r.base() + __logf(r.sum) : p.lse[row], log_sum = t.base() + __logf(t.sum);
+        const bool some = !(t.most == -INFINITY && t.sum == 0.0f);
+        float loss = 0;
+        for (int j = sub; j < 4 * fours; j += TPR) {
+            const float lp = share[j] - log_sum, part = cls[j] >= 0 ? exp_of(lp) : 0.0f;
+            if (LOSS && cls[j] >= 0 && lp != -INFINITY) loss += part * (lp - __builtin_fmaf(at_class[j], p.inv_t, -lse));
+            share[j] = part;
+        }
+        T *const out = static_cast<T *>(p.grad) + row * p.ldg;
+        const float f = GRAD && some ? p.factor * (p.up ? p.up[row * p.up_step] : 1.0f) : 0.0f;
+        if constexpr (GRAD) {
+            const auto grad_of = [&](float x) { return some ? f * exp_of(__builtin_fmaf(x, p.inv_t, -lse)) : 0.0f; };
+            const auto write = [&](const Vec<T> &x, int k) {
+                T w[N];
 #pragma unroll
-                for (int i = 0; i < N; ++i) {
-                    x[i] = at + i < p.v ? v.at(i) * p.inv_t : -INFINITY;
-                    m = fmaxf(m, x[i]);
-                }
-                const float b = fmaxf(m, r.most) == -INFINITY ? 0.0f : fmaxf(m, r.most);
-                r.sum *= exp_of(r.most - b);
+                for (int i = 0; i < N; ++i) w[i] = T(grad_of(x.at(i)));
+                if (k < whole) __builtin_memcpy(out + int64_t(k) * N, w, 16);
+            };
+            keep_packed(v);
 #pragma unroll
-                for (int i = 0; i < N; ++i) r.sum += exp_of(x[i] - b);
-                r.most = fmaxf(m, r.most);
+            for (int i = 0; i < U; ++i) write(v[i], sub + i * TPR);
+            for (int k = U * TPR + sub; k < whole; k += U * TPR) {
+                Vec<T> w[U];
+                load_vectors<T, TPR, U>(z, k, whole, w);
+#pragma unroll
+                for (int i = 0; i < U; ++i) write(w[i], k + i * TPR);
             }
-            r = Group<TPR>::join(r, room_r[1]);
-            lse = r.base() + __logf(r.sum);
-            float loss = 0;
-            for (int j = sub; j < p.top; j += TPR) {
-                const float lp = e.p[j] - log_sum;
-                if (e.c[j] >= 0 && lp != -INFINITY) loss += exp_of(lp) * (lp - __builtin_fmaf(e.at[j], p.inv_t, -lse));
+            if (sub < rest) out[int64_t(whole) * N + sub] = T(grad_of(last));
+        }
+        if constexpr (LOSS) {
+#pragma unroll
+            for (int d = 1; d < 64; d *= 2) loss += __shfl_xor(loss, d);
+            if (TPR > 64 && (threadIdx.x & 63) == 0) losses[threadIdx.x >> 6] = loss;
+        }
+        if (GRAD) __threadfence_block();                 // (the stores of the row are done before some of it is written again)
+        meet();
+        if (LOSS && sub == 0) {
+            if constexpr (TPR > 64) {
+                loss = losses[0];
+#pragma unroll
+                for (int i = 1; i < WAVES; ++i) loss += losses[i];
             }
-            loss = Group<TPR>::add(loss, room_f);
-            if (sub == 0) {
-                p.loss[row] = some ? loss * p.t2 : 0.0f;
-                if (p.lse) p.lse[row] = lse;
-            }
-        } else {
-            lse = p.lse[row];
+            p.loss[row] = some ? loss * p.t2 : 0.0f;
+            if (p.lse) p.lse[row] = lse;
         }
         if constexpr (GRAD) {
-            T *const out = static_cast<T *>(p.grad) + row * p.ldg;
-            const float f = some ? p.factor * (p.up ? p.up[row * p.up_step] : 1.0f) : 0.0f;
-            for (int64_t at = int64_t(sub) * N; at < p.v; at += TPR * N) {
-                const Vec<T> v = load_vec(z, at, p.v);
-                float g[N];
-#pragma unroll
-                for (int i = 0; i < N; ++i) g[i] = some ? f * exp_of(__builtin_fmaf(v.at(i), p.inv_t, -lse)) : 0.0f;
-                store_grads<T>(g, out, at, p.v);
-            }
-            __threadfence_block();                       // (the stores of the row are done before some of it is written again)
-            Group<TPR>::meet();
             for (int j = sub; j < p.top && some; j += TPR) {
-                const int c = e.c[j];
+                const int c = cls[j];
                 if (c < 0) continue;
                 bool first = true;
-                float share = 0;
-                for (int i = 0; i < p.top; ++i)
-                    if (e.c[i] == c) {
-                        first = first && i >= j;
-                        share += exp_of(e.p[i] - log_sum);
-                    }
-                if (first) out[c] = T(f * (exp_of(__builtin_fmaf(e.at[j], p.inv_t, -lse)) - share));
+                float off = 0;
+                for (int i = 0; i < fours; ++i) {
+                    const v4i others = reinterpret_cast<const v4i *>(cls)[i];
+                    const f4 shares = reinterpret_cast<const f4 *>(share)[i];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (others[q] == c) {
+                            first = first && 4 * i + q >= j;
+                            off += shares[q];
+                        }
+                }
+                if (first) out[c] = T(f * (exp_of(__builtin_fmaf(at_class[j], p.inv_t, -lse)) - off));
             }
         }
-        Group<TPR>::meet();                              // (the entries are read)
+        if (row + int64_t(gridDim.x) * RPW < p.rows) meet();             // (the entries are read)
     }
 }
 
@@ -235,11 +261,22 @@ distill_total_kernel(const float *__restrict__ loss, int64_t rows, double scale,
 template <typename T, bool LOSS, bool GRAD>
 void launch_rows(const DistillRows &p, hipStream_t st)
 {
-    const size_t lds = size_t(p.top) * 12;
-    const unsigned most = 1 << 20;
-    if (p.v <= 4096) hipLaunchKernelGGL((distill_kernel<T, 64, LOSS, GRAD>), dim3(unsigned(std::min<int64_t>((p.rows + 3) / 4, most))), dim3(256), 4 * lds, st, p);
-    else if (p.v <= 16384) hipLaunchKernelGGL((distill_kernel<T, 256, LOSS, GRAD>), dim3(unsigned(std::min<int64_t>(p.rows, most))), dim3(256), lds, st, p);
-    else hipLaunchKernelGGL((distill_kernel<T, 1024, LOSS, GRAD>), dim3(unsigned(std::min<int64_t>(p.rows, most))), dim3(1024), lds, st, p);
+    const size_t lds = size_t((p.top + 3) / 4) * 48;
+    const int64_t vecs = (int64_t(p.v) + Vec<T>::N - 1) / Vec<T>::N;
+#define PCONV_LAUNCH(TPR, KEEP)                                                                                                    do {                                                                                                                               constexpr int RPW = TPR < 256 ? 256 / TPR : 1;                                                                                 hipLaunchKernelGGL((distill_kernel<T, TPR, KEEP, LOSS, GRAD>), dim3(unsigned(std::min<int64_t>((p.rows + RPW - 1) / RPW, 1 << 20))),                             dim3(RPW * TPR), RPW * lds, st, p);                                                                     } while (0)
+    // (the loss has the same bits with and without its gradient: the same threads a row for both)
+    if constexpr (LOSS) {
+        if (vecs <= 64 * 2) PCONV_LAUNCH(64, 2);
+        else if (vecs <= 64 * 4) PCONV_LAUNCH(64, 4);
+        else if (vecs <= 256 * 4) PCONV_LAUNCH(256, 4);
+        else if (vecs <= 256 * 8) PCONV_LAUNCH(256, 8);
+        else if (vecs <= 512 * 8) PCONV_LAUNCH(512, 8);
+        else PCONV_LAUNCH(1024, 8);
+    } else {
+        if (vecs <= 64 * 4) PCONV_LAUNCH(64, 4);
+        else PCONV_LAUNCH(256, 4);
+    }
+#undef PCONV_LAUNCH
 }
 
 }  // namespace
