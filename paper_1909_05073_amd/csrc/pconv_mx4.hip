@@ -384,6 +384,135 @@ matmul_mx4_join_kernel(const Mx4Product p, int splits, const float *__restrict__
     }
 }
 
+// Few rows (up to 16): 16 channels a workgroup, whose waves share k in turns of 16 blocks and add their sums in LDS.
+// Reading the weights is all of it; they come in a ring of D turns in LDS that is the wave's own, past the registers, and
+// no barrier stands in the loop.  The rows of activations, kFewBytes of them at most, lie in LDS for all waves: they come as
+// floats, and every workgroup quantises all of them while its first weights are on their way (less than a launch for it
+// takes), or as blocks (T is uint8_t).
+constexpr int kFewRows = 16, kTurn = 16;                 // (blocks)
+constexpr int64_t kFewBytes = 32768;
+
+// Rows in LDS: values, and behind them the scales, both in whole turns.
+struct FewRows {
+    int pitch, scales, scale_pitch;
+    int bytes;
+};
+
+__host__ __device__ __forceinline__ FewRows few_rows(int m, int blocks)
+{
+    const int turns = (blocks + kTurn - 1) / kTurn;
+    FewRows f;
+    f.pitch = turns * 256 + 16;                          // (16 rows that are read at once in different banks)
+    f.scale_pitch = turns * 16 + 4;
+    f.scales = m * f.pitch;
+    f.bytes = (f.scales + m * f.scale_pitch + 15) / 16 * 16;
+    return f;
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(512)
+linear_mx4_rows_kernel(const Mx4Product p, const T *__restrict__ x, int64_t ldx, int k)
+{
+    constexpr int WAVES = 8, TURN_BYTES = 16 * 256 + 256;
+    extern __shared__ v4i few_lds[];
+    __shared__ v4i ring[WAVES][D * TURN_BYTES / 16];
+    const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), r = lane & 15, g = lane >> 4;
+    const int n0 = int(blockIdx.x) * 16;
+    const int turns = (p.blocks + kTurn - 1) / kTurn, slabs = (p.blocks + 7) / 8;
+    const FewRows few = few_rows(p.m, p.blocks);
+    uint8_t *const a = reinterpret_cast<uint8_t *>(few_lds);
+
+    // a turn is 16 rows of 256 bytes, 16 lanes read a row together, and the word of scales that each lane will use itself
+    const v4u at_b = buffer_at(reinterpret_cast<const int8_t *>(p.b) + int64_t(n0) * p.ldb);
+    uint32_t off[4];
+    int piece[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = i * 4 + g;
+        piece[i] = r ^ row;
+        off[i] = uint32_t(min(row, p.n - 1 - n0)) * uint32_t(p.ldb) + uint32_t(piece[i]) * 16u;
+    }
+    const uint8_t *const scales_b = p.sb + int64_t(min(n0 + r, p.n - 1)) * 8 + (g & 1) * 4;
+    const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(ring[wave]));
+    const int mine = turns > wave ? (turns - wave + WAVES - 1) / WAVES : 0;
+    auto issue = [&](int t) {
+        if (t >= mine) return;
+        const int turn = wave + t * WAVES, have = p.blocks - turn * kTurn;
+        const uint32_t to = base + uint32_t(t % D) * uint32_t(TURN_BYTES), at = uint32_t(turn) * 256u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            asm volatile("s_mov_b32 m0, %1\n s_nop 0\n buffer_load_dwordx4 %0, %2, %3 offen lds"
+                         ::"v"(piece[i] < have ? off[i] : kNowhere), "s"(to + uint32_t(i * 1024)), "s"(at_b), "s"(at) : "memory");
+        // (behind the last slab the last one again, for nothing)
+        asm volatile("s_mov_b32 m0, %1\n s_nop 0\n global_load_lds_dword %0, off"
+                     ::"v"(scales_b + int64_t(min(turn * 2 + (g >> 1), slabs - 1)) * p.slab_b), "s"(to + 4096u) : "memory");
+    };
+#pragma unroll 1
+    for (int t = 0; t < D; ++t) issue(t);
+
+    if constexpr (sizeof(T) == 1) {
+        // blocks and scales as they are; zeros behind their ends
+        const int pieces = turns * kTurn;
+        for (int u = int(threadIdx.x); u < p.m * pieces; u += WAVES * 64) {
+            const int row = u / pieces, block = u - row * pieces;
+            v4i v = {0, 0, 0, 0};
+            uint8_t s = 0;
+            if (block < p.blocks) {
+                __builtin_memcpy(&v, x + row * ldx + block * 16, 16);
+                s = p.sa[int64_t(block >> 3) * p.slab_a + row * 8 + (block & 7)];
+            }
+            __builtin_memcpy(a + row * few.pitch + block * 16, &v, 16);
+            a[few.scales + row * few.scale_pitch + block] = s;
+        }
+    } else {
+        const int eights = turns * (kTurn * 4);
+        for (int u = int(threadIdx.x); u < p.m * eights; u += WAVES * 64) {
+            const int row = u / eights, at = u - row * eights;
+            const Eight<T> e = load_eight(x + row * ldx, at * 8, k);
+            const uint32_t byte = block_scale(most_of_block(e.most()));
+            const uint32_t w = byte == 255u ? 0u : e.codes(scale_value(byte));
+            __builtin_memcpy(a + row * few.pitch + at * 4, &w, 4);
+            if (at % 4 == 0) a[few.scales + row * few.scale_pitch + at / 4] = uint8_t(byte);
+        }
+    }
+    __syncthreads();
+    const uint8_t *const row_a = a + min(r, p.m - 1) * few.pitch + g * 64, *const row_s = a + few.scales + min(r, p.m - 1) * few.scale_pitch + g * 4;
+    f4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll 1
+    for (int t = 0; t < mine; ++t) {
+        wait_for_loads<D - 1, 5>(min(D - 1, mine - 1 - t));
+        const v4i *const st = ring[wave] + (t % D) * (TURN_BYTES / 16);
+        const int turn = wave + t * WAVES;
+        v4i va[4], vb[4];
+        int sa, sb = reinterpret_cast<const int *>(st + 256)[lane];
+        __builtin_memcpy(&sa, row_s + turn * 16, 4);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            vb[s] = st[r * 16 + ((4 * g + s) ^ r)];
+            __builtin_memcpy(&va[s], row_a + turn * 256 + s * 16, 16);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");               // (read, so that it may be overwritten)
+        issue(t + D);
+        // (of a block that is not there the scale may be any byte)
+        sb &= int(0xFFFFFFFFull >> max(0, min(32, (g * 4 + 4 - (p.blocks - turn * kTurn)) * 8)));
+        acc[0] = multiply_blocks<0>(vb[0], va[0], acc[0], sb, sa);
+        acc[1] = multiply_blocks<1>(vb[1], va[1], acc[1], sb, sa);
+        acc[0] = multiply_blocks<2>(vb[2], va[2], acc[0], sb, sa);
+        acc[1] = multiply_blocks<3>(vb[3], va[3], acc[1], sb, sa);
+    }
+    reinterpret_cast<f4 *>(ring[wave])[lane] = acc[0] + acc[1];
+    __syncthreads();
+    if (wave) return;
+    f4 s = reinterpret_cast<const f4 *>(ring[0])[lane];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) s += reinterpret_cast<const f4 *>(ring[w])[lane];
+    const int n = n0 + g * 4;
+    if (r >= p.m || n >= p.n) return;
+    const f4 v = values_of(p, s, bias_at(p, n));
+    if (p.y_bf16) store_channels<__bf16, 4>(p, r, n, __builtin_convertvector(v, b4));
+    else store_channels<float, 4>(p, r, n, v);
+}
+
 // How a product is cut up: the tile (an index into launch_tiles) and over how many workgroups the length of k is split.
 struct Cut { int tile, splits; };
 
@@ -423,7 +552,28 @@ void launch_tiles(const Mx4Product &p, int splits, float *part, hipStream_t st)
     else hipLaunchKernelGGL((matmul_mx4_kernel<float, BM, BN, WM, WN, S, KG>), dim3(grid), dim3(KG * WM * WN * 64), 0, st, p, splits, part);
 }
 
+int64_t rows_groups(int64_t n) { return (n + 15) / 16; }
+
+// Whether rows are so few and short that every workgroup has all of them in LDS.
+bool few(int64_t m, int64_t blocks) { return m <= kFewRows && m * blocks * 16 <= kFewBytes; }
+
+template <typename T>
+int launch_few(const Mx4Product &p, const T *x, int64_t ldx, int k, hipStream_t st)
+{
+    if (rows_groups(p.n) > kMaxGroups) return too_many_groups();
+    hipLaunchKernelGGL((linear_mx4_rows_kernel<T, 2>), dim3(unsigned(rows_groups(p.n))), dim3(512), size_t(few_rows(p.m, p.blocks).bytes), st, p, x, ldx, k);
+    return check_launch("pconv_linear_mx4 (few rows)");
+}
+
 }  // namespace
+
+bool linear_mx4_fused(int64_t m, int64_t blocks) { return few(m, blocks); }
+
+int launch_linear_mx4_fused(const Mx4Product &p, const void *x, int64_t ldx, int bf16, int64_t k, void *stream)
+{
+    const hipStream_t st = static_cast<hipStream_t>(stream);
+    return bf16 ? launch_few(p, static_cast<const __bf16 *>(x), ldx, int(k), st) : launch_few(p, static_cast<const float *>(x), ldx, int(k), st);
+}
 
 int launch_quantize_mx4(const void *x, int64_t ldx, int bf16, int64_t rows, int64_t cols, uint8_t *q, int64_t ldq, uint8_t *scale,
                         int64_t slab_stride, void *stream)
@@ -439,18 +589,21 @@ int launch_quantize_mx4(const void *x, int64_t ldx, int bf16, int64_t rows, int6
 
 int64_t matmul_mx4_work_bytes(int64_t m, int64_t n, int64_t blocks)
 {
+    if (few(m, blocks)) return 0;
     const Cut c = cut_of(m, n, blocks);
     return c.splits > 1 ? c.splits * m * ((n + 3) / 4 * 4) * 4 : 0;
 }
 
 int check_matmul_mx4(int64_t m, int64_t n, int64_t blocks)
 {
+    if (few(m, blocks)) return rows_groups(n) > kMaxGroups ? too_many_groups() : PCONV_OK;
     const Cut c = cut_of(m, n, blocks);
     return tiles_of(c, m, n) * c.splits > kMaxGroups ? too_many_groups() : PCONV_OK;
 }
 
 pconv_mx4_plan matmul_mx4_plan(int64_t m, int64_t n, int64_t blocks)
 {
+    if (few(m, blocks)) return pconv_mx4_plan{1, 0, 0, 0, 0};
     const Cut c = cut_of(m, n, blocks);
     return pconv_mx4_plan{2, kTileM[c.tile], kTileN[c.tile], sets_of(c, tiles_of(c, m, n)), c.splits};
 }
@@ -458,6 +611,7 @@ pconv_mx4_plan matmul_mx4_plan(int64_t m, int64_t n, int64_t blocks)
 int launch_matmul_mx4(const Mx4Product &p, void *work, void *stream)
 {
     const hipStream_t st = static_cast<hipStream_t>(stream);
+    if (few(p.m, p.blocks)) return launch_few(p, p.a, p.lda, 0, st);
     const Cut c = cut_of(p.m, p.n, p.blocks);
     const int64_t tiles = tiles_of(c, p.m, p.n);
     if (tiles * c.splits > kMaxGroups) return too_many_groups();

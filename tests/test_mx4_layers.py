@@ -489,7 +489,7 @@ def test_plans_of_the_products():
     tiles = {(p.tile_m, p.tile_n) for p in plans if p.kernel == 2}
     assert tiles == {(32, 128), (64, 128), (128, 128), (256, 256)}, tiles
     assert any(p.splits > 1 for p in plans) and any(p.splits == 1 for p in plans if p.kernel == 2)
-    assert {p.sets for p in plans if p.kernel == 2} == {1, 2}
+    assert {p.sets for p in plans if p.kernel == 2} == {1, 2} and {p.kernel for p in plans} == {1, 2}
     for m, n, blocks in ((0, 1, 1), (1, 0, 1), (1, 1, -1), ((1 << 30) + 1, 1, 1), (1, 1, (1 << 19) + 1)):
         with pytest.raises(P.PconvError):
             P.pconv_debug_mx4_plan(m, n, blocks)
@@ -547,7 +547,7 @@ def test_unknown_types_are_refused_at_the_c_entries():
 
 def test_calls_of_more_than_2_to_32_threads_are_unsupported():
     p, big = 1 << 20, 1 << 30
-    for m, n in ((big, 1 << 20), (1 << 20, big)):
+    for m, n in ((big, 1 << 20), (1 << 20, big), (1, (1 << 27) - 15), (16, big)):
         with pytest.raises(P.PconvError) as e:
             P.pconv_matmul_mx4(p, 512, p, 8 * m, p, 512, p, 8 * n, 0, p, n, "f32", m, n, 32, False, p, P.pconv_matmul_mx4_workspace(m, n, 32))
         assert e.value.status == P.UNSUPPORTED and "too many workgroups" in str(e.value)
