@@ -384,15 +384,19 @@ matmul_mx4_join_kernel(const Mx4Product p, int splits, const float *__restrict__
     }
 }
 
-// Few rows (up to 16): 16 channels a workgroup, whose waves share k in turns of 16 blocks and add their sums in LDS.
-// Reading the weights is all of it; they come in a ring of D turns in LDS that is the wave's own, past the registers, and
-// no barrier stands in the loop.  The rows of activations, kFewBytes of them at most, lie in LDS for all waves: they come as
-// floats, and every workgroup quantises all of them while its first weights are on their way (less than a launch for it
-// takes), or as blocks (T is uint8_t).
+// Few rows (up to 16): 16 channels a workgroup, whose waves share k and add their sums in LDS.  Reading the weights is all
+// of it; they come in turns of 16 blocks, in a ring of D turns in LDS that is the wave's own, past the registers, and no
+// barrier stands in the loop.  The waves take whole turns in rounds, and what is left behind the last whole round is dealt
+// out among all of them: a turn of one wave alone at the end takes a whole latency of memory (25088 -> 8192: 25.5 us with
+// one turn left over, 21.5 without).  Workgroups begin with different rounds, so that rows that lie a power of two apart
+// are not all read in the same places at one time (32768 -> 4096: 19.5 us if they are, 17.0).  The rows of activations, kFewBytes of them
+// at most, lie in LDS for all waves: they come as floats, and every workgroup quantises all of them while its first weights
+// are on their way (less than a launch for it takes), or as blocks (T is uint8_t).
 constexpr int kFewRows = 16, kTurn = 16;                 // (blocks)
 constexpr int64_t kFewBytes = 32768;
+constexpr size_t kFewRing = 8 * (16 * 256 + 256);        // bytes of one turn of all waves
 
-// Rows in LDS: values, and behind them the scales, both in whole turns.
+// Rows in LDS: values, and behind all of them the scales; behind each row room for what a wave's last turn reads for nothing.
 struct FewRows {
     int pitch, scales, scale_pitch;
     int bytes;
@@ -400,10 +404,10 @@ struct FewRows {
 
 __host__ __device__ __forceinline__ FewRows few_rows(int m, int blocks)
 {
-    const int turns = (blocks + kTurn - 1) / kTurn;
+    const int wide = (blocks + kTurn - 1) / kTurn * kTurn + kTurn;
     FewRows f;
-    f.pitch = turns * 256 + 16;                          // (16 rows that are read at once in different banks)
-    f.scale_pitch = turns * 16 + 4;
+    f.pitch = wide * 16 + 16;                            // (16 rows that are read at once in different banks)
+    f.scale_pitch = wide + 4;
     f.scales = m * f.pitch;
     f.bytes = (f.scales + m * f.scale_pitch + 15) / 16 * 16;
     return f;
@@ -413,14 +417,25 @@ template <typename T, int D>
 __global__ void __launch_bounds__(512)
 linear_mx4_rows_kernel(const Mx4Product p, const T *__restrict__ x, int64_t ldx, int k)
 {
-    constexpr int WAVES = 8, TURN_BYTES = 16 * 256 + 256;
+    constexpr int WAVES = 8, TURN_BYTES = 16 * 256 + 256, ROUND = WAVES * kTurn;
     extern __shared__ v4i few_lds[];
     __shared__ v4i ring[WAVES][D * TURN_BYTES / 16];
     const int lane = int(threadIdx.x) & 63, wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x) >> 6), r = lane & 15, g = lane >> 4;
     const int n0 = int(blockIdx.x) * 16;
-    const int turns = (p.blocks + kTurn - 1) / kTurn, slabs = (p.blocks + 7) / 8;
     const FewRows few = few_rows(p.m, p.blocks);
     uint8_t *const a = reinterpret_cast<uint8_t *>(few_lds);
+
+    const int rounds = p.blocks / ROUND, left = p.blocks - rounds * ROUND;
+    const int share = ((left + WAVES - 1) / WAVES + 3) / 4 * 4;          // (whole words of scales)
+    const int mine = rounds + (wave * share < left ? 1 : 0);
+    const int first_round = rounds > 0 ? int(blockIdx.x >> 3) % rounds : 0;
+    // the first block of a turn and how many it has
+    auto first_of = [&](int t) {
+        if (t >= rounds) return rounds * ROUND + wave * share;
+        t += first_round;
+        return (t < rounds ? t : t - rounds) * ROUND + wave * kTurn;
+    };
+    auto count_of = [&](int t) { return t < rounds ? kTurn : min(share, left - wave * share); };
 
     // a turn is 16 rows of 256 bytes, 16 lanes read a row together, and the word of scales that each lane will use itself
     const v4u at_b = buffer_at(reinterpret_cast<const int8_t *>(p.b) + int64_t(n0) * p.ldb);
@@ -432,49 +447,62 @@ linear_mx4_rows_kernel(const Mx4Product p, const T *__restrict__ x, int64_t ldx,
         piece[i] = r ^ row;
         off[i] = uint32_t(min(row, p.n - 1 - n0)) * uint32_t(p.ldb) + uint32_t(piece[i]) * 16u;
     }
-    const uint8_t *const scales_b = p.sb + int64_t(min(n0 + r, p.n - 1)) * 8 + (g & 1) * 4;
+    const uint8_t *const scales_b = p.sb + int64_t(min(n0 + r, p.n - 1)) * 8;
     const uint32_t base = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(ring[wave]));
-    const int mine = turns > wave ? (turns - wave + WAVES - 1) / WAVES : 0;
     auto issue = [&](int t) {
         if (t >= mine) return;
-        const int turn = wave + t * WAVES, have = p.blocks - turn * kTurn;
-        const uint32_t to = base + uint32_t(t % D) * uint32_t(TURN_BYTES), at = uint32_t(turn) * 256u;
+        const int first = first_of(t), have = count_of(t);
+        const uint32_t to = base + uint32_t(t % D) * uint32_t(TURN_BYTES), at = uint32_t(first) * 16u;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             asm volatile("s_mov_b32 m0, %1\n s_nop 0\n buffer_load_dwordx4 %0, %2, %3 offen lds"
                          ::"v"(piece[i] < have ? off[i] : kNowhere), "s"(to + uint32_t(i * 1024)), "s"(at_b), "s"(at) : "memory");
-        // (behind the last slab the last one again, for nothing)
+        // (of blocks that are not there the turn's first word again, for nothing)
+        const int word = first + (g * 4 < have ? g * 4 : 0);
         asm volatile("s_mov_b32 m0, %1\n s_nop 0\n global_load_lds_dword %0, off"
-                     ::"v"(scales_b + int64_t(min(turn * 2 + (g >> 1), slabs - 1)) * p.slab_b), "s"(to + 4096u) : "memory");
+                     ::"v"(scales_b + int64_t(word >> 3) * p.slab_b + (word & 4)), "s"(to + 4096u) : "memory");
     };
-#pragma unroll 1
-    for (int t = 0; t < D; ++t) issue(t);
+    constexpr int AHEAD = 2;                             // (what a wave asks for behind its weights is waited for with them)
+#pragma unroll
+    for (int t = 0; t < AHEAD; ++t) issue(t);
 
     if constexpr (sizeof(T) == 1) {
-        // blocks and scales as they are; zeros behind their ends
-        const int pieces = turns * kTurn;
-        for (int u = int(threadIdx.x); u < p.m * pieces; u += WAVES * 64) {
-            const int row = u / pieces, block = u - row * pieces;
-            v4i v = {0, 0, 0, 0};
-            uint8_t s = 0;
-            if (block < p.blocks) {
-                __builtin_memcpy(&v, x + row * ldx + block * 16, 16);
-                s = p.sa[int64_t(block >> 3) * p.slab_a + row * 8 + (block & 7)];
-            }
+#pragma unroll 2
+        for (int u = int(threadIdx.x); u < p.m * p.blocks; u += WAVES * 64) {
+            const int row = u / p.blocks, block = u - row * p.blocks;
+            v4i v;
+            __builtin_memcpy(&v, x + row * ldx + block * 16, 16);
+            const uint8_t s = p.sa[int64_t(block >> 3) * p.slab_a + row * 8 + (block & 7)];
             __builtin_memcpy(a + row * few.pitch + block * 16, &v, 16);
             a[few.scales + row * few.scale_pitch + block] = s;
         }
     } else {
-        const int eights = turns * (kTurn * 4);
-        for (int u = int(threadIdx.x); u < p.m * eights; u += WAVES * 64) {
-            const int row = u / eights, at = u - row * eights;
-            const Eight<T> e = load_eight(x + row * ldx, at * 8, k);
-            const uint32_t byte = block_scale(most_of_block(e.most()));
-            const uint32_t w = byte == 255u ? 0u : e.codes(scale_value(byte));
-            __builtin_memcpy(a + row * few.pitch + at * 4, &w, 4);
-            if (at % 4 == 0) a[few.scales + row * few.scale_pitch + at / 4] = uint8_t(byte);
+        // (several at once, so that their loads are under way together; four lanes have a block, so that nothing ends within one)
+        constexpr int AT_ONCE = 4;
+        const int eights = p.blocks * 4, all = p.m * eights;
+#pragma unroll 1
+        for (int first = int(threadIdx.x); first < all; first += AT_ONCE * WAVES * 64) {
+            Eight<T> e[AT_ONCE];
+            int row[AT_ONCE], at[AT_ONCE];
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) {
+                if (first + i * WAVES * 64 >= all) continue;
+                row[i] = (first + i * WAVES * 64) / eights;
+                at[i] = first + i * WAVES * 64 - row[i] * eights;
+                e[i] = load_eight(x + row[i] * ldx, at[i] * 8, k);
+            }
+#pragma unroll
+            for (int i = 0; i < AT_ONCE; ++i) {
+                if (first + i * WAVES * 64 >= all) continue;
+                const uint32_t byte = block_scale(most_of_block(e[i].most()));
+                const uint32_t w = byte == 255u ? 0u : e[i].codes(scale_value(byte));
+                __builtin_memcpy(a + row[i] * few.pitch + at[i] * 4, &w, 4);
+                if (at[i] % 4 == 0) a[few.scales + row[i] * few.scale_pitch + at[i] / 4] = uint8_t(byte);
+            }
         }
     }
+#pragma unroll
+    for (int t = AHEAD; t < D; ++t) issue(t);
     __syncthreads();
     const uint8_t *const row_a = a + min(r, p.m - 1) * few.pitch + g * 64, *const row_s = a + few.scales + min(r, p.m - 1) * few.scale_pitch + g * 4;
     f4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
@@ -482,19 +510,21 @@ linear_mx4_rows_kernel(const Mx4Product p, const T *__restrict__ x, int64_t ldx,
     for (int t = 0; t < mine; ++t) {
         wait_for_loads<D - 1, 5>(min(D - 1, mine - 1 - t));
         const v4i *const st = ring[wave] + (t % D) * (TURN_BYTES / 16);
-        const int turn = wave + t * WAVES;
+        const int first = first_of(t);
         v4i va[4], vb[4];
         int sa, sb = reinterpret_cast<const int *>(st + 256)[lane];
-        __builtin_memcpy(&sa, row_s + turn * 16, 4);
+        __builtin_memcpy(&sa, row_s + first, 4);
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             vb[s] = st[r * 16 + ((4 * g + s) ^ r)];
-            __builtin_memcpy(&va[s], row_a + turn * 256 + s * 16, 16);
+            __builtin_memcpy(&va[s], row_a + first * 16 + s * 16, 16);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");               // (read, so that it may be overwritten)
         issue(t + D);
-        // (of a block that is not there the scale may be any byte)
-        sb &= int(0xFFFFFFFFull >> max(0, min(32, (g * 4 + 4 - (p.blocks - turn * kTurn)) * 8)));
+        // (of blocks that are not there the weights are zeros and the scales may be any byte)
+        const int mask = int(0xFFFFFFFFull >> max(0, min(32, (g * 4 + 4 - count_of(t)) * 8)));
+        sa &= mask;
+        sb &= mask;
         acc[0] = multiply_blocks<0>(vb[0], va[0], acc[0], sb, sa);
         acc[1] = multiply_blocks<1>(vb[1], va[1], acc[1], sb, sa);
         acc[0] = multiply_blocks<2>(vb[2], va[2], acc[0], sb, sa);
@@ -561,7 +591,15 @@ template <typename T>
 int launch_few(const Mx4Product &p, const T *x, int64_t ldx, int k, hipStream_t st)
 {
     if (rows_groups(p.n) > kMaxGroups) return too_many_groups();
-    hipLaunchKernelGGL((linear_mx4_rows_kernel<T, 2>), dim3(unsigned(rows_groups(p.n))), dim3(512), size_t(few_rows(p.m, p.blocks).bytes), st, p, x, ldx, k);
+    const size_t lds = size_t(few_rows(p.m, p.blocks).bytes);
+    const dim3 grid(unsigned(rows_groups(p.n)));
+    // Three turns of each wave under way where a compute unit has one workgroup (1x25088 -> 8192 24.2 us with two, 23.0),
+    // two where it has two (8192 -> 8192 8.5 us, and one with three turns 10.7).
+    // (with kFewBytes of rows, their scales, and the room behind 16 of them)
+    constexpr size_t kLds = 160 * 1024;
+    static_assert(kFewRing * 3 + kFewBytes + kFewBytes / 16 + kFewRows * (kTurn * 34 + 36) <= kLds, "");
+    if (int64_t(grid.x) > kUnits && 2 * (kFewRing * 2 + lds) <= kLds) hipLaunchKernelGGL((linear_mx4_rows_kernel<T, 2>), grid, dim3(512), lds, st, p, x, ldx, k);
+    else hipLaunchKernelGGL((linear_mx4_rows_kernel<T, 3>), grid, dim3(512), lds, st, p, x, ldx, k);
     return check_launch("pconv_linear_mx4 (few rows)");
 }
 
