@@ -584,13 +584,17 @@ void launch_tiles(const Mx4Product &p, int splits, float *part, hipStream_t st)
 
 int64_t rows_groups(int64_t n) { return (n + 15) / 16; }
 
-// Whether rows are so few and short that every workgroup has all of them in LDS.
-bool few(int64_t m, int64_t blocks) { return m <= kFewRows && m * blocks * 16 <= kFewBytes; }
+// Whether rows are so few and short that every workgroup has all of them in LDS: kFewBytes together, less where a compute unit
+// has several workgroups to run (4x8192 -> 4096 8.3 us, in tiles 15.5; 4x8192 -> 8192 14.1 and 15.3, 6x8192 -> 8192 16.8
+// and 15.3, 8x8192 -> 8192 19.6 and 15.6).
+bool few(int64_t m, int64_t n, int64_t blocks)
+{
+    return m <= kFewRows && m * blocks * 16 * ((rows_groups(n) + kUnits - 1) / kUnits) <= kFewBytes && blocks > 0;
+}
 
 template <typename T>
 int launch_few(const Mx4Product &p, const T *x, int64_t ldx, int k, hipStream_t st)
 {
-    if (rows_groups(p.n) > kMaxGroups) return too_many_groups();
     const size_t lds = size_t(few_rows(p.m, p.blocks).bytes);
     const dim3 grid(unsigned(rows_groups(p.n)));
     // Three turns of each wave under way where a compute unit has one workgroup (1x25088 -> 8192 24.2 us with two, 23.0),
@@ -605,7 +609,7 @@ int launch_few(const Mx4Product &p, const T *x, int64_t ldx, int k, hipStream_t 
 
 }  // namespace
 
-bool linear_mx4_fused(int64_t m, int64_t blocks) { return few(m, blocks); }
+bool linear_mx4_fused(int64_t m, int64_t n, int64_t blocks) { return few(m, n, blocks); }
 
 int launch_linear_mx4_fused(const Mx4Product &p, const void *x, int64_t ldx, int bf16, int64_t k, void *stream)
 {
@@ -627,21 +631,21 @@ int launch_quantize_mx4(const void *x, int64_t ldx, int bf16, int64_t rows, int6
 
 int64_t matmul_mx4_work_bytes(int64_t m, int64_t n, int64_t blocks)
 {
-    if (few(m, blocks)) return 0;
+    if (few(m, n, blocks)) return 0;
     const Cut c = cut_of(m, n, blocks);
     return c.splits > 1 ? c.splits * m * ((n + 3) / 4 * 4) * 4 : 0;
 }
 
 int check_matmul_mx4(int64_t m, int64_t n, int64_t blocks)
 {
-    if (few(m, blocks)) return rows_groups(n) > kMaxGroups ? too_many_groups() : PCONV_OK;
+    if (few(m, n, blocks)) return PCONV_OK;
     const Cut c = cut_of(m, n, blocks);
     return tiles_of(c, m, n) * c.splits > kMaxGroups ? too_many_groups() : PCONV_OK;
 }
 
 pconv_mx4_plan matmul_mx4_plan(int64_t m, int64_t n, int64_t blocks)
 {
-    if (few(m, blocks)) return pconv_mx4_plan{1, 0, 0, 0, 0};
+    if (few(m, n, blocks)) return pconv_mx4_plan{1, 0, 0, 0, 0};
     const Cut c = cut_of(m, n, blocks);
     return pconv_mx4_plan{2, kTileM[c.tile], kTileN[c.tile], sets_of(c, tiles_of(c, m, n)), c.splits};
 }
@@ -649,7 +653,7 @@ pconv_mx4_plan matmul_mx4_plan(int64_t m, int64_t n, int64_t blocks)
 int launch_matmul_mx4(const Mx4Product &p, void *work, void *stream)
 {
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    if (few(p.m, p.blocks)) return launch_few(p, p.a, p.lda, 0, st);
+    if (few(p.m, p.n, p.blocks)) return launch_few(p, p.a, p.lda, 0, st);
     const Cut c = cut_of(p.m, p.n, p.blocks);
     const int64_t tiles = tiles_of(c, p.m, p.n);
     if (tiles * c.splits > kMaxGroups) return too_many_groups();

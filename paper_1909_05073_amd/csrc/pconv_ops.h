@@ -63,7 +63,7 @@ int check_matmul_mx4(int64_t m, int64_t n, int64_t blocks);              // whet
 pconv_mx4_plan matmul_mx4_plan(int64_t m, int64_t n, int64_t blocks);
 int launch_matmul_mx4(const Mx4Product &p, void *work, void *stream);
 // Whether rows are so few that they are quantised within the product, and that product (p.a, lda, sa, slab_a unused).
-bool linear_mx4_fused(int64_t m, int64_t blocks);
+bool linear_mx4_fused(int64_t m, int64_t n, int64_t blocks);
 int launch_linear_mx4_fused(const Mx4Product &p, const void *x, int64_t ldx, int bf16, int64_t k, void *stream);
 
 // s = x + r (r: or null), h = s / sqrt(mean s^2 + eps) * weight (or null), q and scale of h; sum: where s goes (or null).

@@ -329,7 +329,7 @@ int64_t pconv_linear_mx4_workspace(int64_t m, int64_t n, int64_t k)
 {
     if (k < 0 || k > kMaxBlocks * 32 || !mx4_sizes_fit(m, n, (k + 31) / 32)) return 0;
     const int64_t blocks = (k + 31) / 32;
-    if (linear_mx4_fused(m, blocks)) return 0;
+    if (linear_mx4_fused(m, n, blocks)) return 0;
     return m * blocks * 16 + round16((blocks + 7) / 8 * m * 8) + matmul_mx4_work_bytes(m, n, blocks);
 }
 
@@ -349,7 +349,7 @@ int pconv_linear_mx4(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, c
     if (!stride_fits(m, k, x_stride)) return invalid(who, "rows must lie at least their length apart");
     if (const int rc = check_work(who, work, work_bytes, pconv_linear_mx4_workspace(m, n, k))) return rc;
     if (const int rc = check_matmul_mx4(m, n, blocks)) return rc;
-    if (linear_mx4_fused(m, blocks)) return launch_linear_mx4_fused(p, x_dev, x_stride, x_dtype == PCONV_BF16, k, hip_stream);
+    if (linear_mx4_fused(m, n, blocks)) return launch_linear_mx4_fused(p, x_dev, x_stride, x_dtype == PCONV_BF16, k, hip_stream);
     uint8_t *const q = static_cast<uint8_t *>(work), *const scale = q + m * blocks * 16;
     if (k)
         if (const int rc = launch_quantize_mx4(x_dev, x_stride, x_dtype == PCONV_BF16, m, k, q, blocks * 16, scale, m * 8, hip_stream)) return rc;

@@ -547,7 +547,7 @@ def test_unknown_types_are_refused_at_the_c_entries():
 
 def test_calls_of_more_than_2_to_32_threads_are_unsupported():
     p, big = 1 << 20, 1 << 30
-    for m, n in ((big, 1 << 20), (1 << 20, big), (1, (1 << 27) - 15), (16, big)):
+    for m, n in ((big, 1 << 20), (1 << 20, big), (1, big), (16, big)):
         with pytest.raises(P.PconvError) as e:
             P.pconv_matmul_mx4(p, 512, p, 8 * m, p, 512, p, 8 * n, 0, p, n, "f32", m, n, 32, False, p, P.pconv_matmul_mx4_workspace(m, n, 32))
         assert e.value.status == P.UNSUPPORTED and "too many workgroups" in str(e.value)
