@@ -17,6 +17,17 @@ namespace {
 // N values of a row in 32 bits.
 template <int N> struct Values { float v[N]; };
 
+template <typename T, bool PASSING>
+__device__ __forceinline__ Vec<T> load_vector(const T *row, int k)
+{
+    v4i w;
+    if constexpr (PASSING) w = load_passing<v4i>(row + int64_t(k) * Vec<T>::N);
+    else __builtin_memcpy(&w, row + int64_t(k) * Vec<T>::N, 16);
+    Vec<T> v;
+    __builtin_memcpy(&v, &w, 16);
+    return v;
+}
+
 template <typename T>
 __device__ __forceinline__ Values<Vec<T>::N> sums_of(const Vec<T> &x, const Vec<T> &r, bool add)
 {
@@ -26,28 +37,30 @@ __device__ __forceinline__ Values<Vec<T>::N> sums_of(const Vec<T> &x, const Vec<
     return s;
 }
 
+// The vector k of a row of sums (r: or null).
+template <typename T, bool PASSING = false>
+__device__ __forceinline__ Values<Vec<T>::N> load_sums(const T *x, const T *r, int k)
+{
+    const Vec<T> a = load_vector<T, PASSING>(x, k);
+    return sums_of(a, r ? load_vector<T, PASSING>(r, k) : a, r != nullptr);
+}
+
 template <typename T>
-__device__ __forceinline__ void store_sums(const Values<Vec<T>::N> &s, T *row, int64_t at, int64_t cols)
+__device__ __forceinline__ void store_sums(const Values<Vec<T>::N> &s, T *row, int k)
 {
     constexpr int N = Vec<T>::N;
     T w[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) w[i] = T(s.v[i]);
-    if (__builtin_expect(at + N <= cols, 1)) {
-        __builtin_memcpy(row + at, w, sizeof(w));
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (at + i < cols) row[at + i] = w[i];
-    }
+    __builtin_memcpy(row + int64_t(k) * N, w, sizeof(w));
 }
 
 // The row's factor 1 / sqrt(mean + eps), taken in two parts where the values are so large that it would be a denormal number.
 struct Factor { float lift, inv; };
 
-__device__ __forceinline__ Factor factor_of(double squares, int64_t cols, float eps)
+__device__ __forceinline__ Factor factor_of(double squares, double count, float eps)
 {
-    const double mean = squares / double(max(cols, int64_t(1))) + double(eps);
+    const double mean = squares / count + double(eps);
     Factor f;
     f.lift = mean > 0x1p200 ? 0x1p-64f : 1.0f;
     f.inv = float(1.0 / (sqrt(mean) * double(f.lift)));
@@ -56,20 +69,17 @@ __device__ __forceinline__ Factor factor_of(double squares, int64_t cols, float 
 
 // s becomes h.
 template <int N>
-__device__ __forceinline__ void normalise(Values<N> &s, const Factor &f, const float *__restrict__ weight, int64_t at, int64_t cols)
+__device__ __forceinline__ void normalise(Values<N> &s, const Factor &f, const float *__restrict__ weight, int k)
 {
-    float w[N];
-    if (!weight) {
+    if (weight) {
+        float w[N];
+        __builtin_memcpy(w, weight + int64_t(k) * N, sizeof(w));
 #pragma unroll
-        for (int i = 0; i < N; ++i) w[i] = 1.0f;
-    } else if (__builtin_expect(at + N <= cols, 1)) {
-        __builtin_memcpy(w, weight + at, sizeof(w));
+        for (int i = 0; i < N; ++i) s.v[i] = s.v[i] * f.lift * f.inv * w[i];
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) w[i] = at + i < cols ? weight[at + i] : 0.0f;
+        for (int i = 0; i < N; ++i) s.v[i] = s.v[i] * f.lift * f.inv;
     }
-#pragma unroll
-    for (int i = 0; i < N; ++i) s.v[i] = s.v[i] * f.lift * f.inv * w[i];
 }
 
 template <int N>
@@ -80,25 +90,25 @@ __device__ __forceinline__ uint32_t most_of_values(const Values<N> &s, uint32_t 
     return most;
 }
 
-template <int N>
-__device__ __forceinline__ void store_quantized(const Values<N> &s, const RowScale &r, int8_t *row, int64_t at, int64_t q_cols)
+template <bool LIFT, int N>
+__device__ __forceinline__ void quantize_values(const Values<N> &s, const RowScale &r, uint32_t (&w)[N / 4])
 {
-    uint32_t w[N / 4];
 #pragma unroll
     for (int j = 0; j < N / 4; ++j) {
         uint32_t q[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) q[i] = __builtin_expect(r.lifts, 0) ? quantize<true>(s.v[4 * j + i], r) : quantize<false>(s.v[4 * j + i], r);
+        for (int i = 0; i < 4; ++i) q[i] = quantize<LIFT>(s.v[4 * j + i], r);
         w[j] = (__builtin_amdgcn_perm(q[1], q[0], 0x0C0C0400u) | __builtin_amdgcn_perm(q[3], q[2], 0x04000C0Cu)) & r.mask;
     }
-    if (__builtin_expect(at + N <= q_cols, 1)) {
-        __builtin_memcpy(row + at, w, N);
-    } else if (__builtin_expect(at < q_cols, 0)) {
-        uint64_t all = w[0];
-        if (N == 8) all |= uint64_t(w[N / 4 - 1]) << 32;
-#pragma unroll 1
-        for (int64_t i = at; i < q_cols; ++i, all >>= 8) row[i] = int8_t(all);
-    }
+}
+
+template <int N>
+__device__ __forceinline__ void store_quantized(const Values<N> &s, const RowScale &r, int8_t *row, int k)
+{
+    uint32_t w[N / 4];
+    if (__builtin_expect(r.lifts, 0)) quantize_values<true>(s, r, w);
+    else quantize_values<false>(s, r, w);
+    __builtin_memcpy(row + int64_t(k) * N, w, N);
 }
 
 // The sum over the LANES (up to 64) neighbouring lanes that share a row, in an order that depends on nothing.
@@ -111,9 +121,11 @@ __device__ __forceinline__ double sum_of_lanes(double v)
 }
 
 // TPR threads of a workgroup share a row; each keeps its first KEEP vectors of 16 bytes in registers as they are normalised and
-// quantised, and reads what lies beyond three times (from a cache).  Squares are summed in 64 bits, which no row of fp32
-// numbers leaves.  `sum` may be x or r: a thread has read what it overwrites.
-template <typename T, int TPR, int KEEP, int THREADS>
+// quantised, and reads what lies beyond three times (from a cache).  The elements behind the last whole vector go to a
+// thread each (one that has up to a vector of them, and loops, takes 2111x4099 fp32 from 13 to 41 us).  Squares are summed
+// in 64 bits, which no row of fp32 numbers leaves.  `sum` may be x or r: a thread has read what it overwrites.  Bound by
+// memory: 100352x256 bf16 with sums 34.5 us, 5.2 TB/s.
+template <typename T, int TPR, int KEEP, int THREADS, bool PASSING>
 __global__ void __launch_bounds__(THREADS)
 add_rms_norm_i8_kernel(const NormRows p, const T *x, const T *r, T *sum)
 {
@@ -121,35 +133,57 @@ add_rms_norm_i8_kernel(const NormRows p, const T *x, const T *r, T *sum)
     __shared__ double squares_of[WAVES];
     __shared__ uint32_t most_of_wave[WAVES];
     const int sub = int(threadIdx.x) % TPR;
-    const bool add = r != nullptr;
-    const int64_t groups = (p.rows + RPW - 1) / RPW;
+    const int whole = int(p.cols / N), rest = int(p.cols % N);
+    const bool tail = sub < rest;
+    const int64_t at_tail = int64_t(whole) * N + sub, groups = (p.rows + RPW - 1) / RPW;
     for (int64_t g = blockIdx.x; g < groups; g += gridDim.x) {
         const int64_t row = g * RPW + int(threadIdx.x) / TPR;
         const bool live = row < p.rows;
         const int64_t at_row = live ? row : p.rows - 1;
-        const T *xr = x + at_row * p.ldx, *rr = add ? r + at_row * p.ldr : xr;
-        T *sr = sum ? sum + at_row * p.ldsum : nullptr;
+        const T *const xr = x + at_row * p.ldx, *const rr = r ? r + at_row * p.ldr : nullptr;
+        T *const sr = sum + (sum ? at_row * p.ldsum : 0);
         Values<N> s[KEEP];
         double squares = 0;
-        auto add_squares = [&](const Values<N> &v) {
+        const auto add_squares = [&](const Values<N> &v) {
 #pragma unroll
             for (int i = 0; i < N; ++i) squares = __builtin_fma(double(v.v[i]), double(v.v[i]), squares);
         };
-        {
+        if constexpr (THREADS < 1024) {
+            // (all loads first: with the sums between them they are waited for one by one, 100352x256 bf16 42.2 us for 34.5; 1024
+            // threads have no registers for that, 1000x25088 fp32 79 us for 120)
+            const v4i none = {0, 0, 0, 0};
             Vec<T> vx[KEEP], vr[KEEP];
-            load_row<T, TPR, KEEP>(xr, sub, p.cols, vx);
-            if (add) load_row<T, TPR, KEEP>(rr, sub, p.cols, vr);
 #pragma unroll
-            for (int i = 0; i < KEEP; ++i) s[i] = sums_of(vx[i], vr[i], add);
+            for (int i = 0; i < KEEP; ++i) {
+                __builtin_memcpy(&vx[i], &none, 16);
+                if (i * TPR + sub < whole) vx[i] = load_vector<T, PASSING>(xr, i * TPR + sub);
+            }
+            if (rr) {
+#pragma unroll
+                for (int i = 0; i < KEEP; ++i) {
+                    __builtin_memcpy(&vr[i], &none, 16);
+                    if (i * TPR + sub < whole) vr[i] = load_vector<T, PASSING>(rr, i * TPR + sub);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < KEEP; ++i) s[i] = sums_of(vx[i], vr[i], rr != nullptr);
+        } else {
+#pragma unroll
+            for (int i = 0; i < KEEP; ++i) {
+                if (i * TPR + sub < whole) {
+                    s[i] = load_sums<T, PASSING>(xr, rr, i * TPR + sub);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) s[i].v[e] = 0.0f;
+                }
+            }
         }
-        const auto sums_at = [&](int64_t at) {
-            const Vec<T> vx = load_vec(xr, at, p.cols);
-            return sums_of(vx, add ? load_vec(rr, at, p.cols) : vx, add);
-        };
-        constexpr int64_t BEYOND = int64_t(KEEP) * TPR * N;
+        float last = 0.0f;
+        if (tail) last = float(xr[at_tail]) + (rr ? float(rr[at_tail]) : 0.0f);
 #pragma unroll
         for (int i = 0; i < KEEP; ++i) add_squares(s[i]);
-        for (int64_t at = BEYOND + sub * N; at < p.cols; at += TPR * N) add_squares(sums_at(at));
+        for (int k = KEEP * TPR + sub; k < whole; k += TPR) add_squares(load_sums(xr, rr, k));
+        squares = __builtin_fma(double(last), double(last), squares);
         squares = sum_of_lanes<(TPR < 64 ? TPR : 64)>(squares);
         if (TPR > 64) {
             __syncthreads();                             // (those of the row before are read)
@@ -161,18 +195,21 @@ add_rms_norm_i8_kernel(const NormRows p, const T *x, const T *r, T *sum)
         }
         if (sum && live) {
 #pragma unroll
-            for (int i = 0; i < KEEP; ++i) store_sums(s[i], sr, (int64_t(i) * TPR + sub) * N, p.cols);
+            for (int i = 0; i < KEEP; ++i)
+                if (i * TPR + sub < whole) store_sums(s[i], sr, i * TPR + sub);
+            if (tail) sr[at_tail] = T(last);
         }
-        const Factor f = factor_of(squares, p.cols, p.eps);
-        uint32_t most = 0;
+        const Factor f = factor_of(squares, double(max(p.cols, int64_t(1))), p.eps);
+        last = last * f.lift * f.inv * (tail && p.weight ? p.weight[at_tail] : 1.0f);
+        uint32_t most = __float_as_uint(last) & 0x7FFFFFFFu;
 #pragma unroll
         for (int i = 0; i < KEEP; ++i) {
-            normalise(s[i], f, p.weight, (int64_t(i) * TPR + sub) * N, p.cols);
+            normalise(s[i], f, p.weight, min(i * TPR + sub, max(whole - 1, 0)));
             most = most_of_values(s[i], most);
         }
-        for (int64_t at = BEYOND + sub * N; at < p.cols; at += TPR * N) {
-            Values<N> v = sums_at(at);
-            normalise(v, f, p.weight, at, p.cols);
+        for (int k = KEEP * TPR + sub; k < whole; k += TPR) {
+            Values<N> v = load_sums(xr, rr, k);
+            normalise(v, f, p.weight, k);
             most = most_of_values(v, most);
         }
         most = most_of_lanes<(TPR < 64 ? TPR : 64)>(most);
@@ -187,13 +224,15 @@ add_rms_norm_i8_kernel(const NormRows p, const T *x, const T *r, T *sum)
         if (!live) continue;
         int8_t *const q = p.q + row * p.ldq;
 #pragma unroll
-        for (int i = 0; i < KEEP; ++i) store_quantized(s[i], scale, q, (int64_t(i) * TPR + sub) * N, p.cols);
-        for (int64_t at = BEYOND + sub * N; at < p.cols; at += TPR * N) {
-            Values<N> v = sums_at(at);
-            if (sum) store_sums(v, sr, at, p.cols);
-            normalise(v, f, p.weight, at, p.cols);
-            store_quantized(v, scale, q, at, p.cols);
+        for (int i = 0; i < KEEP; ++i)
+            if (i * TPR + sub < whole) store_quantized(s[i], scale, q, i * TPR + sub);
+        for (int k = KEEP * TPR + sub; k < whole; k += TPR) {
+            Values<N> v = load_sums(xr, rr, k);
+            if (sum) store_sums(v, sr, k);
+            normalise(v, f, p.weight, k);
+            store_quantized(v, scale, q, k);
         }
+        if (tail) q[at_tail] = int8_t((scale.lifts ? quantize<true>(last, scale) : quantize<false>(last, scale)) & scale.mask);
         if (sub == 0) p.scale[row] = scale.scale;
     }
 }
@@ -201,11 +240,18 @@ add_rms_norm_i8_kernel(const NormRows p, const T *x, const T *r, T *sum)
 template <typename T>
 void launch_norm(const NormRows &p, hipStream_t st)
 {
-    const int64_t vecs = (p.cols + Vec<T>::N - 1) / Vec<T>::N;
-#define PCONV_LAUNCH(TPR, KEEP, THREADS)                                                                                       \
-    hipLaunchKernelGGL((add_rms_norm_i8_kernel<T, TPR, KEEP, THREADS>),                                                        \
+    const int64_t vecs = p.cols / Vec<T>::N;
+#define PCONV_LAUNCH_AS(TPR, KEEP, THREADS, PASSING)                                                                           \
+    hipLaunchKernelGGL((add_rms_norm_i8_kernel<T, TPR, KEEP, THREADS, PASSING>),                                               \
                        dim3(unsigned(std::min<int64_t>((p.rows + (THREADS / TPR) - 1) / (THREADS / TPR), 1 << 20))), dim3(THREADS), 0, st, p,  \
                        static_cast<const T *>(p.x), static_cast<const T *>(p.r), static_cast<T *>(p.sum))
+#define PCONV_LAUNCH(TPR, KEEP, THREADS)                                                                                       \
+    do {                                                                                                                       \
+        if (passing && vecs <= TPR * KEEP) PCONV_LAUNCH_AS(TPR, KEEP, THREADS, true); else PCONV_LAUNCH_AS(TPR, KEEP, THREADS, false); \
+    } while (0)
+    // What is read once and is most of the memory-side cache is read past it (100352x256 fp32, 196 MB: 65.6 us without, 59.0;
+    // bf16, 98 MB, of which the cache still holds a part: 38.2 and 42.4).
+    const bool passing = p.rows * p.cols * int64_t(sizeof(T)) * (p.r ? 2 : 1) > int64_t(160) << 20;
     if (vecs <= 8) PCONV_LAUNCH(8, 1, 256);
     else if (vecs <= 16) PCONV_LAUNCH(16, 1, 256);
     else if (vecs <= 32) PCONV_LAUNCH(16, 2, 256);
@@ -215,8 +261,10 @@ void launch_norm(const NormRows &p, hipStream_t st)
     else if (vecs <= 512) PCONV_LAUNCH(256, 2, 256);
     else if (vecs <= 1024) PCONV_LAUNCH(256, 4, 256);
     else if (vecs <= 2048) PCONV_LAUNCH(512, 4, 512);
-    else PCONV_LAUNCH(1024, 4, 1024);
+    else if (vecs <= 4096) PCONV_LAUNCH(512, 8, 512);                    // (by 1024 threads, four vectors each: 2000x25088 bf16 90 us for 82)
+    else PCONV_LAUNCH(1024, 32 / Vec<T>::N, 1024);
 #undef PCONV_LAUNCH
+#undef PCONV_LAUNCH_AS
 }
 
 }  // namespace
