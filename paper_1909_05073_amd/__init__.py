@@ -1166,61 +1166,24 @@ def _distill_call(student, teacher, classes, temperature, reduction):
                          classes.element_size(), m, v, top, float(temperature), 1 if reduction == "mean" else 0)
 
 
-def _distill_losses(student, m, reduction):
-    """(the rows' losses, the result, or None where it is the rows' losses)."""
-    import torch
-    loss = torch.empty_strided((m,), (1,), dtype=torch.float32, device=student.device)
-    return loss, None if reduction == "none" else torch.empty_strided((), (), dtype=torch.float32, device=student.device)
+_distill_entries = None                              # of the library that is loaded: (it, addresses of its entries)
 
 
-def _distill_forward(student, teacher, classes, temperature, reduction, keep):
-    import torch
+def _distill(student, teacher, classes, temperature, reduction, what):
+    """The loss (what: 0), with a node for autograd (1), or the loss and its gradient (2); by csrc/pconv_tensors.cpp."""
+    global _distill_entries
+    L = _lib or lib()
+    if _distill_entries is None or _distill_entries[0] is not L:
+        _distill_entries = L, tuple(C.cast(f, C.c_void_p).value for f in (L.pconv_distill_loss, L.pconv_distill_grad, L.pconv_distill_loss_grad,
+                                                                          L.pconv_last_error))
     index, m, v, call = _distill_call(student, teacher, classes, temperature, reduction)
-    loss, total = _distill_losses(student, m, reduction)
-    lse = torch.empty_strided((m,), (1,), dtype=torch.float32, device=student.device) if keep else None
-    rc = (_lib or lib()).pconv_distill_loss(*call, loss.data_ptr() or None, total.data_ptr() if total is not None else None,
-                                            (lse.data_ptr() or None) if keep else None, _stream(index))
-    if rc != OK:
-        _check(rc)
-    return (loss.view(student.shape[:-1]) if total is None else total), lse
-
-
-_distill_function = None
-
-
-def _distill_autograd():
-    """The loss as autograd takes it (made when it is first asked for, as torch is loaded then)."""
-    global _distill_function
-    if _distill_function is not None:
-        return _distill_function
-    import torch
-
-    class DistillLoss(torch.autograd.Function):
-        @staticmethod
-        def forward(ctx, student, teacher, classes, temperature, reduction):
-            value, lse = _distill_forward(student, teacher, classes, temperature, reduction, True)
-            ctx.save_for_backward(student, teacher, classes, lse)
-            ctx.how = temperature, reduction
-            return value
-
-        @staticmethod
-        @torch.autograd.function.once_differentiable
-        def backward(ctx, up):
-            student, teacher, classes, lse = ctx.saved_tensors
-            temperature, reduction = ctx.how
-            index, m, v, call = _distill_call(student, teacher, classes, temperature, reduction)
-            up = up.to(torch.float32)
-            if reduction == "none":
-                up = up.reshape(-1).contiguous()
-            grad = _empty(student.shape[:-1], m, v, student.dtype, student)
-            rc = (_lib or lib()).pconv_distill_grad(*call, lse.data_ptr() or None, up.data_ptr() or None, 1 if reduction == "none" else 0,
-                                                    grad.data_ptr() or None, v, _stream(index))
-            if rc != OK:
-                _check(rc)
-            return grad, None, None, None, None
-
-    _distill_function = DistillLoss
-    return DistillLoss
+    try:
+        return _tensor_list_calls().distill(_distill_entries[1], student, teacher, classes,
+                                            (m, v, call[11], call[1], call[4], call[7], call[8], call[2], call[5], call[12]), _REDUCTIONS.index(reduction), what)
+    except RuntimeError as e:
+        if str(e).startswith("pconv status -"):
+            _check(int(str(e).split()[2].rstrip(":")))
+        raise
 
 
 def distill_loss(student, teacher, classes, temperature: float = 1.0, reduction: str = "mean"):
@@ -1232,12 +1195,10 @@ def distill_loss(student, teacher, classes, temperature: float = 1.0, reduction:
     Recorded for autograd: a gradient goes to the student (of its type), none to the teacher."""
     import torch
     if not torch.is_grad_enabled():
-        return _distill_forward(student, teacher, classes, temperature, reduction, False)[0]
+        return _distill(student, teacher, classes, temperature, reduction, 0)
     if teacher.requires_grad:
         raise ValueError("no gradient goes to the teacher: detach it")
-    if student.requires_grad:
-        return _distill_autograd().apply(student, teacher, classes, temperature, reduction)
-    return _distill_forward(student, teacher, classes, temperature, reduction, False)[0]
+    return _distill(student, teacher, classes, temperature, reduction, 1 if student.requires_grad else 0)
 
 
 def distill_loss_grad(student, teacher, classes, temperature: float = 1.0, reduction: str = "mean", out=None):
@@ -1245,15 +1206,18 @@ def distill_loss_grad(student, teacher, classes, temperature: float = 1.0, reduc
     the sum.  For loops that go on from the logits themselves: student.backward(grad).
 
     out: where the gradient goes, of the student's type; it must not overlap an input.  Nothing is recorded for autograd."""
+    if out is None:
+        return _distill(student, teacher, classes, temperature, reduction, 2)
+    import torch
     index, m, v, call = _distill_call(student, teacher, classes, temperature, reduction)
     grad, g_step = _output(out, student.shape[:-1], m, v, student.dtype, student)
-    if out is not None and not _tensor_list_calls().apart(grad, student, teacher, classes):
+    if not _tensor_list_calls().apart(grad, student, teacher, classes):
         _refuse_overlap((grad, m, v, g_step), (student, m, v, call[1]), (teacher, m, call[11], call[4]), (classes, m, call[11], call[7]))
-    loss, total = _distill_losses(student, m, reduction)
+    loss = torch.empty_strided((m,), (1,), dtype=torch.float32, device=student.device)
+    total = None if reduction == "none" else torch.empty_strided((), (), dtype=torch.float32, device=student.device)
     rc = (_lib or lib()).pconv_distill_loss_grad(*call, loss.data_ptr() or None, total.data_ptr() if total is not None else None,
                                                  grad.data_ptr() or None, g_step, _stream(index))
     if rc != OK:
         _check(rc)
-    if out is not None:
-        _tensor_list_calls().changed([grad])
+    _tensor_list_calls().changed([grad])
     return (loss.view(student.shape[:-1]) if total is None else total), grad

@@ -45,9 +45,10 @@ def _run(cmd):
 def build_tensors(verbose: bool = False) -> str:
     torch = importlib.util.find_spec("torch").submodule_search_locations[0]
     # (torch's libraries are in the process already when it is loaded)
-    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-isystem", os.path.join(torch, "include"),
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__", "-isystem", "/opt/rocm/include",
+           "-isystem", os.path.join(torch, "include"),
            "-isystem", os.path.join(torch, "include", "torch", "csrc", "api", "include"), "-isystem", sysconfig.get_paths()["include"],
-           os.path.join(CSRC, "pconv_tensors.cpp"), "-o", TENSORS, "-L", os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+           os.path.join(CSRC, "pconv_tensors.cpp"), "-o", TENSORS, "-L", os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"]
     if verbose:
         print(" ".join(cmd))
     _run(cmd)

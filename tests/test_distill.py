@@ -397,8 +397,9 @@ def test_wrong_tensors_are_refused():
             with pytest.raises(ValueError):
                 call()
                 pytest.fail(f"call {i} was not refused")
-        with pytest.raises(P.PconvError, match="temperature"):
-            f(s, t, c, 0.0)
+        for leaf in (s, s.clone().requires_grad_()):
+            with pytest.raises(P.PconvError, match="temperature"):
+                f(leaf, t, c, 0.0)
     for out in (z(4, 9), z(4, 8).bfloat16(), s, s.view(-1)[:32].view(4, 8)):
         with pytest.raises(ValueError):
             P.distill_loss_grad(s, t, c, out=out)
