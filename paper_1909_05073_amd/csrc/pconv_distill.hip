@@ -126,10 +126,11 @@ __device__ __forceinline__ void join_vectors(Running &r, Vec<T> (&v)[U], float i
 // sums to the gradient, and what lies beyond is read twice.  The entries' shares and classes lie in LDS.  The gradient is written as if there were no entries; behind a barrier the first
 // entry that names a class writes it again with the shares of all that name it taken off.
 template <typename T, int TPR, int U, bool LOSS, bool GRAD>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR)
+__global__ void __launch_bounds__(TPR == 64 ? 256 : TPR)
 distill_kernel(const DistillRows p)
 {
-    constexpr int N = Vec<T>::N, THREADS = TPR < 256 ? 256 : TPR, RPW = THREADS / TPR, WAVES = TPR / 64;
+    // (four rows a workgroup where each has a wave; where there are barriers all threads share one)
+    constexpr int N = Vec<T>::N, THREADS = TPR == 64 ? 256 : TPR, RPW = THREADS / TPR, WAVES = TPR / 64;
     extern __shared__ float entries[];
     __shared__ Running room[THREADS / 64][2];
     __shared__ float losses[THREADS / 64];
@@ -263,17 +264,25 @@ void launch_rows(const DistillRows &p, hipStream_t st)
 {
     const size_t lds = size_t((p.top + 3) / 4) * 48;
     const int64_t vecs = (int64_t(p.v) + Vec<T>::N - 1) / Vec<T>::N;
-#define PCONV_LAUNCH(TPR, KEEP)                                                                                                    do {                                                                                                                               constexpr int RPW = TPR < 256 ? 256 / TPR : 1;                                                                                 hipLaunchKernelGGL((distill_kernel<T, TPR, KEEP, LOSS, GRAD>), dim3(unsigned(std::min<int64_t>((p.rows + RPW - 1) / RPW, 1 << 20))),                             dim3(RPW * TPR), RPW * lds, st, p);                                                                     } while (0)
-    // (the loss has the same bits with and without its gradient: the same threads a row for both)
+#define PCONV_LAUNCH(TPR, U)                                                                                                   \
+    do {                                                                                                                       \
+        constexpr int RPW = TPR == 64 ? 4 : 1;                                                                                 \
+        hipLaunchKernelGGL((distill_kernel<T, TPR, U, LOSS, GRAD>), dim3(unsigned(std::min<int64_t>((p.rows + RPW - 1) / RPW, 1 << 20))),  \
+                           dim3(RPW * TPR), RPW * lds, st, p);                                                                 \
+    } while (0)
+    // The loss has the same bits with and without its gradient: the same threads a row for both.  More threads a row meet more
+    // often than what they do in between is worth (8192x4000 bf16 47.2 us by 256, 40.5 by 64; 1999x10007 fp32 45.3 by 512, 41.7 by
+    // 256; 4096x32768 bf16 183 by 1024, 129 by 512), fewer read more of a row twice (136 by 256).
     if constexpr (LOSS) {
         if (vecs <= 64 * 2) PCONV_LAUNCH(64, 2);
         else if (vecs <= 64 * 4) PCONV_LAUNCH(64, 4);
+        else if (vecs <= 64 * 8) PCONV_LAUNCH(64, 8);
         else if (vecs <= 256 * 4) PCONV_LAUNCH(256, 4);
-        else if (vecs <= 256 * 8) PCONV_LAUNCH(256, 8);
-        else if (vecs <= 512 * 8) PCONV_LAUNCH(512, 8);
-        else PCONV_LAUNCH(1024, 8);
+        else if (vecs <= 256 * 10) PCONV_LAUNCH(256, 8);
+        else if (vecs <= 512 * 8) PCONV_LAUNCH(512, 4);
+        else PCONV_LAUNCH(512, 8);
     } else {
-        if (vecs <= 64 * 4) PCONV_LAUNCH(64, 4);
+        if (vecs <= 64 * 8) PCONV_LAUNCH(64, 4);
         else PCONV_LAUNCH(256, 4);
     }
 #undef PCONV_LAUNCH
