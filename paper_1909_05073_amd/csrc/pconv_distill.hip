@@ -247,6 +247,7 @@ distill_total_kernel(const float *__restrict__ loss, int64_t rows, double scale,
 {
     __shared__ double room[16];
     double s = 0;
+#pragma unroll 8
     for (int64_t i = threadIdx.x; i < rows; i += 1024) s += double(loss[i]);
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) s += __shfl_xor(s, d);

@@ -483,13 +483,48 @@ def test_written_outputs_count_as_changed():
 
 # ---- plans ---------------------------------------------------------------------------------------------------------------
 
+FORMS = {(1, 0, 0, False): (9, 40, 256), (2, 32, 1, False): (129, 11206, 64), (2, 32, 1, True): (1, 9309, 22924), (2, 32, 2, False): (20, 64, 256),
+         (2, 32, 2, True): (7, 33, 10096), (2, 64, 1, False): (145, 18962, 40), (2, 64, 1, True): (17908, 15, 19019), (2, 64, 2, False): (8816, 20, 64),
+         (2, 64, 2, True): (613, 20, 17291), (2, 128, 1, False): (34014, 20, 64), (2, 128, 1, True): (4750, 1, 19083),
+         (2, 128, 2, False): (16767, 20, 64), (2, 128, 2, True): (4750, 20, 19083), (2, 256, 1, False): (22236, 276, 64)}
+
+
+def form_of(m, n, k):
+    p = P.pconv_debug_mx4_plan(m, n, -(-k // 32))
+    return p.kernel, p.tile_m, p.sets, p.splits > 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("form", FORMS)
+def test_every_form_of_the_product(form):
+    """Equal scales: sums are exact, whoever adds them."""
+    import torch
+    m, n, k = FORMS[form]
+    say(f"[case] matmul_mx4 {m}x{n}x{k}, form {form}")
+    assert form_of(m, n, k) == form
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(m + k)
+    table = torch.tensor(VALUES, device="cuda")
+    made = []
+    for rows in (m, n):
+        blocks = -(-k // 32)
+        q = torch.randint(0, 256, (rows, blocks * 16), generator=gen, device="cuda", dtype=torch.uint8)
+        q[:, (k + 1) // 2:] = 0
+        if k % 2:
+            q[:, k // 2] &= 15
+        s = torch.full((-(-blocks // 8), rows, 8), 125, dtype=torch.uint8, device="cuda")
+        made.append((q, s, torch.stack([table[(q & 15).int()], table[(q >> 4).int()]], 2).view(rows, -1) / 4))
+    (a, sa, va), (b, sb, vb) = made
+    bias = torch.randn(n, generator=gen, device="cuda")
+    want = va @ vb.t().contiguous()
+    assert torch.equal(P.matmul_mx4(a, sa, b, sb), want.float())
+    want = (want.float() + bias).clamp(min=0).bfloat16()
+    assert torch.equal(P.matmul_mx4(a, sa, b, sb, bias, relu=True, out_dtype=torch.bfloat16), want)
+
+
 def test_plans_of_the_products():
-    """Every tile and both ways to share k are reached by sizes of the tests above."""
-    plans = [P.pconv_debug_mx4_plan(m, n, -(-k // 32)) for m, n, k in SIZES + [(7900, 4000, 592), (1024, 4096, 2304), (5000, 1030, 1056), (40_000, 200, 320)]]
-    tiles = {(p.tile_m, p.tile_n) for p in plans if p.kernel == 2}
-    assert tiles == {(32, 128), (64, 128), (128, 128), (256, 256)}, tiles
-    assert any(p.splits > 1 for p in plans) and any(p.splits == 1 for p in plans if p.kernel == 2)
-    assert {p.sets for p in plans if p.kernel == 2} == {1, 2} and {p.kernel for p in plans} == {1, 2}
+    for form, size in FORMS.items():
+        assert form_of(*size) == form
     for m, n, blocks in ((0, 1, 1), (1, 0, 1), (1, 1, -1), ((1 << 30) + 1, 1, 1), (1, 1, (1 << 19) + 1)):
         with pytest.raises(P.PconvError):
             P.pconv_debug_mx4_plan(m, n, blocks)
