@@ -1,0 +1,115 @@
+"""The norm, the layers in few bits and the distillation together, as a program uses them: the example, each of its served steps
+against plain 64 bits on the same inputs, a whole pass captured and replayed, and a training step's gradients."""
+import os
+import sys
+
+import numpy as np
+import pytest
+
+import paper_1909_05073_amd as P
+
+from gpu_util import say
+from test_add_rms_norm import check_norm
+from test_distill import check_grad, plain_distill
+from test_i8_layers import check as check_i8
+from test_i8_layers import plain_product as plain_i8
+from test_mx4_layers import check as check_mx4
+from test_mx4_layers import plain_product as plain_mx4
+from test_mx4_layers import plain_quantize as plain_quantize_mx4
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def load():
+    sys.path.insert(0, os.path.join(ROOT, "examples"))
+    try:
+        import distill_and_serve
+    finally:
+        sys.path.pop(0)
+    return distill_and_serve
+
+
+@pytest.mark.gpu
+def test_the_example_trains_and_serves():
+    import torch
+    say("[case] examples/distill_and_serve.py")
+    E = load()
+    losses, norms, right = E.main(steps=30, say=say)
+    assert losses.shape == norms.shape == (30,) and bool(torch.isfinite(losses).all()) and bool(torch.isfinite(norms).all())
+    assert len(right) == 3 and all(0.0 <= r <= 1.0 for r in right)
+
+
+def unpacked(q, scale):
+    """(codes, scales) of the test's plain functions from what the library keeps."""
+    q, s = q.cpu().numpy(), scale.cpu().numpy()
+    codes = np.stack([q & 15, q >> 4], 2).reshape(len(q), -1)
+    return codes, s.transpose(1, 0, 2).reshape(len(q), -1)[:, :q.shape[1] // 16]
+
+
+@pytest.mark.gpu
+def test_every_served_step_against_64_bits():
+    import torch
+    say("[case] a pass of examples/distill_and_serve.py")
+    E = load()
+    student, _, pid, conn = E.prune(E.parameters(4))
+    served = E.Served(student, pid, conn)
+    x, _ = E.images(6, seed=3)
+    y = P.conv2d(served.conv, x, served.conv_b, relu=True, layout="nhwc")
+    r = P.linear_i8(x, *served.beside)
+    q, scale, s = P.add_rms_norm_i8(y, r, served.gain, E.EPS)
+    rows = 6 * E.SIDE * E.SIDE
+    flat = lambda t: t.detach().cpu().numpy().reshape(rows, -1)
+    check_norm((q.view(rows, -1), scale.view(-1), s.view(rows, -1)), flat(y), flat(r), flat(served.gain.expand_as(y))[0], np.float32(E.EPS), "f32")
+    z = P.matmul_i8(q, scale, *served.point, served.point_b, relu=True)
+    want, bound = plain_i8(flat(q).astype(np.int64), scale.cpu().numpy().reshape(-1), served.point[0].cpu().numpy(), served.point[1].cpu().numpy(),
+                           served.point_b.cpu().numpy(), True)
+    check_i8(z.view(rows, -1), want, bound, "matmul_i8")
+    mean = z.mean((1, 2))
+    logits = P.linear_mx4(mean, *served.fc, served.fc_b)
+    want, bound = plain_mx4(plain_quantize_mx4(mean.cpu().numpy()), unpacked(*served.fc), served.fc_b.cpu().numpy(), False)
+    check_mx4(logits, want, bound, "linear_mx4")
+    assert torch.equal(served(x), logits)
+
+
+@pytest.mark.gpu
+def test_replays_of_a_captured_pass():
+    import torch
+    say("[case] a captured pass of examples/distill_and_serve.py")
+    E = load()
+    student, _, pid, conn = E.prune(E.parameters(5))
+    served = E.Served(student, pid, conn)
+    x, _ = E.images(8, seed=0)
+    top, classes = torch.randn(8, E.TOP, device="cuda"), torch.randint(E.CLASSES, (8, E.TOP), device="cuda")
+    served(x)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        logits = served(x)
+        loss, grad = P.distill_loss_grad(logits, top, classes, 2.0)
+    for i in range(4):
+        x.copy_(E.images(8, seed=20 + i)[0])
+        g.replay()
+        torch.cuda.synchronize()
+        want = served(x)
+        assert torch.equal(logits, want), f"replay {i}"
+        both = P.distill_loss_grad(want, top, classes, 2.0)
+        assert torch.equal(loss, both[0]) and torch.equal(grad, both[1]), f"replay {i}"
+
+
+@pytest.mark.gpu
+def test_a_training_step_has_the_gradients_of_the_formula():
+    """The logits' gradient against 64 bits; the rest of the graph is torch's, and is fed with it."""
+    import torch
+    say("[case] a step of examples/distill_and_serve.py")
+    E = load()
+    teacher = E.parameters(6)
+    student, mask, _, _ = E.prune(teacher)
+    x, label = E.images(16, seed=2)
+    logits = E.forward(student, x)
+    logits.retain_grad()
+    with torch.no_grad():
+        top, classes = E.forward(teacher, x).topk(E.TOP, 1)
+    E.from_teacher(teacher)(logits, x, label).backward()
+    _, _, grad, off = plain_distill(logits.detach().cpu().numpy(), top.cpu().numpy(), classes.cpu().numpy(), 2.0, np.full(16, 1 / 16))
+    check_grad(logits.grad, grad, off, "f32", "logits")
+    assert all(bool(t.grad.isfinite().all()) and bool(t.grad.any()) for t in student.values())
