@@ -560,11 +560,17 @@ def _prod(sizes) -> int:
     return n
 
 
+def _refuse_foreign_capture(device):
+    """A graph captured by others than torch would keep the address of memory that goes back to torch's pool."""
+    import torch
+    if torch.cuda.is_current_stream_capturing() and not _graph_pool_serves(device):
+        raise RuntimeError("the stream is being captured by others than torch: call the pconv_... function with work space of your own")
+
+
 def _scratch(size: int, like):
     """Work space out of torch's pool for a call on the current stream."""
     import torch
-    if torch.cuda.is_current_stream_capturing() and not _graph_pool_serves(like.device):
-        raise RuntimeError("the stream is being captured by others than torch: call the pconv_... function with work space of your own")
+    _refuse_foreign_capture(like.device)
     return torch.empty_strided((size,), (1,), dtype=torch.uint8, device=like.device)
 
 
@@ -1177,6 +1183,8 @@ def _distill(student, teacher, classes, temperature, reduction, what):
         _distill_entries = L, tuple(C.cast(f, C.c_void_p).value for f in (L.pconv_distill_loss, L.pconv_distill_grad, L.pconv_distill_loss_grad,
                                                                           L.pconv_last_error))
     index, m, v, call = _distill_call(student, teacher, classes, temperature, reduction)
+    if what == 1 or reduction != "none":                 # (the rows' losses, or what the gradient needs, are no result)
+        _refuse_foreign_capture(student.device)
     try:
         return _tensor_list_calls().distill(_distill_entries[1], student, teacher, classes,
                                             (m, v, call[11], call[1], call[4], call[7], call[8], call[2], call[5], call[12]), _REDUCTIONS.index(reduction), what)
@@ -1213,6 +1221,8 @@ def distill_loss_grad(student, teacher, classes, temperature: float = 1.0, reduc
     grad, g_step = _output(out, student.shape[:-1], m, v, student.dtype, student)
     if not _tensor_list_calls().apart(grad, student, teacher, classes):
         _refuse_overlap((grad, m, v, g_step), (student, m, v, call[1]), (teacher, m, call[11], call[4]), (classes, m, call[11], call[7]))
+    if reduction != "none":
+        _refuse_foreign_capture(student.device)
     loss = torch.empty_strided((m,), (1,), dtype=torch.float32, device=student.device)
     total = None if reduction == "none" else torch.empty_strided((), (), dtype=torch.float32, device=student.device)
     rc = (_lib or lib()).pconv_distill_loss_grad(*call, loss.data_ptr() or None, total.data_ptr() if total is not None else None,

@@ -344,6 +344,48 @@ def test_autograd_keeps_its_rules():
     assert torch.equal(s.grad, 2 * one)
 
 
+@pytest.mark.gpu
+def test_a_capture_that_torch_does_not_know_of_is_refused_where_memory_would_be_lent():
+    """The rows' losses and what a gradient needs go back to torch's pool, which such a graph must not keep; calls whose every
+    output is handed out are captured."""
+    import ctypes as C
+
+    import torch
+    say("[case] distill captured by the HIP runtime")
+    L = P.lib()
+
+    def hip(name, *args):
+        fn = getattr(L, name)
+        fn.restype = C.c_int
+        assert fn(*args) == 0, name
+    z, t, c = (dev(a) for a in make(np.random.default_rng(8), 20, 300, 6))
+    out, leaf = torch.empty_like(z), z.clone().requires_grad_()
+    side = torch.cuda.Stream()
+    want = P.distill_loss_grad(z, t, c, 2.0, "none")
+    P.distill_loss_grad(z, t, c, 2.0, "none", out=out)
+    torch.cuda.synchronize()
+    st, graph, ready = C.c_void_p(side.cuda_stream), C.c_void_p(), C.c_void_p()
+    with torch.cuda.stream(side):
+        P.distill_loss_grad(z, t, c, 2.0, "none")            # (its memory is in the stream's pool)
+        hip("hipStreamBeginCapture", st, C.c_int(2))
+        for call in (lambda: P.distill_loss(z, t, c), lambda: P.distill_loss_grad(z, t, c), lambda: P.distill_loss_grad(z, t, c, out=out),
+                     lambda: P.distill_loss(leaf, t, c, reduction="none")):
+            with pytest.raises(RuntimeError, match="captured by others"):
+                call()
+        loss, grad = P.distill_loss_grad(z, t, c, 2.0, "none")
+        hip("hipStreamEndCapture", st, C.byref(graph))
+    hip("hipGraphInstantiate", C.byref(ready), graph, None, None, C.c_size_t(0))
+    for i in range(3):
+        z.copy_(dev(make(np.random.default_rng(9 + i), 20, 300, 6)[0]))
+        torch.cuda.synchronize()
+        hip("hipGraphLaunch", ready, st)
+        torch.cuda.synchronize()
+        want = P.distill_loss_grad(z, t, c, 2.0, "none")
+        assert torch.equal(loss, want[0]) and torch.equal(grad, want[1]), f"replay {i}"
+    hip("hipGraphExecDestroy", ready)
+    hip("hipGraphDestroy", graph)
+
+
 # ---- refusals ------------------------------------------------------------------------------------------------------------
 
 def c_calls():
