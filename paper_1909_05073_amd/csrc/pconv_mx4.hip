@@ -231,11 +231,14 @@ __device__ __forceinline__ void finish_tile(const Mx4Product &p, const f4 (&acc)
     }
 }
 
-// Order of the blocks of a row in LDS: place block ^ key.  16 lanes read 16 rows at once, of 128 bytes each: the eight rows
-// that begin in the same half of LDS's 256 bytes of banks have eight keys.  (Activations are read row by row, weights as they
-// are dealt.)
-__device__ __forceinline__ int key_of_row(int row) { return (row >> 1) & 7; }
-template <typename Y> __device__ __forceinline__ int key_of_channel(int row) { return sizeof(Y) == 4 ? (row >> 1) & 7 : ((row >> 1) & 1) | ((row >> 2) & 6); }
+// Order of the blocks of a row in LDS: place block ^ key.  A read of 16 bytes a lane goes by sixteen lanes at once: of rows 0 to 3
+// and 12 to 15 with one block and 4 to 11 with that of the next group of lanes, two blocks further, and the other way round.
+// Rows lie 128 bytes apart, so that the eight that begin in the same half of LDS's 256 bytes of banks need eight places: the
+// first four have keys 0 to 3, which an exchange of blocks two apart keeps among themselves, the others 4 to 7.  (Keys 0 to 7 in
+// order: half of the cycles in which LDS is read are conflicts.)  Activations are read row by row, weights as they are dealt.
+__device__ __forceinline__ int key_of(int h) { return (h & 3) | (((h >> 1) ^ (h >> 2)) & 1) << 2; }
+__device__ __forceinline__ int key_of_row(int row) { return key_of((row >> 1) & 7); }
+template <typename Y> __device__ __forceinline__ int key_of_channel(int row) { return key_of(sizeof(Y) == 4 ? (row >> 1) & 7 : ((row >> 1) & 1) | ((row >> 2) & 6)); }
 
 // Tiles of BM rows of y and BN channels, WM x WN waves, and KG such sets of waves that take the stages in turn.  A slab of
 // all the tile's rows is a stage: 128 bytes of values and 8 of scales a row; S stages lie in LDS.  A row of a stage is
@@ -272,7 +275,7 @@ matmul_mx4_kernel(const Mx4Product p, int splits, float *part)
     const int stages = (p.blocks + 7) / 8;
     const int s_begin = int(int64_t(stages) * split / splits), s_end = int(int64_t(stages) * (split + 1) / splits);
 
-    auto key_b = [](int row) { return key_of_channel<Y>(row); };
+    const int key = key_of(r >> 1);                      // (of all the rows that the lane reads)
 
     f4 acc[MT][NT];
 #pragma unroll
@@ -295,12 +298,12 @@ matmul_mx4_kernel(const Mx4Product p, int splits, float *part)
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
                 const int row = wm + i * 16 + r;
-                a[i] = st[row * 8 + ((2 * g + KK) ^ key_of_row(row))];
+                a[i] = st[row * 8 + ((2 * g + KK) ^ key)];
             }
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
                 const int row = wn + Deal<Y>::row(j, r);
-                b[j] = st[BM * 8 + row * 8 + ((2 * g + KK) ^ key_b(row))];
+                b[j] = st[BM * 8 + row * 8 + ((2 * g + KK) ^ key)];
             }
 #pragma unroll
             for (int i = 0; i < MT; ++i)
@@ -324,7 +327,7 @@ matmul_mx4_kernel(const Mx4Product p, int splits, float *part)
 #pragma unroll
     for (int i = 0; i < PB; ++i) {
         const int row = (i * NW + wave) * 8 + (lane >> 3);
-        end_b[i] = (lane & 7) ^ key_b(row);
+        end_b[i] = (lane & 7) ^ key_of_channel<Y>(row);
         off_b[i] = uint32_t(min(row, p.n - 1 - n0)) * uint32_t(p.ldb) + uint32_t(end_b[i] * 16);
     }
     // 32 rows of one operand have 256 bytes of scales, a word a lane
