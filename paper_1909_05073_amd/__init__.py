@@ -634,6 +634,18 @@ def _tensor_list_calls():
     return _tensors_module
 
 
+_native_entries = {}                                 # of the library that is loaded: addresses by the names of the functions that take them
+
+
+def _native(name, *entries):
+    """(csrc/pconv_tensors.cpp's function of this name, the addresses of the library's entries that it takes)."""
+    L = _lib or lib()
+    known = _native_entries.get(name)
+    if known is None or known[0] is not L:
+        known = _native_entries[name] = L, getattr(_tensor_list_calls(), name), tuple(C.cast(getattr(L, e), C.c_void_p).value for e in entries)
+    return known[1], known[2]
+
+
 def _refuse_overlap(out, *inputs):
     """out and each of the inputs: (tensor or None, rows, columns, elements from row to row)."""
     run = lambda t, rows, columns, step: (t.data_ptr(), rows, columns * t.element_size(), step * t.element_size())
@@ -796,6 +808,11 @@ def add_rms_norm_i8(x, residual=None, weight=None, eps: float = 1e-6, out=None):
 
     The rows of q lie a multiple of 16 bytes apart, as matmul_i8 reads them fastest.  out: where s goes; x or residual, or a
     tensor that overlaps neither nor weight.  Nothing is recorded for autograd."""
+    if out is None:
+        call, entries = _native("add_rms_norm_i8", "pconv_add_rms_norm_i8")
+        made = call(entries, x, residual, weight, eps)
+        if made is not None:
+            return made
     import torch
     dtype = _type_of(x, "x")
     index = _device_index(x, residual, weight, out)
@@ -901,6 +918,10 @@ def _blocks(q, scale, rows_first, what):
 def quantize_mx4(x):
     """x: CUDA tensor [..., k], fp32 or bf16.  Returns (q [..., 16 * blocks] uint8, scale [slabs, rows, 8] uint8), 32 values of k a block and
     8 blocks a slab; see include/pconv.h.  rows: of all leading dimensions together.  Nothing is recorded for autograd."""
+    call, entries = _native("quantize_mx4", "pconv_quantize_mx4")
+    made = call(entries, x)
+    if made is not None:
+        return made
     import torch
     dtype = _type_of(x, "x")
     index = _device_index(x)
@@ -922,6 +943,11 @@ def matmul_mx4(a, a_scale, b, b_scale, bias=None, relu: bool = False, out_dtype=
     bias [n]: fp32.  out_dtype: torch.float32 (unless `out` says otherwise) or torch.bfloat16.  out: where the result goes; it
     must not overlap an input (its rows may lie between those of one).  Nothing is recorded for autograd."""
     import torch
+    if out is None and (out_dtype is None or out_dtype is torch.float32 or out_dtype is torch.bfloat16):
+        call, entries = _native("matmul_mx4", "pconv_matmul_mx4", "pconv_matmul_mx4_workspace")
+        y = call(entries, a, a_scale, b, b_scale, bias, relu, out_dtype is torch.bfloat16)
+        if y is not None:
+            return y
     index = _device_index(a, a_scale, b, b_scale, bias, out)
     m, blocks, a_step, a_slab = _blocks(a, a_scale, False, "a")
     n, kb, b_step, b_slab = _blocks(b, b_scale, True, "b")
@@ -953,6 +979,11 @@ def linear_mx4(x, w, w_scale, bias=None, relu: bool = False, out_dtype=None, out
 
     Returns matmul_mx4(*quantize_mx4(x), w, w_scale, bias, relu) [..., n], of x's type unless `out_dtype` or `out` says
     otherwise.  out: as there.  Nothing is recorded for autograd."""
+    if out is None and out_dtype is None:
+        call, entries = _native("linear_mx4", "pconv_linear_mx4", "pconv_linear_mx4_workspace")
+        y = call(entries, x, w, w_scale, bias, relu)
+        if y is not None:
+            return y
     x_type = _type_of(x, "x")
     index = _device_index(x, w, w_scale, bias, out)
     m, k, x_step = _rows(x, "x")
@@ -1172,22 +1203,14 @@ def _distill_call(student, teacher, classes, temperature, reduction):
                          classes.element_size(), m, v, top, float(temperature), 1 if reduction == "mean" else 0)
 
 
-_distill_entries = None                              # of the library that is loaded: (it, addresses of its entries)
-
-
 def _distill(student, teacher, classes, temperature, reduction, what):
     """The loss (what: 0), with a node for autograd (1), or the loss and its gradient (2); by csrc/pconv_tensors.cpp."""
-    global _distill_entries
-    L = _lib or lib()
-    if _distill_entries is None or _distill_entries[0] is not L:
-        _distill_entries = L, tuple(C.cast(f, C.c_void_p).value for f in (L.pconv_distill_loss, L.pconv_distill_grad, L.pconv_distill_loss_grad,
-                                                                          L.pconv_last_error))
-    index, m, v, call = _distill_call(student, teacher, classes, temperature, reduction)
+    call, entries = _native("distill", "pconv_distill_loss", "pconv_distill_grad", "pconv_distill_loss_grad", "pconv_last_error")
+    index, m, v, n = _distill_call(student, teacher, classes, temperature, reduction)
     if what == 1 or reduction != "none":                 # (the rows' losses, or what the gradient needs, are no result)
         _refuse_foreign_capture(student.device)
     try:
-        return _tensor_list_calls().distill(_distill_entries[1], student, teacher, classes,
-                                            (m, v, call[11], call[1], call[4], call[7], call[8], call[2], call[5], call[12]), _REDUCTIONS.index(reduction), what)
+        return call(entries, student, teacher, classes, (m, v, n[11], n[1], n[4], n[7], n[8], n[2], n[5], n[12]), _REDUCTIONS.index(reduction), what)
     except RuntimeError as e:
         if str(e).startswith("pconv status -"):
             _check(int(str(e).split()[2].rstrip(":")))

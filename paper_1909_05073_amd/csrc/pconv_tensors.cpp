@@ -15,7 +15,14 @@
 // distill(entries, student, teacher, classes, numbers, reduction, what) -> the loss (what: 0), with its node (1), or the loss and its
 // gradient (2); entries: the addresses of pconv_distill_loss, .._grad, .._loss_grad and pconv_last_error; numbers: what these
 // take besides tensors (see DistillCall).  The arguments have been checked.
+//
+// quantize_mx4, matmul_mx4, linear_mx4, add_rms_norm_i8 (entries, tensors, ..) -> what the binding's functions of these names give, for
+// ordinary calls: tensors on the current device whose rows lie as they are made (rows of one matrix with any step), outputs of
+// their own, no capture where work space is lent.  None for all others, wrong ones and failed ones among them: those go the
+// long way, which knows what to say.  In Python a call takes the host 7 to 11 us, here 4 to 5.
 #include <Python.h>
+#include <c10/hip/HIPFunctions.h>
+#include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/function.h>
@@ -24,6 +31,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/autograd/saved_variable.h>
 
+#include <algorithm>
 #include <exception>
 #include <mutex>
 #include <vector>
@@ -238,9 +246,204 @@ PyObject *distill(PyObject *, PyObject *const *args, Py_ssize_t count)
     END_HANDLE_TH_ERRORS
 }
 
-PyMethodDef methods[] = {{"distill", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(distill)), METH_FASTCALL, nullptr},
-                         {"apart", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(apart)), METH_FASTCALL, nullptr},
-                         {"places", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(places)), METH_FASTCALL, nullptr},
+// ---- ordinary calls ---------------------------------------------------------------------------------------------------
+
+using Addresses = unsigned long long[8];
+
+// The addresses that begin every call's arguments.
+bool addresses_of(PyObject *tuple, Addresses &at, Py_ssize_t count)
+{
+    if (!PyTuple_Check(tuple) || PyTuple_GET_SIZE(tuple) != count) return false;
+    for (Py_ssize_t i = 0; i < count; ++i) at[i] = PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(tuple, i));
+    return !PyErr_Occurred();
+}
+
+// The tensor of an argument (null: None); false for anything else.
+bool tensor_of(PyObject *o, const at::Tensor *&t)
+{
+    t = nullptr;
+    if (o == Py_None) return true;
+    if (!THPVariable_Check(o)) return false;
+    t = &THPVariable_Unpack(o);
+    return true;
+}
+
+// Rows of a tensor [.., length] and the step between them.
+struct RowsOf { int64_t rows, length, step; };
+
+bool rows_of(const at::Tensor &t, RowsOf &r)
+{
+    if (t.dim() == 2 && t.size(1) > 0 && t.stride(1) == 1 && (t.stride(0) >= t.size(1) || t.size(0) <= 1)) {
+        r = RowsOf{t.size(0), t.size(1), std::max(t.stride(0), t.size(1))};
+        return true;
+    }
+    if (t.dim() < 1 || !t.is_contiguous() || t.size(-1) == 0) return false;
+    r = RowsOf{t.numel() / t.size(-1), t.size(-1), t.size(-1)};
+    return true;
+}
+
+bool is_float(const at::Tensor &t) { return t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16; }
+int type_of(at::ScalarType t) { return t == at::kBFloat16 ? 1 : 0; }
+
+// The current device if the tensor is on it, else -1.
+c10::DeviceIndex current_device_of(const at::Tensor &t)
+{
+    if (!t.is_cuda()) return -1;
+    const c10::DeviceIndex here = c10::hip::current_device();
+    return t.device().index() == here ? here : -1;
+}
+
+bool is_here(const at::Tensor &t, c10::DeviceIndex here) { return here >= 0 && t.is_cuda() && t.device().index() == here; }
+
+bool is_vector(const at::Tensor *t, int64_t n, c10::DeviceIndex here)
+{
+    return !t || (t->scalar_type() == at::kFloat && t->numel() == n && t->is_contiguous() && is_here(*t, here));
+}
+
+// 4-bit rows [.., 16 * blocks] with scales [slabs, rows, 8], made in one piece (the scales also as some of the rows of such).
+bool blocks_of(const at::Tensor &q, const at::Tensor &scale, c10::DeviceIndex here, RowsOf &r, int64_t &blocks, int64_t &slab)
+{
+    if (q.scalar_type() != at::kByte || scale.scalar_type() != at::kByte || !is_here(q, here) || !is_here(scale, here) || !rows_of(q, r) || r.length % 16 != 0) return false;
+    blocks = r.length / 16;
+    if (scale.dim() != 3 || scale.size(0) != (blocks + 7) / 8 || scale.size(1) != r.rows || scale.size(2) != 8 || scale.stride(2) != 1 || scale.stride(1) != 8 ||
+        scale.stride(0) < 8 * r.rows)
+        return false;
+    slab = scale.stride(0);
+    return true;
+}
+
+std::vector<int64_t> sizes_with(const at::Tensor &like, int64_t last)
+{
+    std::vector<int64_t> sizes(like.sizes().begin(), like.sizes().end());
+    sizes.back() = last;
+    return sizes;
+}
+
+// Work space for a call on the current stream; false where a capture would keep its address.
+bool lend(int64_t size, const at::Tensor &like, at::Tensor &work)
+{
+    if (size == 0) return true;
+    if (c10::hip::currentStreamCaptureStatusMayInitCtx() != c10::hip::CaptureStatus::None) return false;
+    work = at::empty({size}, like.options().dtype(at::kByte));
+    return true;
+}
+
+#define PCONV_TRY HANDLE_TH_ERRORS const at::NoGradGuard no_grad;
+#define PCONV_LONG_WAY do { if (PyErr_Occurred()) return nullptr; Py_RETURN_NONE; } while (0)
+
+PyObject *quantize_mx4(PyObject *, PyObject *const *args, Py_ssize_t count)
+{
+    PCONV_TRY
+    using Entry = int (*)(const void *, int64_t, int, int64_t, int64_t, uint8_t *, int64_t, uint8_t *, int64_t, void *);
+    Addresses at;
+    const at::Tensor *x;
+    RowsOf r;
+    if (count != 2 || !addresses_of(args[0], at, 1) || !tensor_of(args[1], x) || !x) PCONV_LONG_WAY;
+    if (!is_float(*x) || current_device_of(*x) < 0 || !rows_of(*x, r)) PCONV_LONG_WAY;
+    const int64_t wide = (r.length + 31) / 32 * 16;
+    const auto bytes = x->options().dtype(at::kByte);
+    at::Tensor q = at::empty(sizes_with(*x, wide), bytes), scale = at::empty({(r.length + 255) / 256, r.rows, 8}, bytes);
+    if (reinterpret_cast<Entry>(at[0])(address<void>(*x), r.step, type_of(x->scalar_type()), r.rows, r.length, address<uint8_t>(q), wide, address<uint8_t>(scale), 8 * r.rows,
+                                       stream_of(*x)) != 0)
+        PCONV_LONG_WAY;
+    return Py_BuildValue("(NN)", THPVariable_Wrap(std::move(q)), THPVariable_Wrap(std::move(scale)));
+    END_HANDLE_TH_ERRORS
+}
+
+using ProductEntry = int (*)(const uint8_t *, int64_t, const uint8_t *, int64_t, const uint8_t *, int64_t, const uint8_t *, int64_t, const float *, void *, int64_t, int, int64_t,
+                             int64_t, int64_t, int, void *, int64_t, void *);
+using LayerEntry = int (*)(const void *, int64_t, int, const uint8_t *, int64_t, const uint8_t *, int64_t, const float *, void *, int64_t, int, int64_t, int64_t, int64_t, int, void *,
+                           int64_t, void *);
+using WorkEntry = int64_t (*)(int64_t, int64_t, int64_t);
+
+PyObject *matmul_mx4(PyObject *, PyObject *const *args, Py_ssize_t count)
+{
+    PCONV_TRY
+    Addresses at;
+    const at::Tensor *a, *sa, *b, *sb, *bias;
+    RowsOf ra, rb;
+    int64_t blocks, others, slab_a, slab_b;
+    if (count != 8 || !addresses_of(args[0], at, 2) || !tensor_of(args[1], a) || !tensor_of(args[2], sa) || !tensor_of(args[3], b) || !tensor_of(args[4], sb) ||
+        !tensor_of(args[5], bias) || !a || !sa || !b || !sb)
+        PCONV_LONG_WAY;
+    const int relu = PyObject_IsTrue(args[6]), half = PyObject_IsTrue(args[7]);
+    if (relu < 0 || half < 0) return nullptr;
+    const auto here = current_device_of(*a);
+    if (b->dim() != 2 || !blocks_of(*a, *sa, here, ra, blocks, slab_a) || !blocks_of(*b, *sb, here, rb, others, slab_b) || blocks != others || !is_vector(bias, rb.rows, here)) PCONV_LONG_WAY;
+    const int64_t size = reinterpret_cast<WorkEntry>(at[1])(ra.rows, rb.rows, blocks);
+    at::Tensor work;
+    if (!lend(size, *a, work)) PCONV_LONG_WAY;
+    at::Tensor y = at::empty(sizes_with(*a, rb.rows), a->options().dtype(half ? at::kBFloat16 : at::kFloat));
+    if (reinterpret_cast<ProductEntry>(at[0])(address<uint8_t>(*a), ra.step, address<uint8_t>(*sa), slab_a, address<uint8_t>(*b), rb.step, address<uint8_t>(*sb), slab_b,
+                                              bias ? address<float>(*bias) : nullptr, address<void>(y), rb.rows, half, ra.rows, rb.rows, blocks, relu,
+                                              size ? work.data_ptr() : nullptr, size, stream_of(*a)) != 0)
+        PCONV_LONG_WAY;
+    return THPVariable_Wrap(std::move(y));
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject *linear_mx4(PyObject *, PyObject *const *args, Py_ssize_t count)
+{
+    PCONV_TRY
+    Addresses at;
+    const at::Tensor *x, *w, *sw, *bias;
+    RowsOf rx, rw;
+    int64_t blocks, slab;
+    if (count != 6 || !addresses_of(args[0], at, 2) || !tensor_of(args[1], x) || !tensor_of(args[2], w) || !tensor_of(args[3], sw) || !tensor_of(args[4], bias) || !x || !w || !sw)
+        PCONV_LONG_WAY;
+    const int relu = PyObject_IsTrue(args[5]);
+    if (relu < 0) return nullptr;
+    const auto here = current_device_of(*x);
+    if (!is_float(*x) || !is_here(*x, here) || !rows_of(*x, rx) || w->dim() != 2 || !blocks_of(*w, *sw, here, rw, blocks, slab) || (rx.length + 31) / 32 != blocks ||
+        !is_vector(bias, rw.rows, here))
+        PCONV_LONG_WAY;
+    const int64_t size = reinterpret_cast<WorkEntry>(at[1])(rx.rows, rw.rows, rx.length);
+    at::Tensor work;
+    if (!lend(size, *x, work)) PCONV_LONG_WAY;
+    at::Tensor y = at::empty(sizes_with(*x, rw.rows), x->options());
+    const int type = type_of(x->scalar_type());
+    if (reinterpret_cast<LayerEntry>(at[0])(address<void>(*x), rx.step, type, address<uint8_t>(*w), rw.step, address<uint8_t>(*sw), slab, bias ? address<float>(*bias) : nullptr,
+                                            address<void>(y), rw.rows, type, rx.rows, rw.rows, rx.length, relu, size ? work.data_ptr() : nullptr, size, stream_of(*x)) != 0)
+        PCONV_LONG_WAY;
+    return THPVariable_Wrap(std::move(y));
+    END_HANDLE_TH_ERRORS
+}
+
+PyObject *add_rms_norm_i8(PyObject *, PyObject *const *args, Py_ssize_t count)
+{
+    PCONV_TRY
+    using Entry = int (*)(const void *, int64_t, const void *, int64_t, void *, int64_t, int, const float *, float, int64_t, int64_t, int8_t *, int64_t, float *, void *);
+    Addresses at;
+    const at::Tensor *x, *r, *weight;
+    RowsOf rx, rr{0, 0, 0};
+    if (count != 5 || !addresses_of(args[0], at, 1) || !tensor_of(args[1], x) || !tensor_of(args[2], r) || !tensor_of(args[3], weight) || !x || !PyFloat_Check(args[4])) PCONV_LONG_WAY;
+    const float eps = float(PyFloat_AS_DOUBLE(args[4]));
+    const auto here = current_device_of(*x);
+    if (!is_float(*x) || !is_here(*x, here) || !rows_of(*x, rx) || !is_vector(weight, rx.length, here)) PCONV_LONG_WAY;
+    if (r && (r->scalar_type() != x->scalar_type() || r->sizes() != x->sizes() || !is_here(*r, here) || !rows_of(*r, rr))) PCONV_LONG_WAY;
+    const int64_t wide = (rx.length + 15) / 16 * 16;
+    at::Tensor q = at::empty(sizes_with(*x, wide), x->options().dtype(at::kChar)), scale = at::empty(x->sizes().slice(0, size_t(x->dim() - 1)), x->options().dtype(at::kFloat)), sum;
+    if (r) sum = at::empty(x->sizes(), x->options().memory_format(at::MemoryFormat::Contiguous));
+    if (reinterpret_cast<Entry>(at[0])(address<void>(*x), rx.step, r ? address<void>(*r) : nullptr, rr.step, r ? address<void>(sum) : nullptr, rx.length, type_of(x->scalar_type()),
+                                       weight ? address<float>(*weight) : nullptr, eps, rx.rows, rx.length, address<int8_t>(q), wide, address<float>(scale), stream_of(*x)) != 0)
+        PCONV_LONG_WAY;
+    if (wide != rx.length) q = q.narrow(-1, 0, rx.length);
+    PyObject *const s = r ? THPVariable_Wrap(std::move(sum)) : (Py_INCREF(args[1]), args[1]);
+    return Py_BuildValue("(NNN)", THPVariable_Wrap(std::move(q)), THPVariable_Wrap(std::move(scale)), s);
+    END_HANDLE_TH_ERRORS
+}
+
+#undef PCONV_TRY
+#undef PCONV_LONG_WAY
+
+template <PyObject *(*F)(PyObject *, PyObject *const *, Py_ssize_t)>
+PyMethodDef method(const char *name)
+{
+    return PyMethodDef{name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F)), METH_FASTCALL, nullptr};
+}
+
+PyMethodDef methods[] = {method<distill>("distill"), method<quantize_mx4>("quantize_mx4"), method<matmul_mx4>("matmul_mx4"), method<linear_mx4>("linear_mx4"),
+                         method<add_rms_norm_i8>("add_rms_norm_i8"), method<apart>("apart"), method<places>("places"),
                          {"changed", changed, METH_O, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -481,6 +481,27 @@ def test_written_outputs_count_as_changed():
     assert out._version > before
 
 
+@pytest.mark.gpu
+def test_ordinary_calls_and_the_long_way_give_the_same():
+    """Ordinary calls are made in native code; an output given, a type asked for or a step of its own go the long way."""
+    import torch
+    rng = np.random.default_rng(6)
+    for m, n, k in ((1, 40, 200), (30, 70, 333), (300, 100, 1000)):
+        say(f"[case] both ways {m}x{n}x{k}")
+        (w, s), x, bias = on_card(make_layer4(rng, n, k, 3)), dev(make_x(rng, m, k)), dev(rng.standard_normal(n).astype(np.float32))
+        y = P.linear_mx4(x, w, s, bias, relu=True)
+        assert torch.equal(y, P.linear_mx4(x, w, s, bias, True, out=torch.empty_like(y))) and torch.equal(y, P.linear_mx4(x, w, s, bias, True, torch.float32))
+        q, sq = P.quantize_mx4(x)
+        q3, sq3 = P.quantize_mx4(torch.nn.functional.pad(x, (0, 3))[:, :k].unsqueeze(1).expand(m, 1, k))
+        assert torch.equal(q, q3.view_as(q)) and torch.equal(sq, sq3)
+        assert torch.equal(y, P.matmul_mx4(q, sq, w, s, bias, True)) and torch.equal(y, P.matmul_mx4(q, sq, w, s, bias, True, out=torch.empty_like(y)))
+        wide = torch.zeros(n, w.shape[1] + 32, dtype=torch.uint8, device="cuda")
+        wide[:, :w.shape[1]] = w
+        assert torch.equal(y, P.linear_mx4(x, wide[:, :w.shape[1]], s, bias, relu=True))
+        with pytest.raises(RuntimeError):
+            P.linear_mx4(x, w, s, bias, relu=torch.ones(3))
+
+
 # ---- plans ---------------------------------------------------------------------------------------------------------------
 
 FORMS = {(1, 0, 0, False): (9, 40, 256), (2, 32, 1, False): (129, 11206, 64), (2, 32, 1, True): (1, 9309, 22924), (2, 32, 2, False): (20, 64, 256),
