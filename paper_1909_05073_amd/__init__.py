@@ -1206,11 +1206,14 @@ def _distill_call(student, teacher, classes, temperature, reduction):
 def _distill(student, teacher, classes, temperature, reduction, what):
     """The loss (what: 0), with a node for autograd (1), or the loss and its gradient (2); by csrc/pconv_tensors.cpp."""
     call, entries = _native("distill", "pconv_distill_loss", "pconv_distill_grad", "pconv_distill_loss_grad", "pconv_last_error")
-    index, m, v, n = _distill_call(student, teacher, classes, temperature, reduction)
-    if what == 1 or reduction != "none":                 # (the rows' losses, or what the gradient needs, are no result)
-        _refuse_foreign_capture(student.device)
     try:
-        return call(entries, student, teacher, classes, (m, v, n[11], n[1], n[4], n[7], n[8], n[2], n[5], n[12]), _REDUCTIONS.index(reduction), what)
+        made = call(entries, student, teacher, classes, temperature, reduction, what, None, False)
+        if made is not None:
+            return made
+        index, m, v, n = _distill_call(student, teacher, classes, temperature, reduction)
+        if what == 1 or reduction != "none":
+            _refuse_foreign_capture(student.device)
+        return call(entries, student, teacher, classes, temperature, reduction, what, (m, v, n[11], n[1], n[4], n[7], n[8], n[2], n[5], n[12]), True)
     except RuntimeError as e:
         if str(e).startswith("pconv status -"):
             _check(int(str(e).split()[2].rstrip(":")))

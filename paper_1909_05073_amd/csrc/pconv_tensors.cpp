@@ -12,9 +12,10 @@
 // apart(tensor, tensor or None, ..) -> bool: whether the first shares no byte with the others because the runs of memory from
 // their first elements to their last ones share none.
 //
-// distill(entries, student, teacher, classes, numbers, reduction, what) -> the loss (what: 0), with its node (1), or the loss and its
-// gradient (2); entries: the addresses of pconv_distill_loss, .._grad, .._loss_grad and pconv_last_error; numbers: what these
-// take besides tensors (see DistillCall).  The arguments have been checked.
+// distill(entries, student, teacher, classes, temperature, reduction, what, numbers, allowed) -> the loss (what: 0), with its node
+// (1), or the loss and its gradient (2); entries: the addresses of pconv_distill_loss, .._grad, .._loss_grad and
+// pconv_last_error.  numbers: None, or of arguments that have been checked what these take besides tensors (see DistillCall).
+// allowed: whether a capture may keep memory of the call.  None as below.
 //
 // quantize_mx4, matmul_mx4, linear_mx4, add_rms_norm_i8 (entries, tensors, ..) -> what the binding's functions of these names give, for
 // ordinary calls: tensors on the current device whose rows lie as they are made (rows of one matrix with any step), outputs of
@@ -190,61 +191,6 @@ struct DistillNode : torch::autograd::Node {
         return (*refuse)({grad.requires_grad_()});
     }
 };
-
-PyObject *distill(PyObject *, PyObject *const *args, Py_ssize_t count)
-{
-    HANDLE_TH_ERRORS
-    unsigned long long at[4];
-    DistillCall n;
-    if (count != 7 || !PyArg_ParseTuple(args[0], "KKKK", at, at + 1, at + 2, at + 3) || !THPVariable_Check(args[1]) || !THPVariable_Check(args[2]) || !THPVariable_Check(args[3]) ||
-        !PyArg_ParseTuple(args[4], "LLLLLLLiif", &n.rows, &n.v, &n.top, &n.z_step, &n.t_step, &n.c_step, &n.class_bytes, &n.z_type, &n.t_type, &n.temperature)) {
-        if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "distill: four addresses, three tensors, numbers, a reduction and what to do are wanted");
-        return nullptr;
-    }
-    const long reduction = PyLong_AsLong(args[5]), what = PyLong_AsLong(args[6]);
-    if (PyErr_Occurred()) return nullptr;
-    n.mean = reduction == kMean ? 1 : 0;
-    const DistillEntries e{reinterpret_cast<decltype(DistillEntries::loss)>(at[0]), reinterpret_cast<decltype(DistillEntries::grad)>(at[1]),
-                           reinterpret_cast<decltype(DistillEntries::both)>(at[2]), reinterpret_cast<decltype(DistillEntries::last_error)>(at[3])};
-    const at::Tensor &z = THPVariable_Unpack(args[1]), &t = THPVariable_Unpack(args[2]), &c = THPVariable_Unpack(args[3]);
-    at::Tensor value, grad;
-    {
-        const pybind11::gil_scoped_release no_gil;
-        at::Tensor sums;
-        {
-            const at::NoGradGuard no_grad;
-            const auto numbers = z.options().dtype(at::kFloat);
-            const at::Tensor rows = at::empty({n.rows}, numbers);
-            if (reduction != kNone) value = at::empty({}, numbers);
-            float *const total = reduction != kNone ? address<float>(value) : nullptr;
-            if (what == 2) {
-                grad = at::empty(z.sizes(), z.options().memory_format(at::MemoryFormat::Contiguous));
-                check_status(e, e.both(address<void>(z), n.z_step, n.z_type, address<void>(t), n.t_step, n.t_type, address<void>(c), n.c_step, int(n.class_bytes), n.rows, n.v,
-                                       n.top, n.temperature, n.mean, address<float>(rows), total, address<void>(grad), n.v, stream_of(z)));
-            } else {
-                if (what == 1) sums = at::empty({n.rows}, numbers);
-                check_status(e, e.loss(address<void>(z), n.z_step, n.z_type, address<void>(t), n.t_step, n.t_type, address<void>(c), n.c_step, int(n.class_bytes), n.rows, n.v,
-                                       n.top, n.temperature, n.mean, address<float>(rows), total, what == 1 ? address<float>(sums) : nullptr, stream_of(z)));
-            }
-            if (reduction == kNone) value = rows.view(z.sizes().slice(0, size_t(z.dim() - 1)));
-        }
-        if (what == 1) {
-            const std::shared_ptr<DistillNode> node(new DistillNode(), torch::autograd::deleteNode);
-            node->set_next_edges(torch::autograd::collect_next_edges(z));
-            node->entries = e;
-            node->call = n;
-            node->reduction = Reduction(reduction);
-            node->student = torch::autograd::SavedVariable(z, false);
-            node->teacher = torch::autograd::SavedVariable(t, false);
-            node->classes = torch::autograd::SavedVariable(c, false);
-            node->lse = torch::autograd::SavedVariable(sums, false);
-            torch::autograd::set_history(value, node);
-        }
-    }
-    if (what != 2) return THPVariable_Wrap(std::move(value));
-    return Py_BuildValue("(NN)", THPVariable_Wrap(std::move(value)), THPVariable_Wrap(std::move(grad)));
-    END_HANDLE_TH_ERRORS
-}
 
 // ---- ordinary calls ---------------------------------------------------------------------------------------------------
 
@@ -430,6 +376,87 @@ PyObject *add_rms_norm_i8(PyObject *, PyObject *const *args, Py_ssize_t count)
     if (wide != rx.length) q = q.narrow(-1, 0, rx.length);
     PyObject *const s = r ? THPVariable_Wrap(std::move(sum)) : (Py_INCREF(args[1]), args[1]);
     return Py_BuildValue("(NNN)", THPVariable_Wrap(std::move(q)), THPVariable_Wrap(std::move(scale)), s);
+    END_HANDLE_TH_ERRORS
+}
+
+// The call on ordinary tensors; false for all others.
+bool ordinary(const at::Tensor &z, const at::Tensor &t, const at::Tensor &c, PyObject *temperature, DistillCall &n)
+{
+    const auto here = current_device_of(z);
+    RowsOf rz, rt, rc;
+    if (!PyFloat_Check(temperature) || !is_float(z) || !is_float(t) || (c.scalar_type() != at::kLong && c.scalar_type() != at::kInt) || !is_here(z, here) || !is_here(t, here) ||
+        !is_here(c, here) || t.sizes() != c.sizes() || !rows_of(z, rz) || !rows_of(t, rt) || !rows_of(c, rc) || t.dim() != z.dim() ||
+        t.sizes().slice(0, size_t(t.dim() - 1)) != z.sizes().slice(0, size_t(z.dim() - 1)))
+        return false;
+    n = DistillCall{rz.rows, rz.length, rt.length, rz.step, rt.step, rc.step, int64_t(c.itemsize()), type_of(z.scalar_type()), type_of(t.scalar_type()), 0,
+                    float(PyFloat_AS_DOUBLE(temperature))};
+    return true;
+}
+
+PyObject *distill(PyObject *, PyObject *const *args, Py_ssize_t count)
+{
+    HANDLE_TH_ERRORS
+    Addresses at;
+    DistillCall n;
+    if (count != 9 || !addresses_of(args[0], at, 4) || !PyUnicode_Check(args[5])) PCONV_LONG_WAY;
+    const bool given = args[7] != Py_None;
+    const at::Tensor *student, *teacher, *entries;
+    if (!tensor_of(args[1], student) || !tensor_of(args[2], teacher) || !tensor_of(args[3], entries) || !student || !teacher || !entries) PCONV_LONG_WAY;
+    const at::Tensor &z = *student, &t = *teacher, &c = *entries;
+    if (!given && !ordinary(z, t, c, args[4], n)) PCONV_LONG_WAY;
+    if (given && !PyArg_ParseTuple(args[7], "LLLLLLLiif", &n.rows, &n.v, &n.top, &n.z_step, &n.t_step, &n.c_step, &n.class_bytes, &n.z_type, &n.t_type, &n.temperature)) return nullptr;
+    const bool is_sum = PyUnicode_CompareWithASCIIString(args[5], "sum") == 0, is_mean = PyUnicode_CompareWithASCIIString(args[5], "mean") == 0;
+    if (!is_sum && !is_mean && PyUnicode_CompareWithASCIIString(args[5], "none") != 0) PCONV_LONG_WAY;
+    const Reduction reduction = is_sum ? kSum : is_mean ? kMean : kNone;
+    n.mean = is_mean;
+    const long what = PyLong_AsLong(args[6]);
+    const int allowed = PyObject_IsTrue(args[8]);
+    if (PyErr_Occurred()) return nullptr;
+    const bool captured = c10::hip::currentStreamCaptureStatusMayInitCtx() != c10::hip::CaptureStatus::None;
+    if (captured && !allowed && (what == 1 || reduction != kNone)) PCONV_LONG_WAY;      // (the rows' losses, or what the gradient needs, are no result)
+    if (captured && what == 1) {
+        const auto sink = z.grad_fn() ? nullptr : torch::autograd::impl::try_get_grad_accumulator(z);
+        TORCH_CHECK(!sink || !sink->stream() || *sink->stream() == c10::hip::getCurrentHIPStream(z.device().index()).unwrap(),
+                    "a graph of another stream still holds the student: its gradient cannot be captured here while that lives");
+    }
+    const DistillEntries e{reinterpret_cast<decltype(DistillEntries::loss)>(at[0]), reinterpret_cast<decltype(DistillEntries::grad)>(at[1]),
+                           reinterpret_cast<decltype(DistillEntries::both)>(at[2]), reinterpret_cast<decltype(DistillEntries::last_error)>(at[3])};
+    at::Tensor value, grad;
+    {
+        const pybind11::gil_scoped_release no_gil;
+        at::Tensor sums;
+        {
+            const at::NoGradGuard no_grad;
+            const auto numbers = z.options().dtype(at::kFloat);
+            const at::Tensor rows = at::empty({n.rows}, numbers);
+            if (reduction != kNone) value = at::empty({}, numbers);
+            float *const total = reduction != kNone ? address<float>(value) : nullptr;
+            if (what == 2) {
+                grad = at::empty(z.sizes(), z.options().memory_format(at::MemoryFormat::Contiguous));
+                check_status(e, e.both(address<void>(z), n.z_step, n.z_type, address<void>(t), n.t_step, n.t_type, address<void>(c), n.c_step, int(n.class_bytes), n.rows, n.v,
+                                       n.top, n.temperature, n.mean, address<float>(rows), total, address<void>(grad), n.v, stream_of(z)));
+            } else {
+                if (what == 1) sums = at::empty({n.rows}, numbers);
+                check_status(e, e.loss(address<void>(z), n.z_step, n.z_type, address<void>(t), n.t_step, n.t_type, address<void>(c), n.c_step, int(n.class_bytes), n.rows, n.v,
+                                       n.top, n.temperature, n.mean, address<float>(rows), total, what == 1 ? address<float>(sums) : nullptr, stream_of(z)));
+            }
+            if (reduction == kNone) value = rows.view(z.sizes().slice(0, size_t(z.dim() - 1)));
+        }
+        if (what == 1) {
+            const std::shared_ptr<DistillNode> node(new DistillNode(), torch::autograd::deleteNode);
+            node->set_next_edges(torch::autograd::collect_next_edges(z));
+            node->entries = e;
+            node->call = n;
+            node->reduction = reduction;
+            node->student = torch::autograd::SavedVariable(z, false);
+            node->teacher = torch::autograd::SavedVariable(t, false);
+            node->classes = torch::autograd::SavedVariable(c, false);
+            node->lse = torch::autograd::SavedVariable(sums, false);
+            torch::autograd::set_history(value, node);
+        }
+    }
+    if (what != 2) return THPVariable_Wrap(std::move(value));
+    return Py_BuildValue("(NN)", THPVariable_Wrap(std::move(value)), THPVariable_Wrap(std::move(grad)));
     END_HANDLE_TH_ERRORS
 }
 

@@ -386,6 +386,59 @@ def test_a_capture_that_torch_does_not_know_of_is_refused_where_memory_would_be_
     hip("hipGraphDestroy", graph)
 
 
+@pytest.mark.gpu
+def test_a_capture_while_a_graph_of_another_stream_holds_the_student_is_refused():
+    """The gradient would be added on that graph's stream, which the capture does not know."""
+    import torch
+    say("[case] distill captured while an eager graph lives")
+    z, t, c = (dev(a) for a in make(np.random.default_rng(12), 20, 300, 6))
+    leaf, y = z.clone().requires_grad_(), torch.zeros(8, device="cuda")
+    alive = P.distill_loss(leaf, t, c, 2.0)
+    g = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(g):
+        with pytest.raises(RuntimeError, match="still holds the student"):
+            P.distill_loss(leaf, t, c, 2.0)
+        with torch.no_grad():
+            loss = P.distill_loss(leaf, t, c, 2.0)
+        y.add_(1.0)
+    for i in range(3):
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(loss, alive.detach()) and float(y[0]) == i + 1
+    alive.backward()
+    want = P.distill_loss_grad(z, t, c, 2.0)[1]
+    assert torch.equal(leaf.grad, want)
+    del alive
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        grad, = torch.autograd.grad(P.distill_loss(leaf, t, c, 2.0), leaf)
+    for _ in range(3):
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(grad, want)
+
+
+@pytest.mark.gpu
+def test_ordinary_calls_and_the_long_way_give_the_same():
+    """Ordinary calls are looked at in native code; a temperature that is no float, or rows in more dimensions with a step, go the long way."""
+    import torch
+    rng = np.random.default_rng(13)
+    for rows, v, top in ((1, 5, 1), (12, 333, 9)):
+        z, t, c = (dev(a) for a in make(rng, rows, v, top))
+        wide = torch.nn.functional.pad(z, (0, 7))[:, :v].unsqueeze(1)            # [rows, 1, v], v + 7 apart
+        for reduction in ("none", "sum", "mean"):
+            say(f"[case] both ways {rows}x{v} top={top} {reduction}")
+            loss, grad = P.distill_loss_grad(z, t, c, 2.0, reduction)
+            assert torch.equal(loss, P.distill_loss(z, t, c, 2, reduction)) and torch.equal(loss, P.distill_loss(z, t, c, np.float32(2), reduction))
+            far, slope = P.distill_loss_grad(wide, t.unsqueeze(1), c.unsqueeze(1), 2.0, reduction)
+            assert far.shape == ((rows, 1) if reduction == "none" else ()) and torch.equal(far.view_as(loss), loss) and torch.equal(slope.view_as(grad), grad)
+            for leaf, tt, cc in ((z.clone(), t, c), (wide.clone().expand(rows, 1, v), t.unsqueeze(1), c.unsqueeze(1))):
+                leaf = leaf.requires_grad_()
+                P.distill_loss(leaf, tt, cc, 2, reduction).sum().backward()
+                assert torch.equal(leaf.grad.view_as(grad), grad)
+
+
 # ---- refusals ------------------------------------------------------------------------------------------------------------
 
 def c_calls():
