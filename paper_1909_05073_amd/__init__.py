@@ -729,6 +729,11 @@ def matmul_i8(a, a_scale, b, b_scale, bias=None, relu: bool = False, out_dtype=N
     out: where the result goes; it must not overlap an input (its rows may lie between those of one).  Nothing is recorded for
     autograd."""
     import torch
+    if out is None and (out_dtype is None or out_dtype is torch.float32 or out_dtype is torch.bfloat16):
+        call, entries = _native("matmul_i8", "pconv_matmul_i8", "pconv_matmul_i8_workspace")
+        y = call(entries, a, a_scale, b, b_scale, bias, relu, out_dtype is torch.bfloat16)
+        if y is not None:
+            return y
     if a.dtype != torch.int8 or b.dtype != torch.int8 or b.dim() != 2:
         raise ValueError("a [..., k] and b [n, k] must be int8")
     index = _device_index(a, a_scale, b, b_scale, bias, out)

@@ -17,7 +17,7 @@
 // pconv_last_error.  numbers: None, or of arguments that have been checked what these take besides tensors (see DistillCall).
 // allowed: whether a capture may keep memory of the call.  None as below.
 //
-// quantize_mx4, matmul_mx4, linear_mx4, add_rms_norm_i8 (entries, tensors, ..) -> what the binding's functions of these names give, for
+// quantize_mx4, matmul_mx4, linear_mx4, add_rms_norm_i8, matmul_i8 (entries, tensors, ..) -> what the binding's functions of these names give, for
 // ordinary calls: tensors on the current device whose rows lie as they are made (rows of one matrix with any step), outputs of
 // their own, no capture where work space is lent.  None for all others, wrong ones and failed ones among them: those go the
 // long way, which knows what to say.  In Python a call takes the host 7 to 11 us, here 4 to 5.
@@ -379,6 +379,37 @@ PyObject *add_rms_norm_i8(PyObject *, PyObject *const *args, Py_ssize_t count)
     END_HANDLE_TH_ERRORS
 }
 
+PyObject *matmul_i8(PyObject *, PyObject *const *args, Py_ssize_t count)
+{
+    PCONV_TRY
+    using Entry = int (*)(const int8_t *, int64_t, const float *, const int8_t *, int64_t, const float *, const float *, void *, int64_t, int, int64_t, int64_t, int64_t, int, void *,
+                          int64_t, void *);
+    using Work = int64_t (*)(int64_t, int64_t, int64_t, int);
+    Addresses at;
+    const at::Tensor *a, *sa, *b, *sb, *bias;
+    RowsOf ra, rb;
+    if (count != 8 || !addresses_of(args[0], at, 2) || !tensor_of(args[1], a) || !tensor_of(args[2], sa) || !tensor_of(args[3], b) || !tensor_of(args[4], sb) ||
+        !tensor_of(args[5], bias) || !a || !sa || !b || !sb)
+        PCONV_LONG_WAY;
+    const int relu = PyObject_IsTrue(args[6]), half = PyObject_IsTrue(args[7]);
+    if (relu < 0 || half < 0) return nullptr;
+    const auto here = current_device_of(*a);
+    if (a->scalar_type() != at::kChar || b->scalar_type() != at::kChar || b->dim() != 2 || !is_here(*a, here) || !is_here(*b, here) || !rows_of(*a, ra) || !rows_of(*b, rb) ||
+        ra.length != rb.length || !is_vector(sa, ra.rows, here) || !is_vector(sb, rb.rows, here) || !is_vector(bias, rb.rows, here))
+        PCONV_LONG_WAY;
+    const int8_t *const pa = address<int8_t>(*a), *const pb = address<int8_t>(*b);
+    const uint64_t places = reinterpret_cast<uintptr_t>(pa) | reinterpret_cast<uintptr_t>(pb) | uint64_t(ra.step) | uint64_t(rb.step);
+    const int64_t size = reinterpret_cast<Work>(at[1])(ra.rows, rb.rows, ra.length, places % 16 == 0);
+    at::Tensor work;
+    if (!lend(size, *a, work)) PCONV_LONG_WAY;
+    at::Tensor y = at::empty(sizes_with(*a, rb.rows), a->options().dtype(half ? at::kBFloat16 : at::kFloat));
+    if (reinterpret_cast<Entry>(at[0])(pa, ra.step, address<float>(*sa), pb, rb.step, address<float>(*sb), bias ? address<float>(*bias) : nullptr, address<void>(y), rb.rows, half, ra.rows,
+                                       rb.rows, ra.length, relu, size ? work.data_ptr() : nullptr, size, stream_of(*a)) != 0)
+        PCONV_LONG_WAY;
+    return THPVariable_Wrap(std::move(y));
+    END_HANDLE_TH_ERRORS
+}
+
 // The call on ordinary tensors; false for all others.
 bool ordinary(const at::Tensor &z, const at::Tensor &t, const at::Tensor &c, PyObject *temperature, DistillCall &n)
 {
@@ -470,6 +501,7 @@ PyMethodDef method(const char *name)
 }
 
 PyMethodDef methods[] = {method<distill>("distill"), method<quantize_mx4>("quantize_mx4"), method<matmul_mx4>("matmul_mx4"), method<linear_mx4>("linear_mx4"),
+                         method<matmul_i8>("matmul_i8"),
                          method<add_rms_norm_i8>("add_rms_norm_i8"), method<apart>("apart"), method<places>("places"),
                          {"changed", changed, METH_O, nullptr},
                          {nullptr, nullptr, 0, nullptr}};

@@ -170,6 +170,26 @@ def test_the_layer_that_reads_it():
 
 
 @pytest.mark.gpu
+def test_ordinary_calls_and_the_long_way_give_the_same():
+    """Ordinary calls are looked at in native code; an output given, or rows in more dimensions with a step, go the long way: of the
+    norm and of the layer that reads it."""
+    import torch
+    rng = np.random.default_rng(21)
+    for m, k, n in ((1, 96, 40), (37, 333, 70), (300, 1000, 130)):
+        say(f"[case] both ways {m}x{k} -> {n}")
+        x, r, w = (dev(rng.standard_normal(size).astype(np.float32)) for size in ((m, k), (m, k), k))
+        b, sb = P.quantize_rows(dev(rng.standard_normal((n, k)).astype(np.float32)))
+        apart = torch.nn.functional.pad(x, (0, 5))[:, :k].unsqueeze(1).expand(m, 1, k)
+        q, scale, s = P.add_rms_norm_i8(x, r, w)
+        for q2, scale2, s2 in (P.add_rms_norm_i8(x, r, w, out=torch.empty_like(x)), P.add_rms_norm_i8(apart, r.unsqueeze(1), w), P.add_rms_norm_i8(x, r, w, eps=np.float32(1e-6))):
+            assert torch.equal(q2.reshape(m, k), q) and torch.equal(scale2.flatten(), scale) and torch.equal(s2.view_as(s), s)
+        for half in (None, torch.float32, torch.bfloat16):
+            y = P.matmul_i8(q, scale, b, sb, w[:n] if n <= k else None, True, half)
+            assert torch.equal(y, P.matmul_i8(q, scale, b, sb, w[:n] if n <= k else None, True, out=torch.empty_like(y)))
+            assert torch.equal(y, P.matmul_i8(q, scale.unsqueeze(1), b, sb, w[:n] if n <= k else None, True, half))
+
+
+@pytest.mark.gpu
 def test_sizes_of_zero():
     import torch
     say("[case] add_rms_norm_i8, sizes of zero")
