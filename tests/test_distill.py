@@ -144,6 +144,18 @@ def test_lists_of_unequal_length_and_classes_named_twice(rows, v, top, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("top", [63, 64, 65, 127, 128, 129, 255, 256, 257, 511, 512, 513])
+@pytest.mark.parametrize("v", [600, 9001, 21000])
+def test_lists_longer_than_the_threads_of_a_row(v, top):
+    """A wave, 256 or 512 threads share a row; a thread asks for its first entry, or first two, before the others."""
+    say(f"[case] distill long lists 3x{v} top {top}")
+    rng = np.random.default_rng(v + top)
+    z, t, c = make(rng, 3, v, top, ragged=True, twice=True)
+    c[0, [0, top - 1]] = c[0, top // 2] = 5              # one class first, in the middle and last
+    run_all(z, t, c, 2.0, "f32", "f32")
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("v", [50, 5000, 40000])
 def test_masked_classes_and_logits_of_minus_infinity(v):
     """Classes that the student may not take, teacher's logits that are none, rows of nothing else."""
