@@ -286,7 +286,8 @@ int pconv_add_rms_norm_i8(const void *x_dev, int64_t x_stride, const void *resid
  * call to the next.  Outputs must not overlap inputs.  A call whose size needs more than 2^32 threads gives PCONV_UNSUPPORTED.
  *
  * pconv_quantize_mx4 - q and scale of x [rows][cols], fp32 or bf16; weights by the same call, one row for each output channel.
- * q_stride and slab_stride in bytes; cols up to 2^24. */
+ * q_stride and slab_stride in bytes; cols up to 2^24.  Long rows are read fastest where they lie a multiple of 128 bytes apart
+ * (1908x10592 -> 2440: 52 us, and 41). */
 int pconv_quantize_mx4(const void *x_dev, int64_t x_stride, pconv_dtype x_dtype, int64_t rows, int64_t cols,
                        uint8_t *q_dev, int64_t q_stride, uint8_t *scale_dev, int64_t slab_stride, void *hip_stream);
 

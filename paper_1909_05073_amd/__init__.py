@@ -581,6 +581,11 @@ def _per_channel(t, n, what):
     return t.data_ptr() or None
 
 
+def _quantized_step(size: int) -> int:
+    """Bytes from row to row of quantised rows: long ones begin where lines of the caches do."""
+    return size if size < 1024 else (size + 127) // 128 * 128
+
+
 def _empty(lead, m, n, dtype, like):
     """A new tensor [..., n] of m rows.  (For [m, n] by sizes and steps: 0.5 us less than by its shape.)"""
     import torch
@@ -712,7 +717,7 @@ def quantize_rows(x):
     index = _device_index(x)
     m, k, step = _rows(x, "x")
     lead = x.shape[:-1]
-    wide = (k + 15) // 16 * 16
+    wide = _quantized_step((k + 15) // 16 * 16)
     q = _empty(lead, m, wide, torch.int8, x)
     scale = torch.empty_strided((m,), (1,), dtype=torch.float32, device=x.device) if len(lead) == 1 else x.new_empty(lead, dtype=torch.float32)
     rc = (_lib or lib()).pconv_quantize_rows(x.data_ptr() or None, step, dtype, m, k, q.data_ptr() or None, wide,
@@ -811,7 +816,7 @@ def add_rms_norm_i8(x, residual=None, weight=None, eps: float = 1e-6, out=None):
     s = x + residual [..., k], of x's type (x itself without a residual), and q * scale[..., None] is about
     s / sqrt(mean(s^2) + eps) * weight, the norm taken of the sums before they are rounded.
 
-    The rows of q lie a multiple of 16 bytes apart, as matmul_i8 reads them fastest.  out: where s goes; x or residual, or a
+    The rows of q lie a multiple of 16 bytes apart, of 128 where they are 1024 and more, as matmul_i8 reads them fastest.  out: where s goes; x or residual, or a
     tensor that overlaps neither nor weight.  Nothing is recorded for autograd."""
     if out is None:
         call, entries = _native("add_rms_norm_i8", "pconv_add_rms_norm_i8")
@@ -839,7 +844,7 @@ def add_rms_norm_i8(x, residual=None, weight=None, eps: float = 1e-6, out=None):
         to = (s_ptr, s_step if m > 1 else 0)
         others = [t for t in ((x, m, k, step), (residual, m, k, r_step)) if (t[0].data_ptr() or None, t[3] if m > 1 else 0) != to]
         _refuse_overlap((s, m, k, s_step), *others, (weight, 1, k, k))
-    wide = (k + 15) // 16 * 16
+    wide = _quantized_step((k + 15) // 16 * 16)
     q = _empty(lead, m, wide, torch.int8, x)
     scale = torch.empty_strided((m,), (1,), dtype=torch.float32, device=x.device) if len(lead) == 1 else x.new_empty(lead, dtype=torch.float32)
     rc = (_lib or lib()).pconv_add_rms_norm_i8(x.data_ptr() or None, step, r_ptr, r_step, s_ptr, s_step, dtype, w_ptr, eps, m, k,
@@ -922,7 +927,8 @@ def _blocks(q, scale, rows_first, what):
 
 def quantize_mx4(x):
     """x: CUDA tensor [..., k], fp32 or bf16.  Returns (q [..., 16 * blocks] uint8, scale [slabs, rows, 8] uint8), 32 values of k a block and
-    8 blocks a slab; see include/pconv.h.  rows: of all leading dimensions together.  Nothing is recorded for autograd."""
+    8 blocks a slab; see include/pconv.h.  Rows of 1024 bytes and more lie a multiple of 128 bytes apart, as the products read them
+    fastest.  rows: of all leading dimensions together.  Nothing is recorded for autograd."""
     call, entries = _native("quantize_mx4", "pconv_quantize_mx4")
     made = call(entries, x)
     if made is not None:
@@ -932,13 +938,14 @@ def quantize_mx4(x):
     index = _device_index(x)
     m, k, step = _rows(x, "x")
     wide = (k + 31) // 32 * 16
-    q = _empty(x.shape[:-1], m, wide, torch.uint8, x)
+    apart = _quantized_step(wide)
+    q = _empty(x.shape[:-1], m, apart, torch.uint8, x)
     scale = torch.empty_strided(((k + 255) // 256, m, 8), (8 * m or 1, 8, 1), dtype=torch.uint8, device=x.device)
-    rc = (_lib or lib()).pconv_quantize_mx4(x.data_ptr() or None, step, dtype, m, k, q.data_ptr() or None, wide,
+    rc = (_lib or lib()).pconv_quantize_mx4(x.data_ptr() or None, step, dtype, m, k, q.data_ptr() or None, apart,
                                             scale.data_ptr() or None, 8 * m, _stream(index))
     if rc != OK:
         _check(rc)
-    return q, scale
+    return (q if apart == wide else q[..., :wide]), scale
 
 
 def matmul_mx4(a, a_scale, b, b_scale, bias=None, relu: bool = False, out_dtype=None, out=None):

@@ -223,10 +223,18 @@ bool rows_of(const at::Tensor &t, RowsOf &r)
         r = RowsOf{t.size(0), t.size(1), std::max(t.stride(0), t.size(1))};
         return true;
     }
-    if (t.dim() < 1 || !t.is_contiguous() || t.size(-1) == 0) return false;
-    r = RowsOf{t.numel() / t.size(-1), t.size(-1), t.size(-1)};
+    if (t.dim() < 1 || t.size(-1) == 0) return false;
+    if (!t.is_contiguous()) {                            // (rows in more dimensions, one step apart throughout)
+        if (t.dim() < 3 || t.numel() == 0 || t.stride(-1) != 1 || t.stride(-2) < t.size(-1)) return false;
+        for (int64_t d = t.dim() - 3; d >= 0; --d)
+            if (t.stride(d) != t.stride(d + 1) * t.size(d + 1)) return false;
+    }
+    r = RowsOf{t.numel() / t.size(-1), t.size(-1), t.is_contiguous() ? t.size(-1) : t.stride(-2)};
     return true;
 }
+
+// Bytes from row to row of quantised rows: long ones begin where lines of the caches do.
+int64_t step_of(int64_t bytes) { return bytes < 1024 ? bytes : (bytes + 127) / 128 * 128; }
 
 bool is_float(const at::Tensor &t) { return t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16; }
 int type_of(at::ScalarType t) { return t == at::kBFloat16 ? 1 : 0; }
@@ -288,10 +296,12 @@ PyObject *quantize_mx4(PyObject *, PyObject *const *args, Py_ssize_t count)
     if (!is_float(*x) || current_device_of(*x) < 0 || !rows_of(*x, r)) PCONV_LONG_WAY;
     const int64_t wide = (r.length + 31) / 32 * 16;
     const auto bytes = x->options().dtype(at::kByte);
-    at::Tensor q = at::empty(sizes_with(*x, wide), bytes), scale = at::empty({(r.length + 255) / 256, r.rows, 8}, bytes);
-    if (reinterpret_cast<Entry>(at[0])(address<void>(*x), r.step, type_of(x->scalar_type()), r.rows, r.length, address<uint8_t>(q), wide, address<uint8_t>(scale), 8 * r.rows,
+    const int64_t step = step_of(wide);
+    at::Tensor q = at::empty(sizes_with(*x, step), bytes), scale = at::empty({(r.length + 255) / 256, r.rows, 8}, bytes);
+    if (reinterpret_cast<Entry>(at[0])(address<void>(*x), r.step, type_of(x->scalar_type()), r.rows, r.length, address<uint8_t>(q), step, address<uint8_t>(scale), 8 * r.rows,
                                        stream_of(*x)) != 0)
         PCONV_LONG_WAY;
+    if (step != wide) q = q.narrow(-1, 0, wide);
     return Py_BuildValue("(NN)", THPVariable_Wrap(std::move(q)), THPVariable_Wrap(std::move(scale)));
     END_HANDLE_TH_ERRORS
 }
@@ -367,7 +377,7 @@ PyObject *add_rms_norm_i8(PyObject *, PyObject *const *args, Py_ssize_t count)
     const auto here = current_device_of(*x);
     if (!is_float(*x) || !is_here(*x, here) || !rows_of(*x, rx) || !is_vector(weight, rx.length, here)) PCONV_LONG_WAY;
     if (r && (r->scalar_type() != x->scalar_type() || r->sizes() != x->sizes() || !is_here(*r, here) || !rows_of(*r, rr))) PCONV_LONG_WAY;
-    const int64_t wide = (rx.length + 15) / 16 * 16;
+    const int64_t wide = step_of((rx.length + 15) / 16 * 16);
     at::Tensor q = at::empty(sizes_with(*x, wide), x->options().dtype(at::kChar)), scale = at::empty(x->sizes().slice(0, size_t(x->dim() - 1)), x->options().dtype(at::kFloat)), sum;
     if (r) sum = at::empty(x->sizes(), x->options().memory_format(at::MemoryFormat::Contiguous));
     if (reinterpret_cast<Entry>(at[0])(address<void>(*x), rx.step, r ? address<void>(*r) : nullptr, rr.step, r ? address<void>(sum) : nullptr, rx.length, type_of(x->scalar_type()),
