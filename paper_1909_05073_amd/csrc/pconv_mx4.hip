@@ -585,20 +585,21 @@ constexpr int64_t kUnits = 256;                          // compute units
 int64_t tiles_of(const Cut &c, int64_t m, int64_t n) { return ((m + kTileM[c.tile] - 1) / kTileM[c.tile]) * ((n + kTileN[c.tile] - 1) / kTileN[c.tile]); }
 
 // The cheapest by a count of cycles: a compute unit takes its tiles one after the other, each with a start and an end that two
-// of the smaller ones on it share, a stage of a tile at the rate of the matrix units (half of their peak) or of what 40 bytes
-// a cycle bring from the level-2 cache, whichever is slower.  Joining the parts of k is one more launch and reads and writes
-// the sums.  Of 19 products of 20 to 100352 rows the choice takes at most 1.1 times the best of all tiles and parts.
+// of the smaller ones on it share, and the stages of its part of k.  Joining the parts is one more launch and reads and writes the
+// sums.  The constants are those that choose best for 460 products of 17 to 20000 rows, 8 to 4096 channels and lengths up to
+// 25088 that were timed with every tile and split: the choice takes 1.008 times the best of them on average and at most 1.16 times
+// (stages by the rates of the matrix units and the level-2 cache, and one start for all tiles: 1.06 and 1.57).
 Cut cut_of(int64_t m, int64_t n, int64_t blocks)
 {
-    constexpr int64_t stage_cycles[kTiles] = {512, 614, 1100, 4096}, start = 4000, join = 9000;
+    constexpr int64_t stage[kTiles] = {600, 800, 1000, 3400}, start[kTiles] = {1900, 2900, 5500, 9600}, join = 3000;
     const int64_t stages = (blocks + 7) / 8;
     Cut best{0, 1};
     double least = 0;
     for (int t = 0; t < kTiles; ++t)
-        for (int64_t s = 1; s == 1 || (s <= 32 && s * 4 <= stages); s *= 2) {
+        for (int64_t s = 1; s == 1 || (s <= 32 && s * 2 <= stages); s *= 2) {
             const int64_t rounds = (tiles_of(Cut{t, int(s)}, m, n) * s + kUnits - 1) / kUnits;
-            double c = double(rounds) * double((stages + s - 1) / s) * double(stage_cycles[t]) + double(t < 3 ? (rounds + 1) / 2 : rounds) * start;
-            if (s > 1) c += join + double(s) * double(m) * double(n) * 8 / 2000;
+            double c = double(rounds) * double((stages + s - 1) / s) * double(stage[t]) + double(t < 3 ? (rounds + 1) / 2 : rounds) * double(start[t]);
+            if (s > 1) c += double(join) + double(s) * double(m) * double(n) * 8 / 1700;
             if ((t == 0 && s == 1) || c < least || (c == least && s == 1)) { least = c; best = Cut{t, int(s)}; }
         }
     return best;

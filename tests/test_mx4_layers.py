@@ -505,9 +505,10 @@ def test_ordinary_calls_and_the_long_way_give_the_same():
 # ---- plans ---------------------------------------------------------------------------------------------------------------
 
 FORMS = {(1, 0, 0, False): (9, 40, 256), (2, 32, 1, False): (129, 11206, 64), (2, 32, 1, True): (1, 9309, 22924), (2, 32, 2, False): (20, 64, 256),
-         (2, 32, 2, True): (7, 33, 10096), (2, 64, 1, False): (145, 18962, 40), (2, 64, 1, True): (17908, 15, 19019), (2, 64, 2, False): (8816, 20, 64),
-         (2, 64, 2, True): (613, 20, 17291), (2, 128, 1, False): (34014, 20, 64), (2, 128, 1, True): (4750, 1, 19083),
-         (2, 128, 2, False): (16767, 20, 64), (2, 128, 2, True): (4750, 20, 19083), (2, 256, 1, False): (22236, 276, 64)}
+         (2, 32, 2, True): (7, 33, 10096), (2, 64, 1, False): (145, 18962, 40), (2, 64, 1, True): (33, 9394, 32445), (2, 64, 2, False): (8395, 9, 562),
+         (2, 64, 2, True): (2105, 20, 9403), (2, 128, 1, False): (34014, 20, 64), (2, 128, 1, True): (17908, 15, 19019),
+         (2, 128, 2, False): (17004, 2, 1026), (2, 128, 2, True): (4750, 20, 19083), (2, 256, 1, False): (41430, 130, 64),
+         (2, 256, 1, True): (773, 1782, 152295)}
 
 
 def form_of(m, n, k):
