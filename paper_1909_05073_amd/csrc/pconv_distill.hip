@@ -128,7 +128,8 @@ __device__ __forceinline__ void join_vectors(Running &r, Vec<T> (&v)[U], float i
 
 // LOSS: the loss and lse of each row; GRAD: its gradient, from lse where LOSS is false.  TPR threads share a row, which they
 // read U vectors of 16 bytes a thread at a time; where both are computed the first U of each stay in registers from the
-// sums to the gradient, and what lies beyond is read twice.  The entries' shares and classes lie in LDS.  The gradient is written as if there were no entries; behind a barrier the first
+// sums to the gradient, and what lies beyond is read twice.  Bound by memory where rows are long and many: both of 4096x32768 bf16
+// 116 us, 4.6 TB/s.  The entries' shares and classes lie in LDS.  The gradient is written as if there were no entries; behind a barrier the first
 // entry that names a class writes it again with the shares of all that name it taken off.
 template <typename T, int TPR, int U, bool LOSS, bool GRAD>
 __global__ void __launch_bounds__(TPR == 64 ? 256 : TPR)
@@ -305,15 +306,17 @@ void launch_rows(const DistillRows &p, hipStream_t st)
                            dim3(RPW * TPR), RPW * lds, st, p);                                                                 \
     } while (0)
     // The loss has the same bits with and without its gradient: the same threads a row for both.  More threads a row meet more
-    // often than what they do in between is worth (8192x4000 bf16 47.2 us by 256, 40.5 by 64; 1999x10007 fp32 45.3 by 512, 41.7 by
-    // 256; 4096x32768 bf16 183 by 1024, 129 by 512), fewer read more of a row twice (136 by 256).
+    // often than what they do in between is worth (8192x4000 bf16 38.4 us by 256, 34.7 by 64; 1999x10007 fp32 through autograd 59.8
+    // by 512, 54.2 by 256; 4096x32768 bf16 171 by 1024, 116 by 512; 4x41829 16.2 by 1024, 14.6), fewer read more of a row
+    // twice (4096x32768 133 by 256).  Eight vectors a thread keep longer rows, but take as long where the last are missing
+    // (4096 vectors a row 125 us by four, 116 by eight; 3750 of them 106.1 by four, 107.5 by eight).
     if constexpr (LOSS) {
         if (vecs <= 64 * 2) PCONV_LAUNCH(64, 2);
         else if (vecs <= 64 * 4) PCONV_LAUNCH(64, 4);
         else if (vecs <= 64 * 8) PCONV_LAUNCH(64, 8);
         else if (vecs <= 256 * 4) PCONV_LAUNCH(256, 4);
         else if (vecs <= 256 * 10) PCONV_LAUNCH(256, 8);
-        else if (vecs <= 512 * 8) PCONV_LAUNCH(512, 4);
+        else if (vecs <= 512 * 15 / 2) PCONV_LAUNCH(512, 4);
         else PCONV_LAUNCH(512, 8);
     } else {
         if (vecs <= 64 * 8) PCONV_LAUNCH(64, 4);

@@ -1,6 +1,6 @@
 // What the binding asks of many of torch's tensors at once; in Python each question takes 0.05 us a tensor, here
 // 0.01.  And the node that the distillation's loss leaves in autograd's graph: as a Python function a step of it takes the host
-// 96 us, most of it in handing the interpreter to autograd's thread and back.
+// 96 us, most of it in handing the interpreter to autograd's thread and back, here 50.
 //
 // places(list, ..) -> bytes: where the tensors of the lists lie, and as what: for each its address, type, number of
 // dimensions, sizes and steps, as words of 64 bits, so that two calls give equal bytes exactly if nothing of that has
