@@ -1,4 +1,4 @@
-"""Build in-tree the HIP library, paper_1909_05073_amd/libpconv.so (gfx950 only), and the binding's look at torch's tensors,
+"""Build in-tree the HIP library, paper_1909_05073_amd/libpconv.so (gfx950 only), and the binding's native part against torch's headers,
 _tensors.so (host code)."""
 import importlib.util
 import os
