@@ -190,6 +190,20 @@ def test_ordinary_calls_and_the_long_way_give_the_same():
 
 
 @pytest.mark.gpu
+def test_steps_of_the_quantised_rows():
+    """A multiple of 16 bytes, and of 128 from 1024 on."""
+    import torch
+    for k, step in ((40, 48), (1008, 1008), (1009, 1024), (1024, 1024), (1025, 1152)):
+        say(f"[case] steps of rows of {k}")
+        x, r, w = (dev(a) for a in make(np.random.default_rng(k), 6, k))
+        q, scale, s = P.add_rms_norm_i8(x.view(2, 3, k), r.view(2, 3, k), w)
+        assert q.shape == (2, 3, k) and q.stride() == (3 * step, step, 1)
+        check_norm((q, scale, s), x.cpu().numpy(), r.cpu().numpy(), w.cpu().numpy(), np.float32(1e-6), "f32")
+        q2, scale2, _ = P.add_rms_norm_i8(x.view(2, 3, k), r.view(2, 3, k), w, out=torch.empty_like(s))
+        assert q2.stride() == q.stride() and torch.equal(q, q2) and torch.equal(scale, scale2)
+
+
+@pytest.mark.gpu
 def test_sizes_of_zero():
     import torch
     say("[case] add_rms_norm_i8, sizes of zero")

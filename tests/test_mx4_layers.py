@@ -502,6 +502,26 @@ def test_ordinary_calls_and_the_long_way_give_the_same():
             P.linear_mx4(x, w, s, bias, relu=torch.ones(3))
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("lead", [(7,), (3, 5), (2, 1, 20)])
+def test_long_rows_lie_a_multiple_of_128_bytes_apart(lead):
+    """1008 bytes of values end where the next row begins; of 1024 and more there may be room between."""
+    import torch
+    rng = np.random.default_rng(len(lead))
+    for k in (2016, 2048, 2049, 2100):
+        say(f"[case] steps of rows {lead} {k}")
+        blocks, rows = -(-k // 32), int(np.prod(lead))
+        x = make_x(rng, rows, k)
+        q, s = P.quantize_mx4(dev(x).view(*lead, k))
+        wide = 16 * blocks
+        assert q.shape == (*lead, wide) and q.stride(-2) == (wide if wide < 1024 else -(-wide // 128) * 128)
+        want = P.quantize_mx4(torch.nn.functional.pad(dev(x), (0, 1))[:, :k])
+        assert torch.equal(q.reshape(rows, wide), want[0]) and torch.equal(s, want[1])
+        (w, ws), y = on_card(make_layer4(rng, 40, k, 3)), torch.empty(*lead, 40, device="cuda")
+        assert torch.equal(P.matmul_mx4(q, s, w, ws), P.matmul_mx4(q.contiguous(), s, w.contiguous(), ws, out=y))
+        assert torch.equal(y, P.linear_mx4(dev(x).view(*lead, k), w, ws))
+
+
 # ---- plans ---------------------------------------------------------------------------------------------------------------
 
 FORMS = {(1, 0, 0, False): (9, 40, 256), (2, 32, 1, False): (129, 11206, 64), (2, 32, 1, True): (1, 9309, 22924), (2, 32, 2, False): (20, 64, 256),
