@@ -1,5 +1,6 @@
 """Build in-tree the HIP library, paper_1909_05073_amd/libpconv.so (gfx950 only), and the binding's native part against torch's headers,
 _tensors.so (host code)."""
+import concurrent.futures
 import importlib.util
 import os
 import subprocess
@@ -58,15 +59,13 @@ def build_tensors(verbose: bool = False) -> str:
 def build(verbose: bool = False) -> str:
     build_tensors(verbose)
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
-    objs = []
     gen_dir = os.path.join(HERE, "_build", "gen")
     os.makedirs(gen_dir, exist_ok=True)
     # the record loop of the tiled kernel is generated assembly text
     subprocess.run([sys.executable, os.path.join(CSRC, "gen_tiled_compute.py"),
                     os.path.join(gen_dir, "pconv_tiled_compute.inc")], check=True)
-    for src in sources():
+    def compile_one(src):
         obj = os.path.join(HERE, "_build", os.path.basename(src) + ".o")
-        os.makedirs(os.path.dirname(obj), exist_ok=True)
         cmd = [hipcc, *HIP_FLAGS, *EXTRA_FLAGS.get(os.path.basename(src), []),
                "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-I", gen_dir, "-c"]
         if src.endswith(".cpp"):
@@ -75,7 +74,11 @@ def build(verbose: bool = False) -> str:
         if verbose:
             print(" ".join(cmd))
         _run(cmd)
-        objs.append(obj)
+        return obj
+
+    # a few at once: one after the other they take six minutes
+    with concurrent.futures.ThreadPoolExecutor(min(4, os.cpu_count() or 1)) as pool:
+        objs = list(pool.map(compile_one, sources()))
     cmd = [hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs]
     if verbose:
         print(" ".join(cmd))
