@@ -522,6 +522,24 @@ def test_long_rows_lie_a_multiple_of_128_bytes_apart(lead):
         assert torch.equal(y, P.linear_mx4(dev(x).view(*lead, k), w, ws))
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("m,n,k", [(70, 290, 200), (300, 401, 70), (1100, 515, 600), (3000, 1101, 64), (9000, 1299, 96)])
+def test_bf16_outputs_that_begin_within_a_word(m, n, k):
+    """Rows an odd number of elements apart, and all of them at odd places: the same sums as in fp32, rounded, and nothing beside them."""
+    import torch
+    rng = np.random.default_rng(n)
+    (w, ws), x, bias = on_card(make_layer4(rng, n, k, 3)), dev(make_x(rng, m, k)), dev(rng.standard_normal(n).astype(np.float32))
+    q, s = P.quantize_mx4(x)
+    want = P.matmul_mx4(q, s, w, ws, bias, True).bfloat16()
+    for step, first in ((n | 1, 0), ((n | 1) + 1, 1), (n + 7 | 1, 1), (n + 8, 2)):
+        say(f"[case] bf16 rows {m}x{n}x{k} {step} apart from {first} on")
+        room = torch.full((m * step + 64,), 7.0, dtype=torch.bfloat16, device="cuda")
+        out = room[first:first + m * step].view(m, step)[:, :n]
+        assert P.matmul_mx4(q, s, w, ws, bias, True, out=out) is out and torch.equal(out, want)
+        out.fill_(7.0)
+        assert bool((room == 7.0).all())
+
+
 # ---- plans ---------------------------------------------------------------------------------------------------------------
 
 FORMS = {(1, 0, 0, False): (9, 40, 256), (2, 32, 1, False): (129, 11206, 64), (2, 32, 1, True): (1, 9309, 22924), (2, 32, 2, False): (20, 64, 256),
