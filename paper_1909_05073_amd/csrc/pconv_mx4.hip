@@ -91,9 +91,11 @@ __device__ __forceinline__ Eight<T> load_eight(const T *row, int64_t at, int64_t
     if (__builtin_expect(at + 8 <= cols, 1)) {
         __builtin_memcpy(&e.v, row + at, 8 * sizeof(T));
     } else {
-        T all[8];
+        T all[8] = {};
+        if (__builtin_expect(at < cols, 0)) {            // (a row's last eight values)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) all[i] = at + i < cols ? row[at + i] : T(0.0f);
+            for (int i = 0; i < 8; ++i) all[i] = at + i < cols ? row[at + i] : T(0.0f);
+        }
         __builtin_memcpy(&e.v, all, 8 * sizeof(T));
     }
     return e;
@@ -464,17 +466,15 @@ matmul_mx4_join_kernel(const Mx4Product p, int splits, const float *__restrict__
     }
 }
 
-// Few rows (up to 16): 16 channels a workgroup, whose waves share k and add their sums in LDS.  Reading the weights is all
+// Few rows (up to 32, RG groups of 16): 16 channels a workgroup, whose waves share k and add their sums in LDS.  Reading the weights is all
 // of it; they come in turns of 16 blocks, in a ring of D turns in LDS that is the wave's own, past the registers, and no
 // barrier stands in the loop.  The waves take whole turns in rounds, and what is left behind the last whole round is dealt
 // out among all of them: a turn of one wave alone at the end takes a whole latency of memory (25088 -> 8192: 25.5 us with
 // one turn left over, 21.5 without).  Workgroups begin with different rounds, so that rows that lie a power of two apart
 // are not all read in the same places at one time (32768 -> 4096: 19.5 us if they are, 17.0).  1x25088 -> 4096 fp32 takes 11.7 us,
-// 4.7 TB/s.  The rows of activations, kFewBytes of them
-// at most, lie in LDS for all waves: they come as floats, and every workgroup quantises all of them while its first weights
-// are on their way (less than a launch for it takes), or as blocks (T is uint8_t).
-constexpr int kFewRows = 16, kTurn = 16;                 // (blocks)
-constexpr int64_t kFewBytes = 32768;
+// 4.7 TB/s.  The rows of activations lie in LDS for all waves: they come as floats, and every workgroup quantises all of them
+// while its first weights are on their way, or as blocks (T is uint8_t).
+constexpr int kFewRows = 32, kTurn = 16;                 // (blocks)
 constexpr size_t kFewRing = 8 * (16 * 256 + 256);        // bytes of one turn of all waves
 
 // Rows in LDS: values, and behind all of them the scales; behind each row room for what a wave's last turn reads for nothing.
@@ -494,7 +494,7 @@ __host__ __device__ __forceinline__ FewRows few_rows(int m, int blocks)
     return f;
 }
 
-template <typename T, int D>
+template <typename T, int D, int RG>
 __global__ void __launch_bounds__(512)
 linear_mx4_rows_kernel(const Mx4Product p, const T *__restrict__ x, int64_t ldx, int k)
 {
@@ -585,43 +585,56 @@ linear_mx4_rows_kernel(const Mx4Product p, const T *__restrict__ x, int64_t ldx,
 #pragma unroll
     for (int t = AHEAD; t < D; ++t) issue(t);
     __syncthreads();
-    const uint8_t *const row_a = a + min(r, p.m - 1) * few.pitch + g * 64, *const row_s = a + few.scales + min(r, p.m - 1) * few.scale_pitch + g * 4;
-    f4 acc[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    const uint8_t *row_a[RG], *row_s[RG];
+#pragma unroll
+    for (int i = 0; i < RG; ++i) {
+        row_a[i] = a + min(i * 16 + r, p.m - 1) * few.pitch + g * 64;
+        row_s[i] = a + few.scales + min(i * 16 + r, p.m - 1) * few.scale_pitch + g * 4;
+    }
+    f4 acc[RG][2];
+#pragma unroll
+    for (int i = 0; i < RG; ++i) acc[i][0] = acc[i][1] = f4{0, 0, 0, 0};
 #pragma unroll 1
     for (int t = 0; t < mine; ++t) {
         wait_for_loads<D - 1, 5>(min(D - 1, mine - 1 - t));
         const v4i *const st = ring[wave] + (t % D) * (TURN_BYTES / 16);
         const int first = first_of(t);
-        v4i va[4], vb[4];
-        int sa, sb = reinterpret_cast<const int *>(st + 256)[lane];
-        __builtin_memcpy(&sa, row_s + first, 4);
+        v4i va[RG][4], vb[4];
+        int sa[RG], sb = reinterpret_cast<const int *>(st + 256)[lane];
+#pragma unroll
+        for (int i = 0; i < RG; ++i) __builtin_memcpy(&sa[i], row_s[i] + first, 4);
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             vb[s] = st[r * 16 + ((4 * g + s) ^ r)];
-            __builtin_memcpy(&va[s], row_a + first * 16 + s * 16, 16);
+#pragma unroll
+            for (int i = 0; i < RG; ++i) __builtin_memcpy(&va[i][s], row_a[i] + first * 16 + s * 16, 16);
         }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");               // (read, so that it may be overwritten)
         issue(t + D);
         // (of blocks that are not there the weights are zeros and the scales may be any byte)
         const int mask = int(0xFFFFFFFFull >> max(0, min(32, (g * 4 + 4 - count_of(t)) * 8)));
-        sa &= mask;
         sb &= mask;
-        acc[0] = multiply_blocks<0>(vb[0], va[0], acc[0], sb, sa);
-        acc[1] = multiply_blocks<1>(vb[1], va[1], acc[1], sb, sa);
-        acc[0] = multiply_blocks<2>(vb[2], va[2], acc[0], sb, sa);
-        acc[1] = multiply_blocks<3>(vb[3], va[3], acc[1], sb, sa);
-    }
-    reinterpret_cast<f4 *>(ring[wave])[lane] = acc[0] + acc[1];
-    __syncthreads();
-    if (wave) return;
-    f4 s = reinterpret_cast<const f4 *>(ring[0])[lane];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) s += reinterpret_cast<const f4 *>(ring[w])[lane];
-    const int n = n0 + g * 4;
-    if (r >= p.m || n >= p.n) return;
+        for (int i = 0; i < RG; ++i) {
+            sa[i] &= mask;
+            acc[i][0] = multiply_blocks<0>(vb[0], va[i][0], acc[i][0], sb, sa[i]);
+            acc[i][1] = multiply_blocks<1>(vb[1], va[i][1], acc[i][1], sb, sa[i]);
+            acc[i][0] = multiply_blocks<2>(vb[2], va[i][2], acc[i][0], sb, sa[i]);
+            acc[i][1] = multiply_blocks<3>(vb[3], va[i][3], acc[i][1], sb, sa[i]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < RG; ++i) reinterpret_cast<f4 *>(ring[wave])[i * 64 + lane] = acc[i][0] + acc[i][1];
+    __syncthreads();
+    if (wave >= RG) return;
+    f4 s = reinterpret_cast<const f4 *>(ring[0])[wave * 64 + lane];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) s += reinterpret_cast<const f4 *>(ring[w])[wave * 64 + lane];
+    const int m = wave * 16 + r, n = n0 + g * 4;
+    if (m >= p.m || n >= p.n) return;
     const f4 v = values_of(p, s, bias_at(p, n));
-    if (p.y_bf16) store_channels<__bf16, 4>(p, r, n, __builtin_convertvector(v, b4));
-    else store_channels<float, 4>(p, r, n, v);
+    if (p.y_bf16) store_channels<__bf16, 4>(p, m, n, __builtin_convertvector(v, b4));
+    else store_channels<float, 4>(p, m, n, v);
 }
 
 // How a product is cut up: the tile (an index into launch_tiles) and over how many workgroups the length of k is split.
@@ -667,32 +680,42 @@ void launch_tiles(const Mx4Product &p, int splits, float *part, hipStream_t st)
 
 int64_t rows_groups(int64_t n) { return (n + 15) / 16; }
 
-// Whether rows are so few and short that every workgroup has all of them in LDS: kFewBytes together, less where a compute unit
-// has several workgroups to run (4x8192 -> 4096 8.3 us, in tiles 15.5; 4x8192 -> 8192 14.1 and 15.3, 6x8192 -> 8192 16.8
-// and 15.3, 8x8192 -> 8192 19.6 and 15.6).
+constexpr int64_t kLds = 160 * 1024;
+
+// Whether rows are so few and short that every workgroup has all of them in LDS beside two turns of weights, less of them where a
+// compute unit has several workgroups to run (4x8192 -> 8192 14.1 us, and 15.3 in tiles, 6x8192 -> 8192 16.8 and 15.3, 8x8192 ->
+// 8192 19.6 and 15.6).
 bool few(int64_t m, int64_t n, int64_t blocks)
 {
-    return m <= kFewRows && m * blocks * 16 * ((rows_groups(n) + kUnits - 1) / kUnits) <= kFewBytes && blocks > 0;
+    if (m > kFewRows || blocks == 0 || blocks > 2048 || m * blocks * 16 > kLds) return false;
+    const int64_t rounds = (rows_groups(n) + kUnits - 1) / kUnits;
+    return rounds == 1 ? int64_t(kFewRing) * 2 + few_rows(int(m), int(blocks)).bytes <= kLds : m * blocks * 16 * rounds <= 32768;
+}
+
+template <typename T, int RG>
+void launch_few_of(const Mx4Product &p, const T *x, int64_t ldx, int k, hipStream_t st)
+{
+    const int64_t lds = few_rows(p.m, p.blocks).bytes;
+    const dim3 grid(unsigned(rows_groups(p.n)));
+    // Three turns of each wave under way where a compute unit has one workgroup (1x25088 -> 8192 24.2 us with two, 23.0),
+    // two where it has two (8192 -> 8192 8.5 us, and one with three turns 10.7) or the rows leave no room.
+    const bool two = (int64_t(grid.x) > kUnits && 2 * (int64_t(kFewRing) * 2 + lds) <= kLds) || int64_t(kFewRing) * 3 + lds > kLds;
+    if (two) hipLaunchKernelGGL((linear_mx4_rows_kernel<T, 2, RG>), grid, dim3(512), size_t(lds), st, p, x, ldx, k);
+    else hipLaunchKernelGGL((linear_mx4_rows_kernel<T, 3, RG>), grid, dim3(512), size_t(lds), st, p, x, ldx, k);
 }
 
 template <typename T>
 int launch_few(const Mx4Product &p, const T *x, int64_t ldx, int k, hipStream_t st)
 {
-    const size_t lds = size_t(few_rows(p.m, p.blocks).bytes);
-    const dim3 grid(unsigned(rows_groups(p.n)));
-    // Three turns of each wave under way where a compute unit has one workgroup (1x25088 -> 8192 24.2 us with two, 23.0),
-    // two where it has two (8192 -> 8192 8.5 us, and one with three turns 10.7).
-    // (with kFewBytes of rows, their scales, and the room behind 16 of them)
-    constexpr size_t kLds = 160 * 1024;
-    static_assert(kFewRing * 3 + kFewBytes + kFewBytes / 16 + kFewRows * (kTurn * 34 + 36) <= kLds, "");
-    if (int64_t(grid.x) > kUnits && 2 * (kFewRing * 2 + lds) <= kLds) hipLaunchKernelGGL((linear_mx4_rows_kernel<T, 2>), grid, dim3(512), lds, st, p, x, ldx, k);
-    else hipLaunchKernelGGL((linear_mx4_rows_kernel<T, 3>), grid, dim3(512), lds, st, p, x, ldx, k);
+    if (p.m <= 16) launch_few_of<T, 1>(p, x, ldx, k, st);
+    else launch_few_of<T, 2>(p, x, ldx, k, st);
     return check_launch("pconv_linear_mx4 (few rows)");
 }
 
 }  // namespace
 
-bool linear_mx4_fused(int64_t m, int64_t n, int64_t blocks) { return few(m, n, blocks); }
+// (Every workgroup quantises all rows: 8x4096 -> 4096 5.9 us, and 6.0 with a launch for it; 16x4096 8.4 and 6.5.)
+bool linear_mx4_fused(int64_t m, int64_t n, int64_t blocks) { return few(m, n, blocks) && m * blocks <= 1024; }
 
 int launch_linear_mx4_fused(const Mx4Product &p, const void *x, int64_t ldx, int bf16, int64_t k, void *stream)
 {

@@ -234,6 +234,16 @@ def test_product_and_layer_against_the_formula(m, n, k, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("m,n,k", [(17, 40, 4096), (32, 130, 4095), (31, 16, 1023), (32, 40, 1024), (32, 40, 1025), (16, 50, 8190), (4, 300, 25088), (6, 40, 25088),
+                                   (7, 40, 25088), (32, 4100, 512), (20, 9000, 200), (30, 33, 4700), (2, 50, 65536), (2, 50, 65537)])
+def test_few_rows(m, n, k):
+    """One or two groups of 16 rows, two or three turns of weights under way, quantised by all workgroups or by a launch; the largest that fit and the
+    first that do not."""
+    test_product_and_layer_against_the_formula(m, n, k, "f32")
+    test_product_and_layer_against_the_formula(m, n, k, "bf16")
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("m,n,k", [(1, 40, 12000), (16, 33, 2048), (40, 40, 12000), (100, 200, 5000), (300, 300, 2000), (1000, 1000, 700), (600, 2100, 900)])
 def test_sums_of_equal_scales_are_exact(m, n, k):
     """All scales alike: every partial sum is a whole number of quarters, so that the order of nothing counts."""
@@ -542,8 +552,8 @@ def test_bf16_outputs_that_begin_within_a_word(m, n, k):
 
 # ---- plans ---------------------------------------------------------------------------------------------------------------
 
-FORMS = {(1, 0, 0, False): (9, 40, 256), (2, 32, 1, False): (129, 11206, 64), (2, 32, 1, True): (1, 9309, 22924), (2, 32, 2, False): (20, 64, 256),
-         (2, 32, 2, True): (7, 33, 10096), (2, 64, 1, False): (145, 18962, 40), (2, 64, 1, True): (33, 9394, 32445), (2, 64, 2, False): (8395, 9, 562),
+FORMS = {(1, 0, 0, False): (9, 40, 256), (2, 32, 1, False): (129, 11206, 64), (2, 32, 1, True): (1, 9309, 22924), (2, 32, 2, False): (40, 64, 256),
+         (2, 32, 2, True): (40, 33, 10096), (2, 64, 1, False): (145, 18962, 40), (2, 64, 1, True): (33, 9394, 32445), (2, 64, 2, False): (8395, 9, 562),
          (2, 64, 2, True): (2105, 20, 9403), (2, 128, 1, False): (34014, 20, 64), (2, 128, 1, True): (17908, 15, 19019),
          (2, 128, 2, False): (17004, 2, 1026), (2, 128, 2, True): (4750, 20, 19083), (2, 256, 1, False): (41430, 130, 64),
          (2, 256, 1, True): (773, 1782, 152295)}
