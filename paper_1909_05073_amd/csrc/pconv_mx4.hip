@@ -682,8 +682,9 @@ int64_t rows_groups(int64_t n) { return (n + 15) / 16; }
 
 constexpr int64_t kLds = 160 * 1024;
 
-// Whether rows are so few and short that every workgroup has all of them in LDS beside two turns of weights, less of them where a
-// compute unit has several workgroups to run (4x8192 -> 8192 14.1 us, and 15.3 in tiles, 6x8192 -> 8192 16.8 and 15.3, 8x8192 ->
+// Whether rows are so few and short that every workgroup has all of them in LDS beside two turns of weights (32x4096 -> 4096 with a
+// launch that quantises 7.8 us, 10.1 in tiles; 4x25088 -> 4096 13.7 and 16.4), less of them where a compute unit has several
+// workgroups to run (4x8192 -> 8192 14.1 us, and 15.3 in tiles, 6x8192 -> 8192 16.8 and 15.3, 8x8192 ->
 // 8192 19.6 and 15.6).
 bool few(int64_t m, int64_t n, int64_t blocks)
 {
