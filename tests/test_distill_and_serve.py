@@ -113,3 +113,45 @@ def test_a_training_step_has_the_gradients_of_the_formula():
     _, _, grad, off = plain_distill(logits.detach().cpu().numpy(), top.cpu().numpy(), classes.cpu().numpy(), 2.0, np.full(16, 1 / 16))
     check_grad(logits.grad, grad, off, "f32", "logits")
     assert all(bool(t.grad.isfinite().all()) and bool(t.grad.any()) for t in student.values())
+
+
+@pytest.mark.gpu
+def test_calls_in_inference_mode_and_from_several_threads():
+    """The same bits as ever, whoever calls."""
+    import threading
+
+    import torch
+    say("[case] inference mode, threads")
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(3)
+    randn = lambda *shape: torch.randn(*shape, generator=gen, device="cuda")
+    x, z, top, classes = randn(40, 300), randn(8, 100), randn(8, 5), torch.randint(0, 100, (8, 5), generator=gen, device="cuda")
+    w, ws = P.quantize_mx4(randn(50, 300))
+    b, sb = P.quantize_rows(randn(50, 300))
+
+    def call():
+        q, scale, s = P.add_rms_norm_i8(x, x)
+        return P.linear_mx4(x, w, ws), *P.quantize_mx4(x), q, s, P.matmul_i8(q, scale, b, sb), P.distill_loss(z, top, classes, 2.0), P.distill_loss_grad(z, top, classes, 2.0)[1]
+    want, leaf = call(), z.clone().requires_grad_()
+    P.distill_loss(leaf, top, classes, 2.0).backward()
+    with torch.inference_mode():
+        assert all(torch.equal(a, b) for a, b in zip(call(), want))
+    wrong = []
+
+    def work():
+        try:
+            mine = z.clone().requires_grad_()
+            for _ in range(50):
+                got = call()
+                mine.grad = None
+                P.distill_loss(mine, top, classes, 2.0).backward()
+            torch.cuda.synchronize()
+            assert torch.equal(mine.grad, leaf.grad) and all(torch.equal(a, b) for a, b in zip(got, want))
+        except BaseException as e:
+            wrong.append(e)
+    threads = [threading.Thread(target=work) for _ in range(4)]
+    for thread in threads:
+        thread.start()
+    for thread in threads:
+        thread.join()
+    assert not wrong, wrong
