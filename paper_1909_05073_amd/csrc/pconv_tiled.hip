@@ -1005,8 +1005,10 @@ conv_tiled_kernel(const TiledArgs a)
         }
         if constexpr (VEC && SPLIT) {
             if (hands_on) {
-                // the barrier orders every thread's stores before the release below, which makes
+                // every wave waits until its stores are done (a barrier alone waits for LDS only, and the release
+                // below for its own wave's stores), the barrier orders them before the release, which makes
                 // them visible to the whole device before the successor is told
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 __syncthreads();
                 if (threadIdx.x == 0)
                     __hip_atomic_store(a.flags + blockIdx.x, a.epoch, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_AGENT);
