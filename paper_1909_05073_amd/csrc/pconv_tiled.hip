@@ -28,6 +28,7 @@
 #include <cstdlib>
 
 #include "pconv_internal.h"
+#include "pconv_shares.h"
 #include "pconv_tiled_codes.h"
 
 // Hand-over words for callers that cannot let the library allocate (pconv_conv2d_static): one row
@@ -104,7 +105,7 @@ struct TiledArgs {
     int split_units;            // 1: a workgroup's share of the work may begin and end inside a unit
     int priv;                   // 1: the 16 waves are 16 channel ranges of one filter block (channels last)
     int one_set;                // 1 (with split_units): the iterations are dealt over all workgroups as one set
-    uint32_t *flags;            // [gridDim.x] hand-over words of this call (split_units only)
+    uint32_t *flags;            // [kFlagWords] hand-over words of this call (split_units only), the last one the tickets
     uint32_t n_records;         // records of the stream (the padding record's index)
     uint32_t epoch;             // value that marks a hand-over word as set by this call (never 0)
     uint32_t x_bytes;           // size of the input tensor (VEC kernel: below 2^31)
@@ -134,12 +135,11 @@ __device__ __forceinline__ size_t act_at(int n, int c, int y, int x, int C, int 
 //                      or more consecutive workgroups of the set, each taking a range of its chunks
 //                      (with one_set: over all workgroups as a single set, whatever their XCD).
 // The workgroups that share a unit add their partial sums through the output tensor itself, in
-// order of their ids: each one adds what its predecessor left there, and either leaves the new
+// order of their places in the set: each one adds what its predecessor left there, and either leaves the new
 // sum for its successor (raw, no bias) or, if it holds the unit's last chunk, finishes the
-// outputs.  A workgroup runs the piece it must hand on first and the piece it takes over last;
-// the hardware starts workgroups in order of their ids, so whatever a workgroup waits for
-// belongs to a workgroup that has already started and handed over at its very beginning.
-//
+// outputs.  A workgroup runs the piece it must hand on first and the piece it takes over last.
+// pconv_shares.h has the shares and pieces, and why whatever a workgroup waits for belongs to a workgroup that has
+// already started.
 //
 // PRIV: few units of work, channels last (pconv_lone.hip does the same for NCHW, where a wave loads its
 // channels by itself).  A workgroup is one filter block, its 16 waves are 16 ranges of channels, and the 16
@@ -210,8 +210,21 @@ conv_tiled_kernel(const TiledArgs a)
     // (PRIV: XCD s gets the s-th eighth of the units, so that its L2 serves few tiles)
     const int per_xcd = PRIV ? (a.n_units + 7) >> 3 : 0;
     const int set = one_set ? 0 : int(blockIdx.x & 7);
-    const int j_in_set = PRIV ? int(blockIdx.x & 7) * per_xcd + int(blockIdx.x >> 3) : one_set ? int(blockIdx.x) : int(blockIdx.x >> 3);
-    const int set_stride = one_set ? 1 : 8;
+    int j_in_set = PRIV ? int(blockIdx.x & 7) * per_xcd + int(blockIdx.x >> 3) : one_set ? int(blockIdx.x) : int(blockIdx.x >> 3);
+    if constexpr (SPLIT) {
+        if (shares_by_ticket(one_set)) {
+            // (nobody asks behind the last one, who leaves the counter as a later call wants it)
+            if (threadIdx.x == 0) {
+                const uint32_t t = __hip_atomic_fetch_add(a.flags + (kFlagWords - 1), 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                if (t + 1 == gridDim.x) __hip_atomic_store(a.flags + (kFlagWords - 1), 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                sync_words[7] = t;
+            }
+            __syncthreads();
+            j_in_set = __builtin_amdgcn_readfirstlane(int(sync_words[7]));
+        }
+    }
+    // the word that a workgroup sets for its successor, and how far the one of its predecessor lies before it
+    const int flag_at = one_set ? j_in_set : int(blockIdx.x), set_stride = one_set ? 1 : 8;
     // set s: the contiguous block of tiles [s * tps, (s + 1) * tps): neighbouring tiles (which share
     // input rows and columns) then run next to each other in time on one XCD and find them in its L2
     // (with tiles s, s + 8, ... in a set, conv2 of VGG-16 fetched 699 MB for its 411 MB input; now 444)
@@ -219,43 +232,17 @@ conv_tiled_kernel(const TiledArgs a)
     const int set_tile0 = set * tps;
     const int set_units = one_set ? a.n_units : max(0, min(a.n_tiles, set_tile0 + tps) - set_tile0) * a.n_groups;
     // SPLIT: iteration = (unit of the set) * n_chunks + chunk; otherwise one whole unit per workgroup
-    int ua = j_in_set, ub = j_in_set, head_c0 = 0, tail_c1 = n_chunks;
+    UnitShare share{j_in_set, j_in_set, 0, n_chunks};
     if constexpr (SPLIT) {
-        const int wgs_in_set = one_set ? int(gridDim.x) : (int(gridDim.x) - set + 7) >> 3;
-        const int64_t iters = int64_t(set_units) * n_chunks;
-        const int64_t takers = iters < wgs_in_set ? iters : wgs_in_set;       // nobody gets an empty range in between
-        if (j_in_set >= takers) return;
-        int64_t it0 = iters * j_in_set / takers, it1 = iters * (j_in_set + 1) / takers;
-        // When every unit is shared by the same number P of workgroups, those finish their chunks at
-        // the same time and then pass the sums on one after the other, each link of that chain taking
-        // about as long as 2.5 chunks.  Their shares are therefore graded, the first the smallest and
-        // 2.5 chunks more for each successor (boundary k at k n / P - 2.5 k (P - k) / 2), so that a
-        // workgroup finishes about when its predecessor's sums arrive.
-        const int P = int(takers / set_units);
-        if (set_units * P == takers && P >= 2 && 4 * n_chunks >= P * (16 + 5 * (P - 1))) {
-            const int u = j_in_set / P, kk = j_in_set - u * P;
-            auto bound = [&](int q) { return (4 * q * n_chunks / P - 5 * q * (P - q)) / 4; };
-            it0 = int64_t(u) * n_chunks + bound(kk);
-            it1 = int64_t(u) * n_chunks + bound(kk + 1);
-        }
-        ua = int(it0 / n_chunks); ub = int((it1 - 1) / n_chunks);            // first and last unit touched
-        head_c0 = int(it0 - int64_t(ua) * n_chunks);                         // > 0: unit ua begins elsewhere
-        tail_c1 = int(it1 - int64_t(ub) * n_chunks);                         // < n_chunks: unit ub ends elsewhere
+        if (!unit_share(j_in_set, one_set ? int(gridDim.x) : (int(gridDim.x) - set + 7) >> 3, set_units, n_chunks, share)) return;
     } else {
         if (j_in_set >= set_units || (PRIV && int(blockIdx.x >> 3) >= per_xcd)) return;
     }
-    const bool has_head = head_c0 > 0, has_tail = tail_c1 < n_chunks;
-    const bool one_piece = ua == ub;
-    // order: the piece to hand on, whole units, the piece taken over
-    const int first_whole = has_head ? ua + 1 : ua, last_whole = has_tail ? ub - 1 : ub;
-    const int n_whole = last_whole >= first_whole ? last_whole - first_whole + 1 : 0;
-    const int n_pieces = SPLIT ? (has_tail ? 1 : 0) + n_whole + ((has_head && !(one_piece && has_tail)) ? 1 : 0) : 1;
+    const int n_pieces = SPLIT ? unit_pieces(share, n_chunks) : 1;
 
     for (int piece = 0; piece < n_pieces; ++piece) {
-        int unit, c_begin = 0, c_end = n_chunks;
-        if (has_tail && piece == 0) { unit = ub; c_end = tail_c1; if (one_piece) c_begin = head_c0; }
-        else if (piece - (has_tail ? 1 : 0) < n_whole) unit = first_whole + piece - (has_tail ? 1 : 0);
-        else { unit = ua; c_begin = head_c0; }
+        const UnitPiece here = SPLIT ? unit_piece(share, n_chunks, piece) : UnitPiece{j_in_set, 0, n_chunks};
+        const int unit = here.unit, c_begin = here.c_begin, c_end = here.c_end;
         const bool takes_over = SPLIT && c_begin > 0, hands_on = SPLIT && c_end < n_chunks;
         const int tile = (one_set ? 0 : set_tile0) + unit / a.n_groups, group = unit % a.n_groups;
         const int fblk = PRIV ? group : group * fw + (wave - ksplit * fw);
@@ -855,7 +842,7 @@ conv_tiled_kernel(const TiledArgs a)
         const bool writer = active && (PRIV ? wave < FB : ksplit == 0) && pidx_e < a.n_patches;
         if constexpr (VEC && SPLIT) {
             if (takes_over) {
-                // The predecessor (id - 8: same set, previous range) started before this workgroup
+                // The predecessor (same set, previous range) started before this workgroup
                 // and ran the shared unit first, so this wait is normally over before it begins.
                 // It is bounded all the same; if it ever expires the outputs are poisoned with NaN.
                 // One wave polls, and only its successful read is followed by the (costly)
@@ -863,7 +850,7 @@ conv_tiled_kernel(const TiledArgs a)
                 if (wave == 0) {
                     bool there = false;
                     for (int guard = 0; guard < (a.spin_limit >> 2) && !there; ++guard) {
-                        there = __hip_atomic_load(a.flags + (blockIdx.x - set_stride), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.epoch;
+                        there = __hip_atomic_load(a.flags + (flag_at - set_stride), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.epoch;
                         if (!there) __builtin_amdgcn_s_sleep(8);
                     }
                     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
@@ -1011,7 +998,7 @@ conv_tiled_kernel(const TiledArgs a)
                 asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 __syncthreads();
                 if (threadIdx.x == 0)
-                    __hip_atomic_store(a.flags + blockIdx.x, a.epoch, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_AGENT);
+                    __hip_atomic_store(a.flags + flag_at, a.epoch, __ATOMIC_RELEASE, __HIP_MEMORY_SCOPE_AGENT);
             }
         }
     }
@@ -1445,11 +1432,12 @@ int launch_conv_tiled(const pconv_handle *h, const void *x, void *y, const float
     if (a.split_units) {
         // one workgroup per slot, but no fewer than two chunks each
         const int64_t iters = units * a.n_chunks;
-        wgs = std::min<int64_t>(std::min<int>(slots, kFlagWords), std::max<int64_t>(8, iters / 2));
+        // (and a word of the row for each, beside that of the tickets)
+        wgs = std::min<int64_t>(std::min<int>(slots, kFlagWords - 1), std::max<int64_t>(8, iters / 2));
         if (static_scratch) {
             // the one row of the device's static array, cleared by a small kernel ahead of the
             // convolution on the same stream (calls that overlap on one device would race here)
-            if (wgs > kFlagWords) { set_error("pconv_conv2d_static: more workgroups than hand-over words"); return PCONV_UNSUPPORTED; }
+            if (wgs >= kFlagWords) { set_error("pconv_conv2d_static: more workgroups than hand-over words"); return PCONV_UNSUPPORTED; }
             uint32_t *row = static_flags(h->device);
             if (!row) return PCONV_HIP_ERROR;
             hipLaunchKernelGGL(fill_words_kernel, dim3((kFlagWords + 255) / 256), dim3(256), 0,
