@@ -135,6 +135,9 @@ add_rms_norm_i8_kernel(const NormRows p, const T *x, const T *r, T *sum)
     const int sub = int(threadIdx.x) % TPR;
     const int whole = int(p.cols / N), rest = int(p.cols % N);
     const bool tail = sub < rest;
+    // (of rows without a whole vector no weight is read but their elements'; elsewhere threads beyond a row's vectors, whose values
+    // are zeros, read its last one)
+    const float *const weight = whole > 0 ? p.weight : nullptr;
     const int64_t at_tail = int64_t(whole) * N + sub, groups = (p.rows + RPW - 1) / RPW;
     for (int64_t g = blockIdx.x; g < groups; g += gridDim.x) {
         const int64_t row = g * RPW + int(threadIdx.x) / TPR;
@@ -204,12 +207,12 @@ add_rms_norm_i8_kernel(const NormRows p, const T *x, const T *r, T *sum)
         uint32_t most = __float_as_uint(last) & 0x7FFFFFFFu;
 #pragma unroll
         for (int i = 0; i < KEEP; ++i) {
-            normalise(s[i], f, p.weight, min(i * TPR + sub, max(whole - 1, 0)));
+            normalise(s[i], f, weight, min(i * TPR + sub, max(whole - 1, 0)));
             most = most_of_values(s[i], most);
         }
         for (int k = KEEP * TPR + sub; k < whole; k += TPR) {
             Values<N> v = load_sums(xr, rr, k);
-            normalise(v, f, p.weight, k);
+            normalise(v, f, weight, k);
             most = most_of_values(v, most);
         }
         most = most_of_lanes<(TPR < 64 ? TPR : 64)>(most);
@@ -229,7 +232,7 @@ add_rms_norm_i8_kernel(const NormRows p, const T *x, const T *r, T *sum)
         for (int k = KEEP * TPR + sub; k < whole; k += TPR) {
             Values<N> v = load_sums(xr, rr, k);
             if (sum) store_sums(v, sr, k);
-            normalise(v, f, p.weight, k);
+            normalise(v, f, weight, k);
             store_quantized(v, scale, q, k);
         }
         if (tail) q[at_tail] = int8_t((scale.lifts ? quantize<true>(last, scale) : quantize<false>(last, scale)) & scale.mask);

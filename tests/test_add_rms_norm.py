@@ -124,6 +124,23 @@ def test_rows_that_lie_apart_and_begin_anywhere(k, offset, extra):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("behind", ["nan", "inf", "-inf"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k", [1, 2, 3, 4, 5, 6, 7, 8, 9, 15, 17, 130, 513])
+def test_what_lies_behind_the_weight_is_nothing(k, dtype, behind):
+    """Rows shorter than one vector of 16 bytes among them."""
+    import torch
+    rng = np.random.default_rng(500 + k)
+    m = 5
+    x, r, w = make(rng, m, k)
+    (xd, x), (rd, r) = as_type(x, dtype), as_type(r, dtype)
+    wd = torch.cat([torch.from_numpy(w), torch.full((8,), float(behind))]).cuda()[:k]
+    say(f"[case] k={k} {dtype} {behind} behind the weight")
+    check_norm(P.add_rms_norm_i8(xd, rd, wd), x, r, w, 1e-6, dtype)
+    check_norm(P.add_rms_norm_i8(xd, None, wd), x, None, w, 1e-6, dtype)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("k", [5, 64, 300, 9001])
 def test_rows_with_tiny_huge_infinite_and_nan_values(k):
     say(f"[case] add_rms_norm_i8 odd values k={k}")
