@@ -156,11 +156,54 @@ T *address(const at::Tensor &t) { return t.numel() ? static_cast<T *>(t.data_ptr
 
 void *stream_of(const at::Tensor &t) { return c10::hip::getCurrentHIPStream(t.device().index()).stream(); }
 
+// Rows of a tensor [.., length] and the step between them.
+struct RowsOf { int64_t rows, length, step; };
+
+bool rows_of(const at::Tensor &t, RowsOf &r)
+{
+    if (t.dim() == 2 && t.size(1) > 0 && t.stride(1) == 1 && (t.stride(0) >= t.size(1) || t.size(0) <= 1)) {
+        r = RowsOf{t.size(0), t.size(1), std::max(t.stride(0), t.size(1))};
+        return true;
+    }
+    if (t.dim() < 1 || t.size(-1) == 0) return false;
+    if (!t.is_contiguous()) {                            // (rows in more dimensions, one step apart throughout)
+        if (t.dim() < 3 || t.numel() == 0 || t.stride(-1) != 1 || t.stride(-2) < t.size(-1)) return false;
+        for (int64_t d = t.dim() - 3; d >= 0; --d)
+            if (t.stride(d) != t.stride(d + 1) * t.size(d + 1)) return false;
+    }
+    r = RowsOf{t.numel() / t.size(-1), t.size(-1), t.is_contiguous() ? t.size(-1) : t.stride(-2)};
+    return true;
+}
+
+// What a saved tensor was; hooks may hand back another one, which lies elsewhere and otherwise.
+struct SavedAs {
+    c10::Device device = c10::kCPU;
+    at::ScalarType type = at::kFloat;
+    std::vector<int64_t> sizes, strides;
+    int64_t row_step = 0;
+
+    SavedAs(const at::Tensor &t, int64_t step) : device(t.device()), type(t.scalar_type()), sizes(t.sizes().vec()), strides(t.strides().vec()), row_step(step) {}
+    SavedAs() = default;
+    // The tensor as rows, and the step from one to the next.
+    at::Tensor rows(const at::Tensor &t, int64_t &step, const char *what) const
+    {
+        TORCH_CHECK(t.defined() && t.device() == device && t.scalar_type() == type && t.sizes() == at::IntArrayRef(sizes), "distill_loss: a hook of saved tensors has changed the ", what,
+                    "'s device, type or shape");
+        RowsOf r;
+        step = row_step;
+        if (t.numel() == 0 || t.strides() == at::IntArrayRef(strides)) return t;
+        const at::Tensor as_rows = rows_of(t, r) ? t : t.contiguous();
+        step = rows_of(as_rows, r) ? r.step : t.size(-1);
+        return as_rows;
+    }
+};
+
 struct DistillNode : torch::autograd::Node {
     DistillEntries entries;
     DistillCall call;
     Reduction reduction;
     torch::autograd::SavedVariable student, teacher, classes, lse;
+    SavedAs student_as, teacher_as, classes_as, lse_as;
     std::mutex mutex;
 
     std::string name() const override { return "DistillLossBackward"; }
@@ -176,13 +219,16 @@ struct DistillNode : torch::autograd::Node {
     {
         const std::lock_guard<std::mutex> lock(mutex);
         if (!task_should_compute_output(0) || !ups[0].defined()) return {at::Tensor()};
-        const at::Tensor z = student.unpack(), t = teacher.unpack(), c = classes.unpack(), sums = lse.unpack();
+        const at::Tensor z_saved = student.unpack(), t_saved = teacher.unpack(), c_saved = classes.unpack(), lse_saved = lse.unpack();
         at::Tensor grad;
         {
             const at::NoGradGuard no_grad;
+            int64_t z_step, t_step, c_step, one;
+            const at::Tensor z = student_as.rows(z_saved, z_step, "student"), t = teacher_as.rows(t_saved, t_step, "teacher"), c = classes_as.rows(c_saved, c_step, "classes"),
+                             sums = lse_as.rows(lse_saved, one, "sums");
             const at::Tensor up = reduction == kNone ? ups[0].reshape({-1}).contiguous() : ups[0];
             grad = at::empty(z.sizes(), z.options().memory_format(at::MemoryFormat::Contiguous));
-            check_status(entries, entries.grad(address<void>(z), call.z_step, call.z_type, address<void>(t), call.t_step, call.t_type, address<void>(c), call.c_step,
+            check_status(entries, entries.grad(address<void>(z), z_step, call.z_type, address<void>(t), t_step, call.t_type, address<void>(c), c_step,
                                                int(call.class_bytes), call.rows, call.v, call.top, call.temperature, call.mean, address<float>(sums), address<float>(up),
                                                reduction == kNone ? 1 : 0, address<void>(grad), call.v, stream_of(z)));
         }
@@ -211,25 +257,6 @@ bool tensor_of(PyObject *o, const at::Tensor *&t)
     if (o == Py_None) return true;
     if (!THPVariable_Check(o)) return false;
     t = &THPVariable_Unpack(o);
-    return true;
-}
-
-// Rows of a tensor [.., length] and the step between them.
-struct RowsOf { int64_t rows, length, step; };
-
-bool rows_of(const at::Tensor &t, RowsOf &r)
-{
-    if (t.dim() == 2 && t.size(1) > 0 && t.stride(1) == 1 && (t.stride(0) >= t.size(1) || t.size(0) <= 1)) {
-        r = RowsOf{t.size(0), t.size(1), std::max(t.stride(0), t.size(1))};
-        return true;
-    }
-    if (t.dim() < 1 || t.size(-1) == 0) return false;
-    if (!t.is_contiguous()) {                            // (rows in more dimensions, one step apart throughout)
-        if (t.dim() < 3 || t.numel() == 0 || t.stride(-1) != 1 || t.stride(-2) < t.size(-1)) return false;
-        for (int64_t d = t.dim() - 3; d >= 0; --d)
-            if (t.stride(d) != t.stride(d + 1) * t.size(d + 1)) return false;
-    }
-    r = RowsOf{t.numel() / t.size(-1), t.size(-1), t.is_contiguous() ? t.size(-1) : t.stride(-2)};
     return true;
 }
 
@@ -489,6 +516,10 @@ PyObject *distill(PyObject *, PyObject *const *args, Py_ssize_t count)
             node->entries = e;
             node->call = n;
             node->reduction = reduction;
+            node->student_as = SavedAs(z, n.z_step);
+            node->teacher_as = SavedAs(t, n.t_step);
+            node->classes_as = SavedAs(c, n.c_step);
+            node->lse_as = SavedAs(sums, n.rows);
             node->student = torch::autograd::SavedVariable(z, false);
             node->teacher = torch::autograd::SavedVariable(t, false);
             node->classes = torch::autograd::SavedVariable(c, false);

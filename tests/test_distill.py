@@ -357,6 +357,40 @@ def test_autograd_keeps_its_rules():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,v,top", [(5, 10, 4), (7, 1003, 9), (6, 12001, 300)])
+def test_hooks_of_saved_tensors_may_lay_them_out_otherwise(rows, v, top, dtype):
+    """Rows cut out of wider ones come back from a hook without what lay between them, or with something else there."""
+    import torch
+    from torch.autograd.graph import save_on_cpu, saved_tensors_hooks
+    say(f"[case] distill hooks {rows}x{v} top {top} {dtype}")
+    z, t, c = make(np.random.default_rng(v), rows, v, top, twice=True)
+
+    def apart(a, extra, fill, dtype=None):
+        wide = torch.full((rows, a.shape[1] + extra), fill, dtype=dtype or dev(a).dtype, device="cuda")
+        wide[:, :a.shape[1]] = dev(a)
+        return wide[:, :a.shape[1]]
+    zd = apart(z, 3, float("nan"), torch.bfloat16 if dtype == "bf16" else torch.float32).requires_grad_()
+    td, cd = apart(t, 2, float("nan")), apart(c, 5, 0)
+    up = dev(np.random.default_rng(1).uniform(0.5, 2, rows).astype(np.float32))
+    want, = torch.autograd.grad(P.distill_loss(zd, td, cd, 2.0, "none"), zd, up)
+    other = lambda t: t if t.dim() < 2 else torch.nn.functional.pad(t, (4, 7))[..., 4:-7]
+    columns = lambda t: t if t.dim() < 2 else t.transpose(0, -1).contiguous().transpose(0, -1)
+    packs = (lambda t: t.contiguous(), lambda t: t.clone(), other, columns)
+    for hooks in [save_on_cpu()] + [saved_tensors_hooks(pack, lambda t: t) for pack in packs]:
+        for wide in (lambda t: t, lambda t: t.unsqueeze(1)):
+            with hooks:
+                loss = P.distill_loss(wide(zd), wide(td), wide(cd), 2.0, "none")
+            got, = torch.autograd.grad(loss, zd, up.view_as(loss))
+            assert torch.equal(got, want)
+    for pack in (lambda t: t.double() if t.is_floating_point() else t, lambda t: t[..., :1], lambda t: t.cpu()):
+        with saved_tensors_hooks(pack, lambda t: t):
+            loss = P.distill_loss(zd, td, cd, 2.0)
+        with pytest.raises(RuntimeError, match="hook of saved tensors"):
+            loss.backward()
+
+
+@pytest.mark.gpu
 def test_a_capture_that_torch_does_not_know_of_is_refused_where_memory_would_be_lent():
     """The rows' losses and what a gradient needs go back to torch's pool, which such a graph must not keep; calls whose every
     output is handed out are captured."""
