@@ -219,7 +219,8 @@ distill_kernel(const DistillRows p)
         float loss = 0;
         for (int j = sub; j < 4 * fours; j += TPR) {
             const float lp = share[j] - log_sum, part = cls[j] >= 0 ? exp_of(lp) : 0.0f;
-            if (LOSS && cls[j] >= 0 && lp != -INFINITY) loss += part * (lp - __builtin_fmaf(at_class[j], p.inv_t, -lse));
+            // (a share that is 0, or too small for fp32, counts nothing, also where the student rules its class out)
+            if (LOSS && part != 0.0f) loss += part * (lp - __builtin_fmaf(at_class[j], p.inv_t, -lse));
             share[j] = part;
         }
         T *const out = static_cast<T *>(p.grad) + row * p.ldg;

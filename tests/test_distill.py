@@ -173,6 +173,38 @@ def test_masked_classes_and_logits_of_minus_infinity(v):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype,tt", [("f32", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("T", [1.0, 2.0, 0.5])
+@pytest.mark.parametrize("v", [50, 5000, 40000])
+def test_shares_that_vanish_count_nothing(v, T, dtype, tt):
+    """A teacher masked with its type's lowest value, or far below its largest logit, where the student has -infinity."""
+    import torch
+    say(f"[case] distill vanishing shares v={v} T={T} {dtype} {tt}")
+    rng = np.random.default_rng(v)
+    z, t, c = make(rng, 5, v, 8)
+    low = float(torch.finfo(torch.bfloat16 if tt == "bf16" else torch.float32).min)
+    for r, value in enumerate((low, -1e30, t[2].max() - 300 * T, t[3].max() - 2000 * T)):
+        t[r, 4:] = value
+        z[r, c[r, 4:]] = -np.inf
+    t[4, 3] = -np.inf                                    # p = 0 exactly, as well
+    z[4, c[4, 3]] = -np.inf
+    # (what p counts there is below exp(-300) of the others: the formulas without those entries)
+    kept = c.copy()
+    kept[:4, 4:] = -1
+    kept[4, 3] = -1
+    zd, zv = as_type(z, dtype)
+    td, tv = as_type(t, tt)
+    loss, loss_off, grad, grad_off = plain_distill(zv, tv, kept, T, np.ones(5))
+    got, slope = P.distill_loss_grad(zd, td, dev(c), T, "none")
+    assert (np.abs(got.cpu().numpy() - loss) <= loss_off + 2.0 ** -126).all(), (got, loss)
+    check_grad(slope, grad, grad_off, dtype, "distill_loss_grad")
+    leaf = zd.clone().requires_grad_()
+    again = P.distill_loss(leaf, td, dev(c), T, "none")
+    again.sum().backward()
+    assert torch.equal(again.detach(), got) and torch.equal(leaf.grad, slope)
+
+
+@pytest.mark.gpu
 def test_infinities_and_nan_stay_in_their_rows():
     import torch
     say("[case] distill NaN")
