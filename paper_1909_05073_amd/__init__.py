@@ -1238,7 +1238,8 @@ def distill_loss(student, teacher, classes, temperature: float = 1.0, reduction:
     from the teacher's over its entries, at temperature T: of each row ("none"), their sum, or that divided by the rows
     ("mean", rows without an entry among them), fp32; see include/pconv.h.
 
-    Recorded for autograd: a gradient goes to the student (of its type), none to the teacher."""
+    Recorded for autograd: a gradient goes to the student (of its type), none to the teacher.  Derivatives in forward mode, and of the
+    gradient, are refused."""
     import torch
     if not torch.is_grad_enabled():
         return _distill(student, teacher, classes, temperature, reduction, 0)

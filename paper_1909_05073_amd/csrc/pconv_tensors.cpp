@@ -481,6 +481,9 @@ PyObject *distill(PyObject *, PyObject *const *args, Py_ssize_t count)
     const int allowed = PyObject_IsTrue(args[8]);
     if (PyErr_Occurred()) return nullptr;
     const bool captured = c10::hip::currentStreamCaptureStatusMayInitCtx() != c10::hip::CaptureStatus::None;
+    // (autograd asks functions of its own for this; distill_loss_grad records nothing)
+    TORCH_CHECK_NOT_IMPLEMENTED(what == 2 || !c10::AutogradState::get_tls_state().get_fw_grad_mode() || (!z._fw_grad(0).defined() && !t._fw_grad(0).defined()),
+                                "distill_loss has no derivative in forward mode: its tangent would be lost");
     if (captured && !allowed && (what == 1 || reduction != kNone)) PCONV_LONG_WAY;      // (the rows' losses, or what the gradient needs, are no result)
     if (captured && what == 1) {
         const auto sink = z.grad_fn() ? nullptr : torch::autograd::impl::try_get_grad_accumulator(z);

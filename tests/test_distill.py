@@ -389,6 +389,33 @@ def test_autograd_keeps_its_rules():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("reduction", ["none", "sum", "mean"])
+def test_forward_mode_and_function_transforms_are_refused(reduction):
+    """A loss without its tangent, or of something that has no memory of its own, would be wrong in silence."""
+    import torch
+    import torch.autograd.forward_ad as fw
+    say(f"[case] distill forward mode {reduction}")
+    z, t, c = (dev(a) for a in make(np.random.default_rng(21), 6, 40, 5))
+    want = P.distill_loss_grad(z, t, c, 2.0, reduction)
+    with fw.dual_level():
+        dual, dual_t, leaf = fw.make_dual(z, torch.ones_like(z)), fw.make_dual(t, torch.ones_like(t)), z.clone().requires_grad_()
+        for T in (2.0, 2):                               # (in native code at once, and the long way)
+            for student, teacher in ((dual, t), (z, dual_t), (fw.make_dual(leaf, torch.ones_like(z)), t)):
+                with pytest.raises(NotImplementedError, match="forward mode"):
+                    P.distill_loss(student, teacher, c, T, reduction)
+                with torch.no_grad(), pytest.raises(NotImplementedError, match="forward mode"):
+                    P.distill_loss(student, teacher, c, T, reduction)
+        got = P.distill_loss_grad(fw.unpack_dual(dual).primal, t, c, 2.0, reduction)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    f = lambda s: P.distill_loss(s, t, c, 2.0, "sum")
+    for call in (lambda: torch.func.jvp(f, (z,), (torch.ones_like(z),)), lambda: torch.func.grad(f)(z),
+                 lambda: torch.func.vmap(lambda s: P.distill_loss(s, t[0], c[0], 2.0, "sum"))(z)):
+        with pytest.raises(RuntimeError):
+            call()
+    assert torch.equal(P.distill_loss(z, t, c, 2.0, reduction), want[0])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("rows,v,top", [(5, 10, 4), (7, 1003, 9), (6, 12001, 300)])
 def test_hooks_of_saved_tensors_may_lay_them_out_otherwise(rows, v, top, dtype):
