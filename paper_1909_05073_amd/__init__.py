@@ -582,7 +582,7 @@ def _per_channel(t, n, what):
 
 
 def _quantized_step(size: int) -> int:
-    """Bytes from row to row of quantised rows: long ones begin where lines of the caches do."""
+    """Bytes from row to row of 4-bit rows and of the norm's: long ones begin where lines of the caches do."""
     return size if size < 1024 else (size + 127) // 128 * 128
 
 
@@ -717,7 +717,7 @@ def quantize_rows(x):
     index = _device_index(x)
     m, k, step = _rows(x, "x")
     lead = x.shape[:-1]
-    wide = _quantized_step((k + 15) // 16 * 16)
+    wide = (k + 15) // 16 * 16
     q = _empty(lead, m, wide, torch.int8, x)
     scale = torch.empty_strided((m,), (1,), dtype=torch.float32, device=x.device) if len(lead) == 1 else x.new_empty(lead, dtype=torch.float32)
     rc = (_lib or lib()).pconv_quantize_rows(x.data_ptr() or None, step, dtype, m, k, q.data_ptr() or None, wide,

@@ -48,3 +48,18 @@ def test_more_rows_than_workgroups():
     want = most / torch.full_like(most, 127.0)
     assert torch.equal(scale, want[:, 0])
     assert torch.equal(q, torch.where(want > 0, x.float() / want, torch.zeros_like(most)).round().to(torch.int8))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lead", [(6,), (2, 3)])
+@pytest.mark.parametrize("k,step", [(40, 48), (1008, 1008), (1024, 1024), (1025, 1040), (2000, 2000), (4112, 4112), (25089, 25104)])
+def test_rows_lie_a_multiple_of_16_bytes_apart(k, step, lead):
+    """So that rows whose length is one are contiguous."""
+    import torch
+    say(f"[case] steps of quantised rows of {k}")
+    x = torch.randn(*lead, k, device="cuda")
+    for t in (x, x.bfloat16()):
+        q, scale = P.quantize_rows(t)
+        assert q.shape == x.shape and q.stride()[-2:] == (step, 1) and q.is_contiguous() == (k % 16 == 0)
+        if k % 16 == 0:
+            assert torch.equal(q.view(-1).view(6, k), P.quantize_rows(t.view(6, k))[0])
