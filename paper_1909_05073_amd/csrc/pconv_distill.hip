@@ -325,7 +325,8 @@ void launch_rows(const DistillRows &p, hipStream_t st)
         hipLaunchKernelGGL((distill_kernel<T, TPR, U, LOSS, GRAD>), dim3(unsigned(std::min<int64_t>((p.rows + RPW - 1) / RPW, 1 << 20))),  \
                            dim3(RPW * TPR), RPW * lds, st, p);                                                                 \
     } while (0)
-    // The loss has the same bits with and without its gradient: the same threads a row for both.  More threads a row meet more
+    // Loss and gradient have the same bits together and apart: the same threads a row for all, which decide in what order the entries'
+    // shares and the logits are added.  More threads a row meet more
     // often than what they do in between is worth (8192x4000 bf16 38.4 us by 256, 34.7 by 64; 1999x10007 fp32 through autograd 59.8
     // by 512, 54.2 by 256; 4096x32768 bf16 171 by 1024, 116 by 512; 4x41829 16.2 by 1024, 14.6), fewer read more of a row
     // twice (4096x32768 133 by 256).  Eight vectors a thread keep longer rows, but take as long where the last are missing
@@ -340,7 +341,8 @@ void launch_rows(const DistillRows &p, hipStream_t st)
         else PCONV_LAUNCH(512, 8);
     } else {
         if (vecs <= 64 * 8) PCONV_LAUNCH(64, 4);
-        else PCONV_LAUNCH(256, 4);
+        else if (vecs <= 256 * 10) PCONV_LAUNCH(256, 4);
+        else PCONV_LAUNCH(512, 4);
     }
 #undef PCONV_LAUNCH
 }

@@ -156,6 +156,26 @@ def test_lists_longer_than_the_threads_of_a_row(v, top):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("top", [5, 130, 300, 1024])
+@pytest.mark.parametrize("v", [1024, 2049, 4097, 10_007, 10_241, 20_481, 21_000, 40_003])
+def test_equal_bits_together_and_apart(v, top, dtype):
+    """Every number of threads a row, lists shorter and longer than it."""
+    import torch
+    say(f"[case] distill equal bits v={v} top={top} {dtype}")
+    z, t, c = make(np.random.default_rng(v + top), 9, v, top, ragged=True, twice=True)
+    zd = as_type(z, dtype)[0]
+    for T in (2.0, 3.0):
+        loss, grad = P.distill_loss_grad(zd, dev(t), dev(c), T, "none")
+        leaf = zd.clone().requires_grad_()
+        apart = P.distill_loss(leaf, dev(t), dev(c), T, "none")
+        apart.sum().backward()
+        assert torch.equal(apart.detach(), loss) and torch.equal(leaf.grad, grad)
+        with torch.no_grad():
+            assert torch.equal(P.distill_loss(leaf, dev(t), dev(c), T, "none"), loss)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("v", [50, 5000, 40000])
 def test_masked_classes_and_logits_of_minus_infinity(v):
     """Classes that the student may not take, teacher's logits that are none, rows of nothing else."""
