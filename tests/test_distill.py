@@ -225,6 +225,42 @@ def test_shares_that_vanish_count_nothing(v, T, dtype, tt):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T", [1.0, 1.3, 3.0, 5.0])
+@pytest.mark.parametrize("v", [50, 5000, 40000])
+def test_rows_of_huge_logits(v, T, dtype):
+    """Rows whose largest logit is the type's lowest value, or so large that a step of it is an exponent's whole range."""
+    import torch
+    say(f"[case] distill huge logits v={v} T={T} {dtype}")
+    z, t, c = make(np.random.default_rng(v), 6, v, 8)
+    low = float(torch.finfo(torch.bfloat16 if dtype == "bf16" else torch.float32).min)
+    z[0] = low
+    z[1] = low
+    z[1, c[1, 0]] = 2.0
+    c[1, 1:] = -1
+    z[2] += 1e6
+    z[3], z[4] = 3e11, -7e20
+    t[5] += 1e9
+    zd, zv = as_type(z, dtype)
+    td, tv = as_type(t, "f32")
+    loss, loss_off, grad, grad_off = plain_distill(zv, tv, c, T, np.ones(6))
+    got, slope = P.distill_loss_grad(zd, td, dev(c), T, "none")
+    # (of rows of equal huge logits U |lse| is more than log v: all that is asked is a number, and no share beyond 1 by more than half a step
+    # of a sum near 1e6, 2^-5)
+    assert bool(got.isfinite().all()) and bool(slope.isfinite().all())
+    assert (np.abs(got.cpu().numpy() - loss) <= loss_off + 2.0 ** -126).all(), (got, loss)
+    off = np.where(grad_off < 1, grad_off, np.inf)
+    fine = ~(off.max(1) == np.inf)
+    assert fine[1]
+    check_grad(slope[dev(np.flatnonzero(fine))], grad[fine], off[fine], dtype, "distill_loss_grad")
+    assert float(slope.abs().max()) <= T * (1 + 2.0 ** -4)
+    leaf = zd.clone().requires_grad_()
+    again = P.distill_loss(leaf, td, dev(c), T, "none")
+    again.sum().backward()
+    assert torch.equal(again.detach(), got) and torch.equal(leaf.grad, slope)
+
+
+@pytest.mark.gpu
 def test_infinities_and_nan_stay_in_their_rows():
     import torch
     say("[case] distill NaN")
