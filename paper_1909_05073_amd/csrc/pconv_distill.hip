@@ -19,9 +19,22 @@ namespace pconv {
 
 namespace {
 
-constexpr float kLog2E = 1.44269504088896340736f;
+constexpr float kLog2E = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
-__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * kLog2E); }
+__device__ __forceinline__ float quick_exp(float x) { return __builtin_amdgcn_exp2f(x * kLog2E); }
+
+// e^x: the exponent's rounding is taken back, which would be |x| / 2 steps of the result.
+__device__ __forceinline__ float exp_of(float x)
+{
+    const float t = x * kLog2E, e = __builtin_amdgcn_exp2f(t), r = __builtin_fmaf(x, kLog2E, -t) * kLn2;
+    return e > 0.0f ? __builtin_fmaf(e, r, e) : e;       // (0 of -infinity; a NaN)
+}
+
+// A logarithm b as an exponent of 2, and the power of two by which that exponent was rounded: e^(x - b) is scale 2^(x log2 e - hi).
+struct Base {
+    float hi, scale;
+    __device__ __forceinline__ explicit Base(float b) : hi(b * kLog2E), scale(__builtin_amdgcn_exp2f(-__builtin_fmaf(b, kLog2E, -hi))) {}
+};
 
 // What all 64 lanes of a wave have together, in an order that depends on nothing; ADD: the sum, else the maximum.
 template <bool ADD>
@@ -48,7 +61,7 @@ struct Running {
     {
         // (a maximum takes a NaN for nothing; the sums hand it on)
         const float m = fmaxf(most, o.most), b = m == -INFINITY ? 0.0f : m;
-        sum = sum * exp_of(most - b) + o.sum * exp_of(o.most - b);
+        sum = sum * quick_exp(most - b) + o.sum * quick_exp(o.most - b);
         most = m;
     }
     // (the maximum first: one exponential a lane instead of two at each step; 8192x1001 bf16 17.0 us -> 15.6)
@@ -56,7 +69,7 @@ struct Running {
     {
         const float mine = most;
         most = of_wave<false>(most);
-        sum = of_wave<true>(sum * exp_of(mine - base()));
+        sum = of_wave<true>(sum * quick_exp(mine - base()));
     }
 };
 
@@ -80,7 +93,7 @@ __device__ __forceinline__ void join_threads(Running &z, Running &t, Running (*r
             for (int i = 1; i < TPR / 64; ++i) r.most = fmaxf(r.most, room[i][which].most);
             const float b = r.base();
 #pragma unroll
-            for (int i = 0; i < TPR / 64; ++i) r.sum += room[i][which].sum * exp_of(room[i][which].most - b);
+            for (int i = 0; i < TPR / 64; ++i) r.sum += room[i][which].sum * quick_exp(room[i][which].most - b);
             return r;
         };
         z = all(0);
@@ -126,36 +139,46 @@ __device__ __forceinline__ void keep_packed(Vec<T> (&v)[U])
     for (int i = 0; i < U; ++i) asm volatile("" : "+v"(v[i].v));
 }
 
-// What a logit is over T, less a maximum or a sum b that was found of such.  Where b is large (FAR) the quotient is rounded as b was: with
-// a fused product what b came from differs from it by up to half a step, whose exponential is infinite from logits of 10^10 on, the type's
-// lowest value among them, unless T is a power of two.  (Rounded always: 2000x50000 bf16 95.8 -> 101.2 us.)
-template <bool FAR>
-__device__ __forceinline__ float less(float z, float inv_t, float b) { return FAR ? z * inv_t - b : __builtin_fmaf(z, inv_t, -b); }
+// e^(z / T - b) for a maximum or a sum b of such quotients; the caller multiplies by the scale of b's Base.  One fused product and one
+// power of two: the exponent is rounded once, by what its difference from b is worth.  Where b is large (FAR) the quotient is rounded as
+// b was: with a fused product what b came from differs from it by up to half a step, whose exponential is infinite from logits of
+// 10^10 on, the type's lowest value among them, unless T is a power of two.  (Rounded always: 2000x50000 bf16 95.8 -> 101.2 us.)
+struct Quotients {
+    float inv_t, log2e_t;                                // 1 / T and log2(e) / T
+    template <bool FAR>
+    __device__ __forceinline__ float exp_less(float z, float b, const Base &base) const
+    {
+        return FAR ? __builtin_amdgcn_exp2f((z * inv_t - b) * kLog2E) : __builtin_amdgcn_exp2f(__builtin_fmaf(z, log2e_t, -base.hi));
+    }
+};
 
 // Whether b is so in some thread of the wave (half a step of 2^20 is 2^-4).
 __device__ __forceinline__ bool is_far(float b) { return __builtin_amdgcn_ballot_w64(fabsf(b) >= 0x1p20f) != 0; }
 
 // The values of vectors, over T, join what a thread has found.
 template <typename T, int U>
-__device__ __forceinline__ void join_vectors(Running &r, Vec<T> (&v)[U], float inv_t)
+__device__ __forceinline__ void join_vectors(Running &r, Vec<T> (&v)[U], const Quotients &q)
 {
     float m = -INFINITY;
 #pragma unroll
     for (int i = 0; i < U; ++i)
 #pragma unroll
         for (int e = 0; e < Vec<T>::N; ++e) m = fmaxf(m, v[i].at(e));
-    m = fmaxf(r.most, m * inv_t);
+    m = fmaxf(r.most, m * q.inv_t);
     const float b = m == -INFINITY ? 0.0f : m;
-    r.sum *= exp_of(r.most - b);
+    r.sum *= quick_exp(r.most - b);
     keep_packed(v);
-    const auto add = [&](auto far) {
+    const Base base(b);
+    const auto sum_of = [&](auto far) {
+        float sum = 0;
 #pragma unroll
         for (int i = 0; i < U; ++i)
 #pragma unroll
-            for (int e = 0; e < Vec<T>::N; ++e) r.sum += exp_of(less<decltype(far)::value>(v[i].at(e), inv_t, b));
+            for (int e = 0; e < Vec<T>::N; ++e) sum += q.exp_less<decltype(far)::value>(v[i].at(e), b, base);
+        return sum;
     };
-    if (__builtin_expect(is_far(b), 0)) add(std::true_type());
-    else add(std::false_type());
+    if (__builtin_expect(is_far(b), 0)) r.sum += sum_of(std::true_type());
+    else r.sum += sum_of(std::false_type()) * base.scale;
     r.most = m;
 }
 
@@ -178,6 +201,7 @@ distill_kernel(const DistillRows p)
     const int fours = (p.top + 3) / 4;
     float *const share = entries + of * 12 * fours, *const at_class = share + 4 * fours;
     int *const cls = reinterpret_cast<int *>(at_class + 4 * fours);
+    const Quotients quot{p.inv_t, p.log2e_t};
     const auto meet = [] {
         if constexpr (TPR > 64) {
             __syncthreads();
@@ -219,29 +243,33 @@ distill_kernel(const DistillRows p)
             enter(j, c, c < 0 ? 0.0f : teacher_at(p, row, j));
         }
         if constexpr (LOSS) {
-            join_vectors<T, U>(r, v, p.inv_t);
+            join_vectors<T, U>(r, v, quot);
             for (int k = U * TPR + sub; k < whole; k += U * TPR) {
                 Vec<T> w[U];
                 load_vectors<T, TPR, U>(z, k, whole, w);
-                join_vectors<T, U>(r, w, p.inv_t);
+                join_vectors<T, U>(r, w, quot);
             }
             if (sub < rest) r.join(Running{last * p.inv_t, last == -INFINITY ? 0.0f : 1.0f});
         }
         join_threads<TPR>(r, t, room + of * WAVES);
-        const float lse = LOSS ? r.base() + __logf(r.sum) : p.lse[row], log_sum = t.base() + __logf(t.sum);
         const bool some = !(t.most == -INFINITY && t.sum == 0.0f);
+        // (maxima and logarithms of sums stay apart where they can: together they are rounded to a step of the maximum)
+        const float z_base = r.base(), z_log = LOSS ? __logf(r.sum) : 0.0f, lse = LOSS ? z_base + z_log : p.lse[row];
+        const float t_base = t.base(), t_log = LOSS ? __logf(t.sum) : 0.0f, t_inv = some ? 1.0f / t.sum : 0.0f;
         float loss = 0;
         for (int j = sub; j < 4 * fours; j += TPR) {
-            const float lp = share[j] - log_sum, part = cls[j] >= 0 ? exp_of(lp) : 0.0f;
+            const float below = share[j] - t_base, part = cls[j] >= 0 ? exp_of(below) * t_inv : 0.0f;
             // (a share that is 0, or too small for fp32, counts nothing, also where the student rules its class out)
-            if (LOSS && part != 0.0f) loss += part * (lp - less<true>(at_class[j], p.inv_t, lse));
+            if (LOSS && part != 0.0f) loss += part * ((below - t_log) - ((at_class[j] * p.inv_t - z_base) - z_log));
             share[j] = part;
         }
         T *const out = static_cast<T *>(p.grad) + row * p.ldg;
         const float f = GRAD && some ? p.factor * (p.up ? p.up[row * p.up_step] : 1.0f) : 0.0f;
+        const Base base(lse);
         if constexpr (GRAD) {
             const auto write_all = [&](auto far) {
-                const auto grad_of = [&](float x) { return some ? f * exp_of(less<decltype(far)::value>(x, p.inv_t, lse)) : 0.0f; };
+                const float scaled = decltype(far)::value ? f : f * base.scale;
+                const auto grad_of = [&](float x) { return some ? scaled * quot.exp_less<decltype(far)::value>(x, lse, base) : 0.0f; };
                 const auto write = [&](const Vec<T> &x, int k) {
                     T w[N];
 #pragma unroll
@@ -306,7 +334,7 @@ distill_kernel(const DistillRows p)
                             }
                     }
                 }
-                if (first) out[c] = T(f * (exp_of(less<true>(at_class[j], p.inv_t, lse)) - off));
+                if (first) out[c] = T(f * (exp_of(at_class[j] * p.inv_t - lse) - off));
             }
         }
         if (row + int64_t(gridDim.x) * RPW < p.rows) meet();             // (the entries are read)

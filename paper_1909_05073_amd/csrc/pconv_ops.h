@@ -86,7 +86,7 @@ struct DistillRows {
     void *grad;
     int64_t ldz, ldt, ldc, ldg, rows, up_step;
     int v, top;
-    float inv_t, t2, factor;           // 1 / T, T^2, T and what the rows are divided by
+    float inv_t, log2e_t, t2, factor;  // 1 / T, log2(e) / T, T^2, T and what the rows are divided by
     int z_bf16, t_bf16, c_wide;
 };
 int launch_distill(const DistillRows &p, bool loss, bool grad, void *stream);
