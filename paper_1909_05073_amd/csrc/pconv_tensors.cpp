@@ -499,8 +499,9 @@ PyObject *distill(PyObject *, PyObject *const *args, Py_ssize_t count)
         {
             const at::NoGradGuard no_grad;
             const auto numbers = z.options().dtype(at::kFloat);
-            const at::Tensor rows = at::empty({n.rows}, numbers);
-            if (reduction != kNone) value = at::empty({}, numbers);
+            // (the rows' losses are handed out as they are made: a view made without autograd could not be changed in place)
+            const at::Tensor rows = reduction == kNone ? at::empty(z.sizes().slice(0, size_t(z.dim() - 1)), numbers) : at::empty({n.rows}, numbers);
+            value = reduction == kNone ? rows : at::empty({}, numbers);
             float *const total = reduction != kNone ? address<float>(value) : nullptr;
             if (what == 2) {
                 grad = at::empty(z.sizes(), z.options().memory_format(at::MemoryFormat::Contiguous));
@@ -511,7 +512,6 @@ PyObject *distill(PyObject *, PyObject *const *args, Py_ssize_t count)
                 check_status(e, e.loss(address<void>(z), n.z_step, n.z_type, address<void>(t), n.t_step, n.t_type, address<void>(c), n.c_step, int(n.class_bytes), n.rows, n.v,
                                        n.top, n.temperature, n.mean, address<float>(rows), total, what == 1 ? address<float>(sums) : nullptr, stream_of(z)));
             }
-            if (reduction == kNone) value = rows.view(z.sizes().slice(0, size_t(z.dim() - 1)));
         }
         if (what == 1) {
             const std::shared_ptr<DistillNode> node(new DistillNode(), torch::autograd::deleteNode);

@@ -445,6 +445,27 @@ def test_autograd_keeps_its_rules():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("lead", [(6,), (2, 3), ()])
+@pytest.mark.parametrize("reduction", ["none", "sum", "mean"])
+def test_losses_may_be_changed_in_place(lead, reduction):
+    import torch
+    say(f"[case] distill in place {lead} {reduction}")
+    z, t, c = (dev(a) for a in make(np.random.default_rng(31), 6, 40, 5))
+    z, t, c = (a.view(*lead, -1) if lead else a[0] for a in (z, t, c))
+    for T in (2.0, 2):
+        leaf, other = z.clone().requires_grad_(), z.clone().requires_grad_()
+        loss = P.distill_loss(leaf, t, c, T, reduction)
+        up = torch.rand_like(loss)
+        want = P.distill_loss(other, t, c, T, reduction)
+        loss *= up
+        loss.sum().backward()
+        want.backward(up)
+        assert torch.equal(leaf.grad, other.grad) and torch.equal(loss.detach(), want.detach() * up)
+        value, _ = P.distill_loss_grad(z, t, c, T, reduction)
+        assert value.shape == loss.shape and torch.equal(value, want.detach())
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("reduction", ["none", "sum", "mean"])
 def test_forward_mode_and_function_transforms_are_refused(reduction):
     """A loss without its tangent, or of something that has no memory of its own, would be wrong in silence."""
