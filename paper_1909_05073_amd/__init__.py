@@ -9,7 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import functools
-import importlib
+import importlib.util
 import os
 
 import numpy as np
@@ -65,6 +65,9 @@ def lib():
     path = library_path()
     if not os.path.exists(path):
         _build.build()
+    # torch brings a HIP runtime of its own: if it is loaded behind this library's there are two in the process, and torch finds no GPU
+    if importlib.util.find_spec("torch") is not None:
+        import torch  # noqa: F401
     L = C.CDLL(path)
     vp, ip = C.c_void_p, C.c_int
     L.pconv_pack.restype = ip
