@@ -102,8 +102,8 @@ int pconv_project(const float *w_dense, const uint16_t *table, int num_patterns,
  * workgroups do not share tiles (a replay would find the words of the one before); where that is
  * the faster form, pconv_conv2d_static keeps it.
  *
- * Every wait inside the kernels is bounded.  If one ever runs out, the affected outputs are set
- * to NaN and the handle remembers it: the next pconv_conv2d / pconv_conv2d_pool2x2 on the handle,
+ * Every wait inside the kernels is bounded.  If one ever runs out, the affected outputs are wrong (NaN,
+ * or 0 behind a ReLU) and the handle remembers it: the next pconv_conv2d / pconv_conv2d_pool2x2 on the handle,
  * or pconv_get_async_error, returns PCONV_HIP_ERROR once (and launches nothing).
  *
  *   x_dev     device, activations [n][c_in][h_in][w_in] (NCHW) or [n][h_in][w_in][c_in]

@@ -296,9 +296,12 @@ template <typename Y> __device__ __forceinline__ int key_of_channel(int row) { r
 // `splits` workgroups share a tile, each with its part of k; their sums go to `part` [splits][m][n4], n4 = n rounded
 // up to four.
 //
-// 8192x4096 -> 4096 takes 69 to 75 us, 3.7 to 4.0 PFLOP/s, and 63 to 68 with zeros: it is the card's power that bounds it, which lets the
-// matrix units alone do 6.0 to 6.7 PFLOP/s with codes as they come, out of registers, and 8.9 with zeros.  Four waves of 128x128, stages
-// of half a slab, two groups of waves in turn, or loads and products of a wave interleaved by hand took 69 to 75 as well.
+// 8192x4096 -> 4096 takes 69 to 75 us, 3.7 to 4.0 PFLOP/s.  The matrix units alone, out of registers, do 6.0 to 6.7 PFLOP/s with codes as
+// they come (45 us) and 8.9 with zeros (31), but zeros take the kernel 63 to 68: the card's power is worth some 6 us, the rest is that three pipes
+// of nearly equal length, loads to LDS (2044 cycles a slab by themselves), reads of LDS (2088) and products (2272), run beside each other
+// only in part from barrier to barrier (3240 to 3580 a slab, the matrix units busy for 45 % of the launch), and that all compute units store their
+// outputs, 64 MiB, at the end of each of two rounds with no product under way.  Four waves of 128x128, stages of half a slab, two groups
+// of waves in turn, or loads and products of a wave interleaved by hand took 69 to 75 as well.
 template <typename Y, int BM, int BN, int WM, int WN, int S, int KG>
 __global__ void __launch_bounds__(KG * WM * WN * 64)
 matmul_mx4_kernel(const Mx4Product p, int splits, float *part)
