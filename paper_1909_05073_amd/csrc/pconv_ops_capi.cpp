@@ -97,8 +97,9 @@ int check_distill(const char *who, const void *z, int64_t ldz, int z_type, const
     if ((v && !z) || (top && (!t || !c))) return invalid(who, "null pointer argument");
     if (!stride_fits(rows, v, ldz) || !stride_fits(rows, top, ldt) || !stride_fits(rows, top, ldc)) return invalid(who, "rows must lie at least their length apart");
     if (!at_type(z, z_type == PCONV_BF16 ? 2 : 4) || !at_type(t, t_type == PCONV_BF16 ? 2 : 4) || !at_type(c, class_bytes)) return invalid(who, "rows must be aligned to their type");
-    p = DistillRows{z, t, c, nullptr, nullptr, nullptr, nullptr, ldz, ldt, ldc, 0, rows, 0, int(v), int(top), 1.0f / temperature,
-                    float(std::min(1.4426950408889634 / double(temperature), double(std::numeric_limits<float>::max()))), temperature * temperature, float(double(temperature) / (mean ? double(rows) : 1.0)), z_type == PCONV_BF16,
+    const double log2e_t = std::min(1.4426950408889634 / double(temperature), double(std::numeric_limits<float>::max()));
+    p = DistillRows{z, t, c, nullptr, nullptr, nullptr, nullptr, ldz, ldt, ldc, 0, rows, 0, int(v), int(top), 1.0f / temperature, float(log2e_t),
+                    temperature * temperature, float(double(temperature) / (mean ? double(rows) : 1.0)), z_type == PCONV_BF16,
                     t_type == PCONV_BF16, class_bytes == 8};
     return PCONV_OK;
 }
