@@ -352,7 +352,7 @@ int pconv_clip_grads(const void *const *grads, void *const *outs, const int64_t 
  *
  * An entry whose class is not 0 .. v - 1 is none, and a teacher's logit of -infinity has p = 0; a row without an entry (or of
  * such logits alone) has loss 0 and a gradient of zeros.  A class may be named more than once.  p = 0 counts 0 in the loss.
- * Infinities and NaN otherwise do what the formulas say.  Exponentials and sums within a row are fp32, rows are added in
+ * Infinities and NaN otherwise do what the formulas say.  Quotients by T, exponentials and sums within a row are fp32, rows are added in
  * fp64 in a fixed order; the same bits from run to run.  No gradient goes to the teacher.
  *
  *   z, grad    fp32 or bf16 (one type for both);  teacher  fp32 or bf16;  classes  integers of class_bytes 4 or 8 bytes
