@@ -185,7 +185,7 @@ __device__ __forceinline__ void join_vectors(Running &r, Vec<T> (&v)[U], const Q
 // LOSS: the loss and lse of each row; GRAD: its gradient, from lse where LOSS is false.  TPR threads share a row, which they
 // read U vectors of 16 bytes a thread at a time; where both are computed the first U of each stay in registers from the
 // sums to the gradient, and what lies beyond is read twice.  Bound by memory where rows are long and many: both of 4096x32768 bf16
-// 116 us, 4.6 TB/s.  The entries' shares and classes lie in LDS.  The gradient is written as if there were no entries; behind a barrier the first
+// 117 us, 4.6 TB/s.  The entries' shares and classes lie in LDS.  The gradient is written as if there were no entries; behind a barrier the first
 // entry that names a class writes it again with the shares of all that name it taken off.
 template <typename T, int TPR, int U, bool LOSS, bool GRAD>
 __global__ void __launch_bounds__(TPR == 64 ? 256 : TPR)
